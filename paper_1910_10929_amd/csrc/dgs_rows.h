@@ -1,0 +1,279 @@
+// Helpers of the training-block kernels: eight consecutive values of a row in a lane, element types, row sums, and the
+// codes of a checkpoint.
+//
+// A lane holds values c .. c + 7 of a row, c a multiple of 8, so that the four lanes of a quad hold the 32 columns that
+// share an exponent, and a run's largest magnitude is two quad permutes away.  Loads and stores are 16 bytes (8 for codes)
+// at any alignment of the element type; the last, shorter piece of a row goes element by element.
+#pragma once
+#include "dgs_wave.h"
+#include "../../include/dgs_blocks.h"
+
+namespace dgs {
+
+typedef _Float16 f16;
+#ifdef DGS_HOST_EMULATION
+struct bf16 { uint16_t bits; };
+#else
+typedef __bf16 bf16;
+#endif
+
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(1)));
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+
+__device__ __forceinline__ float to_float(float v) { return v; }
+__device__ __forceinline__ float to_float(f16 v) { return (float)v; }
+#ifdef DGS_HOST_EMULATION
+__device__ __forceinline__ float to_float(bf16 v) { return __uint_as_float((uint32_t)v.bits << 16); }
+#else
+__device__ __forceinline__ float to_float(bf16 v) { return (float)v; }
+#endif
+
+template <class T> __device__ __forceinline__ T from_float(float v) { return (T)v; }
+#ifdef DGS_HOST_EMULATION
+template <> inline bf16 from_float<bf16>(float v)      // to nearest, halfway cases to even
+{
+    const uint32_t u = __float_as_uint(v);
+    if ((u & 0x7FFFFFFFu) > 0x7F800000u) return bf16{(uint16_t)((u >> 16) | 0x40u)};
+    return bf16{(uint16_t)((u + 0x7FFFu + ((u >> 16) & 1u)) >> 16)};
+}
+#endif
+
+// ---------------------------------------------------------------------------
+// eight values of a row
+// ---------------------------------------------------------------------------
+
+// What is loaded, before it is unpacked (so that loads can be issued a row ahead at the registers the memory format takes).
+template <class T> struct Raw8 { uint32_t w[2 * sizeof(T)]; };
+
+// `n` (at most 8) values at p; the others are 0.
+template <class T> __device__ __forceinline__ Raw8<T> load8(const T *p, uint32_t n)
+{
+    Raw8<T> r;
+    if (n >= 8) {
+        const u32x4_any *q = (const u32x4_any *)p;
+#pragma unroll
+        for (uint32_t i = 0; i < sizeof(T) / 2; ++i) {
+            const u32x4_any v = q[i];
+            r.w[4 * i] = v.x; r.w[4 * i + 1] = v.y; r.w[4 * i + 2] = v.z; r.w[4 * i + 3] = v.w;
+        }
+    } else {
+        T t[8];
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) t[i] = i < n ? p[i] : from_float<T>(0.0f);
+        __builtin_memcpy(&r, t, sizeof(r));
+    }
+    return r;
+}
+
+template <class T> __device__ __forceinline__ void unpack8(const Raw8<T> &r, float (&v)[8])
+{
+    T t[8];
+    __builtin_memcpy(t, &r, sizeof(r));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = to_float(t[i]);
+}
+template <> __device__ __forceinline__ void unpack8<bf16>(const Raw8<bf16> &r, float (&v)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(r.w[i] << 16);
+        v[2 * i + 1] = __uint_as_float(r.w[i] & 0xFFFF0000u);
+    }
+}
+
+template <class T> __device__ __forceinline__ void store8(T *p, uint32_t n, const float (&v)[8])
+{
+    T t[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t[i] = from_float<T>(v[i]);
+    if (n >= 8) {
+        Raw8<T> r;
+        __builtin_memcpy(&r, t, sizeof(r));
+        u32x4_any *q = (u32x4_any *)p;
+#pragma unroll
+        for (uint32_t i = 0; i < sizeof(T) / 2; ++i) {
+            u32x4_any o;
+            o.x = r.w[4 * i]; o.y = r.w[4 * i + 1]; o.z = r.w[4 * i + 2]; o.w = r.w[4 * i + 3];
+            q[i] = o;
+        }
+    } else {
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i)
+            if (i < n) p[i] = t[i];
+    }
+}
+
+// The same for a type that is known at run time: a vector of parameters, a gate.
+__device__ __forceinline__ void load8_f32(const float *p, uint32_t n, float (&v)[8]) { unpack8(load8(p, n), v); }
+
+// How many of the eight values from column c on exist.
+__device__ __forceinline__ uint32_t live8(uint32_t c, uint32_t cols) { return c >= cols ? 0u : min(8u, cols - c); }
+
+// ---------------------------------------------------------------------------
+// sums over lanes
+// ---------------------------------------------------------------------------
+
+#ifdef DGS_HOST_EMULATION
+__device__ __forceinline__ uint32_t lane_read(uint32_t v, uint32_t lane) { return (uint32_t)__builtin_amdgcn_ds_bpermute((int)(lane * 4), (int)v); }
+__device__ __forceinline__ uint32_t quad_xor1(uint32_t v) { return lane_read(v, lane_id() ^ 1u); }
+__device__ __forceinline__ uint32_t quad_xor2(uint32_t v) { return lane_read(v, lane_id() ^ 2u); }
+__device__ __forceinline__ uint32_t half_mirror(uint32_t v) { return lane_read(v, lane_id() ^ 7u); }
+__device__ __forceinline__ uint32_t row_mirror(uint32_t v) { return lane_read(v, lane_id() ^ 15u); }
+#else
+template <int CTRL> __device__ __forceinline__ uint32_t dpp(uint32_t v)
+{
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, true);
+}
+__device__ __forceinline__ uint32_t quad_xor1(uint32_t v) { return dpp<0xB1>(v); }      // quad_perm 1 0 3 2
+__device__ __forceinline__ uint32_t quad_xor2(uint32_t v) { return dpp<0x4E>(v); }      // quad_perm 2 3 0 1
+__device__ __forceinline__ uint32_t half_mirror(uint32_t v) { return dpp<0x141>(v); }
+__device__ __forceinline__ uint32_t row_mirror(uint32_t v) { return dpp<0x140>(v); }
+#endif
+
+// The sum over the wavefront, the same bits in every lane: within rows of 16 lanes by lane permutes, then the four rows.
+__device__ __forceinline__ float wave_sum(float v)
+{
+    v += __uint_as_float(quad_xor1(__float_as_uint(v)));
+    v += __uint_as_float(quad_xor2(__float_as_uint(v)));
+    v += __uint_as_float(half_mirror(__float_as_uint(v)));
+    v += __uint_as_float(row_mirror(__float_as_uint(v)));
+    const int b = (int)__float_as_uint(v);
+    const float r0 = __uint_as_float((uint32_t)__builtin_amdgcn_readlane(b, 0));
+    const float r1 = __uint_as_float((uint32_t)__builtin_amdgcn_readlane(b, 16));
+    const float r2 = __uint_as_float((uint32_t)__builtin_amdgcn_readlane(b, 32));
+    const float r3 = __uint_as_float((uint32_t)__builtin_amdgcn_readlane(b, 48));
+    return (r0 + r1) + (r2 + r3);
+}
+
+// Sums over a team of WAVES wavefronts (a whole workgroup if there are several).  Successive calls of a kernel use the two
+// halves of `lds` in turn (`turn` flips), which makes one barrier a call enough: whoever writes a half again has passed the
+// barrier of the other half's call, and with it every reader of the first.
+template <int WAVES, int N>
+__device__ __forceinline__ void team_sum(float (&v)[N], float (*lds)[2][WAVES], uint32_t &turn)
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
+    if constexpr (WAVES > 1) {
+        float (*half)[WAVES] = lds[turn];
+        turn ^= 1u;
+        const uint32_t wave = threadIdx.x >> 6;
+        if (lane_id() == 0) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) half[i][wave] = v[i];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            float s = half[i][0];
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) s += half[i][w];
+            v[i] = s;
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// checkpoint codes
+// ---------------------------------------------------------------------------
+
+// The exponent byte of the run that this quad of lanes holds, from the bits of its largest magnitude: with top = m 2^E, m in
+// [1, 2), the exponent is E - 6 where 64 m < 127.5, one more otherwise (a carry out of the mantissa).
+__device__ __forceinline__ uint32_t run_byte(const float (&v)[8])
+{
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+    top = max(top, quad_xor1(top));
+    top = max(top, quad_xor2(top));
+    const int byte = (int)((top + 0x10000u) >> 23) - 6;
+    return top >= 0x7F800000u ? 255u : (uint32_t)min(max(byte, 1), 248);
+}
+
+// Eight codes of the run with exponent byte `byte`.  v 2^-e + 1.5 2^23 in one rounding leaves the nearest whole number
+// (halfway cases to even) in the low mantissa bits, its low byte being the code.
+__device__ __forceinline__ void encode8(const float (&v)[8], uint32_t byte, uint32_t (&q)[2])
+{
+    const float scale = __uint_as_float((254u - byte) << 23);
+    uint32_t b[8];
+    if (byte < 248u) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) b[i] = __float_as_uint(__builtin_fmaf(v[i], scale, 12582912.0f)) & 0xFFu;
+    } else {      // the largest exponent, where 128 is cut to 127; or nothing finite
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float c = min(max(v[i] * scale, -127.0f), 127.0f);
+            b[i] = byte == 255u ? 0u : __float_as_uint(c + 12582912.0f) & 0xFFu;
+        }
+    }
+    q[0] = b[0] | (b[1] << 8) | (b[2] << 16) | (b[3] << 24);
+    q[1] = b[4] | (b[5] << 8) | (b[6] << 16) | (b[7] << 24);
+}
+
+__device__ __forceinline__ float run_scale(uint32_t byte) { return __uint_as_float(byte == 255u ? 0x7FC00000u : byte << 23); }
+
+__device__ __forceinline__ void decode8(const uint32_t (&q)[2], float scale, float (&v)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (float)(int)(int8_t)(q[i >> 2] >> (8 * (i & 3))) * scale;
+}
+
+// `n` codes at p; the others are 0.
+__device__ __forceinline__ void load_codes(const int8_t *p, uint32_t n, uint32_t (&q)[2])
+{
+    if (n >= 8) {
+        const u32x2_any v = *(const u32x2_any *)p;
+        q[0] = v.x;
+        q[1] = v.y;
+    } else {
+        q[0] = q[1] = 0;
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i)
+            if (i < n) q[i >> 2] |= (uint32_t)(uint8_t)p[i] << (8 * (i & 3));
+    }
+}
+__device__ __forceinline__ void store_codes(int8_t *p, uint32_t n, const uint32_t (&q)[2])
+{
+    if (n >= 8) {
+        u32x2_any v;
+        v.x = q[0];
+        v.y = q[1];
+        *(u32x2_any *)p = v;
+    } else {
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i)
+            if (i < n) p[i] = (int8_t)(q[i >> 2] >> (8 * (i & 3)));
+    }
+}
+
+// Values c .. c + 7 of a row as a checkpoint: every lane of the wavefront calls this (n = 0 where the row has ended).
+// Values beyond the row are 0 in v.
+__device__ __forceinline__ void save8(int8_t *row, uint8_t *exps, uint32_t c, uint32_t n, const float (&v)[8])
+{
+    const uint32_t byte = run_byte(v);
+    if (n == 0) return;
+    uint32_t q[2];
+    encode8(v, byte, q);
+    store_codes(row + c, n, q);
+    if ((c & (DGS_CHECKPOINT_RUN - 1)) == 0) exps[c / DGS_CHECKPOINT_RUN] = (uint8_t)byte;
+}
+
+// ---------------------------------------------------------------------------
+// host side: arguments
+// ---------------------------------------------------------------------------
+
+static inline uint64_t type_bytes(int type) { return type == DGS_F32 ? 4u : 2u; }
+static inline bool is_type(int type) { return type >= DGS_F32 && type <= DGS_BF16; }
+static inline bool aligned_to(const void *p, uint64_t bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
+static inline bool matrix_ok(const void *p, uint64_t stride, uint64_t cols, int type)
+{
+    return p && stride >= cols && stride < (1ull << 40) && aligned_to(p, type_bytes(type));
+}
+static inline bool codes_ok(const dgs_codes &c, uint64_t cols)
+{
+    return c.codes && c.exps && c.codes_stride >= cols && c.codes_stride < (1ull << 40)
+        && c.exps_stride >= (cols + DGS_CHECKPOINT_RUN - 1) / DGS_CHECKPOINT_RUN && c.exps_stride < (1ull << 40);
+}
+// What a launch that was enqueued without an event leaves.
+static inline int launched() { return hipGetLastError() == hipSuccess ? DGS_OK : DGS_EHIP; }
+
+}  // namespace dgs
