@@ -311,6 +311,8 @@ class Edge:
             if self.pre is None:
                 _refuse("du needs a norm before the block")
             pu = _matrix(du, rows, cols, device, "du")
+            if branch and coded != (saved.pre is not None):
+                _refuse("saved: both norms as checkpoints or both as values")
             if saved.pre is not None:
                 pre = saved.pre._place(rows, cols, device, "saved.pre")
             elif saved.x_out is None:

@@ -53,7 +53,7 @@ __global__ __launch_bounds__(CKPT_THREADS) void k_checkpoint_decode(const int8_t
             for (int i = 0; i < 8; ++i) v[i] = v[i] != v[i] ? v[i] : min(max(v[i], -65504.0f), 65504.0f);
         }
     }
-    store8(out + row * out_stride + c, n, v);
+    store8(out + row * out_stride, c, n, v);
 }
 
 struct Shape {

@@ -24,7 +24,7 @@ struct ForwardArgs {
     float *stats;
     uint64_t x_stride, f_stride, gate_stride, x_out_stride, u_stride;
     uint64_t post_codes_stride, post_exps_stride, pre_codes_stride, pre_exps_stride;
-    uint32_t rows, rows_per_gate, gate_f32;
+    uint32_t rows, rows_per_gate, gate_f32, branch, gated;      // branch, gated: there is one
 };
 
 // 1 / sqrt(v), v > 0 (1 ulp)
@@ -37,35 +37,51 @@ __device__ __forceinline__ float rsqrt_of(float v)
 #endif
 }
 
-// A gate's eight values: fp32, or of the branch's type.
-struct GateRaw { uint32_t w[8]; };
-template <class TF> __device__ __forceinline__ GateRaw load_gate(const void *gate, uint64_t at, uint32_t n, bool f32)
+// A gate's eight values: fp32, or of the branch's type (which is then loaded twice, so that the number of loads does not
+// depend on the type).
+struct GateRaw { u32x4_any lo, hi; };
+template <bool TINY, class TF>
+__device__ __forceinline__ GateRaw load_gate(const void *gate, uint64_t row_at, uint32_t at, uint32_t cols, bool f32)
 {
     GateRaw g;
-    if (f32) {
-        const Raw8<float> r = load8((const float *)gate + at, n);
-        __builtin_memcpy(&g, &r, sizeof(r));
+    if constexpr (TINY) {
+        if (f32) {
+            const Raw8<float> r = load_at<true>((const float *)gate + row_at, at, cols);
+            __builtin_memcpy(&g, &r, sizeof(r));
+        } else {
+            const Raw8<TF> r = load_at<true>((const TF *)gate + row_at, at, cols);
+            __builtin_memcpy(&g, &r, sizeof(r));
+        }
     } else {
-        const Raw8<TF> r = load8((const TF *)gate + at, n);
-        __builtin_memcpy(&g, &r, sizeof(r));
+        const uint32_t bytes = f32 ? 4u : (uint32_t)sizeof(TF);
+        const char *const row = (const char *)gate + row_at * bytes;
+        const uint32_t o = opaque(at * bytes);
+        g.lo = *(const u32x4_any *)(row + o);
+        g.hi = *(const u32x4_any *)(row + (bytes == 4u ? 16u : 0u) + o);
     }
     return g;
 }
-template <class TF> __device__ __forceinline__ void unpack_gate(const GateRaw &g, bool f32, float (&v)[8])
+template <bool TINY, class TF>
+__device__ __forceinline__ void unpack_gate(const GateRaw &g, bool f32, bool ragged, const Place8 &p, float (&v)[8])
 {
     if (f32) {
         Raw8<float> r;
         __builtin_memcpy(&r, &g, sizeof(r));
+        if (ragged) in_place<TINY>(r, p);
         unpack8(r, v);
     } else {
         Raw8<TF> r;
         __builtin_memcpy(&r, &g, sizeof(r));
+        if (ragged) in_place<TINY>(r, p);
         unpack8(r, v);
     }
 }
 
-// Wavefronts of a workgroup whose teams are single wavefronts.
-constexpr uint32_t FORWARD_TEAMS = 4, BACKWARD_TEAMS = 8;
+// Teams of a forward workgroup where they are single wavefronts (otherwise it is one team); wavefronts of a backward workgroup,
+// whatever its teams: fewer workgroups leave fewer partial sums (with 8, two workgroups to a compute unit, 16384 x 4096 took
+// 260 us in place of 249 and 8192 x 768 49 in place of 43).
+constexpr uint32_t FORWARD_TEAMS = 4;
+constexpr int BACKWARD_WAVES = 16;
 
 template <int WAVES, int CHUNKS> struct Team {
     static constexpr uint32_t LANES = WAVES * 64;
@@ -73,10 +89,25 @@ template <int WAVES, int CHUNKS> struct Team {
     static __device__ __forceinline__ uint32_t col(int k) { return ((uint32_t)k * LANES + threadIdx.x % LANES) * 8u; }
 };
 
+// v - by, and 0 behind the row's end in the lane that holds it (where the row's length is no multiple of eight).
+template <int CHUNKS>
+__device__ __forceinline__ void subtract(float (&v)[CHUNKS][8], const Place8 (&p)[CHUNKS], bool ragged, float by)
+{
+#pragma unroll
+    for (int k = 0; k < CHUNKS; ++k) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[k][i] -= by;
+        if (ragged) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[k][i] = (uint32_t)i < p[k].n ? v[k][i] : 0.0f;
+        }
+    }
+}
+
 // Statistics of a row and its normalised values, in place.
-template <int WAVES, int CHUNKS>
-__device__ __forceinline__ void normalise(float (&v)[CHUNKS][8], const uint32_t (&n)[CHUNKS], int kind, float eps, float inv_cols,
-                                          float (*lds)[2][WAVES], uint32_t &turn, float &mean, float &rstd)
+template <int WAVES, int ALL, int CHUNKS>
+__device__ __forceinline__ void normalise(float (&v)[CHUNKS][8], const Place8 (&p)[CHUNKS], bool ragged, int kind, float eps,
+                                          float inv_cols, TeamLds<ALL> &lds, uint32_t &turn, float &mean, float &rstd)
 {
     mean = rstd = 0.0f;
     if (kind == DGS_NORM_NONE) return;
@@ -84,22 +115,25 @@ __device__ __forceinline__ void normalise(float (&v)[CHUNKS][8], const uint32_t 
     if (kind == DGS_NORM_LAYER) {
         s[0] = 0.0f;
 #pragma unroll
-        for (int k = 0; k < CHUNKS; ++k)
+        for (int k = 0; k < CHUNKS; ++k) {
+            float of_lane = v[k][0];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s[0] += v[k][i];
-        team_sum<WAVES, 1>(s, lds, turn);
+            for (int i = 1; i < 8; ++i) of_lane += v[k][i];
+            s[0] += p[k].n ? of_lane : 0.0f;
+        }
+        team_sum<WAVES, ALL, 1>(s, lds, turn);
         mean = s[0] * inv_cols;
-#pragma unroll
-        for (int k = 0; k < CHUNKS; ++k)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[k][i] = (uint32_t)i < n[k] ? v[k][i] - mean : 0.0f;
+        subtract<CHUNKS>(v, p, ragged, mean);
     }
     s[0] = 0.0f;
 #pragma unroll
-    for (int k = 0; k < CHUNKS; ++k)
+    for (int k = 0; k < CHUNKS; ++k) {
+        float of_lane = v[k][0] * v[k][0];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s[0] = __builtin_fmaf(v[k][i], v[k][i], s[0]);
-    team_sum<WAVES, 1>(s, lds, turn);
+        for (int i = 1; i < 8; ++i) of_lane = __builtin_fmaf(v[k][i], v[k][i], of_lane);
+        s[0] += p[k].n ? of_lane : 0.0f;
+    }
+    team_sum<WAVES, ALL, 1>(s, lds, turn);
     rstd = rsqrt_of(__builtin_fmaf(s[0], inv_cols, eps));
 #pragma unroll
     for (int k = 0; k < CHUNKS; ++k)
@@ -107,44 +141,26 @@ __device__ __forceinline__ void normalise(float (&v)[CHUNKS][8], const uint32_t 
         for (int i = 0; i < 8; ++i) v[k][i] *= rstd;
 }
 
-template <class TX, class TF, int CHUNKS> struct ForwardRow {
-    Raw8<TX> x[CHUNKS];
-    Raw8<TF> f[CHUNKS];
-    GateRaw g[CHUNKS];
-};
-
-template <class TX, class TF, int WAVES, int CHUNKS>
-__device__ __forceinline__ void fetch(ForwardRow<TX, TF, CHUNKS> &r, const ForwardArgs &a, uint32_t row, const uint32_t (&c)[CHUNKS],
-                                      const uint32_t (&n)[CHUNKS])
-{
-    const uint64_t gate_at = a.gate ? (uint64_t)(row / a.rows_per_gate) * a.gate_stride : 0u;
-#pragma unroll
-    for (int k = 0; k < CHUNKS; ++k) {
-        r.x[k] = load8((const TX *)a.x + row * a.x_stride + c[k], n[k]);
-        if (a.f) r.f[k] = load8((const TF *)a.f + row * a.f_stride + c[k], n[k]);
-        if (a.gate) r.g[k] = load_gate<TF>(a.gate, gate_at + c[k], n[k], a.gate_f32);
-    }
-}
-
-template <class TX, class TF, int WAVES, int CHUNKS>
+template <class TX, class TF, int WAVES, int CHUNKS, bool TINY>
 __global__ __launch_bounds__(WAVES == 1 ? FORWARD_TEAMS * 64 : WAVES * 64) void k_edge_forward(ForwardArgs a)
 {
     constexpr uint32_t TEAMS = WAVES == 1 ? FORWARD_TEAMS : 1;
-    __shared__ float lds[2][2][WAVES];
+    constexpr int ALL = TEAMS * WAVES;
+    __shared__ TeamLds<ALL> lds;
     uint32_t turn = 0;
     const uint32_t team = uniform(blockIdx.x * TEAMS + threadIdx.x / (WAVES * 64));
     const uint32_t teams = gridDim.x * TEAMS;
     const EdgeLayer &l = a.l;
-    uint32_t c[CHUNKS], n[CHUNKS];
+    const bool ragged = TINY || (l.cols & 7u) != 0;
+    Place8 p[CHUNKS];
     float wp[CHUNKS][8], bp[CHUNKS][8], wn[CHUNKS][8], bn[CHUNKS][8];
 #pragma unroll
     for (int k = 0; k < CHUNKS; ++k) {
-        c[k] = Team<WAVES, CHUNKS>::col(k);
-        n[k] = live8(c[k], l.cols);
-        if (l.post_weight) load8_f32(l.post_weight + c[k], n[k], wp[k]);
-        if (l.post_bias) load8_f32(l.post_bias + c[k], n[k], bp[k]);
-        if (l.pre_weight) load8_f32(l.pre_weight + c[k], n[k], wn[k]);
-        if (l.pre_bias) load8_f32(l.pre_bias + c[k], n[k], bn[k]);
+        p[k] = place8<TINY>(Team<WAVES, CHUNKS>::col(k), l.cols);
+        if (l.post_weight) load8_f32(l.post_weight + p[k].c, p[k].n, wp[k]);
+        if (l.post_bias) load8_f32(l.post_bias + p[k].c, p[k].n, bp[k]);
+        if (l.pre_weight) load8_f32(l.pre_weight + p[k].c, p[k].n, wn[k]);
+        if (l.pre_bias) load8_f32(l.pre_bias + p[k].c, p[k].n, bn[k]);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             if (!l.post_weight) wp[k][i] = 1.0f;
@@ -155,42 +171,76 @@ __global__ __launch_bounds__(WAVES == 1 ? FORWARD_TEAMS * 64 : WAVES * 64) void 
     }
     uint32_t row = team;
     if (row >= a.rows) return;      // (of a workgroup that is one team, all of it)
-    ForwardRow<TX, TF, CHUNKS> next;
-    fetch<TX, TF, WAVES, CHUNKS>(next, a, row, c, n);
+    // What is loaded of a row (f and the gate, if there are none, of x in their place).  Each piece of the next row is asked for
+    // as soon as this row's has been unpacked, so that it has a whole round to arrive and takes no registers of its own.
+    Raw8<TX> raw_x[CHUNKS];
+    Raw8<TF> raw_f[CHUNKS];
+    GateRaw raw_g[CHUNKS];
+    auto fetch_x = [&](uint32_t r) {
+#pragma unroll
+        for (int k = 0; k < CHUNKS; ++k) raw_x[k] = load_at<TINY>((const TX *)a.x + r * a.x_stride, p[k].at, l.cols);
+    };
+    auto fetch_f = [&](uint32_t r) {
+#pragma unroll
+        for (int k = 0; k < CHUNKS; ++k) raw_f[k] = load_at<TINY>((const TF *)a.f + r * a.f_stride, p[k].at, l.cols);
+    };
+    auto fetch_g = [&](uint32_t r) {
+        const uint64_t gate_at = (uint64_t)(r / a.rows_per_gate) * a.gate_stride;
+#pragma unroll
+        for (int k = 0; k < CHUNKS; ++k) raw_g[k] = load_gate<TINY, TF>(a.gate, gate_at, p[k].at, l.cols, a.gate_f32);
+    };
+    fetch_f(row);
+    fetch_x(row);
+    fetch_g(row);
     for (; row < a.rows; row += teams) {
-        const ForwardRow<TX, TF, CHUNKS> now = next;
-        if (row + teams < a.rows) fetch<TX, TF, WAVES, CHUNKS>(next, a, row + teams, c, n);
+        const uint32_t next = row + teams < a.rows ? row + teams : row;
         float x[CHUNKS][8], f[CHUNKS][8];
         float post_mean = 0.0f, post_rstd = 0.0f, pre_mean, pre_rstd;
 #pragma unroll
-        for (int k = 0; k < CHUNKS; ++k) unpack8(now.x[k], x[k]);
-        if (a.f) {
+        for (int k = 0; k < CHUNKS; ++k) {
+            if (ragged) in_place<TINY>(raw_f[k], p[k]);
+            unpack8(raw_f[k], f[k]);
+        }
+        fetch_f(next);
+        if (a.branch) normalise<WAVES, ALL, CHUNKS>(f, p, ragged, l.post, l.post_eps, l.inv_cols, lds, turn, post_mean, post_rstd);
 #pragma unroll
-            for (int k = 0; k < CHUNKS; ++k) unpack8(now.f[k], f[k]);
-            normalise<WAVES, CHUNKS>(f, n, l.post, l.post_eps, l.inv_cols, lds, turn, post_mean, post_rstd);
+        for (int k = 0; k < CHUNKS; ++k) {
+            if (ragged) in_place<TINY>(raw_x[k], p[k]);
+            unpack8(raw_x[k], x[k]);
+        }
+        fetch_x(next);
+        if (a.branch) {
 #pragma unroll
             for (int k = 0; k < CHUNKS; ++k) {
                 if (a.post_codes)
-                    save8(a.post_codes + row * a.post_codes_stride, a.post_exps + row * a.post_exps_stride, c[k], n[k], f[k]);
+                    save8(a.post_codes + row * a.post_codes_stride, a.post_exps + row * a.post_exps_stride, p[k].c, p[k].n, f[k]);
                 float g[8];
-                if (a.gate) unpack_gate<TF>(now.g[k], a.gate_f32, g);
+                unpack_gate<TINY, TF>(raw_g[k], a.gate_f32, ragged, p[k], g);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const float m = a.gate ? l.branch * g[i] : l.branch;
+                    const float m = a.gated ? l.branch * g[i] : l.branch;
                     x[k][i] = __builtin_fmaf(m, __builtin_fmaf(f[k][i], wp[k][i], bp[k][i]), l.skip * x[k][i]);
                 }
-                store8((TX *)a.x_out + row * a.x_out_stride + c[k], n[k], x[k]);
+                store8((TX *)a.x_out + row * a.x_out_stride, p[k].c, p[k].n, x[k]);
+            }
+            // (behind the row's end the gate may be anything: not the sum)
+            if (ragged) {
+#pragma unroll
+                for (int k = 0; k < CHUNKS; ++k)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[k][i] = (uint32_t)i < p[k].n ? x[k][i] : 0.0f;
             }
         }
-        normalise<WAVES, CHUNKS>(x, n, l.pre, l.pre_eps, l.inv_cols, lds, turn, pre_mean, pre_rstd);
+        fetch_g(next);
+        normalise<WAVES, ALL, CHUNKS>(x, p, ragged, l.pre, l.pre_eps, l.inv_cols, lds, turn, pre_mean, pre_rstd);
         if (l.pre != DGS_NORM_NONE) {
 #pragma unroll
             for (int k = 0; k < CHUNKS; ++k) {
                 if (a.pre_codes)
-                    save8(a.pre_codes + row * a.pre_codes_stride, a.pre_exps + row * a.pre_exps_stride, c[k], n[k], x[k]);
+                    save8(a.pre_codes + row * a.pre_codes_stride, a.pre_exps + row * a.pre_exps_stride, p[k].c, p[k].n, x[k]);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) x[k][i] = __builtin_fmaf(x[k][i], wn[k][i], bn[k][i]);
-                store8((TF *)a.u + row * a.u_stride + c[k], n[k], x[k]);
+                store8((TF *)a.u + row * a.u_stride, p[k].c, p[k].n, x[k]);
             }
         }
         if (a.stats && threadIdx.x % (WAVES * 64) == 0) {
@@ -225,186 +275,260 @@ struct BackwardArgs {
     float *partial;         // 5 x blocks x cols (the fifth: the gate's)
     uint64_t dx_out_stride, du_stride, gate_stride, f_stride, x_out_stride, dx_stride, df_stride, dgate_stride;
     uint64_t post_codes_stride, post_exps_stride, pre_codes_stride, pre_exps_stride;
-    uint32_t rows, gate_f32, accumulate, branch;     // branch: there is one
+    uint32_t rows, gate_f32, accumulate, branch, gated, through_pre, arrives, coded;     // (branch .. arrives: there is such)
 };
 
 enum { ACC_POST_WEIGHT, ACC_POST_BIAS, ACC_PRE_WEIGHT, ACC_PRE_BIAS, ACC_GATE, ACCS };
 
 // Normalised values as the forward pass left them: codes, or the values themselves.
-template <class T> struct Kept { Raw8<T> v; uint32_t q[2]; uint32_t byte; };
+template <class T, bool CODED> struct Kept;
+template <class T> struct Kept<T, true> { uint32_t q[2], byte; };
+template <class T> struct Kept<T, false> { Raw8<T> v; };
 
-template <class T>
-__device__ __forceinline__ void fetch_kept(Kept<T> &r, const int8_t *codes, const uint8_t *exps, uint64_t codes_stride,
-                                           uint64_t exps_stride, const void *values, uint64_t stride, uint64_t row, uint32_t c, uint32_t n)
+template <bool TINY, class T, bool CODED>
+__device__ __forceinline__ void fetch_kept(Kept<T, CODED> &r, const int8_t *codes, const uint8_t *exps, uint64_t codes_stride,
+                                           uint64_t exps_stride, const void *values, uint64_t stride, uint64_t row, const Place8 &p,
+                                           uint32_t cols)
 {
-    if (codes) {
-        load_codes(codes + row * codes_stride + c, n, r.q);
-        r.byte = n ? exps[row * exps_stride + c / DGS_CHECKPOINT_RUN] : 1u;
+    if constexpr (CODED) {
+        load_codes_at<TINY>(codes + row * codes_stride, p.at, cols, r.q);
+        r.byte = (exps + row * exps_stride)[opaque(min(p.c, cols - 1u) / DGS_CHECKPOINT_RUN)];
     } else {
-        r.v = load8((const T *)values + row * stride + c, n);
+        r.v = load_at<TINY>((const T *)values + row * stride, p.at, cols);
     }
 }
-template <class T>
-__device__ __forceinline__ void unpack_kept(const Kept<T> &r, bool coded, int kind, float mean, float rstd, uint32_t n, float (&v)[8])
+// The normalised row.
+template <bool TINY, class T, bool CODED, int CHUNKS>
+__device__ __forceinline__ void unpack_kept(Kept<T, CODED> (&r)[CHUNKS], int kind, float mean, float rstd, const Place8 (&p)[CHUNKS],
+                                            bool ragged, float (&v)[CHUNKS][8])
 {
-    if (coded) {
-        decode8(r.q, run_scale(r.byte), v);
-        return;
-    }
-    unpack8(r.v, v);
-    if (kind == DGS_NORM_NONE) return;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = (uint32_t)i < n ? (v[i] - mean) * rstd : 0.0f;
-}
-
-template <class TX, class TF, int CHUNKS> struct BackwardRow {
-    Raw8<TX> d[CHUNKS];
-    Raw8<TF> u[CHUNKS];
-    GateRaw g[CHUNKS];
-    Kept<TF> f[CHUNKS];
-    Kept<TX> x[CHUNKS];
-    f32x4_any stats;
-};
-
-template <class TX, class TF, int WAVES, int CHUNKS>
-__device__ __forceinline__ void fetch(BackwardRow<TX, TF, CHUNKS> &r, const BackwardArgs &a, uint32_t row, const uint32_t (&c)[CHUNKS],
-                                      const uint32_t (&n)[CHUNKS])
-{
-    const uint64_t gate_at = a.gate ? (uint64_t)(row / a.cut.rows_per_gate) * a.gate_stride : 0u;
 #pragma unroll
     for (int k = 0; k < CHUNKS; ++k) {
-        if (a.dx_out) r.d[k] = load8((const TX *)a.dx_out + row * a.dx_out_stride + c[k], n[k]);
-        if (a.du) {
-            r.u[k] = load8((const TF *)a.du + row * a.du_stride + c[k], n[k]);
-            fetch_kept<TX>(r.x[k], a.pre_codes, a.pre_exps, a.pre_codes_stride, a.pre_exps_stride, a.x_out, a.x_out_stride, row, c[k],
-                           n[k]);
+        if constexpr (CODED) {
+            if (ragged) codes_in_place<TINY>(r[k].q, p[k]);
+            decode8(r[k].q, run_scale(r[k].byte), v[k]);
+        } else {
+            if (ragged) in_place<TINY>(r[k].v, p[k]);
+            unpack8(r[k].v, v[k]);
         }
-        if (a.branch)
-            fetch_kept<TF>(r.f[k], a.post_codes, a.post_exps, a.post_codes_stride, a.post_exps_stride, a.f, a.f_stride, row, c[k], n[k]);
-        if (a.gate) r.g[k] = load_gate<TF>(a.gate, gate_at + c[k], n[k], a.gate_f32);
     }
-    r.stats = *(const f32x4_any *)(a.stats + 4 * (uint64_t)row);
+    if constexpr (!CODED) {
+        if (kind == DGS_NORM_NONE) return;
+        if (kind == DGS_NORM_LAYER) subtract<CHUNKS>(v, p, ragged, mean);
+#pragma unroll
+        for (int k = 0; k < CHUNKS; ++k)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[k][i] *= rstd;
+    }
 }
 
-// The gradient through a norm at its normalised output h, times rstd: in place.  Columns beyond the row hold 0 in g and h and
-// are not read of the result.
-template <int WAVES, int CHUNKS>
-__device__ __forceinline__ void through_norm(float (&g)[CHUNKS][8], const float (&h)[CHUNKS][8], int kind, float rstd, float inv_cols,
-                                             float (*lds)[2][WAVES], uint32_t &turn)
+// The gradient through a norm at its normalised output h, in place.
+template <int WAVES, int ALL, int CHUNKS>
+__device__ __forceinline__ void through_norm(float (&g)[CHUNKS][8], const float (&h)[CHUNKS][8], const Place8 (&p)[CHUNKS], bool ragged,
+                                             int kind, float rstd, float inv_cols, TeamLds<ALL> &lds, uint32_t &turn)
 {
     if (kind == DGS_NORM_NONE) return;
     float s[2] = {0.0f, 0.0f};
 #pragma unroll
-    for (int k = 0; k < CHUNKS; ++k)
+    for (int k = 0; k < CHUNKS; ++k) {
+        float of_lane = g[k][0] * h[k][0];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s[0] = __builtin_fmaf(g[k][i], h[k][i], s[0]);
+        for (int i = 1; i < 8; ++i) of_lane = __builtin_fmaf(g[k][i], h[k][i], of_lane);
+        s[0] += p[k].n ? of_lane : 0.0f;
+    }
     if (kind == DGS_NORM_LAYER) {
 #pragma unroll
-        for (int k = 0; k < CHUNKS; ++k)
+        for (int k = 0; k < CHUNKS; ++k) {
+            float of_lane = g[k][0];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s[1] += g[k][i];
+            for (int i = 1; i < 8; ++i) of_lane += g[k][i];
+            s[1] += p[k].n ? of_lane : 0.0f;
+        }
+        team_sum<WAVES, ALL, 2>(s, lds, turn);
+        subtract<CHUNKS>(g, p, ragged, s[1] * inv_cols);
+    } else {
+        float one[1] = {s[0]};
+        team_sum<WAVES, ALL, 1>(one, lds, turn);
+        s[0] = one[0];
     }
-    team_sum<WAVES, 2>(s, lds, turn);
-    const float along = s[0] * inv_cols, mean = s[1] * inv_cols;
+    const float along = -s[0] * inv_cols;
 #pragma unroll
     for (int k = 0; k < CHUNKS; ++k)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) g[k][i] = (__builtin_fmaf(-along, h[k][i], g[k][i]) - mean) * rstd;
+        for (int i = 0; i < 8; ++i) g[k][i] = __builtin_fmaf(along, h[k][i], g[k][i]) * rstd;
 }
 
-template <class T> __device__ __forceinline__ void store_grad8(T *p, uint32_t n, float (&v)[8], bool add)
+template <class T> __device__ __forceinline__ void store_grad8(T *row, uint32_t c, uint32_t n, float (&v)[8], bool add)
 {
     if (add) {
         float o[8];
-        unpack8(load8(p, n), o);
+        unpack8(load8(row + c, n), o);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] += o[i];
     }
-    store8(p, n, v);
+    store8(row, c, n, v);
 }
 
-template <class TX, class TF, int WAVES, int CHUNKS>
-__global__ __launch_bounds__(WAVES == 1 ? BACKWARD_TEAMS * 64 : WAVES * 64) void k_edge_backward(BackwardArgs a)
+// Eight parameters of the backward pass: staged in LDS, or where a row is too long for that (STAGED false) from memory.
+template <bool STAGED>
+__device__ __forceinline__ void parameters8(const float *staged, const float *given, uint32_t c, uint32_t n, float absent, float (&v)[8])
 {
-    constexpr uint32_t TEAMS = WAVES == 1 ? BACKWARD_TEAMS : 1;
-    __shared__ float lds[2][2][WAVES];
+    if constexpr (STAGED) {
+        const f32x4 lo = *(const f32x4 *)(staged + c), hi = *(const f32x4 *)(staged + c + 4);
+        v[0] = lo.x; v[1] = lo.y; v[2] = lo.z; v[3] = lo.w;
+        v[4] = hi.x; v[5] = hi.y; v[6] = hi.z; v[7] = hi.w;
+    } else if (given) {
+        load8_f32(given + c, n, v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = absent;
+    }
+}
+
+template <class TX, class TF, int WAVES, int CHUNKS, bool CODED, bool TINY>
+__global__ __launch_bounds__(BACKWARD_WAVES * 64) void k_edge_backward(BackwardArgs a)
+{
+    constexpr int ALL = BACKWARD_WAVES;
+    constexpr uint32_t TEAMS = ALL / WAVES, WIDTH = WAVES * CHUNKS * 512;
+    constexpr bool STAGED = CHUNKS == 1;
+    __shared__ TeamLds<ALL> lds;
+    // parameters while the rows go by, then the teams' sums
+    constexpr uint32_t PARAMS = STAGED ? 3 * WIDTH : 4, SUMS = TEAMS > 1 ? TEAMS * WIDTH : 4;
+    __shared__ __attribute__((aligned(16))) float room[PARAMS > SUMS ? PARAMS : SUMS];
     uint32_t turn = 0;
     const uint32_t team = uniform(threadIdx.x / (WAVES * 64));
     const EdgeLayer &l = a.l;
-    uint32_t c[CHUNKS], n[CHUNKS];
-    float wp[CHUNKS][8], bp[CHUNKS][8], wn[CHUNKS][8];
+    if constexpr (STAGED) {
+        for (uint32_t j = threadIdx.x; j < WIDTH; j += ALL * 64) {
+            const bool in = j < l.cols;
+            room[j] = in && l.post_weight ? l.post_weight[j] : 1.0f;
+            room[WIDTH + j] = in && l.post_bias ? l.post_bias[j] : 0.0f;
+            room[2 * WIDTH + j] = in && l.pre_weight ? l.pre_weight[j] : 1.0f;
+        }
+        __syncthreads();
+    }
+    constexpr uint32_t AT = STAGED ? WIDTH : 0;
+    const float *const post_weight = room, *const post_bias = room + AT, *const pre_weight = room + 2 * AT;
+    const bool ragged = TINY || (l.cols & 7u) != 0;
+    Place8 p[CHUNKS];
     float acc[ACCS][CHUNKS][8];
 #pragma unroll
     for (int k = 0; k < CHUNKS; ++k) {
-        c[k] = Team<WAVES, CHUNKS>::col(k);
-        n[k] = live8(c[k], l.cols);
-        if (l.post_weight) load8_f32(l.post_weight + c[k], n[k], wp[k]);
-        if (l.post_bias) load8_f32(l.post_bias + c[k], n[k], bp[k]);
-        if (l.pre_weight) load8_f32(l.pre_weight + c[k], n[k], wn[k]);
+        p[k] = place8<TINY>(Team<WAVES, CHUNKS>::col(k), l.cols);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            if (!l.post_weight) wp[k][i] = 1.0f;
-            if (!l.post_bias) bp[k][i] = 0.0f;
-            if (!l.pre_weight) wn[k][i] = 1.0f;
+        for (int i = 0; i < 8; ++i)
 #pragma unroll
             for (int q = 0; q < ACCS; ++q) acc[q][k][i] = 0.0f;
-        }
     }
-    // this team's rows: first, the distance to the next one, where they end; then the same of the next gate row
+    // this team's rows, a round each; rounds are the same for all teams, and a round without a row works on zeros
     const Cut &cut = a.cut;
-    uint32_t gate_row, row, end, gate_end;
-    const uint32_t step = cut.whole ? 1u : TEAMS;
+    uint32_t gate_row, gate_end, row, end, rounds;
     if (cut.whole) {
         gate_row = blockIdx.x * cut.whole + team;
         gate_end = min(cut.gates, (blockIdx.x + 1) * cut.whole);
+        rounds = cut.whole / TEAMS * cut.rows_per_gate;
         row = gate_row < gate_end ? gate_row * cut.rows_per_gate : a.rows;
         end = min(a.rows - row, cut.rows_per_gate) + row;
     } else {
         gate_row = blockIdx.x / cut.parts;
         gate_end = 0;
         const uint32_t first = gate_row * cut.rows_per_gate, part = (blockIdx.x - gate_row * cut.parts) * cut.run;
-        // (parts behind the last row of a short last gate row are empty)
-        const uint32_t of_gate = min(a.rows - first, cut.rows_per_gate);
-        row = first + min(part + team, of_gate);
-        end = first + min(part + cut.run, of_gate);
+        rounds = cut.run / TEAMS;
+        row = first + part + team;
+        end = min(a.rows - first, min(cut.rows_per_gate, part + cut.run)) + first;
     }
-    BackwardRow<TX, TF, CHUNKS> next;
-    bool more = row < end;
-    if (more) fetch<TX, TF, WAVES, CHUNKS>(next, a, row, c, n);
-    while (more) {
-        const BackwardRow<TX, TF, CHUNKS> now = next;
-        const uint32_t this_row = row, this_gate = gate_row;
-        row += step;
-        bool gate_done = false;
-        if (row >= end) {
-            gate_done = cut.whole != 0;
-            more = false;
-            if (cut.whole) {
-                gate_row += TEAMS;
-                if (gate_row < gate_end) {
-                    row = gate_row * cut.rows_per_gate;
-                    end = min(a.rows - row, cut.rows_per_gate) + row;
-                    more = true;
-                }
-            }
+    uint32_t in_gate = 0;       // rounds of the present gate row
+
+    // What is loaded of a row.  Each piece of the next row is asked for as soon as this row's has been unpacked, so that it
+    // has a whole round to arrive and takes no registers of its own.  (Where there is no row, row 0; where there is no
+    // matrix, whatever the workspace holds.)
+    Raw8<TX> raw_d[CHUNKS];
+    Raw8<TF> raw_u[CHUNKS];
+    GateRaw raw_g[CHUNKS];
+    Kept<TX, CODED> raw_x[CHUNKS];
+    Kept<TF, CODED> raw_f[CHUNKS];
+    f32x4_any stats;
+    auto fetch_u = [&](uint32_t r) {
+#pragma unroll
+        for (int k = 0; k < CHUNKS; ++k) {
+            raw_u[k] = load_at<TINY>((const TF *)a.du + r * a.du_stride, p[k].at, l.cols);
+            fetch_kept<TINY>(raw_x[k], a.pre_codes, a.pre_exps, a.pre_codes_stride, a.pre_exps_stride, a.x_out, a.x_out_stride, r, p[k],
+                             l.cols);
         }
-        if (more) fetch<TX, TF, WAVES, CHUNKS>(next, a, row, c, n);
+    };
+    auto fetch_d = [&](uint32_t r) {
+#pragma unroll
+        for (int k = 0; k < CHUNKS; ++k) raw_d[k] = load_at<TINY>((const TX *)a.dx_out + r * a.dx_out_stride, p[k].at, l.cols);
+    };
+    auto fetch_f = [&](uint32_t r) {
+#pragma unroll
+        for (int k = 0; k < CHUNKS; ++k)
+            fetch_kept<TINY>(raw_f[k], a.post_codes, a.post_exps, a.post_codes_stride, a.post_exps_stride, a.f, a.f_stride, r, p[k], l.cols);
+    };
+    auto fetch_g = [&](uint32_t r) {
+        const uint64_t gate_at = (uint64_t)(r / cut.rows_per_gate) * a.gate_stride;
+#pragma unroll
+        for (int k = 0; k < CHUNKS; ++k) raw_g[k] = load_gate<TINY, TF>(a.gate, gate_at, p[k].at, l.cols, a.gate_f32);
+    };
+    auto fetch_stats = [&](uint32_t r) { stats = *(const f32x4_any *)(a.stats + 4 * (uint64_t)r); };
+    {
+        const uint32_t r = row < end ? row : 0u;
+        fetch_stats(r);
+        fetch_u(r);
+        fetch_d(r);
+        fetch_f(r);
+        fetch_g(r);
+    }
+    for (uint32_t round = 0; round < rounds; ++round) {
+        const uint32_t this_row = row, this_gate = gate_row;
+        const bool valid = row < end;
+        bool gate_done = false;
+        if (cut.whole) {
+            ++row;
+            if (++in_gate == cut.rows_per_gate) {
+                in_gate = 0;
+                gate_done = gate_row < gate_end;
+                gate_row += TEAMS;
+                row = gate_row < gate_end ? gate_row * cut.rows_per_gate : a.rows;
+                end = min(a.rows - row, cut.rows_per_gate) + row;
+            }
+        } else {
+            row += TEAMS;
+        }
+        const uint32_t next = row < end ? row : 0u;
+        const f32x4_any st = stats;
+        fetch_stats(next);
 
         // d: through the stream's norm
         float d[CHUNKS][8], h[CHUNKS][8];
-        if (a.du) {
+#pragma unroll
+        for (int k = 0; k < CHUNKS; ++k) {
+            if (ragged) in_place<TINY>(raw_u[k], p[k]);
+            unpack8(raw_u[k], d[k]);
+        }
+        unpack_kept<TINY>(raw_x, l.pre, st.z, st.w, p, ragged, h);
+        fetch_u(next);
+        if (a.through_pre) {
+            if (valid && a.grad[ACC_PRE_BIAS]) {
+#pragma unroll
+                for (int k = 0; k < CHUNKS; ++k)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) acc[ACC_PRE_BIAS][k][i] += d[k][i];
+            }
+            if (valid) {
+#pragma unroll
+                for (int k = 0; k < CHUNKS; ++k)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) acc[ACC_PRE_WEIGHT][k][i] = __builtin_fmaf(d[k][i], h[k][i], acc[ACC_PRE_WEIGHT][k][i]);
+            }
 #pragma unroll
             for (int k = 0; k < CHUNKS; ++k) {
-                unpack8(now.u[k], d[k]);
-                unpack_kept<TX>(now.x[k], a.pre_codes, l.pre, now.stats.z, now.stats.w, n[k], h[k]);
+                float w[8];
+                parameters8<STAGED>(pre_weight, l.pre_weight, p[k].c, p[k].n, 1.0f, w);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    acc[ACC_PRE_WEIGHT][k][i] = __builtin_fmaf(d[k][i], h[k][i], acc[ACC_PRE_WEIGHT][k][i]);
-                    acc[ACC_PRE_BIAS][k][i] += d[k][i];
-                    d[k][i] *= wn[k][i];
-                }
+                for (int i = 0; i < 8; ++i) d[k][i] *= w[i];
             }
-            through_norm<WAVES, CHUNKS>(d, h, l.pre, now.stats.w, l.inv_cols, lds, turn);
+            through_norm<WAVES, ALL, CHUNKS>(d, h, p, ragged, l.pre, st.w, l.inv_cols, lds, turn);
         } else {
 #pragma unroll
             for (int k = 0; k < CHUNKS; ++k)
@@ -413,50 +537,83 @@ __global__ __launch_bounds__(WAVES == 1 ? BACKWARD_TEAMS * 64 : WAVES * 64) void
         }
 #pragma unroll
         for (int k = 0; k < CHUNKS; ++k) {
-            if (a.dx_out) {
-                float o[8];
-                unpack8(now.d[k], o);
+            float o[8];
+            if (ragged) in_place<TINY>(raw_d[k], p[k]);
+            unpack8(raw_d[k], o);
+            if (a.arrives) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) d[k][i] += o[i];
             }
+        }
+        fetch_d(next);
+        if (a.dx && valid) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) d[k][i] = (uint32_t)i < n[k] ? d[k][i] : 0.0f;
-            if (a.dx) {
+            for (int k = 0; k < CHUNKS; ++k) {
                 float o[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) o[i] = l.skip * d[k][i];
-                store8((TX *)a.dx + this_row * a.dx_stride + c[k], n[k], o);
+                store8((TX *)a.dx + this_row * a.dx_stride, p[k].c, p[k].n, o);
             }
         }
         // m and k: through the gate and the branch's norm
+        unpack_kept<TINY>(raw_f, l.post, st.x, st.y, p, ragged, h);
+        fetch_f(next);
+        float g[CHUNKS][8];
+#pragma unroll
+        for (int k = 0; k < CHUNKS; ++k) unpack_gate<TINY, TF>(raw_g[k], a.gate_f32, ragged, p[k], g[k]);
+        fetch_g(next);
         if (a.branch) {
+            float w[CHUNKS][8];
 #pragma unroll
             for (int k = 0; k < CHUNKS; ++k) {
-                unpack_kept<TF>(now.f[k], a.post_codes, l.post, now.stats.x, now.stats.y, n[k], h[k]);
-                float g[8];
-                if (a.gate) unpack_gate<TF>(now.g[k], a.gate_f32, g);
+                parameters8<STAGED>(post_weight, l.post_weight, p[k].c, p[k].n, 1.0f, w[k]);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    d[k][i] *= l.branch;
-                    acc[ACC_GATE][k][i] = __builtin_fmaf(d[k][i], __builtin_fmaf(h[k][i], wp[k][i], bp[k][i]), acc[ACC_GATE][k][i]);
-                    if (a.gate) d[k][i] *= g[i];
-                    acc[ACC_POST_WEIGHT][k][i] = __builtin_fmaf(d[k][i], h[k][i], acc[ACC_POST_WEIGHT][k][i]);
-                    acc[ACC_POST_BIAS][k][i] += d[k][i];
-                    d[k][i] *= wp[k][i];
-                }
+                for (int i = 0; i < 8; ++i) d[k][i] *= l.branch;
             }
-            through_norm<WAVES, CHUNKS>(d, h, l.post, now.stats.y, l.inv_cols, lds, turn);
-            if (a.df) {
+            if (a.gated) {
+                if (valid) {
 #pragma unroll
-                for (int k = 0; k < CHUNKS; ++k) store8((TF *)a.df + this_row * a.df_stride + c[k], n[k], d[k]);
+                    for (int k = 0; k < CHUNKS; ++k) {
+                        float b[8];
+                        parameters8<STAGED>(post_bias, l.post_bias, p[k].c, p[k].n, 0.0f, b);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            acc[ACC_GATE][k][i] = __builtin_fmaf(d[k][i], __builtin_fmaf(h[k][i], w[k][i], b[i]), acc[ACC_GATE][k][i]);
+                    }
+                }
+#pragma unroll
+                for (int k = 0; k < CHUNKS; ++k)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) d[k][i] *= g[k][i];
+            }
+            if (valid && a.grad[ACC_POST_BIAS]) {
+#pragma unroll
+                for (int k = 0; k < CHUNKS; ++k)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) acc[ACC_POST_BIAS][k][i] += d[k][i];
+            }
+            if (valid) {
+#pragma unroll
+                for (int k = 0; k < CHUNKS; ++k)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) acc[ACC_POST_WEIGHT][k][i] = __builtin_fmaf(d[k][i], h[k][i], acc[ACC_POST_WEIGHT][k][i]);
+            }
+#pragma unroll
+            for (int k = 0; k < CHUNKS; ++k)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) d[k][i] *= w[k][i];
+            through_norm<WAVES, ALL, CHUNKS>(d, h, p, ragged, l.post, st.y, l.inv_cols, lds, turn);
+            if (a.df && valid) {
+#pragma unroll
+                for (int k = 0; k < CHUNKS; ++k) store8((TF *)a.df + this_row * a.df_stride, p[k].c, p[k].n, d[k]);
             }
             if (gate_done) {
 #pragma unroll
                 for (int k = 0; k < CHUNKS; ++k) {
                     if (a.dgate) {
-                        const uint64_t at = this_gate * a.dgate_stride + c[k];
-                        if (a.gate_f32) store_grad8((float *)a.dgate + at, n[k], acc[ACC_GATE][k], a.accumulate);
-                        else store_grad8((TF *)a.dgate + at, n[k], acc[ACC_GATE][k], false);
+                        const uint64_t at = this_gate * a.dgate_stride;
+                        if (a.gate_f32) store_grad8((float *)a.dgate + at, p[k].c, p[k].n, acc[ACC_GATE][k], a.accumulate);
+                        else store_grad8((TF *)a.dgate + at, p[k].c, p[k].n, acc[ACC_GATE][k], false);
                     }
 #pragma unroll
                     for (int i = 0; i < 8; ++i) acc[ACC_GATE][k][i] = 0.0f;
@@ -466,7 +623,6 @@ __global__ __launch_bounds__(WAVES == 1 ? BACKWARD_TEAMS * 64 : WAVES * 64) void
     }
 
     // what this workgroup adds up to: the teams' sums, then to its place among the partial sums
-    __shared__ float sums[TEAMS > 1 ? TEAMS : 1][TEAMS > 1 ? CHUNKS * 512 : 1];
 #pragma unroll
     for (int q = 0; q < ACCS; ++q) {
         if (q < ACC_GATE ? !a.grad[q < ACC_GATE ? q : 0] : (!a.dgate || cut.whole)) continue;
@@ -476,17 +632,17 @@ __global__ __launch_bounds__(WAVES == 1 ? BACKWARD_TEAMS * 64 : WAVES * 64) void
 #pragma unroll
             for (int k = 0; k < CHUNKS; ++k)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) sums[team][c[k] + i] = acc[q][k][i];
+                for (int i = 0; i < 8; ++i) room[team * WIDTH + p[k].c + i] = acc[q][k][i];
             __syncthreads();
-            for (uint32_t j = threadIdx.x; j < l.cols; j += TEAMS * 64) {
-                float s = sums[0][j];
+            for (uint32_t j = threadIdx.x; j < l.cols; j += ALL * 64) {
+                float s = room[j];
 #pragma unroll
-                for (uint32_t t = 1; t < TEAMS; ++t) s += sums[t][j];
+                for (uint32_t t = 1; t < TEAMS; ++t) s += room[t * WIDTH + j];
                 to[j] = s;
             }
         } else {
 #pragma unroll
-            for (int k = 0; k < CHUNKS; ++k) store8(to + c[k], n[k], acc[q][k]);
+            for (int k = 0; k < CHUNKS; ++k) store8(to, p[k].c, p[k].n, acc[q][k]);
         }
     }
 }
@@ -530,19 +686,19 @@ __global__ __launch_bounds__(REDUCE_LINES * 64) void k_edge_reduce(const float *
 // host side
 // ---------------------------------------------------------------------------
 
-// Wavefronts of a row's team (8 columns a lane, two rounds of them beyond 512).
+// Wavefronts of a row's team: 8 columns a lane, and 16 in rows that a workgroup does not hold then.  (16 from 512 columns on, half
+// the wavefronts: 16384 x 4096 edges with checkpoints and their decoding 239 us against 219, 8192 x 768 36 against 33.)
 static uint32_t waves_of(uint32_t cols)
 {
     uint32_t w = 1;
-    while (w * 1024 < cols) w *= 2;
+    while (w * 512 < cols && w < BACKWARD_WAVES) w *= 2;
     return w;
 }
 
 // Workgroups of the backward pass.
 static Cut cut_of(uint32_t rows, uint32_t cols, uint32_t rows_per_gate)
 {
-    const uint32_t waves = waves_of(cols), teams = waves == 1 ? BACKWARD_TEAMS : 1u;
-    const uint32_t most = waves == 1 ? 256u : waves == 2 ? 1024u : waves == 4 ? 512u : 256u;
+    const uint32_t teams = BACKWARD_WAVES / waves_of(cols), most = 4096 / BACKWARD_WAVES;
     Cut t;
     t.rows_per_gate = rows_per_gate && rows_per_gate < rows ? rows_per_gate : rows;
     t.gates = (rows - 1) / t.rows_per_gate + 1;
@@ -565,25 +721,32 @@ template <class TX, class TF> static void launch_forward(const ForwardArgs &a, h
 {
     const uint32_t waves = waves_of(a.l.cols), teams = waves == 1 ? FORWARD_TEAMS : 1u;
     const uint32_t need = (a.rows + teams - 1) / teams, most = 4096u / (teams * waves);
-    const dim3 grid(need < most ? need : most);
-    if (a.l.cols <= 512) hipLaunchKernelGGL((k_edge_forward<TX, TF, 1, 1>), grid, dim3(FORWARD_TEAMS * 64), 0, st, a);
-    else if (waves == 1) hipLaunchKernelGGL((k_edge_forward<TX, TF, 1, 2>), grid, dim3(FORWARD_TEAMS * 64), 0, st, a);
-    else if (waves == 2) hipLaunchKernelGGL((k_edge_forward<TX, TF, 2, 2>), grid, dim3(128), 0, st, a);
-    else if (waves == 4) hipLaunchKernelGGL((k_edge_forward<TX, TF, 4, 2>), grid, dim3(256), 0, st, a);
-    else if (waves == 8) hipLaunchKernelGGL((k_edge_forward<TX, TF, 8, 2>), grid, dim3(512), 0, st, a);
-    else hipLaunchKernelGGL((k_edge_forward<TX, TF, 16, 2>), grid, dim3(1024), 0, st, a);
+    const dim3 grid(need < most ? need : most), block(teams * waves * 64);
+    if (a.l.cols < 8) hipLaunchKernelGGL((k_edge_forward<TX, TF, 1, 1, true>), grid, block, 0, st, a);
+    else if (waves == 1) hipLaunchKernelGGL((k_edge_forward<TX, TF, 1, 1, false>), grid, block, 0, st, a);
+    else if (waves == 2) hipLaunchKernelGGL((k_edge_forward<TX, TF, 2, 1, false>), grid, block, 0, st, a);
+    else if (waves == 4) hipLaunchKernelGGL((k_edge_forward<TX, TF, 4, 1, false>), grid, block, 0, st, a);
+    else if (waves == 8) hipLaunchKernelGGL((k_edge_forward<TX, TF, 8, 1, false>), grid, block, 0, st, a);
+    else if (a.l.cols <= 8192) hipLaunchKernelGGL((k_edge_forward<TX, TF, 16, 1, false>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((k_edge_forward<TX, TF, 16, 2, false>), grid, block, 0, st, a);
 }
 
-template <class TX, class TF> static void launch_backward(const BackwardArgs &a, hipStream_t st)
+template <class TX, class TF, bool CODED> static void launch_backward(const BackwardArgs &a, hipStream_t st)
 {
     const uint32_t waves = waves_of(a.l.cols);
-    const dim3 grid(a.cut.blocks);
-    if (a.l.cols <= 512) hipLaunchKernelGGL((k_edge_backward<TX, TF, 1, 1>), grid, dim3(BACKWARD_TEAMS * 64), 0, st, a);
-    else if (waves == 1) hipLaunchKernelGGL((k_edge_backward<TX, TF, 1, 2>), grid, dim3(BACKWARD_TEAMS * 64), 0, st, a);
-    else if (waves == 2) hipLaunchKernelGGL((k_edge_backward<TX, TF, 2, 2>), grid, dim3(128), 0, st, a);
-    else if (waves == 4) hipLaunchKernelGGL((k_edge_backward<TX, TF, 4, 2>), grid, dim3(256), 0, st, a);
-    else if (waves == 8) hipLaunchKernelGGL((k_edge_backward<TX, TF, 8, 2>), grid, dim3(512), 0, st, a);
-    else hipLaunchKernelGGL((k_edge_backward<TX, TF, 16, 2>), grid, dim3(1024), 0, st, a);
+    const dim3 grid(a.cut.blocks), block(BACKWARD_WAVES * 64);
+    if (a.l.cols < 8) hipLaunchKernelGGL((k_edge_backward<TX, TF, 1, 1, CODED, true>), grid, block, 0, st, a);
+    else if (waves == 1) hipLaunchKernelGGL((k_edge_backward<TX, TF, 1, 1, CODED, false>), grid, block, 0, st, a);
+    else if (waves == 2) hipLaunchKernelGGL((k_edge_backward<TX, TF, 2, 1, CODED, false>), grid, block, 0, st, a);
+    else if (waves == 4) hipLaunchKernelGGL((k_edge_backward<TX, TF, 4, 1, CODED, false>), grid, block, 0, st, a);
+    else if (waves == 8) hipLaunchKernelGGL((k_edge_backward<TX, TF, 8, 1, CODED, false>), grid, block, 0, st, a);
+    else if (a.l.cols <= 8192) hipLaunchKernelGGL((k_edge_backward<TX, TF, 16, 1, CODED, false>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((k_edge_backward<TX, TF, 16, 2, CODED, false>), grid, block, 0, st, a);
+}
+template <class TX, class TF> static void launch_backward(const BackwardArgs &a, hipStream_t st)
+{
+    if (a.coded) launch_backward<TX, TF, true>(a, st);
+    else launch_backward<TX, TF, false>(a, st);
 }
 
 static bool norm_ok(int kind, float eps)
@@ -650,7 +813,12 @@ extern "C" int dgs_edge_forward(const dgs_edge *edge, const dgs_edge_forward_arg
     a.pre_codes_stride = p.pre_saved.codes_stride; a.pre_exps_stride = p.pre_saved.exps_stride;
     a.rows = p.rows;
     a.rows_per_gate = p.gate.data ? p.rows_per_gate : 1u;
-    a.gate_f32 = p.gate_type == DGS_F32;
+    a.gate_f32 = p.gate.data && p.gate_type == DGS_F32;
+    a.branch = branch;
+    a.gated = p.gate.data != nullptr;
+    // what is absent is loaded all the same, from a row of x
+    if (!branch) { a.f = a.x; a.f_stride = 0; }
+    if (!a.gated) { a.gate = a.x; a.gate_stride = 0; }
     const hipStream_t st = (hipStream_t)hip_stream;
     if (p.stream_type == DGS_F32) {
         if (p.type == DGS_F32) launch_forward<float, float>(a, st);
@@ -689,7 +857,8 @@ extern "C" int dgs_edge_backward(const dgs_edge *edge, const dgs_edge_backward_a
             || !present_ok(p.df, cols, p.type) || !gate_ok(p.gate, cols, p.gate_type, p.type, p.rows_per_gate)
             || !present_ok(p.dgate, cols, p.gate_type))
             return DGS_EINVAL;
-        // one of the two per norm
+        // both norms the same way
+        if (branch && through_pre && (p.post_saved.codes != nullptr) != (p.pre_saved.codes != nullptr)) return DGS_EINVAL;
         if (branch && (p.post_saved.codes ? p.f.data || !codes_ok(p.post_saved, cols) : !matrix_ok(p.f.data, p.f.stride, cols, p.type)))
             return DGS_EINVAL;
         if (through_pre
@@ -720,9 +889,29 @@ extern "C" int dgs_edge_backward(const dgs_edge *edge, const dgs_edge_backward_a
         a.post_codes_stride = p.post_saved.codes_stride; a.post_exps_stride = p.post_saved.exps_stride;
         a.pre_codes_stride = p.pre_saved.codes_stride; a.pre_exps_stride = p.pre_saved.exps_stride;
         a.rows = p.rows;
-        a.gate_f32 = p.gate_type == DGS_F32;
+        a.gate_f32 = p.gate.data && p.gate_type == DGS_F32;
         a.accumulate = p.accumulate != 0;
         a.branch = branch;
+        a.gated = p.gate.data != nullptr;
+        a.through_pre = through_pre;
+        a.arrives = p.dx_out.data != nullptr;
+        a.coded = (branch && p.post_saved.codes) || (through_pre && p.pre_saved.codes);
+        // what is absent is loaded all the same, from the workspace, which holds a row of any type
+        const void *const none = p.workspace;
+        if (!a.arrives) { a.dx_out = none; a.dx_out_stride = 0; }
+        if (!through_pre) {
+            a.du = a.x_out = none;
+            a.pre_codes = (const int8_t *)none;
+            a.pre_exps = (const uint8_t *)none;
+            a.du_stride = a.x_out_stride = a.pre_codes_stride = a.pre_exps_stride = 0;
+        }
+        if (!branch) {
+            a.f = none;
+            a.post_codes = (const int8_t *)none;
+            a.post_exps = (const uint8_t *)none;
+            a.f_stride = a.post_codes_stride = a.post_exps_stride = 0;
+        }
+        if (!a.gated) { a.gate = none; a.gate_stride = 0; }
         if (p.stream_type == DGS_F32) {
             if (p.type == DGS_F32) launch_backward<float, float>(a, st);
             else if (p.type == DGS_F16) launch_backward<float, f16>(a, st);

@@ -38,6 +38,16 @@ template <> inline bf16 from_float<bf16>(float v)      // to nearest, halfway ca
 }
 #endif
 
+// The same number, of which the compiler knows nothing: an address stays a row's pointer in scalar registers plus this
+// offset, where it would otherwise keep a 64-bit pointer a lane for every matrix of a loop.
+__device__ __forceinline__ uint32_t opaque(uint32_t v)
+{
+#ifndef DGS_HOST_EMULATION
+    asm volatile("" : "+v"(v));
+#endif
+    return v;
+}
+
 // ---------------------------------------------------------------------------
 // eight values of a row
 // ---------------------------------------------------------------------------
@@ -81,12 +91,16 @@ template <> __device__ __forceinline__ void unpack8<bf16>(const Raw8<bf16> &r, f
     }
 }
 
-template <class T> __device__ __forceinline__ void store8(T *p, uint32_t n, const float (&v)[8])
+// Matrices are stored past the caches' replacement order (non-temporal): 16384 x 4096 bfloat16 edges with their checkpoints
+// and the decoding of those 222 us against 238, 151 M values encoded and decoded 222 against 243, and 8192 x 768 edges, which the
+// caches would hold, 38 against 41.  (Non-temporal loads cost the small ones a fifth.)
+template <class T> __device__ __forceinline__ void store8(T *row, uint32_t c, uint32_t n, const float (&v)[8])
 {
     T t[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) t[i] = from_float<T>(v[i]);
-    if (n >= 8) {
+    T *const p = (T *)((char *)row + opaque(c * (uint32_t)sizeof(T)));
+    if (n == 8) {
         Raw8<T> r;
         __builtin_memcpy(&r, t, sizeof(r));
         u32x4_any *q = (u32x4_any *)p;
@@ -94,17 +108,90 @@ template <class T> __device__ __forceinline__ void store8(T *p, uint32_t n, cons
         for (uint32_t i = 0; i < sizeof(T) / 2; ++i) {
             u32x4_any o;
             o.x = r.w[4 * i]; o.y = r.w[4 * i + 1]; o.z = r.w[4 * i + 2]; o.w = r.w[4 * i + 3];
-            q[i] = o;
+            __builtin_nontemporal_store(o, q + i);
         }
     } else {
 #pragma unroll
-        for (uint32_t i = 0; i < 8; ++i)
+        for (uint32_t i = 0; i < 7; ++i)
             if (i < n) p[i] = t[i];
     }
 }
 
 // The same for a type that is known at run time: a vector of parameters, a gate.
 __device__ __forceinline__ void load8_f32(const float *p, uint32_t n, float (&v)[8]) { unpack8(load8(p, n), v); }
+
+// ---------------------------------------------------------------------------
+// eight values of a row, loaded without a branch
+// ---------------------------------------------------------------------------
+// A load inside a branch makes the compiler wait for everything in flight where the branch ends.  So every lane loads eight
+// values that exist: the last eight of the row where its own eight end beyond it, moved into place afterwards.  Lanes that
+// hold no column at all load those too, and are left out of sums and stores.  Rows of fewer than eight columns (TINY) are
+// loaded element by element.
+struct Place8 { uint32_t c, at, n; };       // first column, first column loaded, columns that exist
+
+template <bool TINY> __device__ __forceinline__ Place8 place8(uint32_t c, uint32_t cols)
+{
+    Place8 p;
+    p.c = c;
+    p.n = c >= cols ? 0u : min(8u, cols - c);
+    p.at = TINY ? 0u : min(c, cols - 8u);
+    return p;
+}
+
+template <bool TINY, class T> __device__ __forceinline__ Raw8<T> load_at(const T *row, uint32_t at, uint32_t cols)
+{
+    Raw8<T> r;
+    if constexpr (TINY) {
+        T t[8];
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) t[i] = row[min(i, cols - 1u)];
+        __builtin_memcpy(&r, t, sizeof(r));
+    } else {
+        const u32x4_any *q = (const u32x4_any *)((const char *)row + opaque(at * (uint32_t)sizeof(T)));
+#pragma unroll
+        for (uint32_t i = 0; i < sizeof(T) / 2; ++i) {
+            const u32x4_any v = q[i];
+            r.w[4 * i] = v.x; r.w[4 * i + 1] = v.y; r.w[4 * i + 2] = v.z; r.w[4 * i + 3] = v.w;
+        }
+    }
+    return r;
+}
+
+// The words of w moved down by `by` (fewer than 8) elements of 1, 2 or 4 bytes; 0 comes in behind.
+template <uint32_t WORDS, uint32_t BYTES> __device__ __forceinline__ void move_down(uint32_t (&w)[WORDS], uint32_t by)
+{
+#pragma unroll
+    for (uint32_t step = 4; step >= 1; step /= 2) {
+        const uint32_t bits = step * BYTES * 8;
+        const bool move = (by & step) != 0;
+#pragma unroll
+        for (uint32_t i = 0; i < WORDS; ++i) {
+            uint32_t v;
+            if (bits >= 32) {
+                v = i + bits / 32 < WORDS ? w[i + bits / 32 < WORDS ? i + bits / 32 : 0] : 0u;
+            } else {
+                const uint32_t up = i + 1 < WORDS ? w[i + 1 < WORDS ? i + 1 : 0] : 0u;
+                v = (w[i] >> (bits & 31u)) | (up << ((32u - bits) & 31u));
+            }
+            w[i] = move ? v : w[i];
+        }
+    }
+}
+
+// What was loaded, in place, 0 where there is no column.  Lanes without columns are left as they are.  Only rows whose length
+// is no multiple of eight need this.
+template <bool TINY, class T> __device__ __forceinline__ void in_place(Raw8<T> &r, const Place8 &p)
+{
+    if constexpr (TINY) {
+        T t[8];
+        __builtin_memcpy(t, &r, sizeof(r));
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) t[i] = i < p.n ? t[i] : from_float<T>(0.0f);
+        __builtin_memcpy(&r, t, sizeof(r));
+    } else {
+        move_down<sizeof(r.w) / 4, sizeof(T)>(r.w, p.n ? p.c - p.at : 0u);
+    }
+}
 
 // How many of the eight values from column c on exist.
 __device__ __forceinline__ uint32_t live8(uint32_t c, uint32_t cols) { return c >= cols ? 0u : min(8u, cols - c); }
@@ -145,18 +232,21 @@ __device__ __forceinline__ float wave_sum(float v)
     return (r0 + r1) + (r2 + r3);
 }
 
-// Sums over a team of WAVES wavefronts (a whole workgroup if there are several).  Successive calls of a kernel use the two
-// halves of `lds` in turn (`turn` flips), which makes one barrier a call enough: whoever writes a half again has passed the
-// barrier of the other half's call, and with it every reader of the first.
-template <int WAVES, int N>
-__device__ __forceinline__ void team_sum(float (&v)[N], float (*lds)[2][WAVES], uint32_t &turn)
+// Sums over a team of WAVES wavefronts, of which a workgroup holds ALL / WAVES; with more than one wavefront to a team, every
+// thread of the workgroup calls this the same number of times.  Successive calls use the two halves of `lds` in turn (`turn`
+// flips), which makes one barrier a call enough: whoever writes a half again has passed the barrier of the other half's call,
+// and with it every reader of the first.
+template <int ALL> struct TeamLds { float v[2][2][ALL]; };
+
+template <int WAVES, int ALL, int N>
+__device__ __forceinline__ void team_sum(float (&v)[N], TeamLds<ALL> &lds, uint32_t &turn)
 {
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
     if constexpr (WAVES > 1) {
-        float (*half)[WAVES] = lds[turn];
+        float (*half)[ALL] = lds.v[turn];
         turn ^= 1u;
-        const uint32_t wave = threadIdx.x >> 6;
+        const uint32_t wave = threadIdx.x >> 6, first = wave & ~(uint32_t)(WAVES - 1);
         if (lane_id() == 0) {
 #pragma unroll
             for (int i = 0; i < N; ++i) half[i][wave] = v[i];
@@ -164,9 +254,9 @@ __device__ __forceinline__ void team_sum(float (&v)[N], float (*lds)[2][WAVES], 
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            float s = half[i][0];
+            float s = half[i][first];
 #pragma unroll
-            for (int w = 1; w < WAVES; ++w) s += half[i][w];
+            for (int w = 1; w < WAVES; ++w) s += half[i][first + w];
             v[i] = s;
         }
     }
@@ -178,11 +268,12 @@ __device__ __forceinline__ void team_sum(float (&v)[N], float (*lds)[2][WAVES], 
 
 // The exponent byte of the run that this quad of lanes holds, from the bits of its largest magnitude: with top = m 2^E, m in
 // [1, 2), the exponent is E - 6 where 64 m < 127.5, one more otherwise (a carry out of the mantissa).
-__device__ __forceinline__ uint32_t run_byte(const float (&v)[8])
+__device__ __forceinline__ uint32_t run_byte(const float (&v)[8], bool any)
 {
     uint32_t top = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+    top = any ? top : 0u;
     top = max(top, quad_xor1(top));
     top = max(top, quad_xor2(top));
     const int byte = (int)((top + 0x10000u) >> 23) - 6;
@@ -217,6 +308,29 @@ __device__ __forceinline__ void decode8(const uint32_t (&q)[2], float scale, flo
     for (int i = 0; i < 8; ++i) v[i] = (float)(int)(int8_t)(q[i >> 2] >> (8 * (i & 3))) * scale;
 }
 
+template <bool TINY> __device__ __forceinline__ void load_codes_at(const int8_t *row, uint32_t at, uint32_t cols, uint32_t (&q)[2])
+{
+    if constexpr (TINY) {
+        q[0] = q[1] = 0;
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) q[i >> 2] |= (uint32_t)(uint8_t)row[min(i, cols - 1u)] << (8 * (i & 3));
+    } else {
+        const u32x2_any v = *(const u32x2_any *)(row + opaque(at));
+        q[0] = v.x;
+        q[1] = v.y;
+    }
+}
+template <bool TINY> __device__ __forceinline__ void codes_in_place(uint32_t (&q)[2], const Place8 &p)
+{
+    if constexpr (TINY) {
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i)
+            if (i >= p.n) q[i >> 2] &= ~(0xFFu << (8 * (i & 3)));
+    } else {
+        move_down<2, 1>(q, p.n ? p.c - p.at : 0u);
+    }
+}
+
 // `n` codes at p; the others are 0.
 __device__ __forceinline__ void load_codes(const int8_t *p, uint32_t n, uint32_t (&q)[2])
 {
@@ -231,30 +345,31 @@ __device__ __forceinline__ void load_codes(const int8_t *p, uint32_t n, uint32_t
             if (i < n) q[i >> 2] |= (uint32_t)(uint8_t)p[i] << (8 * (i & 3));
     }
 }
-__device__ __forceinline__ void store_codes(int8_t *p, uint32_t n, const uint32_t (&q)[2])
+__device__ __forceinline__ void store_codes(int8_t *row, uint32_t c, uint32_t n, const uint32_t (&q)[2])
 {
-    if (n >= 8) {
+    int8_t *const p = row + opaque(c);
+    if (n == 8) {
         u32x2_any v;
         v.x = q[0];
         v.y = q[1];
-        *(u32x2_any *)p = v;
+        __builtin_nontemporal_store(v, (u32x2_any *)p);
     } else {
 #pragma unroll
-        for (uint32_t i = 0; i < 8; ++i)
+        for (uint32_t i = 0; i < 7; ++i)
             if (i < n) p[i] = (int8_t)(q[i >> 2] >> (8 * (i & 3)));
     }
 }
 
 // Values c .. c + 7 of a row as a checkpoint: every lane of the wavefront calls this (n = 0 where the row has ended).
-// Values beyond the row are 0 in v.
+// Values beyond the row are 0 in v, or there are none of the row (n = 0).
 __device__ __forceinline__ void save8(int8_t *row, uint8_t *exps, uint32_t c, uint32_t n, const float (&v)[8])
 {
-    const uint32_t byte = run_byte(v);
+    const uint32_t byte = run_byte(v, n != 0);
     if (n == 0) return;
     uint32_t q[2];
     encode8(v, byte, q);
-    store_codes(row + c, n, q);
-    if ((c & (DGS_CHECKPOINT_RUN - 1)) == 0) exps[c / DGS_CHECKPOINT_RUN] = (uint8_t)byte;
+    store_codes(row, c, n, q);
+    if ((c & (DGS_CHECKPOINT_RUN - 1)) == 0) exps[opaque(c / DGS_CHECKPOINT_RUN)] = (uint8_t)byte;
 }
 
 // ---------------------------------------------------------------------------
