@@ -39,6 +39,16 @@ __device__ __forceinline__ u32x2 read_turned(const uint16_t *p)
 }
 #endif
 
+// The upper halves of two words, `lo`'s below.
+__device__ __forceinline__ uint32_t upper_halves(uint32_t lo, uint32_t hi)
+{
+#ifdef DGS_HOST_EMULATION
+    return (lo >> 16) | (hi & 0xFFFF0000u);
+#else
+    return __builtin_amdgcn_perm(hi, lo, 0x07060302u);
+#endif
+}
+
 // The parts of eight values, eight bfloat16 each.
 template <class T> constexpr int PARTS = sizeof(T) == 4 ? 3 : __is_same(T, bf16) ? 1 : 2;
 
@@ -61,7 +71,7 @@ template <class T> __device__ __forceinline__ void split8(const Raw8<T> &r, u32x
                 v[i] = finite ? v[i] - __uint_as_float(b[i] & 0xFFFF0000u) : 0.0f;
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) part[p][i] = (b[2 * i] >> 16) | (b[2 * i + 1] & 0xFFFF0000u);
+            for (int i = 0; i < 4; ++i) part[p][i] = upper_halves(b[2 * i], b[2 * i + 1]);
         }
     }
 }
@@ -73,7 +83,7 @@ __device__ __forceinline__ u32x4 values8(const uint32_t (&q)[2], uint32_t byte)
     decode8(q, run_scale(byte), v);
     u32x4 o;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] = (__float_as_uint(v[2 * i]) >> 16) | (__float_as_uint(v[2 * i + 1]) & 0xFFFF0000u);
+    for (int i = 0; i < 4; ++i) o[i] = upper_halves(__float_as_uint(v[2 * i]), __float_as_uint(v[2 * i + 1]));
     return o;
 }
 
@@ -216,49 +226,406 @@ __global__ __launch_bounds__(GRAD_THREADS) void k_weight_grad(GradArgs a)
     }
 }
 
-// Adds up the splits' partial sums (where there are any) and finishes: one output row a workgroup row, 256 columns a block.
+// ---------------------------------------------------------------------------
+// the large tile
+// ---------------------------------------------------------------------------
+// 256 x 256 to a workgroup of four wavefronts, 128 x 128 to a wavefront: per 16 rows a wavefront reads 8 KB of LDS for 16
+// matrix instructions, half of what the tile above reads, and the LDS keeps up with the matrix units.  One wavefront to a
+// SIMD, so the overlap is written down: the fragments of a slice of 16 rows are read while the slice before is multiplied,
+// the next step's rows are staged between the slices, and the barrier stands before a step's last slice, behind which the
+// first fragments of the next step are read.
+template <uint32_t WIDTH> __device__ __forceinline__ uint32_t wide_at(uint32_t k, uint32_t c) { return k * WIDTH + ((c ^ ((k & 3u) << 2)) << 3); }
+
+template <uint32_t W> struct Width { static constexpr uint32_t value = W; };
+
+// Between two matrix instructions: fragment reads, a share of what the next step's staging takes.
+template <int COUNT> __device__ __forceinline__ void interleave(bool staging)
+{
+#if !defined(DGS_HOST_EMULATION) && 1
+    if (staging) {
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);      // matrix
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);      // LDS read
+            __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);    // vector
+            if (i % 3 == 0) __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);      // LDS write
+            if (i % 2 == 0) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);      // memory read
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        }
+    }
+#endif
+}
+
+template <class T, uint32_t STEP, uint32_t OUTS, uint32_t COLS, uint32_t WAVES, uint32_t TALL, bool RAGGED>
+__global__ __launch_bounds__(WAVES * 64, 2) void k_weight_grad_tile(GradArgs a)
+{
+    constexpr int P = PARTS<T>;
+    // wavefronts: TALL of them one below another, SIDE beside each other, I x J squares of 32 x 32 to each
+    constexpr uint32_t THREADS = WAVES * 64, SIDE = WAVES / TALL, I = OUTS / 32 / TALL, J = COLS / 32 / SIDE, SLICES = STEP / 16;
+    // staging: pieces of eight columns, rows from pass to pass, passes -- of dy, and of the codes
+    constexpr uint32_t PIECES_O = OUTS / 8, APART_O = THREADS / PIECES_O, PASSES_O = STEP / APART_O;
+    constexpr uint32_t PIECES_C = COLS / 8, APART_C = THREADS / PIECES_C, PASSES_C = STEP / APART_C;
+    __shared__ __attribute__((aligned(16))) uint16_t la[2][P][STEP * OUTS], lb[2][STEP * COLS];
+    const uint32_t lane = lane_id(), wave = uniform(threadIdx.x >> 6);
+    const uint32_t total = gridDim.x, die = blockIdx.x & 7u;
+    const uint32_t at = (die * (total >> 3) + min(die, total & 7u)) + (blockIdx.x >> 3);
+    const uint32_t split = at / a.tiles, tile = at - split * a.tiles;
+    const uint32_t tile_o = tile / a.col_tiles, tile_c = tile - tile_o * a.col_tiles;
+    const uint32_t row_first = split * a.split_rows;
+    const uint32_t row_end = min(a.rows - row_first, a.split_rows) + row_first;
+    const uint32_t steps = (row_end - row_first + STEP - 1) / STEP;
+
+    // what this thread stages
+    const uint32_t piece_o = threadIdx.x % PIECES_O, first_o = threadIdx.x / PIECES_O;
+    const uint32_t piece_c = threadIdx.x % PIECES_C, first_c = threadIdx.x / PIECES_C;
+    const Place8 po = place8<false>(tile_o * OUTS + piece_o * 8, a.outs), pc = place8<false>(tile_c * COLS + piece_c * 8, a.cols);
+    const uint32_t run = min(pc.c, a.cols - 1u) / DGS_CHECKPOINT_RUN;
+    // (whether a row ends inside one of this tile's pieces)
+    const bool cut_o = RAGGED && tile_o * OUTS + OUTS > a.outs, cut_c = RAGGED && tile_c * COLS + COLS > a.cols;
+    Raw8<T> ra[PASSES_O];
+    uint32_t rq[PASSES_C][2], rb[PASSES_C];
+    // Step 0 holds the rows that do not fill a step, and the others are full: no step in the loop has to look.
+    const uint32_t head = row_end - row_first - (steps - 1) * STEP;
+    // In the loop addresses are scalar: pointers to a pass's first row, and an offset a lane.
+    const uint64_t dy_bytes = a.dy_stride * sizeof(T);
+    const uint32_t dy_lane = first_o * (uint32_t)dy_bytes + po.at * (uint32_t)sizeof(T);
+    const uint32_t codes_lane = first_c * (uint32_t)a.codes_stride + pc.at, exps_lane = first_c * (uint32_t)a.exps_stride + run;
+    const char *dy_p;
+    const int8_t *codes_p;
+    const uint8_t *exps_p;
+    auto point_to = [&](uint32_t r) {
+        dy_p = (const char *)a.dy + r * dy_bytes;
+        codes_p = a.codes + r * a.codes_stride;
+        exps_p = a.exps + r * a.exps_stride;
+    };
+    auto fetch_o = [&](uint32_t p) {
+        const u32x4_any *const d = (const u32x4_any *)(dy_p + dy_lane);
+#pragma unroll
+        for (uint32_t i = 0; i < sizeof(T) / 2; ++i) {
+            const u32x4_any v = d[i];
+            ra[p].w[4 * i] = v.x; ra[p].w[4 * i + 1] = v.y; ra[p].w[4 * i + 2] = v.z; ra[p].w[4 * i + 3] = v.w;
+        }
+        dy_p += APART_O * dy_bytes;
+    };
+    auto fetch_c = [&](uint32_t p) {
+        const u32x2_any q = *(const u32x2_any *)(codes_p + codes_lane);
+        rq[p][0] = q.x;
+        rq[p][1] = q.y;
+        rb[p] = exps_p[exps_lane];
+        codes_p += APART_C * a.codes_stride;
+        exps_p += APART_C * a.exps_stride;
+    };
+    float bias[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) bias[i] = 0.0f;
+    uint32_t bias_turn = 0;     // step % col_tiles: the column tiles share out the rows of the bias gradient
+    auto add_bias = [&](uint32_t there) {
+        if (a.bias_sums && bias_turn == tile_c) {
+#pragma unroll
+            for (uint32_t p = 0; p < PASSES_O; ++p) {
+                if (first_o + APART_O * p >= there) continue;
+                Raw8<T> r = ra[p];
+                if (cut_o) in_place<false>(r, po);
+                float v[8];
+                unpack8(r, v);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) bias[i] += v[i];
+            }
+        }
+        bias_turn = bias_turn + 1 == a.col_tiles ? 0 : bias_turn + 1;
+    };
+    auto stage_o = [&](uint32_t buf, uint32_t p) {
+        if (cut_o) in_place<false>(ra[p], po);
+        const uint32_t to = wide_at<OUTS>(first_o + APART_O * p, piece_o);
+        u32x4 part[P];
+        split8(ra[p], part);
+#pragma unroll
+        for (int i = 0; i < P; ++i) *(u32x4 *)&la[buf][i][to] = part[i];
+    };
+    auto stage_c = [&](uint32_t buf, uint32_t p) {
+        if (cut_c) codes_in_place<false>(rq[p], pc);
+        *(u32x4 *)&lb[buf][wide_at<COLS>(first_c + APART_C * p, piece_c)] = values8(rq[p], rb[p]);
+    };
+    const uint32_t turn_k = ((lane >> 5) << 3) + ((lane & 15u) >> 2), turn_c = ((lane >> 4) & 1u) * 2u + ((lane & 3u) >> 1);
+    auto fragment = [&](const uint16_t *m, auto width, uint32_t k, uint32_t c) {
+        u32x4 f;
+#pragma unroll
+        for (uint32_t r = 0; r < 2; ++r) {
+            const u32x2 v = read_turned(m + wide_at<width.value>(k + turn_k + 4 * r, c + turn_c) + (lane & 1u) * 4);
+            f[2 * r] = v.x;
+            f[2 * r + 1] = v.y;
+        }
+        return f;
+    };
+    f32x16 acc[I][J];
+#pragma unroll
+    for (uint32_t i = 0; i < I; ++i)
+#pragma unroll
+        for (uint32_t j = 0; j < J; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+    const uint32_t wo = wave / SIDE * (4 * I), wc = wave % SIDE * (4 * J);      // this wavefront's corner, in pieces
+    // fragments of the slice that is multiplied and of the next one
+    u32x4 fa[2][P][I], fb[2][J];
+    auto read = [&](uint32_t set, uint32_t buf, uint32_t slice) {
+#pragma unroll
+        for (uint32_t j = 0; j < J; ++j) fb[set][j] = fragment(lb[buf], Width<COLS>(), slice * 16, wc + 4 * j);
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (uint32_t i = 0; i < I; ++i) fa[set][p][i] = fragment(la[buf][p], Width<OUTS>(), slice * 16, wo + 4 * i);
+    };
+    auto multiply = [&](uint32_t set) {
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (uint32_t i = 0; i < I; ++i)
+#pragma unroll
+                for (uint32_t j = 0; j < J; ++j) acc[i][j] = matrix_unit(fa[set][p][i], fb[set][j], acc[i][j]);
+    };
+
+#pragma unroll
+    for (uint32_t p = 0; p < PASSES_O; ++p)      // (rows that are not there: the last one)
+        ra[p] = load_at<false>((const T *)a.dy + min(row_first + first_o + APART_O * p, row_end - 1u) * a.dy_stride, po.at, a.outs);
+#pragma unroll
+    for (uint32_t p = 0; p < PASSES_C; ++p) {
+        const uint32_t r = min(row_first + first_c + APART_C * p, row_end - 1u);
+        load_codes_at<false>(a.codes + r * a.codes_stride, pc.at, a.cols, rq[p]);
+        rb[p] = (a.exps + r * a.exps_stride)[run];
+    }
+    add_bias(head);
+#pragma unroll
+    for (uint32_t p = 0; p < PASSES_O; ++p) {
+        if (first_o + APART_O * p >= head) {
+#pragma unroll
+            for (uint32_t i = 0; i < 2 * sizeof(T); ++i) ra[p].w[i] = 0;
+        }
+        stage_o(0, p);
+    }
+#pragma unroll
+    for (uint32_t p = 0; p < PASSES_C; ++p) {
+        if (first_c + APART_C * p >= head) {
+            rq[p][0] = rq[p][1] = 0;
+            rb[p] = 1;
+        }
+        stage_c(0, p);
+    }
+    // (what is asked for beyond the last step is not used: the matrix's last rows, of which there are enough)
+    uint32_t row = row_first + head;
+    point_to(min(row, a.rows - STEP));
+#pragma unroll
+    for (uint32_t p = 0; p < PASSES_O; ++p) fetch_o(p);
+#pragma unroll
+    for (uint32_t p = 0; p < PASSES_C; ++p) fetch_c(p);
+    __syncthreads();
+    read(0, 0, 0);
+    for (uint32_t step = 0; step < steps; ++step) {
+        const uint32_t buf = step & 1u;
+        add_bias(step + 1 < steps ? STEP : 0u);
+        row += STEP;
+        if (row > a.rows - STEP) point_to(a.rows - STEP);
+#pragma unroll
+        for (uint32_t slice = 0; slice < SLICES; ++slice) {
+            if (slice + 1 < SLICES) {
+                read((slice + 1) & 1u, buf, slice + 1);
+#pragma unroll
+                for (uint32_t p = slice * PASSES_O / (SLICES - 1); p < (slice + 1) * PASSES_O / (SLICES - 1); ++p) {
+                    constexpr uint32_t EACH = PASSES_O / PASSES_C;
+                    stage_o(buf ^ 1u, p);
+                    if (p % EACH == 0) stage_c(buf ^ 1u, p / EACH);
+                    fetch_o(p);
+                    if (p % EACH == 0) fetch_c(p / EACH);
+                }
+            } else {
+                __syncthreads();
+                read((slice + 1) & 1u, buf ^ 1u, 0);
+            }
+            multiply(slice & 1u);
+            interleave<2 * I * J * P>(slice + 1 < SLICES);
+        }
+    }
+
+    const bool whole = a.dw != nullptr;
+    float *const out = whole ? a.dw : a.sums + (uint64_t)split * a.outs * a.cols;
+    const uint64_t stride = whole ? a.dw_stride : a.cols;
+#pragma unroll
+    for (uint32_t j = 0; j < J; ++j) {
+        const uint32_t c = tile_c * COLS + wc * 8 + 32 * j + (lane & 31u);
+        if (c >= a.cols) continue;
+        const float scale = whole && a.scale ? a.scale[c] : 1.0f;
+#pragma unroll
+        for (uint32_t i = 0; i < I; ++i)
+#pragma unroll
+            for (uint32_t r = 0; r < 16; ++r) {
+                const uint32_t o = tile_o * OUTS + wo * 8 + 32 * i + (r & 3u) + 8 * (r >> 2) + 4 * (lane >> 5);
+                if (o >= a.outs) continue;
+                float *p = out + o * stride + c;
+                const float v = acc[i][j][r] * scale;
+                *p = whole && a.accumulate ? *p + v : v;
+            }
+    }
+    if (a.bias_sums) {      // the threads of a piece of columns, one after another
+        float *const sums = (float *)&la[0][0][0];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sums[first_o * OUTS + piece_o * 8 + i] = bias[i];
+        __syncthreads();
+        const uint32_t o = tile_o * OUTS + threadIdx.x;
+        if (threadIdx.x < OUTS && o < a.outs) {
+            float sum = 0.0f;
+#pragma unroll
+            for (uint32_t q = 0; q < APART_O; ++q) sum += sums[q * OUTS + threadIdx.x];
+            a.bias_sums[((uint64_t)split * a.col_tiles + tile_c) * a.outs + o] = sum;
+        }
+    }
+}
+
+// Adds up the splits' partial sums (where there are any) and finishes: a wavefront an output row and 256 columns, four to a lane.
 __global__ __launch_bounds__(256) void k_weight_grad_finish(const float *sums, const float *bias_sums, const float *scale,
                                                             const float *shift, float *dw, uint64_t dw_stride, float *db, uint32_t outs,
                                                             uint32_t cols, uint32_t splits, uint32_t bias_parts, uint32_t accumulate)
 {
-    const uint32_t o = blockIdx.x, c = blockIdx.y * 256 + threadIdx.x;
-    float bias = 0.0f;
+    const uint32_t o = blockIdx.x * 4 + uniform(threadIdx.x >> 6), c = blockIdx.y * 256 + lane_id() * 4;
+    if (o >= outs) return;
+    const uint32_t n = !dw || c >= cols ? 0u : min(4u, cols - c);
+    float bias = 0.0f, s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     if (bias_sums) {
         for (uint32_t p = lane_id(); p < bias_parts; p += 64) bias += bias_sums[(uint64_t)p * outs + o];
-        bias = wave_sum(bias);
-        if (db && blockIdx.y == 0 && threadIdx.x == 0) db[o] = accumulate ? db[o] + bias : bias;
     }
-    if (!dw || c >= cols) return;
-    const float *p = sums + (uint64_t)o * cols + c;
-    float s = 0.0f;
-#pragma unroll 8
-    for (uint32_t i = 0; i < splits; ++i) s += p[(uint64_t)i * outs * cols];
-    if (scale) s *= scale[c];
-    if (shift) s = __builtin_fmaf(bias, shift[c], s);
-    float *q = dw + o * dw_stride + c;
-    *q = accumulate ? *q + s : s;
+    if (n && cols >= 4) {
+        // (four that exist, eight splits' at a time: where a row ends inside a lane's four, those before its end)
+        const uint32_t at = min(c, cols - 4u);
+        const float *const p = sums + (uint64_t)o * cols + at;
+        for (uint32_t i = 0; i < splits; i += 8) {
+            f32x4_any v[8];
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j) v[j] = *(const f32x4_any *)(p + (uint64_t)min(i + j, splits - 1u) * outs * cols);
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j) {
+                if (i + j >= splits) continue;
+                s[0] += v[j].x; s[1] += v[j].y; s[2] += v[j].z; s[3] += v[j].w;
+            }
+        }
+        if (c != at) {
+            const uint32_t by = c - at;
+            s[0] = by == 1 ? s[1] : by == 2 ? s[2] : s[3];
+            s[1] = by == 1 ? s[2] : s[3];
+            s[2] = s[3];
+        }
+    } else {
+        for (uint32_t i = 0; i < splits; ++i)
+            for (uint32_t j = 0; j < n; ++j) s[j] += sums[((uint64_t)i * outs + o) * cols + c + j];
+    }
+    if (bias_sums) {
+        bias = wave_sum(bias);
+        if (db && blockIdx.y == 0 && lane_id() == 0) db[o] = accumulate ? db[o] + bias : bias;
+    }
+    if (n == 0) return;
+    float *const q = dw + o * dw_stride + c;
+#pragma unroll
+    for (uint32_t j = 0; j < 4; ++j) {
+        if (j >= n) continue;
+        if (scale) s[j] *= scale[c + j];
+        if (shift) s[j] = __builtin_fmaf(bias, shift[c + j], s[j]);
+        if (accumulate) s[j] += q[j];
+    }
+    if (n == 4) {
+        f32x4_any v;
+        v.x = s[0]; v.y = s[1]; v.z = s[2]; v.w = s[3];
+        *(f32x4_any *)q = v;
+    } else {
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j)
+            if (j < n) q[j] = s[j];
+    }
 }
 
 // ---------------------------------------------------------------------------
 // host side
 // ---------------------------------------------------------------------------
 
+// The tiles, largest first, and how a workgroup of each was timed: microseconds for a step of 64 rows with every compute unit
+// busy, for what comes before and behind the steps, and workgroups that run at a time.
+struct GradTile {
+    uint32_t outs, cols, step, at_once;
+    float per_step, fixed;
+};
+enum { TILE_256, TILE_256_128, TILE_128, TILE_ANY, TILES };
+static GradTile tile_of(int tile, int type)
+{
+    const int i = type == DGS_BF16 ? 0 : type == DGS_F16 ? 1 : 2;
+    constexpr float us_256_128[3] = {1.21f, 3.2f, 3.9f}, us_128[3] = {1.45f, 2.9f, 4.3f}, us_any[3] = {3.0f, 5.0f, 7.0f};
+    switch (tile) {
+    case TILE_256: return GradTile{256, 256, 64, 256, 1.92f, 8.0f};
+    case TILE_256_128: return GradTile{256, 128, i == 0 ? 64u : 32u, 256, us_256_128[i], 11.0f};
+    case TILE_128: return GradTile{128, 128, 32, 512, us_128[i], 7.0f};
+    default: return GradTile{GRAD_TILE, GRAD_TILE, GRAD_STEP, 512, us_any[i], 7.0f};
+    }
+}
+
 struct GradPlan {
+    int tile;
     uint32_t out_tiles, col_tiles, splits, split_rows;
 };
-static GradPlan grad_plan(uint32_t rows, uint32_t outs, uint32_t cols)
+static GradPlan plan_of(int tile, uint32_t rows, uint32_t outs, uint32_t cols, int type, float &us)
 {
+    const GradTile t = tile_of(tile, type);
     GradPlan g;
-    g.out_tiles = (outs - 1) / GRAD_TILE + 1;
-    g.col_tiles = (cols - 1) / GRAD_TILE + 1;
+    g.tile = tile;
+    g.out_tiles = (outs - 1) / t.outs + 1;
+    g.col_tiles = (cols - 1) / t.cols + 1;
     const uint64_t tiles = (uint64_t)g.out_tiles * g.col_tiles;
-    const uint32_t steps = rows ? (rows - 1) / GRAD_STEP + 1 : 0;
-    uint64_t splits = tiles >= 512 ? 1 : 512 / tiles;
+    const uint32_t steps = rows ? (rows - 1) / t.step + 1 : 0;
+    uint64_t splits = tiles >= t.at_once ? 1 : t.at_once / tiles;
     if (splits > steps / 4) splits = steps / 4;      // at least four steps each
     if (splits < 1) splits = 1;
-    g.split_rows = (steps + (uint32_t)splits - 1) / (uint32_t)splits * GRAD_STEP;
+    g.split_rows = (steps + (uint32_t)splits - 1) / (uint32_t)splits * t.step;
     g.splits = g.split_rows ? (rows - 1) / g.split_rows + 1 : 1;
+    const float rounds = (float)((tiles * g.splits - 1) / t.at_once + 1);
+    us = rounds * ((float)g.split_rows / 64.0f * t.per_step + t.fixed);
+    if (g.splits > 1) us += 4.0f + (float)g.splits * (float)outs * (float)cols * 8.0f / 4.5e6f;      // partial sums there and back
     return g;
+}
+// The tile that should take the least time.  What a whole tile's loads take for granted -- a step's rows, eight columns -- the
+// last kind does without.
+static GradPlan grad_plan(uint32_t rows, uint32_t outs, uint32_t cols, int type)
+{
+    float best, us;
+    if (rows < 64 || outs < 8 || cols < 8) return plan_of(TILE_ANY, rows, outs, cols, type, us);
+    GradPlan g = plan_of(TILE_128, rows, outs, cols, type, best);
+    for (int tile = type == DGS_BF16 ? TILE_256 : TILE_256_128; tile < TILE_128; ++tile) {
+#ifdef FORCE_TILE
+        if (tile != FORCE_TILE) continue;
+        best = 1e30f;
+#endif
+        const GradPlan other = plan_of(tile, rows, outs, cols, type, us);
+        if (us < best) {
+            best = us;
+            g = other;
+        }
+    }
+    return g;
+}
+template <class T, uint32_t STEP, uint32_t OUTS, uint32_t COLS, uint32_t WAVES, uint32_t TALL>
+static void launch_tile(const GradArgs &a, dim3 grid, hipStream_t st)
+{
+    if ((a.outs | a.cols) & 7u) hipLaunchKernelGGL((k_weight_grad_tile<T, STEP, OUTS, COLS, WAVES, TALL, true>), grid, dim3(WAVES * 64), 0, st, a);
+    else hipLaunchKernelGGL((k_weight_grad_tile<T, STEP, OUTS, COLS, WAVES, TALL, false>), grid, dim3(WAVES * 64), 0, st, a);
+}
+template <class T> static void launch_grad(const GradArgs &a, int tile, dim3 grid, hipStream_t st)
+{
+    constexpr uint32_t STEP = PARTS<T> == 1 ? 64 : 32;
+    if constexpr (PARTS<T> == 1) {
+        if (tile == TILE_256) return launch_tile<T, 64, 256, 256, 8, 2>(a, grid, st);
+    }
+    if (tile == TILE_256_128) launch_tile<T, STEP, 256, 128, 8, 4>(a, grid, st);
+    else if (tile == TILE_128) launch_tile<T, 32, 128, 128, 4, 2>(a, grid, st);
+    else hipLaunchKernelGGL(k_weight_grad<T>, grid, dim3(GRAD_THREADS), 0, st, a);
 }
 // floats of partial sums, and of bias sums
 static void grad_sizes(const GradPlan &g, uint32_t outs, uint32_t cols, uint64_t &sums, uint64_t &bias)
@@ -275,7 +642,7 @@ extern "C" size_t dgs_checkpoint_weight_grad_workspace(uint32_t rows, uint32_t o
 {
     if (outs == 0 || cols == 0 || !is_type(type)) return 0;
     uint64_t sums, bias;
-    grad_sizes(grad_plan(rows, outs, cols), outs, cols, sums, bias);
+    grad_sizes(grad_plan(rows, outs, cols, type), outs, cols, sums, bias);
     return (size_t)(sums + bias) * sizeof(float);
 }
 
@@ -287,8 +654,9 @@ extern "C" int dgs_checkpoint_weight_grad(const dgs_weight_grad_args *args, void
     if (!matrix_ok(p.dw, p.dw_stride, p.cols, DGS_F32) || !aligned_to(p.scale, 4) || !aligned_to(p.shift, 4) || !aligned_to(p.db, 4))
         return DGS_EINVAL;
     if (p.rows && (!matrix_ok(p.dy.data, p.dy.stride, p.outs, p.type) || !codes_ok(p.saved, p.cols))) return DGS_EINVAL;
-    const GradPlan g = grad_plan(p.rows, p.outs, p.cols);
+    const GradPlan g = grad_plan(p.rows, p.outs, p.cols, p.type);
     const uint64_t blocks = (uint64_t)g.out_tiles * g.col_tiles * g.splits;
+    if (p.dy.stride * type_bytes(p.type) > 0xFFFFFFFu || p.saved.codes_stride > 0xFFFFFFFu || p.saved.exps_stride > 0xFFFFFFFu) return DGS_ENOTSUP;
     if (p.rows > 0x7FFFFFFFu || p.outs > 0x7FFFFFu || p.cols > 0x7FFFFFu || blocks > 0xFFFFFFu) return DGS_ENOTSUP;
     uint64_t sums, bias;
     grad_sizes(g, p.outs, p.cols, sums, bias);
@@ -307,12 +675,12 @@ extern "C" int dgs_checkpoint_weight_grad(const dgs_weight_grad_args *args, void
     a.split_rows = g.split_rows;
     a.col_tiles = g.col_tiles; a.tiles = g.out_tiles * g.col_tiles;
     a.accumulate = p.accumulate != 0;
-    const dim3 grid((uint32_t)blocks), block(GRAD_THREADS);
-    if (p.type == DGS_F32) hipLaunchKernelGGL(k_weight_grad<float>, grid, block, 0, st, a);
-    else if (p.type == DGS_F16) hipLaunchKernelGGL(k_weight_grad<f16>, grid, block, 0, st, a);
-    else hipLaunchKernelGGL(k_weight_grad<bf16>, grid, block, 0, st, a);
+    const dim3 grid((uint32_t)blocks);
+    if (p.type == DGS_F32) launch_grad<float>(a, g.tile, grid, st);
+    else if (p.type == DGS_F16) launch_grad<f16>(a, g.tile, grid, st);
+    else launch_grad<bf16>(a, g.tile, grid, st);
     if (partial || p.db)
-        hipLaunchKernelGGL(k_weight_grad_finish, dim3(p.outs, partial ? (p.cols + 255) / 256 : 1), dim3(256), 0, st,
+        hipLaunchKernelGGL(k_weight_grad_finish, dim3((p.outs + 3) / 4, partial ? (p.cols + 255) / 256 : 1), dim3(256), 0, st,
                            (const float *)a.sums, (const float *)a.bias_sums, p.scale, p.shift, partial ? p.dw : nullptr, p.dw_stride,
                            p.db, p.outs, p.cols, g.splits, g.splits * g.col_tiles, a.accumulate);
     return launched();

@@ -371,6 +371,10 @@ int main()
     }
     weight(0, 5, 7, B, true, true, true, 0, false);
     weight(129, 257, 300, B, true, false, false, 0, false);
+    for (int type : {F, H, B}) {
+        weight(300, 257, 300, type, true, true, true, 1, true);
+        weight(700, 264, 512, type, true, false, true, 0, false);
+    }
     printf("%llu values as expected\n", (unsigned long long)checks);
     return 0;
 }
