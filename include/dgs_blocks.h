@@ -9,8 +9,8 @@
  * thrown, and nothing is enqueued when an argument is refused.  There is no context and no state: calls on different
  * streams are independent as long as their buffers are.  Every call may be captured into a HIP graph (kernels only).
  *
- * Matrices are row-major; a stride is the distance of two rows in elements, at least `cols`.  Pointers need the alignment
- * of their element type only.  Rows may have any distance, columns are contiguous.
+ * Matrices are row-major with contiguous columns; a stride is the distance of two rows in elements, at least `cols` and below
+ * 2^32.  Pointers need the alignment of their element type only.  More than 2^31 - 1 rows: DGS_ENOTSUP.
  */
 #ifndef DGS_BLOCKS_H
 #define DGS_BLOCKS_H
@@ -103,8 +103,8 @@ int dgs_edge_forward(const dgs_edge *edge /*host*/, const dgs_edge_forward_args 
  * Any output may be absent.  dgate has gate_type.  accumulate != 0: the four parameter gradients, and a dgate of
  * DGS_F32, are added to; otherwise written.  All sums are taken in fp32, in an order that is fixed by the sizes.
  * dx may be dx_out, df may be du (same stride).
- * workspace: device memory of at least dgs_edge_backward_workspace() bytes (may be 0), 16-byte aligned, whose contents do
- * not matter; not to be used by another call at the same time.
+ * workspace: device memory of at least dgs_edge_backward_workspace() bytes, 16-byte aligned, whose contents do not matter;
+ * not to be used by another call at the same time.  (No rows: none is needed.)
  */
 typedef struct dgs_edge_backward_args {
     uint32_t rows, rows_per_gate;
@@ -118,7 +118,7 @@ typedef struct dgs_edge_backward_args {
     uint64_t workspace_bytes;
 } dgs_edge_backward_args;
 
-/* Bytes for `rows` rows, whatever else the call is given.  Pure host computation; 0 on invalid arguments too. */
+/* Bytes for `rows` rows and, of an edge with a gate, rows_per_gate (0: no gate).  Pure host computation; 0 on invalid arguments too. */
 size_t dgs_edge_backward_workspace(uint32_t rows, uint32_t cols, uint32_t rows_per_gate);
 int dgs_edge_backward(const dgs_edge *edge /*host*/, const dgs_edge_backward_args *args /*host*/, void *hip_stream);
 
@@ -139,8 +139,8 @@ int dgs_checkpoint_decode(uint32_t rows, uint32_t cols, const dgs_codes *from /*
  *
  * dy: rows x outs of `type`.  Every product of dy and a checkpoint value is exact in fp32 -- DGS_F16 and DGS_F32 values go
  * through the matrix units as two and three bfloat16 parts -- and sums are fp32, in an order that is fixed by the sizes.
- * accumulate != 0: dw and db are added to.  workspace: at least dgs_checkpoint_weight_grad_workspace() bytes (may be
- * 0), 16-byte aligned; as above.
+ * accumulate != 0: dw and db are added to.  workspace: at least dgs_checkpoint_weight_grad_workspace() bytes, 16-byte
+ * aligned; as above.  Rows of dy or of the checkpoint 2^28 bytes or more apart: DGS_ENOTSUP.
  */
 typedef struct dgs_weight_grad_args {
     uint32_t rows, outs, cols;

@@ -72,25 +72,25 @@ def _type(t, what):
 
 
 def _on_gpu(t, what):
-    if not t.is_cuda:
+    device = t.get_device()
+    if device < 0:
         _refuse(f"{what} is not on a GPU")
-    return t.get_device()
+    return device
 
 
 def _matrix(t, rows, cols, device, what):
     """Pointer and stride of a rows x cols matrix on `device`."""
-    shape = t.shape
-    if len(shape) != 2 or shape[0] != rows or shape[1] != cols:
-        _refuse(f"{what}: shape {tuple(shape)}, expected ({rows}, {cols})")
+    if t.shape != (rows, cols):
+        _refuse(f"{what}: shape {tuple(t.shape)}, expected ({rows}, {cols})")
     if t.get_device() != device:
         _refuse(f"{what} is on another device")
     stride, unit = t.stride()
     if unit != 1 and cols > 1:
         _refuse(f"{what}: columns are not contiguous")
-    if rows <= 1:
-        stride = max(stride, cols)
-    elif stride < cols:
-        _refuse(f"{what}: rows overlap")
+    if stride < cols:
+        if rows > 1:
+            _refuse(f"{what}: rows overlap")
+        stride = cols
     return t.data_ptr(), stride
 
 
@@ -105,20 +105,24 @@ def _vector(t, n, device, what):
     return t.data_ptr()
 
 
+# the handle of torch's current stream of a device (the short way is a fifth of a small call's time shorter)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda d: torch.cuda.current_stream(d).cuda_stream)
+
+
 def _enqueue(what, device, call, *args):
     """call(*args, stream) on torch's current stream of the device."""
     if torch.cuda.current_device() == device:
-        rc = call(*args, torch.cuda.current_stream(device).cuda_stream)
+        rc = call(*args, _raw_stream(device))
     else:
         with torch.cuda.device(device):
-            rc = call(*args, torch.cuda.current_stream(device).cuda_stream)
+            rc = call(*args, _raw_stream(device))
     if rc:
         raise DgsError(rc, what)
 
 
-def _workspace(given, need, device, what):
+def _workspace(given, need, like, device, what):
     if given is None:
-        return torch.empty(max(need, 16), dtype=torch.uint8, device=torch.device("cuda", device))
+        return like.new_empty(max(need, 16), dtype=torch.uint8)
     if given.get_device() != device or not given.is_contiguous():
         _refuse(f"{what}: workspace is not contiguous memory of the device")
     return given
@@ -129,14 +133,18 @@ class Checkpoint:
 
     def __init__(self, rows, cols, device="cuda:0", codes=None, exps=None):
         self.rows, self.cols = rows, cols
-        runs = (cols + CHECKPOINT_RUN - 1) // CHECKPOINT_RUN
-        self.codes = codes if codes is not None else torch.empty((rows, cols), dtype=torch.int8, device=device)
-        self.exps = exps if exps is not None else torch.empty((rows, runs), dtype=torch.uint8, device=device)
-        if self.codes.dtype != torch.int8 or self.exps.dtype != torch.uint8:
+        runs = self._runs = (cols + CHECKPOINT_RUN - 1) // CHECKPOINT_RUN
+        if codes is None and exps is None:
+            codes = torch.empty((rows, cols), dtype=torch.int8, device=device)
+            self.codes, self.exps = codes, codes.new_empty((rows, runs), dtype=torch.uint8)
+            _on_gpu(codes, "checkpoint")
+            return
+        if codes is None or exps is None or codes.dtype != torch.int8 or exps.dtype != torch.uint8:
             _refuse("a checkpoint's codes are int8 and its exponents uint8")
-        device = _on_gpu(self.codes, "checkpoint")
-        _matrix(self.codes, rows, cols, device, "codes")
-        _matrix(self.exps, rows, runs, device, "exps")
+        self.codes, self.exps = codes, exps
+        device = _on_gpu(codes, "checkpoint")
+        _matrix(codes, rows, cols, device, "codes")
+        _matrix(exps, rows, runs, device, "exps")
 
     @classmethod
     def of(cls, codes, exps):
@@ -146,12 +154,11 @@ class Checkpoint:
     def _place(self, rows, cols, device, what):
         if self.rows != rows or self.cols != cols:
             _refuse(f"{what}: a checkpoint of ({self.rows}, {self.cols}), expected ({rows}, {cols})")
-        if self.codes.get_device() != device:
-            _refuse(f"{what} is on another device")
         codes, exps = self.codes, self.exps
+        if codes.get_device() != device:
+            _refuse(f"{what} is on another device")
         # (one row: any stride will do)
-        return (codes.data_ptr(), max(codes.stride(0), cols), exps.data_ptr(),
-                max(exps.stride(0), (cols + CHECKPOINT_RUN - 1) // CHECKPOINT_RUN))
+        return codes.data_ptr(), max(codes.stride(0), cols), exps.data_ptr(), max(exps.stride(0), self._runs)
 
     def encode(self, x):
         """Hold x from now on."""
@@ -165,7 +172,7 @@ class Checkpoint:
         """The values, times `scale` and plus `shift` (fp32, one for each column), in `out` or a new tensor of `dtype`."""
         device = self.codes.get_device()
         if out is None:
-            out = torch.empty((self.rows, self.cols), dtype=dtype, device=self.codes.device)
+            out = torch.empty_like(self.codes, dtype=dtype)
         data, stride = _matrix(out, self.rows, self.cols, device, "out")
         _enqueue("dgs_checkpoint_decode", device, lib().dgs_checkpoint_decode, self.rows, self.cols,
                  _CODES.pack(*self._place(self.rows, self.cols, device, "checkpoint")),
@@ -208,17 +215,26 @@ class Edge:
         if pre is None and (pre_weight is not None or pre_bias is not None):
             _refuse("pre_weight and pre_bias need a norm")
         self.cols, self.post, self.pre = cols, post, pre
-        self.post_weight, self.post_bias, self.pre_weight, self.pre_bias = post_weight, post_bias, pre_weight, pre_bias
-        self.post_eps = eps if post_eps is None else post_eps
-        self.pre_eps = eps if pre_eps is None else pre_eps
-        self.skip_scale, self.branch_scale = skip_scale, branch_scale
+        self._fixed = (cols, _NORMS[post], _NORMS[pre], eps if post_eps is None else post_eps, eps if pre_eps is None else pre_eps,
+                       skip_scale, branch_scale)
+        vectors = {"post_weight": post_weight, "post_bias": post_bias, "pre_weight": pre_weight, "pre_bias": pre_bias}
+        self._vectors = tuple(vectors.values())
+        self._device = None
+        for name, v in vectors.items():
+            if v is not None:
+                self._device = _on_gpu(v, name) if self._device is None else self._device
+                _vector(v, cols, self._device, name)
+
+    # (fixed when the edge is made)
+    post_weight = property(lambda self: self._vectors[0])
+    post_bias = property(lambda self: self._vectors[1])
+    pre_weight = property(lambda self: self._vectors[2])
+    pre_bias = property(lambda self: self._vectors[3])
 
     def _layer(self, device):
-        cols = self.cols
-        return _EDGE.pack(cols, _NORMS[self.post], _NORMS[self.pre], self.post_eps, self.pre_eps, self.skip_scale,
-                          self.branch_scale, _vector(self.post_weight, cols, device, "post_weight"),
-                          _vector(self.post_bias, cols, device, "post_bias"), _vector(self.pre_weight, cols, device, "pre_weight"),
-                          _vector(self.pre_bias, cols, device, "pre_bias"))
+        if self._device is not None and self._device != device:
+            _refuse("the edge's parameters are on another device")
+        return _EDGE.pack(*self._fixed, *[0 if v is None else v.data_ptr() for v in self._vectors])
 
     def _gate(self, gate, rows_per_gate, rows, device):
         """Pointer and stride, type, rows for each gate row."""
@@ -240,7 +256,7 @@ class Edge:
         device = _on_gpu(x, "x")
         if x.dim() != 2:
             _refuse("x: expected a matrix")
-        rows, cols = x.shape[0], self.cols
+        rows, cols = x.size(0), self.cols
         px = _matrix(x, rows, cols, device, "x")
         stream = _type(x, "x")
         pf = pg = po = pu = _NO_MATRIX
@@ -250,7 +266,7 @@ class Edge:
             pf, kind = _matrix(f, rows, cols, device, "f"), _type(f, "f")
             pg, gate_type, per = self._gate(gate, rows_per_gate, rows, device)
             if x_out is None:
-                x_out = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+                x_out = torch.empty_like(x)
             elif x_out.dtype != x.dtype:
                 _refuse("x_out: expected the type of x")
             po = _matrix(x_out, rows, cols, device, "x_out")
@@ -258,7 +274,7 @@ class Edge:
             _refuse("without f there is no gate and no x_out")
         if self.pre is not None:
             if u is None:
-                u = torch.empty((rows, cols), dtype=x.dtype if f is None else f.dtype, device=x.device)
+                u = torch.empty_like(x if f is None else f)
             elif f is None:
                 kind = _type(u, "u")
             elif u.dtype != f.dtype:
@@ -329,7 +345,7 @@ class Edge:
                 if saved.f.dtype != dtype:
                     _refuse("saved.f: expected the type of du")
             if df is None:
-                df = torch.empty((rows, cols), dtype=dtype, device=given.device)
+                df = torch.empty_like(given, dtype=dtype)
             elif df.dtype != dtype:
                 _refuse("df: expected the type of du")
             pdf = _matrix(df, rows, cols, device, "df")
@@ -341,14 +357,14 @@ class Edge:
                 _refuse("dgate: expected a gate of the same type")
             pdg = _matrix(dgate, gate.shape[0], cols, device, "dgate")
         if dx is None:
-            dx = torch.empty((rows, cols), dtype=stream_dtype, device=given.device)
+            dx = torch.empty_like(given, dtype=stream_dtype)
         elif dx.dtype != stream_dtype:
             _refuse("dx: expected the type of dx_out")
         pdx = _matrix(dx, rows, cols, device, "dx")
         grads = (_vector(post_weight_grad, cols, device, "post_weight_grad"), _vector(post_bias_grad, cols, device, "post_bias_grad"),
                  _vector(pre_weight_grad, cols, device, "pre_weight_grad"), _vector(pre_bias_grad, cols, device, "pre_bias_grad"))
         L = lib()
-        ws = _workspace(workspace, L.dgs_edge_backward_workspace(rows, cols, per), device, "dgs_edge_backward")
+        ws = _workspace(workspace, L.dgs_edge_backward_workspace(rows, cols, per), given, device, "dgs_edge_backward")
         _enqueue("dgs_edge_backward", device, L.dgs_edge_backward, self._layer(device),
                  _BACKWARD.pack(rows, per, _TYPES.get(stream_dtype, -1), _TYPES.get(dtype, -1), gate_type, int(accumulate), *pd, *pu,
                                 *pg, *pf, *px, *post, *pre, _vector(saved.stats, 4 * rows, device, "stats"), *pdx, *pdf, *pdg,
@@ -367,7 +383,7 @@ def weight_grad(dy, saved, dw, db=None, scale=None, shift=None, accumulate=False
         _refuse("dw: expected float32")
     kind = _type(dy, "dy")
     L = lib()
-    ws = _workspace(workspace, L.dgs_checkpoint_weight_grad_workspace(rows, outs, cols, kind), device, "dgs_checkpoint_weight_grad")
+    ws = _workspace(workspace, L.dgs_checkpoint_weight_grad_workspace(rows, outs, cols, kind), dy, device, "dgs_checkpoint_weight_grad")
     _enqueue("dgs_checkpoint_weight_grad", device, L.dgs_checkpoint_weight_grad,
              _GRAD.pack(rows, outs, cols, kind, int(accumulate), 0, *_matrix(dy, rows, outs, device, "dy"),
                         *saved._place(rows, cols, device, "saved"), _vector(scale, cols, device, "scale"),

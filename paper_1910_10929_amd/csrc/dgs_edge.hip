@@ -22,8 +22,8 @@ struct ForwardArgs {
     int8_t *post_codes, *pre_codes;
     uint8_t *post_exps, *pre_exps;
     float *stats;
-    uint64_t x_stride, f_stride, gate_stride, x_out_stride, u_stride;
-    uint64_t post_codes_stride, post_exps_stride, pre_codes_stride, pre_exps_stride;
+    uint32_t x_stride, f_stride, gate_stride, x_out_stride, u_stride;
+    uint32_t post_codes_stride, post_exps_stride, pre_codes_stride, pre_exps_stride;
     uint32_t rows, rows_per_gate, gate_f32, branch, gated;      // branch, gated: there is one
 };
 
@@ -178,11 +178,11 @@ __global__ __launch_bounds__(WAVES == 1 ? FORWARD_TEAMS * 64 : WAVES * 64) void 
     GateRaw raw_g[CHUNKS];
     auto fetch_x = [&](uint32_t r) {
 #pragma unroll
-        for (int k = 0; k < CHUNKS; ++k) raw_x[k] = load_at<TINY>((const TX *)a.x + r * a.x_stride, p[k].at, l.cols);
+        for (int k = 0; k < CHUNKS; ++k) raw_x[k] = load_at<TINY>((const TX *)a.x + (uint64_t)r * a.x_stride, p[k].at, l.cols);
     };
     auto fetch_f = [&](uint32_t r) {
 #pragma unroll
-        for (int k = 0; k < CHUNKS; ++k) raw_f[k] = load_at<TINY>((const TF *)a.f + r * a.f_stride, p[k].at, l.cols);
+        for (int k = 0; k < CHUNKS; ++k) raw_f[k] = load_at<TINY>((const TF *)a.f + (uint64_t)r * a.f_stride, p[k].at, l.cols);
     };
     auto fetch_g = [&](uint32_t r) {
         const uint64_t gate_at = (uint64_t)(r / a.rows_per_gate) * a.gate_stride;
@@ -213,7 +213,7 @@ __global__ __launch_bounds__(WAVES == 1 ? FORWARD_TEAMS * 64 : WAVES * 64) void 
 #pragma unroll
             for (int k = 0; k < CHUNKS; ++k) {
                 if (a.post_codes)
-                    save8(a.post_codes + row * a.post_codes_stride, a.post_exps + row * a.post_exps_stride, p[k].c, p[k].n, f[k]);
+                    save8(a.post_codes + (uint64_t)row * a.post_codes_stride, a.post_exps + (uint64_t)row * a.post_exps_stride, p[k].c, p[k].n, f[k]);
                 float g[8];
                 unpack_gate<TINY, TF>(raw_g[k], a.gate_f32, ragged, p[k], g);
 #pragma unroll
@@ -221,7 +221,7 @@ __global__ __launch_bounds__(WAVES == 1 ? FORWARD_TEAMS * 64 : WAVES * 64) void 
                     const float m = a.gated ? l.branch * g[i] : l.branch;
                     x[k][i] = __builtin_fmaf(m, __builtin_fmaf(f[k][i], wp[k][i], bp[k][i]), l.skip * x[k][i]);
                 }
-                store8((TX *)a.x_out + row * a.x_out_stride, p[k].c, p[k].n, x[k]);
+                store8((TX *)a.x_out + (uint64_t)row * a.x_out_stride, p[k].c, p[k].n, x[k]);
             }
             // (behind the row's end the gate may be anything: not the sum)
             if (ragged) {
@@ -237,10 +237,10 @@ __global__ __launch_bounds__(WAVES == 1 ? FORWARD_TEAMS * 64 : WAVES * 64) void 
 #pragma unroll
             for (int k = 0; k < CHUNKS; ++k) {
                 if (a.pre_codes)
-                    save8(a.pre_codes + row * a.pre_codes_stride, a.pre_exps + row * a.pre_exps_stride, p[k].c, p[k].n, x[k]);
+                    save8(a.pre_codes + (uint64_t)row * a.pre_codes_stride, a.pre_exps + (uint64_t)row * a.pre_exps_stride, p[k].c, p[k].n, x[k]);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) x[k][i] = __builtin_fmaf(x[k][i], wn[k][i], bn[k][i]);
-                store8((TF *)a.u + row * a.u_stride, p[k].c, p[k].n, x[k]);
+                store8((TF *)a.u + (uint64_t)row * a.u_stride, p[k].c, p[k].n, x[k]);
             }
         }
         if (a.stats && threadIdx.x % (WAVES * 64) == 0) {
@@ -255,9 +255,9 @@ __global__ __launch_bounds__(WAVES == 1 ? FORWARD_TEAMS * 64 : WAVES * 64) void 
 // backward
 // ---------------------------------------------------------------------------
 
-// How rows are dealt out to workgroups.  Where gate rows are few, every gate row's rows are cut into `parts` runs of `run`
-// rows, one per workgroup, and the parts of its gradient are added up afterwards; where they are many, a workgroup takes
-// `whole` gate rows and writes their gradients itself.
+// How rows are dealt out to workgroups.  Every gate row's rows are cut into `parts` runs of `run` rows, one per workgroup,
+// and the parts of its gradient are added up afterwards (one part: written at once); or, where there are many gate rows, a
+// workgroup takes `whole` of them, each of which is one team's.
 struct Cut {
     uint32_t blocks, whole, parts, run;
     uint32_t gates, rows_per_gate;
@@ -273,8 +273,8 @@ struct BackwardArgs {
     void *dx, *df, *dgate;
     float *grad[4];         // post weight, post bias, pre weight, pre bias
     float *partial;         // 5 x blocks x cols (the fifth: the gate's)
-    uint64_t dx_out_stride, du_stride, gate_stride, f_stride, x_out_stride, dx_stride, df_stride, dgate_stride;
-    uint64_t post_codes_stride, post_exps_stride, pre_codes_stride, pre_exps_stride;
+    uint32_t dx_out_stride, du_stride, gate_stride, f_stride, x_out_stride, dx_stride, df_stride, dgate_stride;
+    uint32_t post_codes_stride, post_exps_stride, pre_codes_stride, pre_exps_stride;
     uint32_t rows, gate_f32, accumulate, branch, gated, through_pre, arrives, coded;     // (branch .. arrives: there is such)
 };
 
@@ -286,8 +286,8 @@ template <class T> struct Kept<T, true> { uint32_t q[2], byte; };
 template <class T> struct Kept<T, false> { Raw8<T> v; };
 
 template <bool TINY, class T, bool CODED>
-__device__ __forceinline__ void fetch_kept(Kept<T, CODED> &r, const int8_t *codes, const uint8_t *exps, uint64_t codes_stride,
-                                           uint64_t exps_stride, const void *values, uint64_t stride, uint64_t row, const Place8 &p,
+__device__ __forceinline__ void fetch_kept(Kept<T, CODED> &r, const int8_t *codes, const uint8_t *exps, uint32_t codes_stride,
+                                           uint32_t exps_stride, const void *values, uint32_t stride, uint64_t row, const Place8 &p,
                                            uint32_t cols)
 {
     if constexpr (CODED) {
@@ -367,6 +367,13 @@ template <class T> __device__ __forceinline__ void store_grad8(T *row, uint32_t 
         for (int i = 0; i < 8; ++i) v[i] += o[i];
     }
     store8(row, c, n, v);
+}
+
+// A gate's gradient at one place.
+template <class TF> __device__ __forceinline__ void store_gate(void *dgate, uint64_t at, bool f32, bool add, float v)
+{
+    if (f32) ((float *)dgate)[at] = add ? ((float *)dgate)[at] + v : v;
+    else ((TF *)dgate)[at] = from_float<TF>(v);
 }
 
 // Eight parameters of the backward pass: staged in LDS, or where a row is too long for that (STAGED false) from memory.
@@ -451,14 +458,14 @@ __global__ __launch_bounds__(BACKWARD_WAVES * 64) void k_edge_backward(BackwardA
     auto fetch_u = [&](uint32_t r) {
 #pragma unroll
         for (int k = 0; k < CHUNKS; ++k) {
-            raw_u[k] = load_at<TINY>((const TF *)a.du + r * a.du_stride, p[k].at, l.cols);
+            raw_u[k] = load_at<TINY>((const TF *)a.du + (uint64_t)r * a.du_stride, p[k].at, l.cols);
             fetch_kept<TINY>(raw_x[k], a.pre_codes, a.pre_exps, a.pre_codes_stride, a.pre_exps_stride, a.x_out, a.x_out_stride, r, p[k],
                              l.cols);
         }
     };
     auto fetch_d = [&](uint32_t r) {
 #pragma unroll
-        for (int k = 0; k < CHUNKS; ++k) raw_d[k] = load_at<TINY>((const TX *)a.dx_out + r * a.dx_out_stride, p[k].at, l.cols);
+        for (int k = 0; k < CHUNKS; ++k) raw_d[k] = load_at<TINY>((const TX *)a.dx_out + (uint64_t)r * a.dx_out_stride, p[k].at, l.cols);
     };
     auto fetch_f = [&](uint32_t r) {
 #pragma unroll
@@ -552,16 +559,12 @@ __global__ __launch_bounds__(BACKWARD_WAVES * 64) void k_edge_backward(BackwardA
                 float o[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) o[i] = l.skip * d[k][i];
-                store8((TX *)a.dx + this_row * a.dx_stride, p[k].c, p[k].n, o);
+                store8((TX *)a.dx + (uint64_t)this_row * a.dx_stride, p[k].c, p[k].n, o);
             }
         }
         // m and k: through the gate and the branch's norm
         unpack_kept<TINY>(raw_f, l.post, st.x, st.y, p, ragged, h);
         fetch_f(next);
-        float g[CHUNKS][8];
-#pragma unroll
-        for (int k = 0; k < CHUNKS; ++k) unpack_gate<TINY, TF>(raw_g[k], a.gate_f32, ragged, p[k], g[k]);
-        fetch_g(next);
         if (a.branch) {
             float w[CHUNKS][8];
 #pragma unroll
@@ -582,10 +585,14 @@ __global__ __launch_bounds__(BACKWARD_WAVES * 64) void k_edge_backward(BackwardA
                     }
                 }
 #pragma unroll
-                for (int k = 0; k < CHUNKS; ++k)
+                for (int k = 0; k < CHUNKS; ++k) {
+                    float g[8];
+                    unpack_gate<TINY, TF>(raw_g[k], a.gate_f32, ragged, p[k], g);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) d[k][i] *= g[k][i];
+                    for (int i = 0; i < 8; ++i) d[k][i] *= g[i];
+                }
             }
+            fetch_g(next);
             if (valid && a.grad[ACC_POST_BIAS]) {
 #pragma unroll
                 for (int k = 0; k < CHUNKS; ++k)
@@ -605,13 +612,13 @@ __global__ __launch_bounds__(BACKWARD_WAVES * 64) void k_edge_backward(BackwardA
             through_norm<WAVES, ALL, CHUNKS>(d, h, p, ragged, l.post, st.y, l.inv_cols, lds, turn);
             if (a.df && valid) {
 #pragma unroll
-                for (int k = 0; k < CHUNKS; ++k) store8((TF *)a.df + this_row * a.df_stride, p[k].c, p[k].n, d[k]);
+                for (int k = 0; k < CHUNKS; ++k) store8((TF *)a.df + (uint64_t)this_row * a.df_stride, p[k].c, p[k].n, d[k]);
             }
             if (gate_done) {
 #pragma unroll
                 for (int k = 0; k < CHUNKS; ++k) {
                     if (a.dgate) {
-                        const uint64_t at = this_gate * a.dgate_stride;
+                        const uint64_t at = (uint64_t)this_gate * a.dgate_stride;
                         if (a.gate_f32) store_grad8((float *)a.dgate + at, p[k].c, p[k].n, acc[ACC_GATE][k], a.accumulate);
                         else store_grad8((TF *)a.dgate + at, p[k].c, p[k].n, acc[ACC_GATE][k], false);
                     }
@@ -622,11 +629,15 @@ __global__ __launch_bounds__(BACKWARD_WAVES * 64) void k_edge_backward(BackwardA
         }
     }
 
-    // what this workgroup adds up to: the teams' sums, then to its place among the partial sums
+    // what this workgroup adds up to: the teams' sums, then to its place among the partial sums, or where it is alone to where
+    // they belong
 #pragma unroll
     for (int q = 0; q < ACCS; ++q) {
         if (q < ACC_GATE ? !a.grad[q < ACC_GATE ? q : 0] : (!a.dgate || cut.whole)) continue;
-        float *to = a.partial + ((uint64_t)q * cut.blocks + blockIdx.x) * l.cols;
+        const bool alone = q < ACC_GATE ? cut.blocks == 1 : cut.parts == 1;
+        float *to = !alone ? a.partial + ((uint64_t)q * cut.blocks + blockIdx.x) * l.cols : q < ACC_GATE ? a.grad[q] : nullptr;
+        const uint64_t gate_at = (uint64_t)gate_row * a.dgate_stride;
+        const bool add = alone && a.accumulate;
         if constexpr (TEAMS > 1) {
             __syncthreads();
 #pragma unroll
@@ -638,11 +649,20 @@ __global__ __launch_bounds__(BACKWARD_WAVES * 64) void k_edge_backward(BackwardA
                 float s = room[j];
 #pragma unroll
                 for (uint32_t t = 1; t < TEAMS; ++t) s += room[t * WIDTH + j];
-                to[j] = s;
+                if (to) to[j] = add ? to[j] + s : s;
+                else store_gate<TF>(a.dgate, gate_at + j, a.gate_f32, a.accumulate, s);
             }
         } else {
 #pragma unroll
-            for (int k = 0; k < CHUNKS; ++k) store8(to, p[k].c, p[k].n, acc[q][k]);
+            for (int k = 0; k < CHUNKS; ++k) {
+                if (to) {
+                    store_grad8(to, p[k].c, p[k].n, acc[q][k], add);
+                } else {
+#pragma unroll
+                    for (uint32_t i = 0; i < 8; ++i)
+                        if (i < p[k].n) store_gate<TF>(a.dgate, gate_at + p[k].c + i, a.gate_f32, a.accumulate, acc[q][k][i]);
+                }
+            }
         }
     }
 }
@@ -703,15 +723,16 @@ static Cut cut_of(uint32_t rows, uint32_t cols, uint32_t rows_per_gate)
     t.rows_per_gate = rows_per_gate && rows_per_gate < rows ? rows_per_gate : rows;
     t.gates = (rows - 1) / t.rows_per_gate + 1;
     t.whole = t.parts = t.run = 0;
-    if (t.gates >= most) {
-        t.whole = (t.gates + most - 1) / most;
-        if (teams > 1) t.whole = (t.whole + teams - 1) / teams * teams;
-        t.blocks = (t.gates + t.whole - 1) / t.whole;
+    const uint32_t rounds = (t.rows_per_gate - 1) / teams + 1;      // of a team, if one workgroup took a gate row
+    // Many gate rows: each goes to one team, if that keeps half the workgroups busy or there are too few rows to share.
+    if (t.gates >= most && (rounds < 2 || t.gates >= most * teams / 2)) {
+        t.whole = ((t.gates + most - 1) / most + teams - 1) / teams * teams;
+        t.blocks = (t.gates - 1) / t.whole + 1;
     } else {
-        const uint32_t rounds = (t.rows_per_gate + teams - 1) / teams;      // of a team, if one workgroup took a gate row
-        t.parts = most / t.gates < rounds ? most / t.gates : rounds;
+        t.parts = t.gates >= most ? 1u : most / t.gates < rounds ? most / t.gates : rounds;
+        if (t.gates == 1 && rounds <= 2) t.parts = 1;      // a second round takes less than a second launch
         t.run = (rounds + t.parts - 1) / t.parts * teams;
-        t.parts = (t.rows_per_gate + t.run - 1) / t.run;
+        t.parts = (t.rows_per_gate - 1) / t.run + 1;
         t.blocks = t.gates * t.parts;
     }
     return t;
@@ -800,17 +821,17 @@ extern "C" int dgs_edge_forward(const dgs_edge *edge, const dgs_edge_forward_arg
     if (e.pre != DGS_NORM_NONE ? !matrix_ok(p.u.data, p.u.stride, cols, p.type) : (p.u.data || p.pre_saved.codes || !branch))
         return DGS_EINVAL;
     if (!saved_ok(p.post_saved, cols) || !saved_ok(p.pre_saved, cols) || !aligned_to(p.stats, 4)) return DGS_EINVAL;
-    if (e.cols > DGS_EDGE_MAX_COLS || !types_have(p.stream_type, p.type)) return DGS_ENOTSUP;
+    if (e.cols > DGS_EDGE_MAX_COLS || p.rows > 0x7FFFFFFFu || !types_have(p.stream_type, p.type)) return DGS_ENOTSUP;
     ForwardArgs a;
     a.l = layer_of(e);
     a.x = p.x.data; a.f = p.f.data; a.gate = p.gate.data; a.x_out = p.x_out.data; a.u = p.u.data;
     a.post_codes = p.post_saved.codes; a.post_exps = p.post_saved.exps;
     a.pre_codes = p.pre_saved.codes; a.pre_exps = p.pre_saved.exps;
     a.stats = p.stats;
-    a.x_stride = p.x.stride; a.f_stride = p.f.stride; a.gate_stride = p.gate.stride;
-    a.x_out_stride = p.x_out.stride; a.u_stride = p.u.stride;
-    a.post_codes_stride = p.post_saved.codes_stride; a.post_exps_stride = p.post_saved.exps_stride;
-    a.pre_codes_stride = p.pre_saved.codes_stride; a.pre_exps_stride = p.pre_saved.exps_stride;
+    a.x_stride = (uint32_t)p.x.stride; a.f_stride = (uint32_t)p.f.stride; a.gate_stride = (uint32_t)p.gate.stride;
+    a.x_out_stride = (uint32_t)p.x_out.stride; a.u_stride = (uint32_t)p.u.stride;
+    a.post_codes_stride = (uint32_t)p.post_saved.codes_stride; a.post_exps_stride = (uint32_t)p.post_saved.exps_stride;
+    a.pre_codes_stride = (uint32_t)p.pre_saved.codes_stride; a.pre_exps_stride = (uint32_t)p.pre_saved.exps_stride;
     a.rows = p.rows;
     a.rows_per_gate = p.gate.data ? p.rows_per_gate : 1u;
     a.gate_f32 = p.gate.data && p.gate_type == DGS_F32;
@@ -867,7 +888,7 @@ extern "C" int dgs_edge_backward(const dgs_edge *edge, const dgs_edge_backward_a
             return DGS_EINVAL;
         if (!p.stats || !aligned_to(p.stats, 4)) return DGS_EINVAL;
     }
-    if (e.cols > DGS_EDGE_MAX_COLS || !types_have(p.stream_type, p.type)) return DGS_ENOTSUP;
+    if (e.cols > DGS_EDGE_MAX_COLS || p.rows > 0x7FFFFFFFu || !types_have(p.stream_type, p.type)) return DGS_ENOTSUP;
     const bool grads = p.post_weight_grad || p.post_bias_grad || p.pre_weight_grad || p.pre_bias_grad;
     BackwardArgs a;
     const hipStream_t st = (hipStream_t)hip_stream;
@@ -884,10 +905,10 @@ extern "C" int dgs_edge_backward(const dgs_edge *edge, const dgs_edge_backward_a
         a.grad[ACC_POST_WEIGHT] = p.post_weight_grad; a.grad[ACC_POST_BIAS] = p.post_bias_grad;
         a.grad[ACC_PRE_WEIGHT] = p.pre_weight_grad; a.grad[ACC_PRE_BIAS] = p.pre_bias_grad;
         a.partial = (float *)p.workspace;
-        a.dx_out_stride = p.dx_out.stride; a.du_stride = p.du.stride; a.gate_stride = p.gate.stride; a.f_stride = p.f.stride;
-        a.x_out_stride = p.x_out.stride; a.dx_stride = p.dx.stride; a.df_stride = p.df.stride; a.dgate_stride = p.dgate.stride;
-        a.post_codes_stride = p.post_saved.codes_stride; a.post_exps_stride = p.post_saved.exps_stride;
-        a.pre_codes_stride = p.pre_saved.codes_stride; a.pre_exps_stride = p.pre_saved.exps_stride;
+        a.dx_out_stride = (uint32_t)p.dx_out.stride; a.du_stride = (uint32_t)p.du.stride; a.gate_stride = (uint32_t)p.gate.stride; a.f_stride = (uint32_t)p.f.stride;
+        a.x_out_stride = (uint32_t)p.x_out.stride; a.dx_stride = (uint32_t)p.dx.stride; a.df_stride = (uint32_t)p.df.stride; a.dgate_stride = (uint32_t)p.dgate.stride;
+        a.post_codes_stride = (uint32_t)p.post_saved.codes_stride; a.post_exps_stride = (uint32_t)p.post_saved.exps_stride;
+        a.pre_codes_stride = (uint32_t)p.pre_saved.codes_stride; a.pre_exps_stride = (uint32_t)p.pre_saved.exps_stride;
         a.rows = p.rows;
         a.gate_f32 = p.gate.data && p.gate_type == DGS_F32;
         a.accumulate = p.accumulate != 0;
@@ -922,8 +943,9 @@ extern "C" int dgs_edge_backward(const dgs_edge *edge, const dgs_edge_backward_a
             launch_backward<bf16, bf16>(a, st);
         }
     }
-    const uint32_t in_parts = p.rows && p.dgate.data && !a.cut.whole ? a.cut.gates : 0u;
-    if (grads || in_parts)
+    const uint32_t in_parts = p.rows && p.dgate.data && a.cut.parts > 1 ? a.cut.gates : 0u;
+    // (a workgroup that is alone has written them)
+    if (!p.rows ? grads : a.cut.blocks > 1 && (grads || in_parts))
         hipLaunchKernelGGL(k_edge_reduce, dim3((e.cols + 63) / 64, 4 + in_parts), dim3(REDUCE_LINES * 64), 0, st,
                            (const float *)p.workspace, p.post_weight_grad, p.post_bias_grad, p.pre_weight_grad, p.pre_bias_grad,
                            p.dgate.data, p.dgate.stride, e.cols, p.rows ? a.cut.blocks : 0u, p.rows ? a.cut.parts : 0u,

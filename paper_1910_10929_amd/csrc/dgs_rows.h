@@ -381,12 +381,12 @@ static inline bool is_type(int type) { return type >= DGS_F32 && type <= DGS_BF1
 static inline bool aligned_to(const void *p, uint64_t bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
 static inline bool matrix_ok(const void *p, uint64_t stride, uint64_t cols, int type)
 {
-    return p && stride >= cols && stride < (1ull << 40) && aligned_to(p, type_bytes(type));
+    return p && stride >= cols && stride < (1ull << 32) && aligned_to(p, type_bytes(type));
 }
 static inline bool codes_ok(const dgs_codes &c, uint64_t cols)
 {
-    return c.codes && c.exps && c.codes_stride >= cols && c.codes_stride < (1ull << 40)
-        && c.exps_stride >= (cols + DGS_CHECKPOINT_RUN - 1) / DGS_CHECKPOINT_RUN && c.exps_stride < (1ull << 40);
+    return c.codes && c.exps && c.codes_stride >= cols && c.codes_stride < (1ull << 32)
+        && c.exps_stride >= (cols + DGS_CHECKPOINT_RUN - 1) / DGS_CHECKPOINT_RUN && c.exps_stride < (1ull << 32);
 }
 // What a launch that was enqueued without an event leaves.
 static inline int launched() { return hipGetLastError() == hipSuccess ? DGS_OK : DGS_EHIP; }

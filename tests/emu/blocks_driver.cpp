@@ -348,6 +348,11 @@ int main()
     edge(1, 1, F, F, R, L, true, 0, false, true, 0);
     edge(5, 7, F, B, L, R, true, 2, false, true, 3);
     edge(67, 96, B, B, R, R, false, 0, false, true, 0);
+    edge(8200, 8, F, B, L, R, true, 32, false, true, 0);
+    edge(3, 96, H, H, R, L, true, 3, false, true, 1);
+    edge(2, 700, B, B, R, L, true, 2, true, true, 1);
+    edge(1, 8200, F, F, L, L, true, 1, true, true, 0);
+    edge(2, 5000, B, B, L, L, true, 2, false, true, 0);
     edge(41, 333, H, H, L, L, true, 1, false, false, 1);
     edge(300, 40, F, H, L, L, true, 300, true, true, 8);
     edge(310, 33, B, B, R, L, true, 1, false, true, 0);
