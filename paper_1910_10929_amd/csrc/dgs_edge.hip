@@ -89,6 +89,12 @@ template <int WAVES, int CHUNKS> struct Team {
     static __device__ __forceinline__ uint32_t col(int k) { return ((uint32_t)k * LANES + threadIdx.x % LANES) * 8u; }
 };
 
+// Whether a team's row ends before this wavefront's first column (CHUNKS = 1).
+template <int WAVES> __device__ __forceinline__ bool idle_wave(uint32_t cols)
+{
+    return uniform((threadIdx.x / 64 % WAVES) * 512u) >= cols;
+}
+
 // v - by, and 0 behind the row's end in the lane that holds it (where the row's length is no multiple of eight).
 template <int CHUNKS>
 __device__ __forceinline__ void subtract(float (&v)[CHUNKS][8], const Place8 (&p)[CHUNKS], bool ragged, float by)
@@ -171,6 +177,15 @@ __global__ __launch_bounds__(WAVES == 1 ? FORWARD_TEAMS * 64 : WAVES * 64) void 
     }
     uint32_t row = team;
     if (row >= a.rows) return;      // (of a workgroup that is one team, all of it)
+    if (WAVES > 1 && idle_wave<WAVES>(l.cols)) {      // (nothing but the other wavefronts' sums)
+        const uint32_t sums = (a.branch ? (uint32_t)l.post : 0u) + (uint32_t)l.pre;      // as `normalise` takes: RMS 1, layer norm 2
+        for (; row < a.rows; row += teams)
+            for (uint32_t i = 0; i < sums; ++i) {
+                float none[1] = {0.0f};
+                team_sum<WAVES, ALL, 1>(none, lds, turn);
+            }
+        return;
+    }
     // What is loaded of a row (f and the gate, if there are none, of x in their place).  Each piece of the next row is asked for
     // as soon as this row's has been unpacked, so that it has a whole round to arrive and takes no registers of its own.
     Raw8<TX> raw_x[CHUNKS];
@@ -485,6 +500,15 @@ __global__ __launch_bounds__(BACKWARD_WAVES * 64) void k_edge_backward(BackwardA
         fetch_d(r);
         fetch_f(r);
         fetch_g(r);
+    }
+    if (WAVES > 1 && idle_wave<WAVES>(l.cols)) {      // (nothing but the other wavefronts' sums)
+        const uint32_t sums = (a.branch && l.post != DGS_NORM_NONE ? 1u : 0u) + (a.through_pre ? 1u : 0u);
+        for (uint32_t round = 0; round < rounds; ++round)
+            for (uint32_t i = 0; i < sums; ++i) {
+                float none[2] = {0.0f, 0.0f};
+                team_sum<WAVES, ALL, 2>(none, lds, turn);
+            }
+        rounds = 0;
     }
     for (uint32_t round = 0; round < rounds; ++round) {
         const uint32_t this_row = row, this_gate = gate_row;

@@ -95,6 +95,10 @@ struct GradArgs {
     float *dw, *sums, *bias_sums;       // where the tiles go: dw itself, or partial sums (splits x outs x cols); splits x col tiles x outs
     uint64_t dy_stride, codes_stride, exps_stride, dw_stride;
     uint32_t rows, outs, cols, split_rows, col_tiles, tiles, accumulate;
+    // one split of few rows: every tile adds up its own rows of the bias gradient, and nothing is left to a second launch
+    const float *shift;
+    float *db;
+    uint32_t own_bias;
 };
 
 // Where eight values of row k, columns 8 c to 8 c + 7, lie in a staged matrix: rows of GRAD_TILE values, their 16-byte pieces
@@ -174,7 +178,7 @@ __global__ __launch_bounds__(GRAD_THREADS) void k_weight_grad(GradArgs a)
     for (uint32_t step = 0; step < steps; ++step) {
         const uint32_t buf = step & 1u;
         if (step + 1 < steps) fetch(step + 1);
-        const bool bias_step = a.bias_sums && bias_turn == tile_c && wc == 0;
+        const bool bias_step = a.own_bias || (a.bias_sums && bias_turn == tile_c && wc == 0);
         bias_turn = bias_turn + 1 == a.col_tiles ? 0 : bias_turn + 1;
 #pragma unroll
         for (uint32_t k = 0; k < GRAD_STEP; k += 16) {
@@ -199,29 +203,46 @@ __global__ __launch_bounds__(GRAD_THREADS) void k_weight_grad(GradArgs a)
     const bool whole = a.dw != nullptr;      // otherwise partial sums
     float *const out = whole ? a.dw : a.sums + (uint64_t)split * a.outs * a.cols;
     const uint64_t stride = whole ? a.dw_stride : a.cols;
+    const uint32_t first_row = tile_o * GRAD_TILE + wo * 8 + 4 * (lane >> 5);
+    const uint32_t there = a.outs - min(a.outs, first_row);      // rows from this lane's first on
 #pragma unroll
     for (uint32_t j = 0; j < 2; ++j) {
         const uint32_t c = tile_c * GRAD_TILE + wc * 8 + 32 * j + (lane & 31u);
         if (c >= a.cols) continue;
-        const float scale = whole && a.scale ? a.scale[c] : 1.0f;
+        if (whole && a.scale) {
+            const float scale = a.scale[c];
+#pragma unroll
+            for (uint32_t i = 0; i < 2; ++i)
+#pragma unroll
+                for (uint32_t r = 0; r < 16; ++r) acc[i][j][r] *= scale;
+        }
+        if (a.own_bias && a.shift) {
+            const float shift = a.shift[c];
+#pragma unroll
+            for (uint32_t i = 0; i < 2; ++i)
+#pragma unroll
+                for (uint32_t r = 0; r < 16; ++r) acc[i][j][r] = __builtin_fmaf(bias[i][r], shift, acc[i][j][r]);
+        }
+        float *const to = out + (uint64_t)first_row * stride + c;
+#pragma unroll
+        for (uint32_t i = 0; i < 2; ++i)
+#pragma unroll
+            for (uint32_t r = 0; r < 16; ++r) {
+                const uint32_t o = 32 * i + (r & 3u) + 8 * (r >> 2);
+                if (o >= there) continue;
+                float *const p = to + o * stride;
+                *p = whole && a.accumulate ? *p + acc[i][j][r] : acc[i][j][r];
+            }
+    }
+    if (((a.own_bias && a.db && tile_c == 0) || a.bias_sums) && wc == 0 && (lane & 31u) == 0) {
 #pragma unroll
         for (uint32_t i = 0; i < 2; ++i)
 #pragma unroll
             for (uint32_t r = 0; r < 16; ++r) {
                 const uint32_t o = tile_o * GRAD_TILE + wo * 8 + 32 * i + (r & 3u) + 8 * (r >> 2) + 4 * (lane >> 5);
                 if (o >= a.outs) continue;
-                float *p = out + o * stride + c;
-                const float v = acc[i][j][r] * scale;
-                *p = whole && a.accumulate ? *p + v : v;
-            }
-    }
-    if (a.bias_sums && wc == 0 && (lane & 31u) == 0) {
-#pragma unroll
-        for (uint32_t i = 0; i < 2; ++i)
-#pragma unroll
-            for (uint32_t r = 0; r < 16; ++r) {
-                const uint32_t o = tile_o * GRAD_TILE + wo * 8 + 32 * i + (r & 3u) + 8 * (r >> 2) + 4 * (lane >> 5);
-                if (o < a.outs) a.bias_sums[((uint64_t)split * a.col_tiles + tile_c) * a.outs + o] = bias[i][r];
+                if (a.own_bias) a.db[o] = a.accumulate ? a.db[o] + bias[i][r] : bias[i][r];
+                else a.bias_sums[((uint64_t)split * a.col_tiles + tile_c) * a.outs + o] = bias[i][r];
             }
     }
 }
@@ -325,7 +346,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_weight_grad_tile(GradArgs a)
     for (int i = 0; i < 8; ++i) bias[i] = 0.0f;
     uint32_t bias_turn = 0;     // step % col_tiles: the column tiles share out the rows of the bias gradient
     auto add_bias = [&](uint32_t there) {
-        if (a.bias_sums && bias_turn == tile_c) {
+        if (a.own_bias || (a.bias_sums && bias_turn == tile_c)) {
 #pragma unroll
             for (uint32_t p = 0; p < PASSES_O; ++p) {
                 if (first_o + APART_O * p >= there) continue;
@@ -450,38 +471,61 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_weight_grad_tile(GradArgs a)
         }
     }
 
-    const bool whole = a.dw != nullptr;
-    float *const out = whole ? a.dw : a.sums + (uint64_t)split * a.outs * a.cols;
-    const uint64_t stride = whole ? a.dw_stride : a.cols;
-#pragma unroll
-    for (uint32_t j = 0; j < J; ++j) {
-        const uint32_t c = tile_c * COLS + wc * 8 + 32 * j + (lane & 31u);
-        if (c >= a.cols) continue;
-        const float scale = whole && a.scale ? a.scale[c] : 1.0f;
-#pragma unroll
-        for (uint32_t i = 0; i < I; ++i)
-#pragma unroll
-            for (uint32_t r = 0; r < 16; ++r) {
-                const uint32_t o = tile_o * OUTS + wo * 8 + 32 * i + (r & 3u) + 8 * (r >> 2) + 4 * (lane >> 5);
-                if (o >= a.outs) continue;
-                float *p = out + o * stride + c;
-                const float v = acc[i][j][r] * scale;
-                *p = whole && a.accumulate ? *p + v : v;
-            }
-    }
-    if (a.bias_sums) {      // the threads of a piece of columns, one after another
-        float *const sums = (float *)&la[0][0][0];
+    // the bias gradient of this tile's rows: the threads of a piece of columns, one after another
+    float *const sums = (float *)&la[0][0][0];
+    if (a.bias_sums || a.own_bias) {
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < 8; ++i) sums[first_o * OUTS + piece_o * 8 + i] = bias[i];
         __syncthreads();
         const uint32_t o = tile_o * OUTS + threadIdx.x;
-        if (threadIdx.x < OUTS && o < a.outs) {
-            float sum = 0.0f;
+        float sum = 0.0f;
+        if (threadIdx.x < OUTS) {
 #pragma unroll
             for (uint32_t q = 0; q < APART_O; ++q) sum += sums[q * OUTS + threadIdx.x];
-            a.bias_sums[((uint64_t)split * a.col_tiles + tile_c) * a.outs + o] = sum;
+            if (o < a.outs && a.bias_sums) a.bias_sums[((uint64_t)split * a.col_tiles + tile_c) * a.outs + o] = sum;
+            if (o < a.outs && a.own_bias && a.db && tile_c == 0) a.db[o] = a.accumulate ? a.db[o] + sum : sum;
         }
+        if (a.own_bias) {
+            __syncthreads();
+            if (threadIdx.x < OUTS) sums[threadIdx.x] = sum;
+            __syncthreads();
+        }
+    }
+    const bool whole = a.dw != nullptr;      // otherwise partial sums
+    float *const out = whole ? a.dw : a.sums + (uint64_t)split * a.outs * a.cols;
+    const uint64_t stride = whole ? a.dw_stride : a.cols;
+    const uint32_t first_row = wo * 8 + 4 * (lane >> 5);      // of the tile; this lane's rows are 32 i + (r % 4) + 8 (r / 4) behind it
+#pragma unroll
+    for (uint32_t j = 0; j < J; ++j) {
+        const uint32_t c = tile_c * COLS + wc * 8 + 32 * j + (lane & 31u);
+        if (c >= a.cols) continue;
+        if (whole && a.scale) {
+            const float scale = a.scale[c];
+#pragma unroll
+            for (uint32_t i = 0; i < I; ++i)
+#pragma unroll
+                for (uint32_t r = 0; r < 16; ++r) acc[i][j][r] *= scale;
+        }
+        if (a.own_bias && a.shift) {
+            const float shift = a.shift[c];
+#pragma unroll
+            for (uint32_t i = 0; i < I; ++i)
+#pragma unroll
+                for (uint32_t r = 0; r < 16; ++r)
+                    acc[i][j][r] = __builtin_fmaf(sums[first_row + 32 * i + (r & 3u) + 8 * (r >> 2)], shift, acc[i][j][r]);
+        }
+        float *const to = out + (uint64_t)(tile_o * OUTS + first_row) * stride + c;
+        const uint32_t there = a.outs - min(a.outs, tile_o * OUTS + first_row);      // rows from this lane's first on
+#pragma unroll
+        for (uint32_t i = 0; i < I; ++i)
+#pragma unroll
+            for (uint32_t r = 0; r < 16; ++r) {
+                const uint32_t o = 32 * i + (r & 3u) + 8 * (r >> 2);
+                if (o >= there) continue;
+                float *const p = to + o * stride;
+                *p = whole && a.accumulate ? *p + acc[i][j][r] : acc[i][j][r];
+            }
     }
 }
 
@@ -572,7 +616,7 @@ struct GradPlan {
     int tile;
     uint32_t out_tiles, col_tiles, splits, split_rows;
 };
-static GradPlan plan_of(int tile, uint32_t rows, uint32_t outs, uint32_t cols, int type, float &us)
+static GradPlan plan_of(int tile, uint32_t rows, uint32_t outs, uint32_t cols, int type, bool one_split, float &us)
 {
     const GradTile t = tile_of(tile, type);
     GradPlan g;
@@ -581,7 +625,7 @@ static GradPlan plan_of(int tile, uint32_t rows, uint32_t outs, uint32_t cols, i
     g.col_tiles = (cols - 1) / t.cols + 1;
     const uint64_t tiles = (uint64_t)g.out_tiles * g.col_tiles;
     const uint32_t steps = rows ? (rows - 1) / t.step + 1 : 0;
-    uint64_t splits = tiles >= t.at_once ? 1 : t.at_once / tiles;
+    uint64_t splits = tiles >= t.at_once || one_split ? 1 : t.at_once / tiles;
     if (splits > steps / 4) splits = steps / 4;      // at least four steps each
     if (splits < 1) splits = 1;
     g.split_rows = (steps + (uint32_t)splits - 1) / (uint32_t)splits * t.step;
@@ -595,18 +639,21 @@ static GradPlan plan_of(int tile, uint32_t rows, uint32_t outs, uint32_t cols, i
 // last kind does without.
 static GradPlan grad_plan(uint32_t rows, uint32_t outs, uint32_t cols, int type)
 {
-    float best, us;
-    if (rows < 64 || outs < 8 || cols < 8) return plan_of(TILE_ANY, rows, outs, cols, type, us);
-    GradPlan g = plan_of(TILE_128, rows, outs, cols, type, best);
-    for (int tile = type == DGS_BF16 ? TILE_256 : TILE_256_128; tile < TILE_128; ++tile) {
+    const bool any = rows < 32 || outs < 8 || cols < 8;
+    GradPlan g = {};
+    float best = 0.0f;
+    for (int tile = any ? TILE_ANY : type == DGS_BF16 ? TILE_256 : TILE_256_128; tile <= (any ? TILE_ANY : TILE_128); ++tile) {
+        if (rows < tile_of(tile, type).step && !any) continue;
 #ifdef FORCE_TILE
         if (tile != FORCE_TILE) continue;
-        best = 1e30f;
 #endif
-        const GradPlan other = plan_of(tile, rows, outs, cols, type, us);
-        if (us < best) {
-            best = us;
-            g = other;
+        for (int one = 0; one < 2; ++one) {
+            float us;
+            const GradPlan other = plan_of(tile, rows, outs, cols, type, one != 0, us);
+            if (best == 0.0f || us < best) {
+                best = us;
+                g = other;
+            }
         }
     }
     return g;
@@ -663,13 +710,18 @@ extern "C" int dgs_checkpoint_weight_grad(const dgs_weight_grad_args *args, void
     if (!p.workspace || !aligned_to(p.workspace, 16)) return DGS_EINVAL;
     if (p.workspace_bytes < (sums + bias) * sizeof(float)) return DGS_ENOMEM;
     const hipStream_t st = (hipStream_t)hip_stream;
-    const bool partial = g.splits > 1 || p.shift;
+    // (beyond a few rows, tiles that all add up the same rows cost more than the second launch)
+    const bool own_bias = g.splits == 1 && p.rows <= 256 && (p.db || p.shift);
+    const bool partial = g.splits > 1 || (p.shift && !own_bias);
     GradArgs a;
     a.dy = p.dy.data; a.codes = p.saved.codes; a.exps = p.saved.exps;
     a.scale = p.scale;
     a.dw = partial ? nullptr : p.dw;
     a.sums = (float *)p.workspace;
-    a.bias_sums = p.db || p.shift ? a.sums + sums : nullptr;
+    a.bias_sums = (p.db || p.shift) && !own_bias ? a.sums + sums : nullptr;
+    a.shift = p.shift;
+    a.db = p.db;
+    a.own_bias = own_bias;
     a.dy_stride = p.dy.stride; a.codes_stride = p.saved.codes_stride; a.exps_stride = p.saved.exps_stride; a.dw_stride = p.dw_stride;
     a.rows = p.rows; a.outs = p.outs; a.cols = p.cols;
     a.split_rows = g.split_rows;
@@ -679,7 +731,7 @@ extern "C" int dgs_checkpoint_weight_grad(const dgs_weight_grad_args *args, void
     if (p.type == DGS_F32) launch_grad<float>(a, g.tile, grid, st);
     else if (p.type == DGS_F16) launch_grad<f16>(a, g.tile, grid, st);
     else launch_grad<bf16>(a, g.tile, grid, st);
-    if (partial || p.db)
+    if (partial || a.bias_sums)
         hipLaunchKernelGGL(k_weight_grad_finish, dim3((p.outs + 3) / 4, partial ? (p.cols + 255) / 256 : 1), dim3(256), 0, st,
                            (const float *)a.sums, (const float *)a.bias_sums, p.scale, p.shift, partial ? p.dw : nullptr, p.dw_stride,
                            p.db, p.outs, p.cols, g.splits, g.splits * g.col_tiles, a.accumulate);

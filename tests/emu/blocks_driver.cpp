@@ -358,6 +358,8 @@ int main()
     edge(310, 33, B, B, R, L, true, 1, false, true, 0);
     edge(531, 24, F, F, L, R, true, 2, true, false, 0);
     edge(90, 768, F, B, L, L, true, 37, false, true, 0);
+    edge(5, 1030, B, B, R, L, true, 0, false, true, 0);
+    edge(4, 4300, F, B, L, R, true, 2, false, true, 0);
     edge(13, 1001, F, F, DGS_NORM_NONE, L, true, 4, true, true, 3);
     edge(9, 1500, B, B, R, R, false, 3, false, true, 0);
     edge(7, 2056, F, B, L, L, true, 0, false, false, 0);
@@ -375,6 +377,8 @@ int main()
         weight(700, 40, 33, type, false, true, false, 1, true);
     }
     weight(0, 5, 7, B, true, true, true, 0, false);
+    weight(40, 140, 150, H, true, true, true, 1, false);
+    weight(70, 300, 136, B, true, true, true, 0, true);
     weight(129, 257, 300, B, true, false, false, 0, false);
     for (int type : {F, H, B}) {
         weight(300, 257, 300, type, true, true, true, 1, true);
