@@ -891,13 +891,14 @@ extern "C" int dgs_edge_backward(const dgs_edge *edge, const dgs_edge_backward_a
     const uint64_t cols = e.cols;
     const bool branch = p.f.data || p.post_saved.codes;
     const bool through_pre = p.du.data != nullptr;
-    if (through_pre && e.pre == DGS_NORM_NONE) return DGS_EINVAL;
-    if (!branch && (e.post != DGS_NORM_NONE || p.gate.data || p.df.data || p.post_weight_grad || p.post_bias_grad)) return DGS_EINVAL;
-    if (p.dgate.data && !p.gate.data) return DGS_EINVAL;
     if (!aligned_to(p.post_weight_grad, 4) || !aligned_to(p.post_bias_grad, 4) || !aligned_to(p.pre_weight_grad, 4)
         || !aligned_to(p.pre_bias_grad, 4))
         return DGS_EINVAL;
+    // (of no rows, pointers say nothing)
     if (p.rows) {
+        if (through_pre && e.pre == DGS_NORM_NONE) return DGS_EINVAL;
+        if (!branch && (e.post != DGS_NORM_NONE || p.gate.data || p.df.data || p.post_weight_grad || p.post_bias_grad)) return DGS_EINVAL;
+        if (p.dgate.data && !p.gate.data) return DGS_EINVAL;
         if (!present_ok(p.dx_out, cols, p.stream_type) || !present_ok(p.du, cols, p.type) || !present_ok(p.dx, cols, p.stream_type)
             || !present_ok(p.df, cols, p.type) || !gate_ok(p.gate, cols, p.gate_type, p.type, p.rows_per_gate)
             || !present_ok(p.dgate, cols, p.gate_type))

@@ -644,8 +644,8 @@ static GradPlan grad_plan(uint32_t rows, uint32_t outs, uint32_t cols, int type)
     float best = 0.0f;
     for (int tile = any ? TILE_ANY : type == DGS_BF16 ? TILE_256 : TILE_256_128; tile <= (any ? TILE_ANY : TILE_128); ++tile) {
         if (rows < tile_of(tile, type).step && !any) continue;
-#ifdef FORCE_TILE
-        if (tile != FORCE_TILE) continue;
+#ifdef DGS_GRAD_TILE      // (a CPU build that is to reach one kind on small matrices)
+        if (!any && tile != DGS_GRAD_TILE) continue;
 #endif
         for (int one = 0; one < 2; ++one) {
             float us;

@@ -332,9 +332,10 @@ static void weight(uint32_t rows, uint32_t outs, uint32_t cols, int type, bool s
     }
 }
 
-int main()
+static const int F = DGS_F32, H = DGS_F16, B = DGS_BF16, R = DGS_NORM_RMS, L = DGS_NORM_LAYER;
+
+static void checkpoints()
 {
-    const int F = DGS_F32, H = DGS_F16, B = DGS_BF16, R = DGS_NORM_RMS, L = DGS_NORM_LAYER;
     for (int type : {F, H, B}) {
         checkpoint(1, 1, type, 0, 1.0, false);
         checkpoint(3, 31, type, 0, 1.0, true);
@@ -344,7 +345,12 @@ int main()
     }
     checkpoint(3, 65, F, 0, 3e38, false);
     checkpoint(3, 65, B, 2, 1e-38, true);
-    // one wavefront a row, in one and two rounds; several; odd sizes, rows beyond one workgroup's share, short last gate rows
+}
+
+// One wavefront a row, in one and two rounds; several; odd sizes, rows beyond one workgroup's share, short last gate rows, one
+// workgroup alone, gate rows shared by teams and one to a team, wavefronts without a column.
+static void edges()
+{
     edge(1, 1, F, F, R, L, true, 0, false, true, 0);
     edge(5, 7, F, B, L, R, true, 2, false, true, 3);
     edge(67, 96, B, B, R, R, false, 0, false, true, 0);
@@ -369,7 +375,11 @@ int main()
     edge(8, 520, B, B, DGS_NORM_NONE, R, false, 0, false, true, 0);
     edge(11, 300, F, B, DGS_NORM_NONE, L, true, 0, false, true, 2, false);
     edge(11, 300, H, H, DGS_NORM_NONE, R, true, 0, false, false, 2, false);
-    // tiles whole and cut, one row, several splits of the rows
+}
+
+// Rows too few for a step, tiles whole and cut, the bias terms in the launch and behind it, several splits of the rows.
+static void weights()
+{
     for (int type : {F, H, B}) {
         weight(1, 1, 1, type, false, false, true, 0, false);
         weight(33, 130, 70, type, true, true, true, 3, true);
@@ -379,11 +389,26 @@ int main()
     weight(0, 5, 7, B, true, true, true, 0, false);
     weight(40, 140, 150, H, true, true, true, 1, false);
     weight(70, 300, 136, B, true, true, true, 0, true);
-    weight(129, 257, 300, B, true, false, false, 0, false);
+}
+
+// The same for the large tiles (of a build in which they are taken at any size).
+static void tiles(bool all)
+{
     for (int type : {F, H, B}) {
-        weight(300, 257, 300, type, true, true, true, 1, true);
-        weight(700, 264, 512, type, true, false, true, 0, false);
+        if (!all && type != B) continue;      // (the largest tile is for bfloat16)
+        weight(64, 256, 256, type, true, true, true, 0, false);
+        weight(300, 257, 150, type, true, true, true, 1, true);
+        weight(330, 40, 264, type, true, false, true, 0, false);
     }
+}
+
+int main(int argc, char **argv)
+{
+    const std::string what = argc > 1 ? argv[1] : "";
+    if (what == "edges") edges();
+    else if (what == "weights") { checkpoints(); weights(); }
+    else if (what == "tiles" || what == "tiles-bf16") tiles(what == "tiles");
+    else return 2;
     printf("%llu values as expected\n", (unsigned long long)checks);
     return 0;
 }
