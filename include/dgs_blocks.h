@@ -140,7 +140,7 @@ int dgs_checkpoint_decode(uint32_t rows, uint32_t cols, const dgs_codes *from /*
  * dy: rows x outs of `type`.  Every product of dy and a checkpoint value is exact in fp32 -- DGS_F16 and DGS_F32 values go
  * through the matrix units as two and three bfloat16 parts -- and sums are fp32, in an order that is fixed by the sizes.
  * accumulate != 0: dw and db are added to.  workspace: at least dgs_checkpoint_weight_grad_workspace() bytes, 16-byte
- * aligned; as above.  Rows of dy or of the checkpoint 2^28 bytes or more apart: DGS_ENOTSUP.
+ * aligned; as above.  Rows of dy or of the checkpoint 2^27 bytes or more apart: DGS_ENOTSUP.
  */
 typedef struct dgs_weight_grad_args {
     uint32_t rows, outs, cols;

@@ -93,7 +93,7 @@ extern "C" int dgs_checkpoint_encode(uint32_t rows, uint32_t cols, int type, con
     if (rows == 0) return DGS_OK;
     if (!matrix_ok(x, x_stride, cols, type) || !codes_ok(*to, cols)) return DGS_EINVAL;
     const Shape s = shape_of(rows, cols);
-    if (cols > 0x7FFFFFE0u || s.blocks > 0xFFFFFFull) return DGS_ENOTSUP;
+    if (cols >= (1u << 29) || s.blocks > 0xFFFFFFull) return DGS_ENOTSUP;
     if (type == DGS_F32) encode<float>(rows, cols, x, x_stride, *to, s, hip_stream);
     else if (type == DGS_F16) encode<f16>(rows, cols, x, x_stride, *to, s, hip_stream);
     else encode<bf16>(rows, cols, x, x_stride, *to, s, hip_stream);
@@ -107,7 +107,7 @@ extern "C" int dgs_checkpoint_decode(uint32_t rows, uint32_t cols, const dgs_cod
     if (rows == 0) return DGS_OK;
     if (!matrix_ok(out, out_stride, cols, type) || !codes_ok(*from, cols)) return DGS_EINVAL;
     const Shape s = shape_of(rows, cols);
-    if (cols > 0x7FFFFFE0u || s.blocks > 0xFFFFFFull) return DGS_ENOTSUP;
+    if (cols >= (1u << 29) || s.blocks > 0xFFFFFFull) return DGS_ENOTSUP;
     if (type == DGS_F32) decode<float>(rows, cols, *from, scale, shift, out, out_stride, s, hip_stream);
     else if (type == DGS_F16) decode<f16>(rows, cols, *from, scale, shift, out, out_stride, s, hip_stream);
     else decode<bf16>(rows, cols, *from, scale, shift, out, out_stride, s, hip_stream);

@@ -81,7 +81,8 @@ __device__ __forceinline__ void unpack_gate(const GateRaw &g, bool f32, bool rag
 // whatever its teams: fewer workgroups leave fewer partial sums (with 8, two workgroups to a compute unit, 16384 x 4096 took
 // 260 us in place of 249 and 8192 x 768 49 in place of 43).
 constexpr uint32_t FORWARD_TEAMS = 4;
-constexpr int BACKWARD_WAVES = 16;
+constexpr int backward_wavefronts(int waves) { return waves % 3 == 0 ? 12 : 16; }
+constexpr uint32_t BACKWARD_BLOCKS = 256;
 
 template <int WAVES, int CHUNKS> struct Team {
     static constexpr uint32_t LANES = WAVES * 64;
@@ -187,7 +188,9 @@ __global__ __launch_bounds__(WAVES == 1 ? FORWARD_TEAMS * 64 : WAVES * 64) void 
         return;
     }
     // What is loaded of a row (f and the gate, if there are none, of x in their place).  Each piece of the next row is asked for
-    // as soon as this row's has been unpacked, so that it has a whole round to arrive and takes no registers of its own.
+    // as soon as this row's has been unpacked, so that it has a whole round to arrive and takes no registers of its own.  (With 16
+    // columns a lane there are none for it: each piece is asked for when it is due.)
+    constexpr bool AHEAD = CHUNKS == 1;
     Raw8<TX> raw_x[CHUNKS];
     Raw8<TF> raw_f[CHUNKS];
     GateRaw raw_g[CHUNKS];
@@ -204,26 +207,31 @@ __global__ __launch_bounds__(WAVES == 1 ? FORWARD_TEAMS * 64 : WAVES * 64) void 
 #pragma unroll
         for (int k = 0; k < CHUNKS; ++k) raw_g[k] = load_gate<TINY, TF>(a.gate, gate_at, p[k].at, l.cols, a.gate_f32);
     };
-    fetch_f(row);
-    fetch_x(row);
-    fetch_g(row);
+    if constexpr (AHEAD) {
+        fetch_f(row);
+        fetch_x(row);
+        fetch_g(row);
+    }
     for (; row < a.rows; row += teams) {
         const uint32_t next = row + teams < a.rows ? row + teams : row;
         float x[CHUNKS][8], f[CHUNKS][8];
         float post_mean = 0.0f, post_rstd = 0.0f, pre_mean, pre_rstd;
+        if constexpr (!AHEAD) fetch_f(row);
 #pragma unroll
         for (int k = 0; k < CHUNKS; ++k) {
             if (ragged) in_place<TINY>(raw_f[k], p[k]);
             unpack8(raw_f[k], f[k]);
         }
-        fetch_f(next);
+        if constexpr (AHEAD) fetch_f(next);
+        else fetch_x(row);
         if (a.branch) normalise<WAVES, ALL, CHUNKS>(f, p, ragged, l.post, l.post_eps, l.inv_cols, lds, turn, post_mean, post_rstd);
 #pragma unroll
         for (int k = 0; k < CHUNKS; ++k) {
             if (ragged) in_place<TINY>(raw_x[k], p[k]);
             unpack8(raw_x[k], x[k]);
         }
-        fetch_x(next);
+        if constexpr (AHEAD) fetch_x(next);
+        else fetch_g(row);
         if (a.branch) {
 #pragma unroll
             for (int k = 0; k < CHUNKS; ++k) {
@@ -246,7 +254,7 @@ __global__ __launch_bounds__(WAVES == 1 ? FORWARD_TEAMS * 64 : WAVES * 64) void 
                     for (int i = 0; i < 8; ++i) x[k][i] = (uint32_t)i < p[k].n ? x[k][i] : 0.0f;
             }
         }
-        fetch_g(next);
+        if constexpr (AHEAD) fetch_g(next);
         normalise<WAVES, ALL, CHUNKS>(x, p, ragged, l.pre, l.pre_eps, l.inv_cols, lds, turn, pre_mean, pre_rstd);
         if (l.pre != DGS_NORM_NONE) {
 #pragma unroll
@@ -408,9 +416,9 @@ __device__ __forceinline__ void parameters8(const float *staged, const float *gi
 }
 
 template <class TX, class TF, int WAVES, int CHUNKS, bool CODED, bool TINY>
-__global__ __launch_bounds__(BACKWARD_WAVES * 64) void k_edge_backward(BackwardArgs a)
+__global__ __launch_bounds__(backward_wavefronts(WAVES) * 64) void k_edge_backward(BackwardArgs a)
 {
-    constexpr int ALL = BACKWARD_WAVES;
+    constexpr int ALL = backward_wavefronts(WAVES);
     constexpr uint32_t TEAMS = ALL / WAVES, WIDTH = WAVES * CHUNKS * 512;
     constexpr bool STAGED = CHUNKS == 1;
     __shared__ TeamLds<ALL> lds;
@@ -463,7 +471,8 @@ __global__ __launch_bounds__(BACKWARD_WAVES * 64) void k_edge_backward(BackwardA
 
     // What is loaded of a row.  Each piece of the next row is asked for as soon as this row's has been unpacked, so that it
     // has a whole round to arrive and takes no registers of its own.  (Where there is no row, row 0; where there is no
-    // matrix, whatever the workspace holds.)
+    // matrix, whatever the workspace holds.  With 16 columns a lane each piece is asked for when it is due.)
+    constexpr bool AHEAD = CHUNKS == 1;
     Raw8<TX> raw_d[CHUNKS];
     Raw8<TF> raw_u[CHUNKS];
     GateRaw raw_g[CHUNKS];
@@ -493,7 +502,7 @@ __global__ __launch_bounds__(BACKWARD_WAVES * 64) void k_edge_backward(BackwardA
         for (int k = 0; k < CHUNKS; ++k) raw_g[k] = load_gate<TINY, TF>(a.gate, gate_at, p[k].at, l.cols, a.gate_f32);
     };
     auto fetch_stats = [&](uint32_t r) { stats = *(const f32x4_any *)(a.stats + 4 * (uint64_t)r); };
-    {
+    if constexpr (AHEAD) {
         const uint32_t r = row < end ? row : 0u;
         fetch_stats(r);
         fetch_u(r);
@@ -527,8 +536,13 @@ __global__ __launch_bounds__(BACKWARD_WAVES * 64) void k_edge_backward(BackwardA
             row += TEAMS;
         }
         const uint32_t next = row < end ? row : 0u;
+        const uint32_t here = valid ? this_row : 0u;
+        if constexpr (!AHEAD) {
+            fetch_stats(here);
+            fetch_u(here);
+        }
         const f32x4_any st = stats;
-        fetch_stats(next);
+        if constexpr (AHEAD) fetch_stats(next);
 
         // d: through the stream's norm
         float d[CHUNKS][8], h[CHUNKS][8];
@@ -538,7 +552,8 @@ __global__ __launch_bounds__(BACKWARD_WAVES * 64) void k_edge_backward(BackwardA
             unpack8(raw_u[k], d[k]);
         }
         unpack_kept<TINY>(raw_x, l.pre, st.z, st.w, p, ragged, h);
-        fetch_u(next);
+        if constexpr (AHEAD) fetch_u(next);
+        else fetch_d(here);
         if (a.through_pre) {
             if (valid && a.grad[ACC_PRE_BIAS]) {
 #pragma unroll
@@ -576,7 +591,8 @@ __global__ __launch_bounds__(BACKWARD_WAVES * 64) void k_edge_backward(BackwardA
                 for (int i = 0; i < 8; ++i) d[k][i] += o[i];
             }
         }
-        fetch_d(next);
+        if constexpr (AHEAD) fetch_d(next);
+        else fetch_f(here);
         if (a.dx && valid) {
 #pragma unroll
             for (int k = 0; k < CHUNKS; ++k) {
@@ -588,7 +604,8 @@ __global__ __launch_bounds__(BACKWARD_WAVES * 64) void k_edge_backward(BackwardA
         }
         // m and k: through the gate and the branch's norm
         unpack_kept<TINY>(raw_f, l.post, st.x, st.y, p, ragged, h);
-        fetch_f(next);
+        if constexpr (AHEAD) fetch_f(next);
+        else fetch_g(here);
         if (a.branch) {
             float w[CHUNKS][8];
 #pragma unroll
@@ -616,7 +633,7 @@ __global__ __launch_bounds__(BACKWARD_WAVES * 64) void k_edge_backward(BackwardA
                     for (int i = 0; i < 8; ++i) d[k][i] *= g[i];
                 }
             }
-            fetch_g(next);
+            if constexpr (AHEAD) fetch_g(next);
             if (valid && a.grad[ACC_POST_BIAS]) {
 #pragma unroll
                 for (int k = 0; k < CHUNKS; ++k)
@@ -730,19 +747,22 @@ __global__ __launch_bounds__(REDUCE_LINES * 64) void k_edge_reduce(const float *
 // host side
 // ---------------------------------------------------------------------------
 
-// Wavefronts of a row's team: 8 columns a lane, and 16 in rows that a workgroup does not hold then.  (16 from 512 columns on, half
-// the wavefronts: 16384 x 4096 edges with checkpoints and their decoding 239 us against 219, 8192 x 768 36 against 33.)
+// Wavefronts of a row's team: 8 columns a lane, and 16 in rows that a workgroup does not hold then; powers of two, and three
+// times those.  (16 columns from 512 on, half the wavefronts: 16384 x 4096 edges with checkpoints and their decoding 239 us against
+// 219, 8192 x 768 36 against 33.  Powers of two alone: 16384 x 1280 in half precision 46 us against 41 forward and 55 against 49
+// backward, 8192 x 6144 100 against 94 and 125 against 117.)
 static uint32_t waves_of(uint32_t cols)
 {
-    uint32_t w = 1;
-    while (w * 512 < cols && w < BACKWARD_WAVES) w *= 2;
-    return w;
+    constexpr uint32_t kinds[] = {1, 2, 3, 4, 6, 8, 12};
+    for (uint32_t w : kinds)
+        if (cols <= w * 512) return w;
+    return 16;
 }
 
 // Workgroups of the backward pass.
 static Cut cut_of(uint32_t rows, uint32_t cols, uint32_t rows_per_gate)
 {
-    const uint32_t teams = BACKWARD_WAVES / waves_of(cols), most = 4096 / BACKWARD_WAVES;
+    const uint32_t waves = waves_of(cols), teams = (uint32_t)backward_wavefronts((int)waves) / waves, most = BACKWARD_BLOCKS;
     Cut t;
     t.rows_per_gate = rows_per_gate && rows_per_gate < rows ? rows_per_gate : rows;
     t.gates = (rows - 1) / t.rows_per_gate + 1;
@@ -765,13 +785,17 @@ static Cut cut_of(uint32_t rows, uint32_t cols, uint32_t rows_per_gate)
 template <class TX, class TF> static void launch_forward(const ForwardArgs &a, hipStream_t st)
 {
     const uint32_t waves = waves_of(a.l.cols), teams = waves == 1 ? FORWARD_TEAMS : 1u;
-    const uint32_t need = (a.rows + teams - 1) / teams, most = 4096u / (teams * waves);
+    // as many workgroups as run at a time: five wavefronts to a SIMD, among which a workgroup's are spread evenly
+    const uint32_t w = teams * waves, most = 256u * (w > 4 ? 5u / ((w + 3u) / 4u) : 20u / w), need = (a.rows + teams - 1) / teams;
     const dim3 grid(need < most ? need : most), block(teams * waves * 64);
     if (a.l.cols < 8) hipLaunchKernelGGL((k_edge_forward<TX, TF, 1, 1, true>), grid, block, 0, st, a);
     else if (waves == 1) hipLaunchKernelGGL((k_edge_forward<TX, TF, 1, 1, false>), grid, block, 0, st, a);
     else if (waves == 2) hipLaunchKernelGGL((k_edge_forward<TX, TF, 2, 1, false>), grid, block, 0, st, a);
+    else if (waves == 3) hipLaunchKernelGGL((k_edge_forward<TX, TF, 3, 1, false>), grid, block, 0, st, a);
     else if (waves == 4) hipLaunchKernelGGL((k_edge_forward<TX, TF, 4, 1, false>), grid, block, 0, st, a);
+    else if (waves == 6) hipLaunchKernelGGL((k_edge_forward<TX, TF, 6, 1, false>), grid, block, 0, st, a);
     else if (waves == 8) hipLaunchKernelGGL((k_edge_forward<TX, TF, 8, 1, false>), grid, block, 0, st, a);
+    else if (waves == 12) hipLaunchKernelGGL((k_edge_forward<TX, TF, 12, 1, false>), grid, block, 0, st, a);
     else if (a.l.cols <= 8192) hipLaunchKernelGGL((k_edge_forward<TX, TF, 16, 1, false>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((k_edge_forward<TX, TF, 16, 2, false>), grid, block, 0, st, a);
 }
@@ -779,12 +803,15 @@ template <class TX, class TF> static void launch_forward(const ForwardArgs &a, h
 template <class TX, class TF, bool CODED> static void launch_backward(const BackwardArgs &a, hipStream_t st)
 {
     const uint32_t waves = waves_of(a.l.cols);
-    const dim3 grid(a.cut.blocks), block(BACKWARD_WAVES * 64);
+    const dim3 grid(a.cut.blocks), block(backward_wavefronts((int)waves) * 64);
     if (a.l.cols < 8) hipLaunchKernelGGL((k_edge_backward<TX, TF, 1, 1, CODED, true>), grid, block, 0, st, a);
     else if (waves == 1) hipLaunchKernelGGL((k_edge_backward<TX, TF, 1, 1, CODED, false>), grid, block, 0, st, a);
     else if (waves == 2) hipLaunchKernelGGL((k_edge_backward<TX, TF, 2, 1, CODED, false>), grid, block, 0, st, a);
+    else if (waves == 3) hipLaunchKernelGGL((k_edge_backward<TX, TF, 3, 1, CODED, false>), grid, block, 0, st, a);
     else if (waves == 4) hipLaunchKernelGGL((k_edge_backward<TX, TF, 4, 1, CODED, false>), grid, block, 0, st, a);
+    else if (waves == 6) hipLaunchKernelGGL((k_edge_backward<TX, TF, 6, 1, CODED, false>), grid, block, 0, st, a);
     else if (waves == 8) hipLaunchKernelGGL((k_edge_backward<TX, TF, 8, 1, CODED, false>), grid, block, 0, st, a);
+    else if (waves == 12) hipLaunchKernelGGL((k_edge_backward<TX, TF, 12, 1, CODED, false>), grid, block, 0, st, a);
     else if (a.l.cols <= 8192) hipLaunchKernelGGL((k_edge_backward<TX, TF, 16, 1, CODED, false>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((k_edge_backward<TX, TF, 16, 2, CODED, false>), grid, block, 0, st, a);
 }

@@ -246,7 +246,7 @@ __device__ __forceinline__ void team_sum(float (&v)[N], TeamLds<ALL> &lds, uint3
     if constexpr (WAVES > 1) {
         float (*half)[ALL] = lds.v[turn];
         turn ^= 1u;
-        const uint32_t wave = threadIdx.x >> 6, first = wave & ~(uint32_t)(WAVES - 1);
+        const uint32_t wave = threadIdx.x >> 6, first = wave / WAVES * WAVES;
         if (lane_id() == 0) {
 #pragma unroll
             for (int i = 0; i < N; ++i) half[i][wave] = v[i];

@@ -703,7 +703,8 @@ extern "C" int dgs_checkpoint_weight_grad(const dgs_weight_grad_args *args, void
     if (p.rows && (!matrix_ok(p.dy.data, p.dy.stride, p.outs, p.type) || !codes_ok(p.saved, p.cols))) return DGS_EINVAL;
     const GradPlan g = grad_plan(p.rows, p.outs, p.cols, p.type);
     const uint64_t blocks = (uint64_t)g.out_tiles * g.col_tiles * g.splits;
-    if (p.dy.stride * type_bytes(p.type) > 0xFFFFFFFu || p.saved.codes_stride > 0xFFFFFFFu || p.saved.exps_stride > 0xFFFFFFFu) return DGS_ENOTSUP;
+    // (a lane's offset, at most 31 rows, is held in 32 bits)
+    if (p.dy.stride * type_bytes(p.type) >= (1u << 27) || p.saved.codes_stride >= (1u << 27) || p.saved.exps_stride >= (1u << 27)) return DGS_ENOTSUP;
     if (p.rows > 0x7FFFFFFFu || p.outs > 0x7FFFFFu || p.cols > 0x7FFFFFu || blocks > 0xFFFFFFu) return DGS_ENOTSUP;
     uint64_t sums, bias;
     grad_sizes(g, p.outs, p.cols, sums, bias);
