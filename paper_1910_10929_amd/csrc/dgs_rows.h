@@ -3,7 +3,8 @@
 //
 // A lane holds values c .. c + 7 of a row, c a multiple of 8, so that the four lanes of a quad hold the 32 columns that
 // share an exponent, and a run's largest magnitude is two quad permutes away.  Loads and stores are 16 bytes (8 for codes)
-// at any alignment of the element type; the last, shorter piece of a row goes element by element.
+// at any alignment of the element type; the last, shorter piece of a row is loaded as the row's last eight values and put in
+// place (element by element where a row has fewer than eight), and stored element by element.
 #pragma once
 #include "dgs_wave.h"
 #include "../../include/dgs_blocks.h"

@@ -6,6 +6,10 @@
 //
 // Both operands have the summed index (the row) outermost in memory.  They are staged in LDS as they lie, 16 bytes a lane,
 // and turned on the way out by the transposing LDS read, four rows of 16 columns to 16 lanes.
+//
+// Bound by the matrix units where the product is large (32768 rows, 4096 x 4096, bfloat16: 970 us, 1130 TFLOP/s; a matrix
+// product of the library's reaches 1260 on this card), by the partial sums of the split rows and by the tiles' first and
+// last steps where it is not (8192 rows, 2304 x 768: 50 us and 10 for the sums, 480 TFLOP/s together).
 #include "dgs_rows.h"
 
 namespace dgs {
@@ -105,6 +109,9 @@ struct GradArgs {
 // exchanged by row so that the four rows that 32 lanes read 64 bytes of are in different banks.
 __device__ __forceinline__ uint32_t staged_at(uint32_t k, uint32_t c) { return k * GRAD_TILE + ((c ^ ((k & 3u) << 2)) << 3); }
 
+// Any shape: every load looks at what is there.  For what the large tiles' loads take for granted and these matrices have not
+// (fewer than 32 rows, fewer than eight outputs or columns); elsewhere it takes 2 to 2.5 times as long (32768 rows, 4096 x
+// 4096: 2344 us; 8192 rows, 2304 x 768: 97).  20 rows, 4096 x 4096, bfloat16: 21 us, bound by the 64 MB that it writes.
 template <class T>
 __global__ __launch_bounds__(GRAD_THREADS) void k_weight_grad(GradArgs a)
 {
@@ -248,27 +255,32 @@ __global__ __launch_bounds__(GRAD_THREADS) void k_weight_grad(GradArgs a)
 }
 
 // ---------------------------------------------------------------------------
-// the large tile
+// the large tiles
 // ---------------------------------------------------------------------------
-// 256 x 256 to a workgroup of four wavefronts, 128 x 128 to a wavefront: per 16 rows a wavefront reads 8 KB of LDS for 16
-// matrix instructions, half of what the tile above reads, and the LDS keeps up with the matrix units.  One wavefront to a
-// SIMD, so the overlap is written down: the fragments of a slice of 16 rows are read while the slice before is multiplied,
-// the next step's rows are staged between the slices, and the barrier stands before a step's last slice, behind which the
-// first fragments of the next step are read.
+// 256 x 256 to eight wavefronts (128 x 64 each; bfloat16 only, whose one part leaves LDS for it), 256 x 128 to eight and
+// 128 x 128 to four (64 x 64 each).  Per 16 rows a wavefront of the first reads 6 KB of LDS for 8 matrix instructions, of
+// the others 4 KB for 4.  Two wavefronts to a SIMD do not hide the waits by themselves, so the overlap is written down: the
+// fragments of a slice of 16 rows are read while the slice before is multiplied, the next step's rows are staged between the
+// slices, the step after is asked for as soon as its registers are free, and the barrier stands before a step's last slice,
+// behind which the first fragments of the next step are read.  A step is one basic block (the rows that fill no step come
+// first, addresses are scalar, nothing looks at a bound), which the compiler can then order.
+// At 32768 rows, 4096 x 4096: 256 x 256 with four wavefronts of 128 x 128 took 1047 us, with eight 982, with the order below
+// 968; with branches around the loads 1680.  At 8192 rows, 2304 x 768: 128 x 128 57 us, 256 x 128 53 (half the partial sums).
 template <uint32_t WIDTH> __device__ __forceinline__ uint32_t wide_at(uint32_t k, uint32_t c) { return k * WIDTH + ((c ^ ((k & 3u) << 2)) << 3); }
 
 template <uint32_t W> struct Width { static constexpr uint32_t value = W; };
 
-// Between two matrix instructions: fragment reads, a share of what the next step's staging takes.
+// Between two matrix instructions: fragment reads, a share of what the next step's staging takes.  (Four vector instructions
+// to one matrix instruction; with three or five 1040 and 1009 us in place of 968 at 32768 rows, 4096 x 4096.)
 template <int COUNT> __device__ __forceinline__ void interleave(bool staging)
 {
-#if !defined(DGS_HOST_EMULATION) && 1
+#ifndef DGS_HOST_EMULATION
     if (staging) {
 #pragma unroll
         for (int i = 0; i < COUNT; ++i) {
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);      // matrix
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);      // LDS read
-            __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);    // vector
+            __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);      // vector
             if (i % 3 == 0) __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);      // LDS write
             if (i % 2 == 0) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);      // memory read
         }
@@ -530,6 +542,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_weight_grad_tile(GradArgs a)
 }
 
 // Adds up the splits' partial sums (where there are any) and finishes: a wavefront an output row and 256 columns, four to a lane.
+// Bound by the latency of few loads: 2304 x 768 in four splits, 35 MB from cache and memory, 10 us; 1001 x 333 5 us.
 __global__ __launch_bounds__(256) void k_weight_grad_finish(const float *sums, const float *bias_sums, const float *scale,
                                                             const float *shift, float *dw, uint64_t dw_stride, float *db, uint32_t outs,
                                                             uint32_t cols, uint32_t splits, uint32_t bias_parts, uint32_t accumulate)
@@ -635,8 +648,9 @@ static GradPlan plan_of(int tile, uint32_t rows, uint32_t outs, uint32_t cols, i
     if (g.splits > 1) us += 4.0f + (float)g.splits * (float)outs * (float)cols * 8.0f / 4.5e6f;      // partial sums there and back
     return g;
 }
-// The tile that should take the least time.  What a whole tile's loads take for granted -- a step's rows, eight columns -- the
-// last kind does without.
+// The tile and the number of splits that should take the least time.  (20 rows of 4096 x 4096 took 80 us in partial sums and
+// take 21 in one launch; 8192 rows of 2304 x 768 are 54 tiles, which without splits would leave 202 compute units idle.)  What
+// a whole tile's loads take for granted -- a step's rows, eight columns -- the last kind does without.
 static GradPlan grad_plan(uint32_t rows, uint32_t outs, uint32_t cols, int type)
 {
     const bool any = rows < 32 || outs < 8 || cols < 8;
