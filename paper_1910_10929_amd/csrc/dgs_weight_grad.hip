@@ -53,6 +53,16 @@ __device__ __forceinline__ uint32_t upper_halves(uint32_t lo, uint32_t hi)
 #endif
 }
 
+// A NaN with its mark in the upper half.
+__device__ __forceinline__ float quiet(float v)
+{
+#ifdef DGS_HOST_EMULATION
+    return v != v ? __uint_as_float(__float_as_uint(v) | 0x00400000u) : v;
+#else
+    return __builtin_canonicalizef(v);
+#endif
+}
+
 // The parts of eight values, eight bfloat16 each.
 template <class T> constexpr int PARTS = sizeof(T) == 4 ? 3 : __is_same(T, bf16) ? 1 : 2;
 
@@ -64,18 +74,18 @@ template <class T> __device__ __forceinline__ void split8(const Raw8<T> &r, u32x
         float v[8];
         unpack8(r, v);
 #pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = quiet(v[i]);
+#pragma unroll
         for (int p = 0; p < PARTS<T>; ++p) {
-            uint32_t b[8];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) part[p][i] = upper_halves(__float_as_uint(v[2 * i]), __float_as_uint(v[2 * i + 1]));
+            if (p + 1 == PARTS<T>) continue;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                b[i] = __float_as_uint(v[i]);
-                // what is left; of infinities and NaN, nothing (a NaN may hold its mark in the low half)
-                const bool finite = (b[i] & 0x7F800000u) != 0x7F800000u;
-                if (!finite && (b[i] & 0x007FFFFFu)) b[i] |= 0x00400000u;
-                v[i] = finite ? v[i] - __uint_as_float(b[i] & 0xFFFF0000u) : 0.0f;
+                const float left = v[i] - __uint_as_float(__float_as_uint(v[i]) & 0xFFFF0000u);
+                // (of infinities and NaN, nothing; what is left of a number is one)
+                v[i] = p > 0 || __builtin_isfinite(v[i]) ? left : 0.0f;
             }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) part[p][i] = upper_halves(b[2 * i], b[2 * i + 1]);
         }
     }
 }
@@ -257,15 +267,18 @@ __global__ __launch_bounds__(GRAD_THREADS) void k_weight_grad(GradArgs a)
 // ---------------------------------------------------------------------------
 // the large tiles
 // ---------------------------------------------------------------------------
-// 256 x 256 to eight wavefronts (128 x 64 each; bfloat16 only, whose one part leaves LDS for it), 256 x 128 to eight and
-// 128 x 128 to four (64 x 64 each).  Per 16 rows a wavefront of the first reads 6 KB of LDS for 8 matrix instructions, of
-// the others 4 KB for 4.  Two wavefronts to a SIMD do not hide the waits by themselves, so the overlap is written down: the
-// fragments of a slice of 16 rows are read while the slice before is multiplied, the next step's rows are staged between the
-// slices, the step after is asked for as soon as its registers are free, and the barrier stands before a step's last slice,
-// behind which the first fragments of the next step are read.  A step is one basic block (the rows that fill no step come
-// first, addresses are scalar, nothing looks at a bound), which the compiler can then order.
-// At 32768 rows, 4096 x 4096: 256 x 256 with four wavefronts of 128 x 128 took 1047 us, with eight 982, with the order below
-// 968; with branches around the loads 1680.  At 8192 rows, 2304 x 768: 128 x 128 57 us, 256 x 128 53 (half the partial sums).
+// 256 x 256 to eight wavefronts (128 x 64 each), 256 x 128 to eight and 128 x 128 to four (64 x 64 each).  Per 16 rows a
+// wavefront of the first reads 6 KB of LDS for 8 matrix instructions, of the others 4 KB for 4 (of bfloat16; each further part
+// of dy 4 KB for 8, and 2 KB for 4).  Two wavefronts to a SIMD do not hide the waits by themselves, so the overlap is written
+// down: a step goes in units, one part of dy in a slice of 16 rows each; the fragments of a unit are read while the one before
+// is multiplied, the next step's rows are staged between the units, the step after is asked for as soon as its registers
+// are free, and the barrier stands before a step's last unit, behind which the first fragments of the next step are read.  A
+// step is one basic block (the rows that fill no step come first, addresses are scalar, nothing looks at a bound), which
+// the compiler can then order.
+// At 32768 rows, 4096 x 4096, bfloat16: 256 x 256 with four wavefronts of 128 x 128 took 1047 us, with eight 982, with the order
+// below 968; with branches around the loads 1680.  Half and fp32 take 2093 and 2595 us there, 3285 and 4075 on 256 x 128 when
+// all parts' fragments were held at a time.  At 8192 rows, 2304 x 768, bfloat16: 128 x 128 57 us, 256 x 128 53 (half the
+// partial sums).
 template <uint32_t WIDTH> __device__ __forceinline__ uint32_t wide_at(uint32_t k, uint32_t c) { return k * WIDTH + ((c ^ ((k & 3u) << 2)) << 3); }
 
 template <uint32_t W> struct Width { static constexpr uint32_t value = W; };
@@ -403,23 +416,23 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_weight_grad_tile(GradArgs a)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
     const uint32_t wo = wave / SIDE * (4 * I), wc = wave % SIDE * (4 * J);      // this wavefront's corner, in pieces
-    // fragments of the slice that is multiplied and of the next one
-    u32x4 fa[2][P][I], fb[2][J];
-    auto read = [&](uint32_t set, uint32_t buf, uint32_t slice) {
+    // A step is multiplied in units, one part of dy in a slice of 16 rows each: fragments of the unit at hand and of the next.
+    constexpr uint32_t UNITS = SLICES * P;
+    u32x4 fa[2][I], fb[2][J];
+    auto read = [&](uint32_t buf, uint32_t unit) {      // (sets by turns: UNITS and SLICES are even)
+        const uint32_t slice = unit / P, part = unit % P;
+        if (part == 0) {
 #pragma unroll
-        for (uint32_t j = 0; j < J; ++j) fb[set][j] = fragment(lb[buf], Width<COLS>(), slice * 16, wc + 4 * j);
+            for (uint32_t j = 0; j < J; ++j) fb[slice & 1u][j] = fragment(lb[buf], Width<COLS>(), slice * 16, wc + 4 * j);
+        }
 #pragma unroll
-        for (int p = 0; p < P; ++p)
-#pragma unroll
-            for (uint32_t i = 0; i < I; ++i) fa[set][p][i] = fragment(la[buf][p], Width<OUTS>(), slice * 16, wo + 4 * i);
+        for (uint32_t i = 0; i < I; ++i) fa[unit & 1u][i] = fragment(la[buf][part], Width<OUTS>(), slice * 16, wo + 4 * i);
     };
-    auto multiply = [&](uint32_t set) {
+    auto multiply = [&](uint32_t unit) {
 #pragma unroll
-        for (int p = 0; p < P; ++p)
+        for (uint32_t i = 0; i < I; ++i)
 #pragma unroll
-            for (uint32_t i = 0; i < I; ++i)
-#pragma unroll
-                for (uint32_t j = 0; j < J; ++j) acc[i][j] = matrix_unit(fa[set][p][i], fb[set][j], acc[i][j]);
+            for (uint32_t j = 0; j < J; ++j) acc[i][j] = matrix_unit(fa[unit & 1u][i], fb[unit / P & 1u][j], acc[i][j]);
     };
 
 #pragma unroll
@@ -456,18 +469,18 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_weight_grad_tile(GradArgs a)
 #pragma unroll
     for (uint32_t p = 0; p < PASSES_C; ++p) fetch_c(p);
     __syncthreads();
-    read(0, 0, 0);
+    read(0, 0);
     for (uint32_t step = 0; step < steps; ++step) {
         const uint32_t buf = step & 1u;
         add_bias(step + 1 < steps ? STEP : 0u);
         row += STEP;
         if (row > a.rows - STEP) point_to(a.rows - STEP);
 #pragma unroll
-        for (uint32_t slice = 0; slice < SLICES; ++slice) {
-            if (slice + 1 < SLICES) {
-                read((slice + 1) & 1u, buf, slice + 1);
+        for (uint32_t unit = 0; unit < UNITS; ++unit) {
+            if (unit + 1 < UNITS) {
+                read(buf, unit + 1);
 #pragma unroll
-                for (uint32_t p = slice * PASSES_O / (SLICES - 1); p < (slice + 1) * PASSES_O / (SLICES - 1); ++p) {
+                for (uint32_t p = unit * PASSES_O / (UNITS - 1); p < (unit + 1) * PASSES_O / (UNITS - 1); ++p) {
                     constexpr uint32_t EACH = PASSES_O / PASSES_C;
                     stage_o(buf ^ 1u, p);
                     if (p % EACH == 0) stage_c(buf ^ 1u, p / EACH);
@@ -476,10 +489,10 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_weight_grad_tile(GradArgs a)
                 }
             } else {
                 __syncthreads();
-                read((slice + 1) & 1u, buf ^ 1u, 0);
+                read(buf ^ 1u, 0);
             }
-            multiply(slice & 1u);
-            interleave<2 * I * J * P>(slice + 1 < SLICES);
+            multiply(unit);
+            interleave<2 * I * J>(unit + 1 < UNITS);
         }
     }
 
@@ -616,9 +629,10 @@ enum { TILE_256, TILE_256_128, TILE_128, TILE_ANY, TILES };
 static GradTile tile_of(int tile, int type)
 {
     const int i = type == DGS_BF16 ? 0 : type == DGS_F16 ? 1 : 2;
-    constexpr float us_256_128[3] = {1.21f, 3.2f, 3.9f}, us_128[3] = {1.45f, 2.9f, 4.3f}, us_any[3] = {3.0f, 5.0f, 7.0f};
+    constexpr float us_256[3] = {1.94f, 4.08f, 5.06f}, us_256_128[3] = {1.22f, 2.37f, 3.21f}, us_128[3] = {1.46f, 2.67f, 3.46f},
+                    us_any[3] = {3.0f, 5.0f, 7.0f};
     switch (tile) {
-    case TILE_256: return GradTile{256, 256, 64, 256, 1.92f, 8.0f};
+    case TILE_256: return GradTile{256, 256, i == 0 ? 64u : 32u, 256, us_256[i], 8.0f};
     case TILE_256_128: return GradTile{256, 128, i == 0 ? 64u : 32u, 256, us_256_128[i], 11.0f};
     case TILE_128: return GradTile{128, 128, 32, 512, us_128[i], 7.0f};
     default: return GradTile{GRAD_TILE, GRAD_TILE, GRAD_STEP, 512, us_any[i], 7.0f};
@@ -656,7 +670,7 @@ static GradPlan grad_plan(uint32_t rows, uint32_t outs, uint32_t cols, int type)
     const bool any = rows < 32 || outs < 8 || cols < 8;
     GradPlan g = {};
     float best = 0.0f;
-    for (int tile = any ? TILE_ANY : type == DGS_BF16 ? TILE_256 : TILE_256_128; tile <= (any ? TILE_ANY : TILE_128); ++tile) {
+    for (int tile = any ? TILE_ANY : TILE_256; tile <= (any ? TILE_ANY : TILE_128); ++tile) {
         if (rows < tile_of(tile, type).step && !any) continue;
 #ifdef DGS_GRAD_TILE      // (a CPU build that is to reach one kind on small matrices)
         if (!any && tile != DGS_GRAD_TILE) continue;
@@ -681,10 +695,8 @@ static void launch_tile(const GradArgs &a, dim3 grid, hipStream_t st)
 template <class T> static void launch_grad(const GradArgs &a, int tile, dim3 grid, hipStream_t st)
 {
     constexpr uint32_t STEP = PARTS<T> == 1 ? 64 : 32;
-    if constexpr (PARTS<T> == 1) {
-        if (tile == TILE_256) return launch_tile<T, 64, 256, 256, 8, 2>(a, grid, st);
-    }
-    if (tile == TILE_256_128) launch_tile<T, STEP, 256, 128, 8, 4>(a, grid, st);
+    if (tile == TILE_256) launch_tile<T, STEP, 256, 256, 8, 2>(a, grid, st);
+    else if (tile == TILE_256_128) launch_tile<T, STEP, 256, 128, 8, 4>(a, grid, st);
     else if (tile == TILE_128) launch_tile<T, 32, 128, 128, 4, 2>(a, grid, st);
     else hipLaunchKernelGGL(k_weight_grad<T>, grid, dim3(GRAD_THREADS), 0, st, a);
 }

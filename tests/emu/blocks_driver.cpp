@@ -392,10 +392,9 @@ static void weights()
 }
 
 // The same for the large tiles (of a build in which they are taken at any size).
-static void tiles(bool all)
+static void tiles()
 {
     for (int type : {F, H, B}) {
-        if (!all && type != B) continue;      // (the largest tile is for bfloat16)
         weight(64, 256, 256, type, true, true, true, 0, false);
         weight(300, 257, 150, type, true, true, true, 1, true);
         weight(330, 40, 264, type, true, false, true, 0, false);
@@ -407,7 +406,7 @@ int main(int argc, char **argv)
     const std::string what = argc > 1 ? argv[1] : "";
     if (what == "edges") edges();
     else if (what == "weights") { checkpoints(); weights(); }
-    else if (what == "tiles" || what == "tiles-bf16") tiles(what == "tiles");
+    else if (what == "tiles") tiles();
     else return 2;
     printf("%llu values as expected\n", (unsigned long long)checks);
     return 0;

@@ -36,7 +36,7 @@ def programs(tmp_path_factory):
 
 def test_block_kernels_on_the_cpu_under_asan_ubsan(programs):
     env = dict(os.environ, ASAN_OPTIONS="detect_leaks=0:detect_stack_use_after_return=0")
-    runs = [("dgs_weight_grad", "edges"), ("dgs_weight_grad", "weights"), ("tile0", "tiles-bf16"), ("tile1", "tiles")]
+    runs = [("dgs_weight_grad", "edges"), ("dgs_weight_grad", "weights"), ("tile0", "tiles"), ("tile1", "tiles")]
     procs = [(run, subprocess.Popen([programs[run[0]], run[1]], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, env=env)) for run in runs]
     try:
         for run, p in procs:

@@ -498,7 +498,8 @@ def test_weight_grad_of_whole_numbers(rows, outs, cols, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, F16, BF16])
-@pytest.mark.parametrize("rows, outs, cols", [(3, 40, 50), (100, 128, 130), (1024, 300, 256), (6000, 256, 512), (8192, 1024, 768)])
+@pytest.mark.parametrize("rows, outs, cols", [(3, 40, 50), (100, 128, 130), (1024, 300, 256), (6000, 256, 512), (8192, 1024, 768),
+                                              (600, 4096, 4096), (1100, 2300, 4001)])
 def test_weight_grad(rows, outs, cols, dtype):
     """Against 64 bits.  Every product is exact; a sum of n of them is rounded n times, its partial sums in random signs are of
     the size of the terms' 2-norm."""
