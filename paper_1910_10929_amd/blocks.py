@@ -12,6 +12,7 @@ anything is enqueued.  Nothing here is recorded by autograd.  There is no CPU fa
 from __future__ import annotations
 
 import ctypes
+import functools
 import struct
 
 import torch
@@ -105,19 +106,36 @@ def _vector(t, n, device, what):
     return t.data_ptr()
 
 
-# the handle of torch's current stream of a device (the short way is a fifth of a small call's time shorter)
+# the handle of torch's current stream of a device, and the current device (the short way is a fifth of a small call's time shorter)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda d: torch.cuda.current_stream(d).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _enqueue(what, device, call, *args):
     """call(*args, stream) on torch's current stream of the device."""
-    if torch.cuda.current_device() == device:
+    if _current_device() == device:
         rc = call(*args, _raw_stream(device))
     else:
         with torch.cuda.device(device):
             rc = call(*args, _raw_stream(device))
     if rc:
         raise DgsError(rc, what)
+
+
+@functools.lru_cache(maxsize=1024)
+def _backward_bytes(rows, cols, rows_per_gate):
+    return lib().dgs_edge_backward_workspace(rows, cols, rows_per_gate)
+
+
+@functools.lru_cache(maxsize=1024)
+def _weight_grad_bytes(rows, outs, cols, kind):
+    return lib().dgs_checkpoint_weight_grad_workspace(rows, outs, cols, kind)
+
+
+def _like(t, dtype, cols):
+    """A new matrix of the shape of `t`, whose columns are contiguous, with its pointer and stride."""
+    new = torch.empty_like(t, dtype=dtype)
+    return new, (new.data_ptr(), cols)
 
 
 def _workspace(given, need, like, device, what):
@@ -172,8 +190,9 @@ class Checkpoint:
         """The values, times `scale` and plus `shift` (fp32, one for each column), in `out` or a new tensor of `dtype`."""
         device = self.codes.get_device()
         if out is None:
-            out = torch.empty_like(self.codes, dtype=dtype)
-        data, stride = _matrix(out, self.rows, self.cols, device, "out")
+            out, (data, stride) = _like(self.codes, dtype, self.cols)
+        else:
+            data, stride = _matrix(out, self.rows, self.cols, device, "out")
         _enqueue("dgs_checkpoint_decode", device, lib().dgs_checkpoint_decode, self.rows, self.cols,
                  _CODES.pack(*self._place(self.rows, self.cols, device, "checkpoint")),
                  _vector(scale, self.cols, device, "scale"), _vector(shift, self.cols, device, "shift"), _type(out, "out"), data,
@@ -266,20 +285,20 @@ class Edge:
             pf, kind = _matrix(f, rows, cols, device, "f"), _type(f, "f")
             pg, gate_type, per = self._gate(gate, rows_per_gate, rows, device)
             if x_out is None:
-                x_out = torch.empty_like(x)
+                x_out, po = _like(x, x.dtype, cols)
             elif x_out.dtype != x.dtype:
                 _refuse("x_out: expected the type of x")
-            po = _matrix(x_out, rows, cols, device, "x_out")
+            else:
+                po = _matrix(x_out, rows, cols, device, "x_out")
         elif gate is not None or x_out is not None:
             _refuse("without f there is no gate and no x_out")
         if self.pre is not None:
             if u is None:
-                u = torch.empty_like(x if f is None else f)
-            elif f is None:
-                kind = _type(u, "u")
-            elif u.dtype != f.dtype:
+                u, pu = _like(x, x.dtype, cols) if f is None else _like(f, f.dtype, cols)
+            elif f is not None and u.dtype != f.dtype:
                 _refuse("u: expected the type of f")
-            pu = _matrix(u, rows, cols, device, "u")
+            else:
+                kind, pu = _type(u, "u"), _matrix(u, rows, cols, device, "u")
         elif u is not None:
             _refuse("u needs a norm before the block")
         post = pre = _NO_CODES
@@ -345,10 +364,11 @@ class Edge:
                 if saved.f.dtype != dtype:
                     _refuse("saved.f: expected the type of du")
             if df is None:
-                df = torch.empty_like(given, dtype=dtype)
+                df, pdf = _like(given, dtype, cols)
             elif df.dtype != dtype:
                 _refuse("df: expected the type of du")
-            pdf = _matrix(df, rows, cols, device, "df")
+            else:
+                pdf = _matrix(df, rows, cols, device, "df")
         elif df is not None:
             _refuse("df: the edge has no branch")
         pg, gate_type, per = self._gate(gate, rows_per_gate, rows, device)
@@ -357,15 +377,15 @@ class Edge:
                 _refuse("dgate: expected a gate of the same type")
             pdg = _matrix(dgate, gate.shape[0], cols, device, "dgate")
         if dx is None:
-            dx = torch.empty_like(given, dtype=stream_dtype)
+            dx, pdx = _like(given, stream_dtype, cols)
         elif dx.dtype != stream_dtype:
             _refuse("dx: expected the type of dx_out")
-        pdx = _matrix(dx, rows, cols, device, "dx")
+        else:
+            pdx = _matrix(dx, rows, cols, device, "dx")
         grads = (_vector(post_weight_grad, cols, device, "post_weight_grad"), _vector(post_bias_grad, cols, device, "post_bias_grad"),
                  _vector(pre_weight_grad, cols, device, "pre_weight_grad"), _vector(pre_bias_grad, cols, device, "pre_bias_grad"))
-        L = lib()
-        ws = _workspace(workspace, L.dgs_edge_backward_workspace(rows, cols, per), given, device, "dgs_edge_backward")
-        _enqueue("dgs_edge_backward", device, L.dgs_edge_backward, self._layer(device),
+        ws = _workspace(workspace, _backward_bytes(rows, cols, per), given, device, "dgs_edge_backward")
+        _enqueue("dgs_edge_backward", device, lib().dgs_edge_backward, self._layer(device),
                  _BACKWARD.pack(rows, per, _TYPES.get(stream_dtype, -1), _TYPES.get(dtype, -1), gate_type, int(accumulate), *pd, *pu,
                                 *pg, *pf, *px, *post, *pre, _vector(saved.stats, 4 * rows, device, "stats"), *pdx, *pdf, *pdg,
                                 *grads, ws.data_ptr(), ws.numel() * ws.element_size()))
@@ -382,9 +402,8 @@ def weight_grad(dy, saved, dw, db=None, scale=None, shift=None, accumulate=False
     if dw.dtype != torch.float32:
         _refuse("dw: expected float32")
     kind = _type(dy, "dy")
-    L = lib()
-    ws = _workspace(workspace, L.dgs_checkpoint_weight_grad_workspace(rows, outs, cols, kind), dy, device, "dgs_checkpoint_weight_grad")
-    _enqueue("dgs_checkpoint_weight_grad", device, L.dgs_checkpoint_weight_grad,
+    ws = _workspace(workspace, _weight_grad_bytes(rows, outs, cols, kind), dy, device, "dgs_checkpoint_weight_grad")
+    _enqueue("dgs_checkpoint_weight_grad", device, lib().dgs_checkpoint_weight_grad,
              _GRAD.pack(rows, outs, cols, kind, int(accumulate), 0, *_matrix(dy, rows, outs, device, "dy"),
                         *saved._place(rows, cols, device, "saved"), _vector(scale, cols, device, "scale"),
                         _vector(shift, cols, device, "shift"), *_matrix(dw, outs, cols, device, "dw"),
