@@ -8,8 +8,8 @@
 //
 // Bound by memory where there are rows enough: forward 8192 x 768, fp32 stream, bfloat16 branch, checkpoint, 88.6 MB in 18.3 us
 // (4.8 TB/s), 16384 x 4096 of bfloat16, 809 MB in 148 us (5.5); backward 8192 x 768 24.6 us and 4.0 for the partial sums
-// (88.6 MB, 3.1 TB/s: 16 wavefronts of one workgroup to a compute unit, four rounds of eight rows each), 16384 x 4096 675 MB in
-// 157 us and 5 (4.2).  A single row of 768: 3.5 us forward, all of it latency.
+// (88.6 MB, 3.1 TB/s: 16 wavefronts of one workgroup to a compute unit, four rounds of eight rows each), 16384 x 4096, 675 MB in
+// 142 us with its sums (4.8).  A single row of 768: 3.5 us forward, all of it latency.
 #include "dgs_rows.h"
 
 namespace dgs {

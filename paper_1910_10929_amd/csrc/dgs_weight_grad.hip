@@ -7,9 +7,10 @@
 // Both operands have the summed index (the row) outermost in memory.  They are staged in LDS as they lie, 16 bytes a lane,
 // and turned on the way out by the transposing LDS read, four rows of 16 columns to 16 lanes.
 //
-// Bound by the matrix units where the product is large (32768 rows, 4096 x 4096, bfloat16: 970 us, 1130 TFLOP/s; a matrix
+// Bound by the matrix units where the product is large (32768 rows, 4096 x 4096, bfloat16: 975 us, 1130 TFLOP/s; a matrix
 // product of the library's reaches 1260 on this card), by the partial sums of the split rows and by the tiles' first and
-// last steps where it is not (8192 rows, 2304 x 768: 50 us and 10 for the sums, 480 TFLOP/s together).
+// last steps where it is not (8192 rows, 2304 x 768: 50 us and 10 for the sums, 480 TFLOP/s together; 1500 rows,
+// 1001 x 333, fp32: 20 us and 5).
 #include "dgs_rows.h"
 
 namespace dgs {
@@ -276,8 +277,8 @@ __global__ __launch_bounds__(GRAD_THREADS) void k_weight_grad(GradArgs a)
 // step is one basic block (the rows that fill no step come first, addresses are scalar, nothing looks at a bound), which
 // the compiler can then order.
 // At 32768 rows, 4096 x 4096, bfloat16: 256 x 256 with four wavefronts of 128 x 128 took 1047 us, with eight 982, with the order
-// below 968; with branches around the loads 1680.  Half and fp32 take 2093 and 2595 us there, 3285 and 4075 on 256 x 128 when
-// all parts' fragments were held at a time.  At 8192 rows, 2304 x 768, bfloat16: 128 x 128 57 us, 256 x 128 53 (half the
+// below 968; with branches around the loads 1680.  Half and fp32 take 2093 and 2595 us there, 3285 and 4075 on 256 x 128
+// with all parts' fragments held at a time and three times the instructions to split a value.  At 8192 rows, 2304 x 768, bfloat16: 128 x 128 57 us, 256 x 128 53 (half the
 // partial sums).
 template <uint32_t WIDTH> __device__ __forceinline__ uint32_t wide_at(uint32_t k, uint32_t c) { return k * WIDTH + ((c ^ ((k & 3u) << 2)) << 3); }
 
