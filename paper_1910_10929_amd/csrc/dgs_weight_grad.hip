@@ -278,8 +278,8 @@ __global__ __launch_bounds__(GRAD_THREADS) void k_weight_grad(GradArgs a)
 // the compiler can then order.
 // At 32768 rows, 4096 x 4096, bfloat16: 256 x 256 with four wavefronts of 128 x 128 took 1047 us, with eight 982, with the order
 // below 968; with branches around the loads 1680.  Half and fp32 take 2093 and 2595 us there, 3285 and 4075 on 256 x 128
-// with all parts' fragments held at a time and three times the instructions to split a value.  At 8192 rows, 2304 x 768, bfloat16: 128 x 128 57 us, 256 x 128 53 (half the
-// partial sums).
+// with all parts' fragments held at a time and three times the instructions to split a value.  At 8192 rows, 2304 x 768,
+// bfloat16: 128 x 128 57 us, 256 x 128 53 (half the partial sums).
 template <uint32_t WIDTH> __device__ __forceinline__ uint32_t wide_at(uint32_t k, uint32_t c) { return k * WIDTH + ((c ^ ((k & 3u) << 2)) << 3); }
 
 template <uint32_t W> struct Width { static constexpr uint32_t value = W; };
