@@ -97,8 +97,9 @@ int dgs_edge_forward(const dgs_edge *edge /*host*/, const dgs_edge_forward_args 
  *     dgate = branch * sum over the gate row's rows of d * (fh * post_weight + post_bias)
  *     post_weight' = sum_rows m fh,  post_bias' = sum_rows m,  pre_weight' = sum_rows du xh,  pre_bias' = sum_rows du
  *
- * fh and xh come from the checkpoints, or are computed from `f` and `x_out` (which then have `type` and `stream_type`)
- * and the stats; both norms the same way.  stats: as dgs_edge_forward wrote them.  du absent or pre = NONE: nothing is
+ * fh and xh come from the checkpoints, or are computed from `f` and `x_out` (which then have `type` and `stream_type`,
+ * and are as the forward pass read and wrote them: of an f that u was written over, nothing is left) and the stats; both
+ * norms the same way.  stats: as dgs_edge_forward wrote them.  du absent or pre = NONE: nothing is
  * read of xh; neither f nor post_saved: an edge without a branch (df, dgate, post gradients must be absent).
  * Any output may be absent.  dgate has gate_type.  accumulate != 0: the four parameter gradients, and a dgate of
  * DGS_F32, are added to; otherwise written.  All sums are taken in fp32, in an order that is fixed by the sizes.

@@ -202,7 +202,8 @@ class Checkpoint:
 
 class Saved:
     """What `Edge.forward` keeps of `rows` rows for `Edge.backward`: the norms' statistics, and of each norm's result a
-    checkpoint (`post`, `pre`) or, with checkpoints=False, the matrices it was taken of (`f`, `x_out`), by reference."""
+    checkpoint (`post`, `pre`) or, with checkpoints=False, the matrices it was taken of (`f`, `x_out`), by reference: those must
+    stay as they are until then."""
 
     def __init__(self, rows, cols, device="cuda:0", checkpoints=True, stats=None, post=None, pre=None, f=None, x_out=None):
         given = post is not None or pre is not None or f is not None or x_out is not None
@@ -271,7 +272,7 @@ class Edge:
 
     def forward(self, x, f=None, gate=None, rows_per_gate=None, x_out=None, u=None, save=None):
         """One pass over the rows; returns (x_out, u).  Without f there is no branch: x_out is x.  Without `pre`, u is None.
-        x_out may be x and u may be f.  save: a `Saved` that is filled."""
+        x_out may be x, and u may be f unless `save` keeps f itself.  save: a `Saved` that is filled."""
         device = _on_gpu(x, "x")
         if x.dim() != 2:
             _refuse("x: expected a matrix")
@@ -311,6 +312,9 @@ class Edge:
                 post = save.post._place(rows, cols, device, "save.post")
             if self.pre is not None and save.pre is not None:
                 pre = save.pre._place(rows, cols, device, "save.pre")
+            # (a tensor without memory is at 0, and so is one that is not there)
+            if (save.post is None and pf[0] and pf[0] in (po[0], pu[0])) or (save.pre is None and pu[0] and pu[0] == (px if f is None else po)[0]):
+                _refuse("save: an output lies over a matrix that is kept for the backward pass")
         _enqueue("dgs_edge_forward", device, lib().dgs_edge_forward, self._layer(device),
                  _FORWARD.pack(rows, per, stream, kind, gate_type, 0, *px, *pf, *pg, *po, *pu, *post, *pre, stats))
         if save is not None:
