@@ -51,12 +51,14 @@ class Stack:
         self.edges = [blocks.Edge(width, post="rms" if b > 0 else None, pre="layer" if b < count else None,
                                   post_weight=p(b - 1, "post_weight"), post_bias=p(b - 1, "post_bias"),
                                   pre_weight=p(b, "pre_weight"), pre_bias=p(b, "pre_bias")) for b in range(count + 1)]
-        self.saved = [blocks.Saved(rows, width, device=device) for _ in range(count + 1)]
+        # (no branch ends at the first edge, no block begins behind the last one)
+        self.saved = [blocks.Saved(rows, width, device=device, post=blocks.Checkpoint(rows, width, device) if b > 0 else None,
+                                   pre=blocks.Checkpoint(rows, width, device) if b < count else None) for b in range(count + 1)]
         self.kept = [(blocks.Checkpoint(rows, hidden, device), blocks.Checkpoint(rows, hidden, device)) for _ in range(count)]
 
     def kept_bytes(self):
         """What the forward pass leaves for the backward pass."""
-        c = [k for pair in self.kept for k in pair] + [k for s in self.saved for k in (s.post, s.pre)]
+        c = [k for pair in self.kept for k in pair] + [k for s in self.saved for k in (s.post, s.pre) if k is not None]
         return sum(k.codes.numel() + k.exps.numel() for k in c) + sum(s.stats.numel() * 4 for s in self.saved)
 
     def forward(self, x):
@@ -85,10 +87,7 @@ class Stack:
                 more.update(pre_weight_grad=g("pre_weight", b), pre_bias_grad=g("pre_bias", b))
             else:
                 more["du"] = None
-            saved = self.saved[b]
-            if b == 0:      # (no branch ends here)
-                saved = blocks.Saved(self.rows, self.width, stats=saved.stats, pre=saved.pre)
-            dx, df = self.edges[b].backward(saved, dx_out=dx, du=more.pop("du", du), accumulate=True, **more)
+            dx, df = self.edges[b].backward(self.saved[b], dx_out=dx, du=more.pop("du", du), accumulate=True, **more)
             if b == 0:
                 return dx
             h, a = self.kept[b - 1]

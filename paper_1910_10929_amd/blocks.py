@@ -203,13 +203,15 @@ class Checkpoint:
 class Saved:
     """What `Edge.forward` keeps of `rows` rows for `Edge.backward`: the norms' statistics, and of each norm's result a
     checkpoint (`post`, `pre`) or, with checkpoints=False, the matrices it was taken of (`f`, `x_out`), by reference: those must
-    stay as they are until then."""
+    stay as they are until then.  `branch`: whether there was one; without a forward pass (None), whether something of it is
+    here."""
 
     def __init__(self, rows, cols, device="cuda:0", checkpoints=True, stats=None, post=None, pre=None, f=None, x_out=None):
         given = post is not None or pre is not None or f is not None or x_out is not None
         self.rows, self.cols = rows, cols
         self.stats = stats if stats is not None else torch.empty((rows, 4), dtype=torch.float32, device=device)
         self.post, self.pre, self.f, self.x_out = post, pre, f, x_out
+        self.branch = None
         if checkpoints and not given:
             self.post, self.pre = Checkpoint(rows, cols, device), Checkpoint(rows, cols, device)
 
@@ -318,6 +320,7 @@ class Edge:
         _enqueue("dgs_edge_forward", device, lib().dgs_edge_forward, self._layer(device),
                  _FORWARD.pack(rows, per, stream, kind, gate_type, 0, *px, *pf, *pg, *po, *pu, *post, *pre, stats))
         if save is not None:
+            save.branch = f is not None
             if save.post is None:
                 save.f = f
             if save.pre is None:
@@ -337,7 +340,12 @@ class Edge:
         rows, cols = saved.rows, self.cols
         if saved.cols != cols:
             _refuse("saved: of another shape")
-        coded, branch = saved.post is not None, saved.post is not None or saved.f is not None
+        coded = saved.post is not None
+        branch = coded or saved.f is not None
+        if saved.branch is not None:
+            if saved.branch and not branch:
+                _refuse("saved: nothing of the branch")
+            branch = saved.branch
         pd = pu = pf = px = pdf = pdg = _NO_MATRIX
         post = pre = _NO_CODES
         stream_dtype = dx_out.dtype if dx_out is not None else (saved.x_out.dtype if saved.x_out is not None else

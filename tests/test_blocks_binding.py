@@ -46,3 +46,53 @@ def test_values_kept_are_not_written_over(calls, post):
     empty = torch.zeros(0, 32, dtype=BF16)      # (tensors without memory share no address)
     e.forward(torch.zeros(0, 32), empty, u=torch.zeros(0, 32, dtype=BF16), save=saved_of(0, 32, checkpoints=False))
     assert len(calls) == 4
+
+
+def forward_of(args):
+    """The packed arguments of a forward call, by name."""
+    v = blocks._FORWARD.unpack(args[1])
+    return dict(zip(("rows", "per", "stream", "type", "gate_type", "reserved", "x", "xs", "f", "fs", "gate", "gs", "xo", "xos", "u", "us", "pc", "pcs",
+                     "pe", "pes", "nc", "ncs", "ne", "nes", "stats"), v))
+
+
+def backward_of(args):
+    v = blocks._BACKWARD.unpack(args[1])
+    return dict(zip(("rows", "per", "stream", "type", "gate_type", "accumulate", "d", "ds", "du", "dus", "gate", "gs", "f", "fs", "x", "xs", "pc",
+                     "pcs", "pe", "pes", "nc", "ncs", "ne", "nes", "stats", "dx", "dxs", "df", "dfs", "dg", "dgs", "gpw", "gpb", "gnw", "gnb", "ws",
+                     "wsb"), v))
+
+
+@pytest.mark.parametrize("coded", [True, False])
+def test_an_edge_without_a_branch_stays_one(calls, coded):
+    """What a Saved has room for says nothing about the forward pass: backward goes by what forward did, the last time."""
+    first, inner = blocks.Edge(32, pre="layer"), blocks.Edge(32, post="rms", pre="layer")
+    x, f = torch.zeros(6, 32), torch.zeros(6, 32)
+    saved = saved_of(6, 32, checkpoints=coded)
+    for branch in (False, True, False):
+        e = inner if branch else first
+        e.forward(x, f if branch else None, save=saved)
+        assert (forward_of(calls[-1][1])["pc"] != 0) == (branch and coded)
+        dx, df = e.backward(saved, dx_out=x, du=f)
+        a = backward_of(calls[-1][1])
+        assert (df is not None) == branch and (a["df"] != 0) == branch
+        assert (a["pc"] != 0) == (branch and coded) and (a["f"] != 0) == (branch and not coded)
+        assert (a["nc"] != 0) == coded and (a["x"] != 0) == (not coded)
+        if not branch:
+            with pytest.raises(dgs.DgsError):
+                e.backward(saved, dx_out=x, du=f, df=torch.zeros(6, 32))
+
+
+def test_saved_that_is_put_together_by_hand(calls):
+    """Without a forward pass, what it holds says what the edge has."""
+    c = lambda: blocks.Checkpoint(6, 32, "cpu")  # noqa: E731
+    x = torch.zeros(6, 32)
+    e, first = blocks.Edge(32, post="rms", pre="layer"), blocks.Edge(32, pre="layer")
+    assert e.backward(saved_of(6, 32, post=c(), pre=c()), dx_out=x, du=x)[1] is not None
+    assert e.backward(saved_of(6, 32, f=x.clone(), x_out=x), dx_out=x, du=x)[1] is not None
+    assert first.backward(saved_of(6, 32, pre=c()), dx_out=x, du=x)[1] is None
+    # what a forward pass with a branch kept has been taken away
+    saved = saved_of(6, 32)
+    e.forward(x, x.clone(), save=saved)
+    saved.post = None
+    with pytest.raises(dgs.DgsError):
+        e.backward(saved, dx_out=x, du=x)
