@@ -82,7 +82,7 @@ class Stack:
             more = {}
             if b > 0:
                 more = dict(gate=self.p[f"{b - 1}.gate"], dgate=g("gate", b - 1), post_weight_grad=g("post_weight", b - 1),
-                            post_bias_grad=g("post_bias", b - 1), df=torch.empty_like(dx, dtype=torch.bfloat16))
+                            post_bias_grad=g("post_bias", b - 1))
             if b < self.count:
                 more.update(pre_weight_grad=g("pre_weight", b), pre_bias_grad=g("pre_bias", b))
             else:

@@ -204,14 +204,14 @@ class Saved:
     """What `Edge.forward` keeps of `rows` rows for `Edge.backward`: the norms' statistics, and of each norm's result a
     checkpoint (`post`, `pre`) or, with checkpoints=False, the matrices it was taken of (`f`, `x_out`), by reference: those must
     stay as they are until then.  `branch`: whether there was one; without a forward pass (None), whether something of it is
-    here."""
+    here.  `dtypes`: the stream's and the branch's."""
 
     def __init__(self, rows, cols, device="cuda:0", checkpoints=True, stats=None, post=None, pre=None, f=None, x_out=None):
         given = post is not None or pre is not None or f is not None or x_out is not None
         self.rows, self.cols = rows, cols
         self.stats = stats if stats is not None else torch.empty((rows, 4), dtype=torch.float32, device=device)
         self.post, self.pre, self.f, self.x_out = post, pre, f, x_out
-        self.branch = None
+        self.branch, self.dtypes = None, (None, None)
         if checkpoints and not given:
             self.post, self.pre = Checkpoint(rows, cols, device), Checkpoint(rows, cols, device)
 
@@ -320,7 +320,7 @@ class Edge:
         _enqueue("dgs_edge_forward", device, lib().dgs_edge_forward, self._layer(device),
                  _FORWARD.pack(rows, per, stream, kind, gate_type, 0, *px, *pf, *pg, *po, *pu, *post, *pre, stats))
         if save is not None:
-            save.branch = f is not None
+            save.branch, save.dtypes = f is not None, (x.dtype, f.dtype if f is not None else u.dtype)
             if save.post is None:
                 save.f = f
             if save.pre is None:
@@ -332,7 +332,8 @@ class Edge:
                  workspace=None):
         """Gradients, from those that arrive at x_out and u (None: zero); returns (dx, df), df None for an edge without a
         branch.  Parameter gradients are written, or with `accumulate` added, to the fp32 vectors given; dgate (gate's type)
-        is written, or added to where it is fp32.  dx may be dx_out, df may be du."""
+        is written, or added to where it is fp32.  dx may be dx_out, df may be du; new ones have the types of dx_out and du, or
+        where those are absent of x and f."""
         given = dx_out if dx_out is not None else du
         if given is None:
             _refuse("dx_out or du is needed")
@@ -348,10 +349,16 @@ class Edge:
             branch = saved.branch
         pd = pu = pf = px = pdf = pdg = _NO_MATRIX
         post = pre = _NO_CODES
-        stream_dtype = dx_out.dtype if dx_out is not None else (saved.x_out.dtype if saved.x_out is not None else
-                                                                dx.dtype if dx is not None else du.dtype)
-        dtype = (du.dtype if du is not None else saved.f.dtype if saved.f is not None else
-                 df.dtype if df is not None else stream_dtype)
+        stream_dtype = (dx_out.dtype if dx_out is not None else saved.x_out.dtype if saved.x_out is not None else
+                        dx.dtype if dx is not None else None)
+        dtype = (du.dtype if du is not None else saved.f.dtype if saved.f is not None else df.dtype if df is not None else None)
+        # A type that nothing given says is that of the forward pass, where that goes with the other type, and otherwise the other.
+        if stream_dtype is None:
+            kept = saved.dtypes[0]
+            stream_dtype = kept if kept in (torch.float32, dtype) else dtype
+        if dtype is None:
+            kept = saved.dtypes[1]
+            dtype = kept if kept is not None and stream_dtype in (torch.float32, kept) else stream_dtype
         if dx_out is not None:
             pd = _matrix(dx_out, rows, cols, device, "dx_out")
         if du is not None:

@@ -96,3 +96,42 @@ def test_saved_that_is_put_together_by_hand(calls):
     saved.post = None
     with pytest.raises(dgs.DgsError):
         e.backward(saved, dx_out=x, du=x)
+
+
+@pytest.mark.parametrize("coded", [True, False])
+@pytest.mark.parametrize("stream, kind", [(F32, BF16), (F32, F16), (F32, F32), (BF16, BF16)])
+def test_gradients_have_the_types_of_the_forward_pass(calls, stream, kind, coded):
+    """Where a gradient is absent and no place is given for the result, its type is that of x or f -- not the other one's."""
+    e, last, first = blocks.Edge(32, post="rms", pre="layer"), blocks.Edge(32, post="rms"), blocks.Edge(32, pre="rms")
+    x, f = torch.zeros(6, 32, dtype=stream), torch.zeros(6, 32, dtype=kind)
+    gate = torch.zeros(1, 32, dtype=kind)
+    number = lambda t: blocks._TYPES[t]  # noqa: E731
+    saved = saved_of(6, 32, checkpoints=coded)
+    e.forward(x, f, gate=gate, save=saved)
+    dx, df = e.backward(saved, du=f, gate=gate)
+    assert (dx.dtype, df.dtype) == (stream, kind)
+    last.forward(x, f, gate=gate, save=saved)
+    dx, df = last.backward(saved, dx_out=x, gate=gate, dgate=torch.zeros_like(gate))
+    assert (dx.dtype, df.dtype) == (stream, kind)
+    a = backward_of(calls[-1][1])
+    assert (a["stream"], a["type"], a["gate_type"]) == (number(stream), number(kind), number(kind))
+    first.forward(x, u=torch.zeros(6, 32, dtype=kind), save=saved)
+    dx, df = first.backward(saved, du=f)
+    assert dx.dtype == stream and df is None
+
+
+def test_gradients_of_other_types_than_the_forward_pass(calls):
+    """What is given goes before what was remembered, and what was remembered is left where it does not go with that."""
+    e = blocks.Edge(32, post="rms", pre="layer")
+    half, full = torch.zeros(6, 32, dtype=BF16), torch.zeros(6, 32)
+    saved = saved_of(6, 32)
+    e.forward(half, half.clone(), save=saved)
+    assert [t.dtype for t in e.backward(saved, dx_out=full, du=full)] == [F32, F32]
+    assert [t.dtype for t in e.backward(saved, du=full)] == [F32, F32]
+    assert [t.dtype for t in e.backward(saved, du=half, dx=full)] == [F32, BF16]
+    assert [t.dtype for t in e.backward(saved, dx_out=full)] == [F32, BF16]
+    assert [t.dtype for t in e.backward(saved, dx_out=full, df=full)] == [F32, F32]
+    # nothing remembered: as the gradient that is there
+    by_hand = saved_of(6, 32, stats=saved.stats, post=saved.post, pre=saved.pre)
+    assert [t.dtype for t in e.backward(by_hand, du=half)] == [BF16, BF16]
+    assert [t.dtype for t in e.backward(by_hand, dx_out=full)] == [F32, F32]

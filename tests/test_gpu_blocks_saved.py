@@ -43,3 +43,17 @@ def test_backward_without_a_branch(case, coded):
         assert_near(got[name], want[name], terms.abs().amax(0), name, extra=8 * rows ** 0.5 * EPS * terms.square().sum(0).sqrt())
     with pytest.raises(dgs.DgsError):
         c.edge.backward(saved, dx_out=d_in, du=u_in, post_weight_grad=torch.zeros(cols, device=DEV))
+
+
+@pytest.mark.parametrize("coded", [True, False])
+def test_absent_gradients_without_places_for_the_results(coded):
+    """An fp32 stream with a bfloat16 branch: a gradient that is absent is one of zeros, and changes no result's type."""
+    c = Case((50, 96, F32, BF16, "rms", "layer", True, 7, BF16, 0))
+    saved = blocks.Saved(50, 96, device=DEV, checkpoints=coded)
+    c.edge.forward(c.x, c.f, gate=c.gate, rows_per_gate=7, save=saved)
+    d, u = c.make(50, 96, F32), c.make(50, 96, BF16)
+    for have, zeros in ((dict(d_in=d, u_in=None), dict(d_in=d, u_in=torch.zeros_like(u))), (dict(d_in=None, u_in=u), dict(d_in=torch.zeros_like(d), u_in=u))):
+        a, b = run_backward(c, saved, **have), run_backward(c, saved, **zeros)
+        assert (a["dx"].dtype, a["df"].dtype) == (F32, BF16)
+        for k in a:
+            assert torch.equal(a[k], b[k]), k
