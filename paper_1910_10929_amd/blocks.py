@@ -262,15 +262,18 @@ class Edge:
         """Pointer and stride, type, rows for each gate row."""
         if gate is None:
             return _NO_MATRIX, F32, 0
+        if gate.dim() != 2:
+            _refuse("gate: expected a matrix")
+        count = gate.shape[0]
         if rows_per_gate is None:
-            count = gate.shape[0]
-            if count == 0 or rows % count:
+            if rows and (count == 0 or rows % count):
                 _refuse("gate: rows_per_gate is needed where the gate rows do not divide the rows")
-            rows_per_gate = max(rows // count, 1)
+            rows_per_gate = max(rows // count, 1) if rows else 1
         elif rows_per_gate < 1:
             _refuse("rows_per_gate is at least 1")
-        return (_matrix(gate, (rows + rows_per_gate - 1) // rows_per_gate, self.cols, device, "gate"), _type(gate, "gate"),
-                rows_per_gate)
+        if rows:      # (any gate goes with no rows)
+            count = (rows + rows_per_gate - 1) // rows_per_gate
+        return _matrix(gate, count, self.cols, device, "gate"), _type(gate, "gate"), rows_per_gate
 
     def forward(self, x, f=None, gate=None, rows_per_gate=None, x_out=None, u=None, save=None):
         """One pass over the rows; returns (x_out, u).  Without f there is no branch: x_out is x.  Without `pre`, u is None.
@@ -408,6 +411,8 @@ class Edge:
                  _BACKWARD.pack(rows, per, _TYPES.get(stream_dtype, -1), _TYPES.get(dtype, -1), gate_type, int(accumulate), *pd, *pu,
                                 *pg, *pf, *px, *post, *pre, _vector(saved.stats, 4 * rows, device, "stats"), *pdx, *pdf, *pdg,
                                 *grads, ws.data_ptr(), ws.numel() * ws.element_size()))
+        if rows == 0 and dgate is not None and not (accumulate and dgate.dtype == torch.float32):
+            dgate.zero_()       # (the library knows of no gate rows then)
         return dx, df
 
 

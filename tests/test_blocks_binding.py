@@ -135,3 +135,24 @@ def test_gradients_of_other_types_than_the_forward_pass(calls):
     by_hand = saved_of(6, 32, stats=saved.stats, post=saved.post, pre=saved.pre)
     assert [t.dtype for t in e.backward(by_hand, du=half)] == [BF16, BF16]
     assert [t.dtype for t in e.backward(by_hand, dx_out=full)] == [F32, F32]
+
+
+@pytest.mark.parametrize("gates, per", [(0, None), (0, 5), (1, None), (1, 7), (3, None), (3, 2)])
+def test_no_rows_under_a_gate(calls, gates, per):
+    """A batch without rows takes the gate that other batches take; its gradient is zero, or with accumulate what it was."""
+    e = blocks.Edge(32, post="rms", pre="layer")
+    none = torch.zeros(0, 32)
+    saved = saved_of(0, 32)
+    for kind in (F32, BF16):
+        f = none.to(kind)
+        gate = torch.zeros(gates, 32, dtype=kind)
+        xo, u = e.forward(none, f, gate=gate, rows_per_gate=per, save=saved)
+        assert xo.shape == u.shape == (0, 32)
+        for accumulate in (False, True):
+            dgate = torch.full_like(gate, 3.0)
+            e.backward(saved, dx_out=none, du=f, gate=gate, rows_per_gate=per, dgate=dgate, accumulate=accumulate)
+            assert bool((dgate == (3.0 if accumulate and kind == F32 else 0.0)).all())
+    assert len(calls) == 6
+    for bad in (dict(gate=torch.zeros(1, 31)), dict(gate=torch.zeros(32)), dict(gate=torch.zeros(1, 32), rows_per_gate=0)):
+        with pytest.raises(dgs.DgsError):
+            e.forward(none, none, **bad)

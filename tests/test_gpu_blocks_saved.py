@@ -57,3 +57,17 @@ def test_absent_gradients_without_places_for_the_results(coded):
         assert (a["dx"].dtype, a["df"].dtype) == (F32, BF16)
         for k in a:
             assert torch.equal(a[k], b[k]), k
+
+
+def test_no_rows_under_a_gate():
+    e = blocks.Edge(64, post="rms", pre="layer")
+    x = torch.empty(0, 64, device=DEV)
+    gate = torch.ones(1, 64, device=DEV)
+    saved = blocks.Saved(0, 64, device=DEV)
+    xo, u = e.forward(x, x.clone(), gate=gate, save=saved)
+    assert xo.shape == u.shape == (0, 64)
+    dgate, grad = torch.full((1, 64), 3.0, device=DEV), torch.full((64,), 3.0, device=DEV)
+    e.backward(saved, dx_out=x, du=x, gate=gate, dgate=dgate, post_weight_grad=grad, accumulate=True)
+    assert bool((dgate == 3.0).all()) and bool((grad == 3.0).all())
+    e.backward(saved, dx_out=x, du=x, gate=gate, dgate=dgate, post_weight_grad=grad)
+    assert bool((dgate == 0.0).all()) and bool((grad == 0.0).all())
