@@ -18,12 +18,13 @@ import struct
 import torch
 
 from . import dgs
-from .dgs import DGS_EINVAL, DgsError
+from .dgs import DGS_EINVAL, DGS_ENOTSUP, DgsError
 
 F32, F16, BF16 = 0, 1, 2
 NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
 EDGE_MAX_COLS = 16384
 CHECKPOINT_RUN = 32
+_MOST = 0x7FFFFFFF      # rows, or columns
 
 EXPORTS = [
     "dgs_edge_forward", "dgs_edge_backward_workspace", "dgs_edge_backward", "dgs_checkpoint_encode", "dgs_checkpoint_decode",
@@ -63,6 +64,12 @@ def lib():
 
 def _refuse(what):
     raise DgsError(DGS_EINVAL, what)
+
+
+def _fits(n, what):
+    """(Sizes go to the library in 32 bits, and would arrive as what is left of them.)"""
+    if n > _MOST:
+        raise DgsError(DGS_ENOTSUP, f"{what}: more than 2^31 - 1")
 
 
 def _type(t, what):
@@ -150,6 +157,8 @@ class Checkpoint:
     """A rows x cols matrix in 8 bits: `codes` (int8) and `exps` (uint8, one for 32 columns of a row)."""
 
     def __init__(self, rows, cols, device="cuda:0", codes=None, exps=None):
+        _fits(rows, "rows")
+        _fits(cols, "columns")
         self.rows, self.cols = rows, cols
         runs = self._runs = (cols + CHECKPOINT_RUN - 1) // CHECKPOINT_RUN
         if codes is None and exps is None:
@@ -207,6 +216,7 @@ class Saved:
     here.  `dtypes`: the stream's and the branch's."""
 
     def __init__(self, rows, cols, device="cuda:0", checkpoints=True, stats=None, post=None, pre=None, f=None, x_out=None):
+        _fits(rows, "rows")
         given = post is not None or pre is not None or f is not None or x_out is not None
         self.rows, self.cols = rows, cols
         self.stats = stats if stats is not None else torch.empty((rows, 4), dtype=torch.float32, device=device)
@@ -236,6 +246,7 @@ class Edge:
             _refuse("post_weight and post_bias need a norm")
         if pre is None and (pre_weight is not None or pre_bias is not None):
             _refuse("pre_weight and pre_bias need a norm")
+        _fits(cols, "columns")
         self.cols, self.post, self.pre = cols, post, pre
         self._fixed = (cols, _NORMS[post], _NORMS[pre], eps if post_eps is None else post_eps, eps if pre_eps is None else pre_eps,
                        skip_scale, branch_scale)
@@ -273,7 +284,7 @@ class Edge:
             _refuse("rows_per_gate is at least 1")
         if rows:      # (any gate goes with no rows)
             count = (rows + rows_per_gate - 1) // rows_per_gate
-        return _matrix(gate, count, self.cols, device, "gate"), _type(gate, "gate"), rows_per_gate
+        return _matrix(gate, count, self.cols, device, "gate"), _type(gate, "gate"), min(rows_per_gate, _MOST)
 
     def forward(self, x, f=None, gate=None, rows_per_gate=None, x_out=None, u=None, save=None):
         """One pass over the rows; returns (x_out, u).  Without f there is no branch: x_out is x.  Without `pre`, u is None.
@@ -282,6 +293,7 @@ class Edge:
         if x.dim() != 2:
             _refuse("x: expected a matrix")
         rows, cols = x.size(0), self.cols
+        _fits(rows, "rows")
         px = _matrix(x, rows, cols, device, "x")
         stream = _type(x, "x")
         pf = pg = po = pu = _NO_MATRIX
@@ -423,6 +435,7 @@ def weight_grad(dy, saved, dw, db=None, scale=None, shift=None, accumulate=False
     if dy.dim() != 2 or dw.dim() != 2:
         _refuse("dy and dw: expected matrices")
     rows, outs, cols = dy.shape[0], dy.shape[1], saved.cols
+    _fits(outs, "outputs")
     if dw.dtype != torch.float32:
         _refuse("dw: expected float32")
     kind = _type(dy, "dy")

@@ -156,3 +156,31 @@ def test_no_rows_under_a_gate(calls, gates, per):
     for bad in (dict(gate=torch.zeros(1, 31)), dict(gate=torch.zeros(32)), dict(gate=torch.zeros(1, 32), rows_per_gate=0)):
         with pytest.raises(dgs.DgsError):
             e.forward(none, none, **bad)
+
+
+def large(rows, cols, dtype):
+    """A matrix without memory."""
+    return torch.empty(rows, cols, dtype=dtype, device="meta")
+
+
+@pytest.mark.parametrize("rows, cols", [(2 ** 31, 1), (2 ** 32, 1), (2 ** 32 + 5, 3), (1, 2 ** 32), (2, 2 ** 32 + 64)])
+def test_sizes_beyond_32_bits(calls, rows, cols):
+    """Sizes go to the library in 32 bits: what does not fit is refused, and not taken for what is left of it."""
+    x = large(rows, cols, F32)
+    bad = [
+        lambda: blocks.Checkpoint(rows, cols, "meta"), lambda: blocks.Checkpoint.of(large(rows, cols, torch.int8), large(rows, (cols + 31) // 32, torch.uint8)),
+        lambda: blocks.Saved(rows, cols, "meta"), lambda: blocks.Edge(cols, pre="rms").forward(x), lambda: blocks.Edge(cols, post="rms").forward(x, x),
+        lambda: blocks.Edge(cols, post="rms").backward(blocks.Saved(rows, cols, "meta", checkpoints=False, f=x), dx_out=x),
+        lambda: blocks.weight_grad(large(4, max(rows, cols), F32), blocks.Checkpoint(4, 32, "meta"), large(max(rows, cols), 32, F32)),
+    ]
+    for call in bad:
+        with pytest.raises(dgs.DgsError) as err:
+            call()
+        assert err.value.code == dgs.DGS_ENOTSUP
+    assert not calls
+
+
+def test_more_rows_for_a_gate_row_than_there_are(calls):
+    x = torch.zeros(6, 32)
+    blocks.Edge(32, post="rms").forward(x, x.clone(), gate=x[:1], rows_per_gate=2 ** 40)
+    assert forward_of(calls[0][1])["per"] >= 6
