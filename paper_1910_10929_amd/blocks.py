@@ -176,6 +176,8 @@ class Checkpoint:
     @classmethod
     def of(cls, codes, exps):
         """A checkpoint that lies in the given tensors."""
+        if codes.dim() != 2:
+            _refuse("codes: expected a matrix")
         return cls(codes.shape[0], codes.shape[1], codes=codes, exps=exps)
 
     def _place(self, rows, cols, device, what):

@@ -184,3 +184,18 @@ def test_more_rows_for_a_gate_row_than_there_are(calls):
     x = torch.zeros(6, 32)
     blocks.Edge(32, post="rms").forward(x, x.clone(), gate=x[:1], rows_per_gate=2 ** 40)
     assert forward_of(calls[0][1])["per"] >= 6
+
+
+def test_what_is_no_matrix(calls):
+    m, c = torch.zeros(6, 32), blocks.Checkpoint(6, 32, "cpu")
+    e, saved = blocks.Edge(32, post="rms", pre="layer"), saved_of(6, 32)
+    for wrong in (torch.zeros(()), torch.zeros(32), torch.zeros(1, 6, 32)):
+        for call in (lambda: blocks.Checkpoint.of(wrong.to(torch.int8), c.exps), lambda: blocks.Checkpoint.of(c.codes, wrong.to(torch.uint8)),
+                     lambda: c.encode(wrong), lambda: c.decode(out=wrong), lambda: e.forward(wrong, m), lambda: e.forward(m, wrong),
+                     lambda: e.forward(m, m, gate=wrong), lambda: e.forward(m, m, gate=wrong, rows_per_gate=6),
+                     lambda: e.backward(saved, dx_out=wrong, du=m), lambda: e.backward(saved, dx_out=m, du=m, gate=m[:1], dgate=wrong),
+                     lambda: blocks.weight_grad(wrong, c, m), lambda: blocks.weight_grad(m, c, wrong)):
+            with pytest.raises(dgs.DgsError) as err:
+                call()
+            assert err.value.code == dgs.DGS_EINVAL
+    assert not calls
