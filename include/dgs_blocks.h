@@ -139,7 +139,8 @@ int dgs_checkpoint_decode(uint32_t rows, uint32_t cols, const dgs_codes *from /*
  *     db = sum_rows dy                                                    outs floats, or NULL
  *
  * dy: rows x outs of `type`.  Every product of dy and a checkpoint value is exact in fp32 -- DGS_F16 and DGS_F32 values go
- * through the matrix units as two and three bfloat16 parts -- and sums are fp32, in an order that is fixed by the sizes.
+ * through the matrix units as two and three bfloat16 parts -- and sums are fp32, in an order that is fixed by the sizes.  (Of a
+ * DGS_F32 value below 2^-110, what is no multiple of 2^-133 is left out.)
  * accumulate != 0: dw and db are added to.  workspace: at least dgs_checkpoint_weight_grad_workspace() bytes, 16-byte
  * aligned; as above.  Rows of dy or of the checkpoint 2^27 bytes or more apart: DGS_ENOTSUP.
  */

@@ -2,7 +2,8 @@
 //
 // A checkpoint's values are exact in bfloat16, so the codes become matrix operands without a second rounding; so does dy,
 // in one part (bfloat16), two (half: 11 bits) or three (fp32: 24 bits), each taken off the rest by truncation.  Products
-// are then exact in fp32 and only the sums round.
+// are then exact in fp32 and only the sums round.  (The matrix units keep subnormal parts, whose unit is 2^-133: an fp32 value
+// below 2^-110 loses what is less.)
 //
 // Both operands have the summed index (the row) outermost in memory.  They are staged in LDS as they lie, 16 bytes a lane,
 // and turned on the way out by the transposing LDS read, four rows of 16 columns to 16 lanes.
