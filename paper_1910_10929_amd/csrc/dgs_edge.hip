@@ -6,10 +6,11 @@
 // once.  The next row's loads are issued piece by piece while a row is worked on; no load stands in a branch, so that a wait
 // is for what is due and not for all that is under way.  Parameters stay in registers from row to row (backward: in LDS).
 //
-// Bound by memory where there are rows enough: forward 8192 x 768, fp32 stream, bfloat16 branch, checkpoint, 88.6 MB in 18.3 us
-// (4.8 TB/s), 16384 x 4096 of bfloat16, 809 MB in 148 us (5.5); backward 8192 x 768 24.6 us and 4.0 for the partial sums
-// (88.6 MB, 3.1 TB/s: 16 wavefronts of one workgroup to a compute unit, four rounds of eight rows each), 16384 x 4096, 675 MB in
-// 142 us with its sums (4.8).  A single row of 768: 3.5 us forward, all of it latency.
+// Bound by memory where there are rows enough.  Calls among others, two launches where there are partial sums: forward 8192 x
+// 768, fp32 stream, bfloat16 branch, checkpoints, 88.6 MB in 18.0 us (4.9 TB/s), 16384 x 4096 of bfloat16 with a gate a row, 809 MB
+// in 154 us (5.3); backward 8192 x 768 25.5 us (88.6 MB, 3.5 TB/s: 16 wavefronts of one workgroup to a compute unit, four rounds of
+// eight rows each), 16384 x 4096, 675 MB in 141 us (4.8).  Kernels by themselves, from a chip that has come to rest: 19.2, 147,
+// 24.8 + 4.0 and 152 + 5.2 us.  A single row of 768: 3.6 us forward, all of it latency.
 #include "dgs_rows.h"
 
 namespace dgs {
@@ -84,8 +85,8 @@ __device__ __forceinline__ void unpack_gate(const GateRaw &g, bool f32, bool rag
 }
 
 // Teams of a forward workgroup where they are single wavefronts (otherwise it is one team); wavefronts of a backward workgroup,
-// whatever its teams: fewer workgroups leave fewer partial sums (with 8, two workgroups to a compute unit, 16384 x 4096 took
-// 260 us in place of 249 and 8192 x 768 49 in place of 43).
+// whatever its teams: fewer workgroups leave fewer partial sums (with 8, two workgroups to a compute unit, 16384 x 4096 takes
+// 151 us in place of 141, 8192 x 768 27.3 in place of 25.6, 20000 x 2100 126 in place of 121, 777 x 1001 of fp32 19.6 in place of 19.4).
 constexpr uint32_t FORWARD_TEAMS = 4;
 constexpr int backward_wavefronts(int waves) { return waves % 3 == 0 ? 12 : 16; }
 constexpr uint32_t BACKWARD_BLOCKS = 256;
@@ -759,9 +760,9 @@ __global__ __launch_bounds__(REDUCE_LINES * 64) void k_edge_reduce(const float *
 // ---------------------------------------------------------------------------
 
 // Wavefronts of a row's team: 8 columns a lane, and 16 in rows that a workgroup does not hold then; powers of two, and three
-// times those.  (16 columns from 512 on, half the wavefronts: 16384 x 4096 edges with checkpoints and their decoding 239 us against
-// 219, 8192 x 768 36 against 33.  Powers of two alone: 16384 x 1280 in half precision 46 us against 41 forward and 55 against 49
-// backward, 8192 x 6144 100 against 94 and 125 against 117.)
+// times those.  (Compared when they were built: 16 columns from 512 on, half the wavefronts: 16384 x 4096 edges with checkpoints
+// and their decoding 239 us against 219, 8192 x 768 36 against 33.  Powers of two alone: 16384 x 1280 in half precision 46 us
+// against 41 forward and 55 against 49 backward, 8192 x 6144 100 against 94 and 125 against 117.)
 static uint32_t waves_of(uint32_t cols)
 {
     constexpr uint32_t kinds[] = {1, 2, 3, 4, 6, 8, 12};
@@ -779,7 +780,10 @@ static Cut cut_of(uint32_t rows, uint32_t cols, uint32_t rows_per_gate)
     t.gates = (rows - 1) / t.rows_per_gate + 1;
     t.whole = t.parts = t.run = 0;
     const uint32_t rounds = (t.rows_per_gate - 1) / teams + 1;      // of a team, if one workgroup took a gate row
-    // Many gate rows: each goes to one team, if that keeps half the workgroups busy or there are too few rows to share.
+    // Many gate rows: each goes to one team, if that keeps half the workgroups busy or there are too few rows to share.  (16384 x
+    // 4096 with 16 or 32 rows a gate row: 144 and 144 us, one gate row to a workgroup or parts of it 163 and 149; 32768 x 1024 with 16
+    // 72 against 94.  Where it does leave half of them idle it loses: 16384 x 4096 with 63 or 64 rows 213 and 221 us against 231
+    // and 140, 32768 x 1024 with 32 100 against 76.  65536 x 512 with 33 rows, on the other side of the line: 99, whole 88.)
     if (t.gates >= most && (rounds < 2 || t.gates >= most * teams / 2)) {
         t.whole = ((t.gates + most - 1) / most + teams - 1) / teams * teams;
         t.blocks = (t.gates - 1) / t.whole + 1;
@@ -796,7 +800,10 @@ static Cut cut_of(uint32_t rows, uint32_t cols, uint32_t rows_per_gate)
 template <class TX, class TF> static void launch_forward(const ForwardArgs &a, hipStream_t st)
 {
     const uint32_t waves = waves_of(a.l.cols), teams = waves == 1 ? FORWARD_TEAMS : 1u;
-    // as many workgroups as run at a time: five wavefronts to a SIMD, among which a workgroup's are spread evenly
+    // As many workgroups as run at a time where five wavefronts go to a SIMD, among which a workgroup's are spread evenly: that is
+    // what the 16-bit kernels' registers allow.  Of an fp32 stream most kernels have registers for four, and the last fifth of
+    // these workgroups begins late: 65536 x 768 of fp32 with checkpoints 215 us, with a grid for four 196, 16384 x 1280 with a
+    // bfloat16 branch 62 and 54; but 16384 x 2048 of fp32 113 and 117, without checkpoints 102 and 112.
     const uint32_t w = teams * waves, most = 256u * (w > 4 ? 5u / ((w + 3u) / 4u) : 20u / w), need = (a.rows + teams - 1) / teams;
     const dim3 grid(need < most ? need : most), block(teams * waves * 64);
     if (a.l.cols < 8) hipLaunchKernelGGL((k_edge_forward<TX, TF, 1, 1, true>), grid, block, 0, st, a);

@@ -8,10 +8,10 @@
 // Both operands have the summed index (the row) outermost in memory.  They are staged in LDS as they lie, 16 bytes a lane,
 // and turned on the way out by the transposing LDS read, four rows of 16 columns to 16 lanes.
 //
-// Bound by the matrix units where the product is large (32768 rows, 4096 x 4096, bfloat16: 975 us, 1130 TFLOP/s; a matrix
-// product of the library's reaches 1260 on this card), by the partial sums of the split rows and by the tiles' first and
-// last steps where it is not (8192 rows, 2304 x 768: 50 us and 10 for the sums, 480 TFLOP/s together; 1500 rows,
-// 1001 x 333, fp32: 20 us and 5).
+// Bound by the matrix units where the product is large (32768 rows, 4096 x 4096, bfloat16: 953 to 1029 us from card to card,
+// 1070 to 1150 TFLOP/s; a matrix product of the library's reaches 1260), by the partial sums of the split rows and by the tiles'
+// first and last steps where it is not (8192 rows, 2304 x 768: 53 us a call, 550 TFLOP/s, of which the sums are 10 by themselves;
+// 1500 rows, 1001 x 333, fp32: 24.7, the sums 5).
 #include "dgs_rows.h"
 
 namespace dgs {
@@ -123,7 +123,8 @@ __device__ __forceinline__ uint32_t staged_at(uint32_t k, uint32_t c) { return k
 
 // Any shape: every load looks at what is there.  For what the large tiles' loads take for granted and these matrices have not
 // (fewer than 32 rows, fewer than eight outputs or columns); elsewhere it takes 2 to 2.5 times as long (32768 rows, 4096 x
-// 4096: 2344 us; 8192 rows, 2304 x 768: 97).  20 rows, 4096 x 4096, bfloat16: 21 us, bound by the 64 MB that it writes.
+// 4096: 2344 us; 8192 rows, 2304 x 768: 97).  20 rows, 4096 x 4096, bfloat16: 17.5 us, with the bias terms 21: 67 MB
+// written at 3.8 and 3.2 TB/s, four bytes a lane, where a copy moves 5.0 to 5.4; 1 row, 8192 x 8192: 57 us, 4.7 TB/s.
 template <class T>
 __global__ __launch_bounds__(GRAD_THREADS) void k_weight_grad(GradArgs a)
 {
@@ -557,7 +558,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_weight_grad_tile(GradArgs a)
 }
 
 // Adds up the splits' partial sums (where there are any) and finishes: a wavefront an output row and 256 columns, four to a lane.
-// Bound by the latency of few loads: 2304 x 768 in four splits, 35 MB from cache and memory, 10 us; 1001 x 333 5 us.
+// Bound by the latency of few loads: 2304 x 768 in four splits, 35 MB from cache and memory, 10 us (6.8 without bias terms);
+// 1001 x 333 5 us.  A wavefront takes its splits eight at a time, one after another: 64 x 64 in 512 splits 57 us, 128 x 128 25.
 __global__ __launch_bounds__(256) void k_weight_grad_finish(const float *sums, const float *bias_sums, const float *scale,
                                                             const float *shift, float *dw, uint64_t dw_stride, float *db, uint32_t outs,
                                                             uint32_t cols, uint32_t splits, uint32_t bias_parts, uint32_t accumulate)
