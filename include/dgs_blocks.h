@@ -160,6 +160,77 @@ typedef struct dgs_weight_grad_args {
 size_t dgs_checkpoint_weight_grad_workspace(uint32_t rows, uint32_t outs, uint32_t cols, int type);
 int dgs_checkpoint_weight_grad(const dgs_weight_grad_args *args /*host*/, void *hip_stream);
 
+/*
+ * The output layer with its loss: logits z = x W^T + bias (W: vocab x cols), softmax cross entropy against one target a row.
+ *
+ *     lse_t  = log sum_v exp z_tv
+ *     loss_t = lse_t - z_t[target_t]               0 where the target is no entry of the vocabulary (negative: padding)
+ *
+ * and for gradients dloss_t and dlse_t that arrive at them (NULL: 1 for every row, and 0), dloss_t taken as 0 for a row whose
+ * target is no entry,
+ *
+ *     dz_t = (dloss_t + dlse_t) softmax_t - dloss_t onehot(target_t)
+ *     dx = dz W,   dweight = dz^T x,   dbias = sum_t dz_t
+ *
+ * Logits are not kept: the backward pass computes them again, a piece of the vocabulary at a time.
+ *
+ * x, weight and dx have `type`; bias, loss, lse, dweight and dbias are fp32.  Sums, exponentials and statistics are fp32, of
+ * products that are exact (DGS_F32: x and W in 22 bits).  dz is held in 22 bits, 11 for a dx of 16 bits.  Of the operands of
+ * the gradients' products, magnitudes below 2^-39 of the largest (of W; of x times its row's gradients) are lost.  A bias of
+ * -infinity takes an entry out; where all of them are out, and where logits are infinite or NaN, lse is what the formula gives or NaN.
+ * A row that nothing arrives at (dloss and dlse 0) leaves no gradient, whatever it holds.
+ *
+ *   forward    reads x, weight, bias, targets; writes loss (or NULL) and lse.
+ *   backward   reads those and lse; writes dx, dweight (rows dweight_stride apart) and dbias, each or none of them.
+ *              accumulate != 0: dweight and dbias are added to.
+ * Outputs overlap nothing.  workspace: at least dgs_head_workspace() bytes for the same arguments (of the pointers their
+ * alignment counts), 16-byte aligned; as above.  More than 2^20 columns, 2^24 rows or entries, or strides of 2^21: DGS_ENOTSUP.
+ */
+typedef struct dgs_head_args {
+    uint32_t rows, cols, vocab;
+    int32_t type, target_bytes, accumulate;     /* targets: 4 or 8 bytes each, signed */
+    dgs_matrix x, weight;
+    const float *bias;
+    const void *targets;
+    float *loss, *lse;
+    const float *dloss, *dlse;
+    dgs_matrix dx;
+    float *dweight;
+    uint64_t dweight_stride;
+    float *dbias;
+    void *workspace;
+    uint64_t workspace_bytes;
+} dgs_head_args;
+
+size_t dgs_head_workspace(const dgs_head_args *args /*host*/, int backward);
+int dgs_head_forward(const dgs_head_args *args /*host*/, void *hip_stream);
+int dgs_head_backward(const dgs_head_args *args /*host*/, void *hip_stream);
+
+/*
+ * Updates of weight matrices, orthogonalised: for each of `count` matrices of one shape, X = G / (|G| + eps) with the Frobenius
+ * norm, `steps` times with A = X X^T (X^T in place of X where rows > cols)
+ *
+ *     X = a X + (b A + c A^2) X
+ *
+ * and out = scale * X, or with accumulate != 0 out + scale * X, rounded once.  Sums are fp32, the norm's in 64 bits.  Results of
+ * DGS_F32 and DGS_F16 take 22 bits of X, A and the polynomial to the products, of DGS_BF16 11.  Values of X, A and the polynomial
+ * must stay below 16, as they do with coefficients that take singular values up to 1 to such near 1.  A matrix that holds an
+ * infinity or NaN leaves NaN; of zeros (with eps > 0) zeros.
+ * in, out: host arrays of `count` matrices each, read before the call returns.  out[i] may be in[i] (same type and stride);
+ * otherwise outputs overlap nothing.  More than 65536 rows or columns: DGS_ENOTSUP.
+ */
+typedef struct dgs_orthogonalise_args {
+    uint32_t count, rows, cols, steps;          /* steps >= 1 */
+    int32_t type, out_type, accumulate, reserved;
+    float a, b, c, eps, scale;                  /* eps >= 0 */
+    const dgs_matrix *in, *out;
+    void *workspace;
+    uint64_t workspace_bytes;
+} dgs_orthogonalise_args;
+
+size_t dgs_orthogonalise_workspace(const dgs_orthogonalise_args *args /*host*/);
+int dgs_orthogonalise(const dgs_orthogonalise_args *args /*host*/, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -28,7 +28,8 @@ _MOST = 0x7FFFFFFF      # rows, or columns
 
 EXPORTS = [
     "dgs_edge_forward", "dgs_edge_backward_workspace", "dgs_edge_backward", "dgs_checkpoint_encode", "dgs_checkpoint_decode",
-    "dgs_checkpoint_weight_grad_workspace", "dgs_checkpoint_weight_grad",
+    "dgs_checkpoint_weight_grad_workspace", "dgs_checkpoint_weight_grad", "dgs_head_workspace", "dgs_head_forward",
+    "dgs_head_backward", "dgs_orthogonalise_workspace", "dgs_orthogonalise",
 ]
 
 _TYPES = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
@@ -40,6 +41,8 @@ _FORWARD = struct.Struct("@II4i" + "PQ" * 5 + "PQPQ" * 2 + "P")
 _BACKWARD = struct.Struct("@II4i" + "PQ" * 5 + "PQPQ" * 2 + "P" + "PQ" * 3 + "4P" + "PQ")
 _CODES = struct.Struct("@PQPQ")
 _GRAD = struct.Struct("@III3i" + "PQ" + "PQPQ" + "PP" + "PQ" + "P" + "PQ")
+_HEAD = struct.Struct("@III3i" + "PQ" * 2 + "PP" + "PP" + "PP" + "PQ" + "PQ" + "P" + "PQ")
+_ORTHOGONALISE = struct.Struct("@IIII4i5f" + "PP" + "PQ")
 
 _lib = None
 
@@ -58,6 +61,13 @@ def lib():
         L.dgs_checkpoint_weight_grad_workspace.restype = ctypes.c_size_t
         L.dgs_checkpoint_weight_grad_workspace.argtypes = [u32, u32, u32, i32]
         L.dgs_checkpoint_weight_grad.argtypes = [vp, vp]
+        L.dgs_head_workspace.restype = ctypes.c_size_t
+        L.dgs_head_workspace.argtypes = [vp, i32]
+        L.dgs_head_forward.argtypes = [vp, vp]
+        L.dgs_head_backward.argtypes = [vp, vp]
+        L.dgs_orthogonalise_workspace.restype = ctypes.c_size_t
+        L.dgs_orthogonalise_workspace.argtypes = [vp]
+        L.dgs_orthogonalise.argtypes = [vp, vp]
         _lib = L
     return _lib
 
@@ -448,3 +458,147 @@ def weight_grad(dy, saved, dw, db=None, scale=None, shift=None, accumulate=False
                         _vector(shift, cols, device, "shift"), *_matrix(dw, outs, cols, device, "dw"),
                         _vector(db, outs, device, "db"), ws.data_ptr(), ws.numel() * ws.element_size()))
     return dw
+
+
+_TARGETS = {torch.int64: 8, torch.int32: 4}
+
+
+class Head:
+    """The output layer with its loss, of which no logits are kept; see dgs_head_args in the header.
+
+        z = x W^T + bias,   lse_t = log sum_v exp z_tv,   loss_t = lse_t - z_t[target_t]
+
+    weight: vocab x cols, of the type that x has; bias: an fp32 vector or None.  Both are read when a call runs, so they may be
+    updated in place between two steps.  A row whose target is no entry of the vocabulary (negative: padding) is left out."""
+
+    def __init__(self, weight, bias=None):
+        if weight.dim() != 2:
+            _refuse("weight: expected a matrix")
+        self.vocab, self.cols = weight.shape
+        if self.vocab == 0 or self.cols == 0:
+            _refuse("weight: no entries or no columns")
+        _fits(self.vocab, "entries")
+        _fits(self.cols, "columns")
+        self._device = _on_gpu(weight, "weight")
+        _type(weight, "weight")
+        _matrix(weight, self.vocab, self.cols, self._device, "weight")
+        _vector(bias, self.vocab, self._device, "bias")
+        self.weight, self.bias = weight, bias
+
+    def _rows(self, x, targets):
+        device = _on_gpu(x, "x")
+        if x.dim() != 2:
+            _refuse("x: expected a matrix")
+        if device != self._device:
+            _refuse("the weight is on another device")
+        if x.dtype != self.weight.dtype:
+            _refuse("x: expected the type of the weight")
+        rows = x.size(0)
+        _fits(rows, "rows")
+        size = _TARGETS.get(targets.dtype)
+        if size is None or targets.numel() != rows or not targets.is_contiguous():
+            _refuse(f"targets: expected {rows} contiguous int64 or int32 values")
+        if targets.get_device() != device:
+            _refuse("targets are on another device")
+        return device, rows, size
+
+    def _call(self, what, call, backward, device, rows, size, accumulate, x, targets, loss, lse, dloss, dlse, dx, dweight, dbias, workspace):
+        fixed = (rows, self.cols, self.vocab, _TYPES[x.dtype], size, int(accumulate), *_matrix(x, rows, self.cols, device, "x"),
+                 *_matrix(self.weight, self.vocab, self.cols, device, "weight"), _vector(self.bias, self.vocab, device, "bias"),
+                 targets.data_ptr(), _vector(loss, rows, device, "loss"), _vector(lse, rows, device, "lse"),
+                 _vector(dloss, rows, device, "dloss"), _vector(dlse, rows, device, "dlse"), *dx, *dweight, dbias)
+        need = lib().dgs_head_workspace(_HEAD.pack(*fixed, 0, 0), backward)
+        ws = _workspace(workspace, need, x, device, what)
+        _enqueue(what, device, call, _HEAD.pack(*fixed, ws.data_ptr(), ws.numel() * ws.element_size()))
+
+    def forward(self, x, targets, loss=None, lse=None, workspace=None):
+        """(loss, lse), fp32, one for each row of x; targets: int64 or int32."""
+        device, rows, size = self._rows(x, targets)
+        if loss is None:
+            loss = x.new_empty(rows, dtype=torch.float32)
+        if lse is None:
+            lse = x.new_empty(rows, dtype=torch.float32)
+        self._call("dgs_head_forward", lib().dgs_head_forward, 0, device, rows, size, False, x, targets, loss, lse, None, None, _NO_MATRIX,
+                   _NO_MATRIX, 0, workspace)
+        return loss, lse
+
+    def backward(self, x, targets, lse, dloss=None, dlse=None, dx=None, dweight=None, dbias=None, need_dx=True, accumulate=False,
+                 workspace=None):
+        """Gradients, from those that arrive at loss (None: 1) and lse (None: 0), fp32 vectors; x, targets and lse as in the forward
+        pass.  Returns dx (None without need_dx); dweight (vocab x cols, fp32, may have any distance between rows) and dbias (fp32) are
+        written, or with `accumulate` added to, where they are given."""
+        device, rows, size = self._rows(x, targets)
+        pdx = pdw = _NO_MATRIX
+        if dx is not None:
+            if dx.dtype != x.dtype:
+                _refuse("dx: expected the type of x")
+            if not need_dx:
+                _refuse("dx is given and not needed")
+            pdx = _matrix(dx, rows, self.cols, device, "dx")
+            if dx.data_ptr() == x.data_ptr() and rows:
+                _refuse("dx lies over x")
+        elif need_dx:
+            dx, pdx = _like(x, x.dtype, self.cols)
+        if dweight is not None:
+            if dweight.dtype != torch.float32:
+                _refuse("dweight: expected float32")
+            pdw = _matrix(dweight, self.vocab, self.cols, device, "dweight")
+            if dweight.data_ptr() == self.weight.data_ptr():
+                _refuse("dweight lies over the weight")
+        if lse is None:
+            _refuse("lse: the forward pass's is needed")
+        self._call("dgs_head_backward", lib().dgs_head_backward, 1, device, rows, size, accumulate, x, targets, None, lse, dloss, dlse, pdx,
+                   pdw, _vector(dbias, self.vocab, device, "dbias"), workspace)
+        return dx
+
+
+def orthogonalise(updates, out=None, steps=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1e-7, scale=1.0, accumulate=False,
+                  workspace=None):
+    """Updates of weight matrices -- one matrix, or a list of matrices of one shape and type -- with their singular vectors kept
+    and their singular values taken near 1 by Newton-Schulz products; see dgs_orthogonalise in the header.  Of each: X = G / (|G| + eps),
+    `steps` times X = a X + (b A + c A^2) X with A = X X^T (of the smaller side), then out = scale X, or with `accumulate` out + scale X.
+    `out`: as `updates`, of any one of the three types, or new ones of the updates' type; may be the updates themselves.  fp32 and half
+    results take 22 bits of the operands to the products, bfloat16 ones 11."""
+    one = isinstance(updates, torch.Tensor)
+    given = [updates] if one else list(updates)
+    if not given:
+        return []
+    if out is None:
+        if accumulate:
+            _refuse("out: nothing to add to")
+        outs = None
+    else:
+        outs = [out] if isinstance(out, torch.Tensor) else list(out)
+        if len(outs) != len(given) or one != isinstance(out, torch.Tensor):
+            _refuse("out: expected as many matrices as updates")
+    first = given[0]
+    device = _on_gpu(first, "updates")
+    if first.dim() != 2:
+        _refuse("updates: expected matrices")
+    rows, cols = first.shape
+    if rows == 0 or cols == 0:
+        _refuse("updates: no rows or no columns")
+    _fits(rows, "rows")
+    _fits(cols, "columns")
+    kind = _type(first, "updates")
+    if outs is None:
+        outs = [torch.empty((rows, cols), dtype=first.dtype, device=first.device) for _ in given]
+    out_kind = _type(outs[0], "out")
+    if not 1 <= steps <= 1000 or len(coefficients) != 3:
+        _refuse("steps: 1 to 1000; coefficients: three")
+    places, out_places = [], []
+    for g, o in zip(given, outs):
+        if g.dtype != first.dtype or o.dtype != outs[0].dtype:
+            _refuse("updates, and out: expected one type each")
+        places += _matrix(g, rows, cols, device, "updates")
+        out_places += _matrix(o, rows, cols, device, "out")
+    if len(set(out_places[::2])) != len(outs):
+        _refuse("out: one matrix twice")
+    table = struct.pack(f"@{2 * len(places)}Q", *places, *out_places)
+    table = ctypes.create_string_buffer(table, len(table))
+    at = ctypes.addressof(table)
+    fixed = (len(given), rows, cols, steps, kind, out_kind, int(accumulate), 0, *coefficients, eps, scale, at, at + 8 * len(places))
+    need = lib().dgs_orthogonalise_workspace(_ORTHOGONALISE.pack(*fixed, 0, 0))
+    ws = _workspace(workspace, need, first, device, "dgs_orthogonalise")
+    _enqueue("dgs_orthogonalise", device, lib().dgs_orthogonalise, _ORTHOGONALISE.pack(*fixed, ws.data_ptr(), ws.numel() * ws.element_size()))
+    return outs[0] if one else outs

@@ -9,7 +9,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdgs.so")
 SOURCES = ["dgs_stream.hip", "dgs_select.hip", "dgs_chain.hip", "dgs_server.hip", "dgs_api.hip",
-           "dgs_edge.hip", "dgs_checkpoint.hip", "dgs_weight_grad.hip"]
+           "dgs_edge.hip", "dgs_checkpoint.hip", "dgs_weight_grad.hip", "dgs_head.hip",
+           "dgs_orthogonal.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

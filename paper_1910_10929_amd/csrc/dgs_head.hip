@@ -1,0 +1,824 @@
+// The output layer with its loss: logits = x W^T + b, softmax cross entropy against one target a row, and the gradients, of
+// which no logits are kept.
+//
+// Forward: a tile of logits stays in a workgroup's sums, of which each row's maximum and sum of exponentials go out; a second
+// launch joins the tiles of a row.  Backward: the same tiles again, a piece of the vocabulary at a time; with the row's lse they
+// become the gradient of the logits, which is written in 16-bit parts (HeadRow), and two products take dx and dweight from it.
+//
+// Numbers.  Sums, statistics and exponentials are fp32.  Logits are products of the operands as they are (bfloat16, half;
+// fp32 in two halves, 22 bits).  The gradient of the logits is divided by a power of two for each row (at least the larger
+// of the incoming gradients) and held in two halves, 22 bits of each value; dx of 16-bit types takes the first, 11 bits
+// where the result is rounded to 8 or 11, dweight, in fp32, both.  The other operand of these products is W or x in half,
+// scaled by powers of two so that the largest magnitude lies below 2^15: a bfloat16 value is exact there down to 2^-31 of the
+// largest, and what is lost of smaller ones is below 2^-39 of it.  x carries the rows' powers of two.
+#include "dgs_product.h"
+
+namespace dgs {
+
+// ---------------------------------------------------------------------------
+// operands
+// ---------------------------------------------------------------------------
+
+constexpr uint32_t RANGE_BLOCKS = 256;      // of rows, and as many of W
+constexpr int NO_RANGE = -100000;           // nothing but zeros
+constexpr int TOP = 15;                     // the largest magnitude of a scaled operand lies below 2^TOP
+constexpr int GRAD_TOP = 14;                // a row's logit gradients are at most 2 after division
+
+// What a row of the backward pass needs: dlogit = pull * softmax - push * onehot, divided by 2^power and scaled to GRAD_TOP.
+struct HeadRow {
+    float lse, pull, push;
+    int power;      // of the incoming gradients' larger one
+};
+// (such a row leaves no gradient, whatever it holds)
+__device__ __forceinline__ bool nothing_arrives(const HeadRow &h) { return h.pull == 0.0f && h.push == 0.0f; }
+struct Ranges {
+    int *x, *w;         // one for each workgroup: largest exponent of x (with the rows' powers), of W
+    int *row;           // of each row of x
+};
+// Exponents by which the whole of x (with the rows' powers) and of W are multiplied.
+struct Scales { int x, w; };
+
+__device__ __forceinline__ int exponent_of(uint32_t magnitude)      // smallest e with |v| < 2^e
+{
+    return magnitude == 0 ? NO_RANGE : max((int)(magnitude >> 23), 1) - 126;
+}
+__device__ __forceinline__ int scale_of(int exponent) { return exponent <= NO_RANGE / 2 ? 0 : TOP - exponent; }
+__device__ __forceinline__ float times_power(float v, int e)
+{
+#ifdef DGS_HOST_EMULATION
+    return ldexpf(v, e);
+#else
+    return __builtin_amdgcn_ldexpf(v, e);
+#endif
+}
+__device__ __forceinline__ float power_of_e(float v)      // e^v
+{
+#ifdef DGS_HOST_EMULATION
+    return exp2f(v * 1.44269504f);
+#else
+    return __builtin_amdgcn_exp2f(v * 1.44269504f);
+#endif
+}
+__device__ __forceinline__ float other_half(float v)      // the value of lane l ^ 32
+{
+    return __uint_as_float((uint32_t)__builtin_amdgcn_ds_bpermute((int)((lane_id() ^ 32u) << 2), (int)__float_as_uint(v)));
+}
+__device__ __forceinline__ int wave_max(int v)
+{
+#pragma unroll
+    for (uint32_t by = 32; by; by >>= 1) v = max(v, __builtin_amdgcn_ds_bpermute((int)((lane_id() ^ by) << 2), v));
+    return v;
+}
+
+struct Targets {
+    const void *at;
+    uint32_t wide;      // 64 bits each
+    uint32_t vocab;
+};
+// A row's target, or the vocabulary's size where it is none of its entries.
+__device__ __forceinline__ uint32_t target_of(const Targets &t, uint32_t row)
+{
+    if (t.wide) {
+        const uint64_t v = ((const uint64_t *)t.at)[row];
+        return v < t.vocab ? (uint32_t)v : t.vocab;
+    }
+    return min(((const uint32_t *)t.at)[row], t.vocab);
+}
+
+// Exponents of x, row by row, and of W; in a backward pass what the rows need besides.  A wavefront a row.
+template <class T>
+__global__ __launch_bounds__(256) void k_head_range(const T *x, uint64_t x_stride, const T *w, uint64_t w_stride, uint32_t rows,
+                                                    uint32_t cols, Targets targets, const float *lse, const float *dloss,
+                                                    const float *dlse, HeadRow *row_info, Ranges to)
+{
+    __shared__ int best[4];
+    const uint32_t wave = uniform(threadIdx.x >> 6), lane = lane_id();
+    const bool of_w = blockIdx.x >= RANGE_BLOCKS;
+    const uint32_t block = of_w ? blockIdx.x - RANGE_BLOCKS : blockIdx.x, count = of_w ? targets.vocab : rows;
+    const T *const m = of_w ? w : x;
+    const uint64_t stride = of_w ? w_stride : x_stride;
+    int most = NO_RANGE;
+    if (of_w ? to.w != nullptr : to.x != nullptr) {
+        for (uint32_t row = block * 4 + wave; row < count; row += RANGE_BLOCKS * 4) {
+            uint32_t top = 0;
+            for (uint32_t c = lane * 8; c < cols; c += 512) {
+                float v[8];
+                unpack8(load8(m + row * stride + c, live8(c, cols)), v);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const uint32_t u = __float_as_uint(v[i]) & 0x7FFFFFFFu;
+                    top = u < 0x7F800000u ? max(top, u) : top;
+                }
+            }
+            int e = wave_max(exponent_of(top));
+            if (!of_w) {
+                int power = 0;
+                if (row_info) {
+                    HeadRow h;
+                    const float up = target_of(targets, row) < targets.vocab ? dloss ? dloss[row] : 1.0f : 0.0f;
+                    const float all = up + (dlse ? dlse[row] : 0.0f);
+                    const float larger = max(__builtin_fabsf(up), __builtin_fabsf(all));
+                    const bool plain = larger > 0.0f && larger < __builtin_inff();
+                    power = plain ? exponent_of(__float_as_uint(larger)) : 0;
+                    h.lse = lse[row];
+                    h.pull = times_power(all, GRAD_TOP - power);
+                    h.push = times_power(up, GRAD_TOP - power);
+                    h.power = power;
+                    if (lane == 0) row_info[row] = h;
+                    // (a row that nothing arrives at asks for no range)
+                    if (up == 0.0f && all == 0.0f) power = NO_RANGE;
+                }
+                if (lane == 0) to.row[row] = e;
+                e = e <= NO_RANGE / 2 || power <= NO_RANGE / 2 ? NO_RANGE : e + power;
+            }
+            most = max(most, e);
+        }
+    }
+    if (lane == 0) best[wave] = most;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        const int v = max(max(best[0], best[1]), max(best[2], best[3]));
+        if (of_w && to.w) to.w[block] = v;
+        if (!of_w && to.x) to.x[block] = v;
+    }
+}
+
+enum CopyKind {
+    COPY_PLAIN,      // 16-bit values as they are, in rows whose length is a multiple of eight
+    COPY_ROWS,       // halves of a matrix, each row scaled by itself
+    COPY_WEIGHED,    // ... all by the same power, and each row times its own
+    COPY_ALL,        // ... all by the same power
+};
+
+// An operand in halves (in one part or two), scaled.  Eight columns a lane; columns up to the next multiple of eight are zeros.
+template <class T, int KIND>
+__global__ __launch_bounds__(256) void k_head_copy(const T *from, uint64_t from_stride, uint32_t rows, uint32_t cols, uint16_t *hi,
+                                                   uint16_t *lo, uint32_t pieces, Ranges ranges, const HeadRow *row_info, Scales *scales)
+{
+    int all = 0;
+    if constexpr (KIND == COPY_WEIGHED || KIND == COPY_ALL) {
+        __shared__ int best[4];
+        const int *const r = KIND == COPY_ALL ? ranges.w : ranges.x;
+        const int e = wave_max(r[threadIdx.x]);      // (as many as there are threads)
+        if (lane_id() == 0) best[threadIdx.x >> 6] = e;
+        __syncthreads();
+        all = scale_of(max(max(best[0], best[1]), max(best[2], best[3])));
+        if (blockIdx.x == 0 && threadIdx.x == 0) (KIND == COPY_ALL ? scales->w : scales->x) = all;
+    }
+    const uint64_t step = (uint64_t)gridDim.x * 256, end = (uint64_t)rows * pieces;
+    for (uint64_t at = (uint64_t)blockIdx.x * 256 + threadIdx.x; at < end; at += step) {
+        const uint32_t row = (uint32_t)(at / pieces), c = (uint32_t)(at - (uint64_t)row * pieces) * 8;
+        const Raw8<T> raw = load8(from + row * from_stride + c, live8(c, cols));
+        u32x4 h, l;
+        if constexpr (KIND == COPY_PLAIN) {
+            __builtin_memcpy(&h, &raw, 16);
+            *(u32x4 *)(hi + at * 8) = h;
+        } else {
+            int e = all;
+            float v[8];
+            unpack8(raw, v);
+            if constexpr (KIND == COPY_ROWS) e = scale_of(ranges.row[row]);
+            if constexpr (KIND == COPY_WEIGHED) {
+                const HeadRow h = row_info[row];
+                e = all + h.power;
+                if (nothing_arrives(h)) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] = 0.0f;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                f16 a, b, c0, d;
+                halves_of(times_power(v[2 * i], e), a, b);
+                halves_of(times_power(v[2 * i + 1], e), c0, d);
+                h[i] = bits_of(a, c0);
+                l[i] = bits_of(b, d);
+            }
+            *(u32x4 *)(hi + at * 8) = h;
+            if (lo) *(u32x4 *)(lo + at * 8) = l;
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// logits
+// ---------------------------------------------------------------------------
+
+struct LogitArgs {
+    Side w, x;
+    uint32_t cols, kind;             // of the products
+    uint32_t rows, vocab, first, end;      // entries of this launch
+    uint32_t v_tiles, t_tiles;
+    const float *bias;
+    Targets targets;
+    const int *x_powers;             // exponents that x's rows and W were multiplied by, fp32 only
+    const Scales *scales;
+    // forward: a row's maximum and sum, for each tile of the vocabulary; the target's logit
+    float2 *stats;
+    float *target_logit;
+    // backward
+    const HeadRow *row_info;
+    uint16_t *grad[2];               // rows x grad_stride each
+    uint64_t grad_stride;
+    float *bias_parts;               // t_tiles x grad_stride
+};
+
+// Entries (m) and rows (n) of a tile.
+template <class E, uint32_t M, uint32_t N, uint32_t WAVES_M, uint32_t WAVES_N, bool BACK>
+__global__ __launch_bounds__(WAVES_M *WAVES_N * 64, 2) void k_head_logits(LogitArgs a)
+{
+    typedef Product<E, M, N, WAVES_M, WAVES_N, false, false> P;
+    __shared__ __attribute__((aligned(16))) typename P::Lds lds;
+    const uint32_t at = tile_of_block(blockIdx.x, gridDim.x);
+    const uint32_t tile_v = at / a.t_tiles, tile_t = at - tile_v * a.t_tiles;
+    const uint32_t v0 = a.first + tile_v * M, t0 = tile_t * N;
+    typename P::Sums z;
+    P::run(lds, a.w, a.x, v0, t0, 0, a.cols, a.kind, z);
+
+    const uint32_t lane = lane_id(), half = lane >> 5, wave = uniform(threadIdx.x >> 6);
+    const uint32_t v_wave = v0 + P::wave_m();
+    uint32_t target[P::J];
+    bool here[P::J];
+#pragma unroll
+    for (uint32_t j = 0; j < P::J; ++j) {
+        const uint32_t t = t0 + P::wave_n() + 32 * j + (lane & 31u);
+        here[j] = t < a.rows;
+        target[j] = here[j] ? target_of(a.targets, t) : a.vocab;
+        if (a.x_powers) {
+            const int e = here[j] ? -a.scales->w - scale_of(a.x_powers[t]) : 0;
+#pragma unroll
+            for (uint32_t i = 0; i < P::I; ++i)
+#pragma unroll
+                for (uint32_t r = 0; r < 16; ++r) z[i][j][r] = times_power(z[i][j][r], e);
+        }
+    }
+    // this lane's first entry of the tile; the others are row_in_square(r) + 32 i behind it
+    const uint32_t v_lane = v_wave + 4 * half, left = a.end - min(v_lane, a.end);
+    if (a.bias) {
+#pragma unroll
+        for (uint32_t i = 0; i < P::I; ++i)
+#pragma unroll
+            for (uint32_t r = 0; r < 16; ++r) {
+                const uint32_t o = 32 * i + row_in_square(r);
+                const float b = o < left ? a.bias[v_lane + o] : 0.0f;
+#pragma unroll
+                for (uint32_t j = 0; j < P::J; ++j) z[i][j][r] += b;
+            }
+    }
+    if constexpr (!BACK) {
+        __syncthreads();      // nobody reads operands any more
+        float2(*const part)[N] = (float2(*)[N])&lds;
+#pragma unroll
+        for (uint32_t j = 0; j < P::J; ++j) {
+            const uint32_t n = P::wave_n() + 32 * j + (lane & 31u), t = t0 + n;
+            float most = -__builtin_inff(), sum = 0.0f, hit = 0.0f;
+            const uint32_t aim = target[j] - v_lane;      // (where the target lies, if it lies here)
+            bool found = false;
+#pragma unroll
+            for (uint32_t i = 0; i < P::I; ++i)
+#pragma unroll
+                for (uint32_t r = 0; r < 16; ++r) {
+                    const uint32_t o = 32 * i + row_in_square(r);
+                    z[i][j][r] = o < left ? z[i][j][r] : -__builtin_inff();
+                    most = max(most, z[i][j][r]);
+                    hit = o == aim ? z[i][j][r] : hit;
+                    found |= o == aim;
+                }
+            if (found && here[j]) a.target_logit[t] = hit;
+            most = max(most, other_half(most));
+            const float from = most == -__builtin_inff() ? 0.0f : most;
+#pragma unroll
+            for (uint32_t i = 0; i < P::I; ++i)
+#pragma unroll
+                for (uint32_t r = 0; r < 16; ++r) sum += power_of_e(z[i][j][r] - from);
+            sum += other_half(sum);
+            if (half == 0) part[wave / WAVES_N][n] = make_float2(most, sum);
+        }
+        __syncthreads();
+        for (uint32_t n = threadIdx.x; n < N; n += P::THREADS) {
+            if (t0 + n >= a.rows) continue;
+            float most = part[0][n].x;
+#pragma unroll
+            for (uint32_t w = 1; w < WAVES_M; ++w) most = max(most, part[w][n].x);
+            const float from = most == -__builtin_inff() ? 0.0f : most;
+            float sum = 0.0f;
+#pragma unroll
+            for (uint32_t w = 0; w < WAVES_M; ++w) sum += part[w][n].y * power_of_e(part[w][n].x - from);
+            a.stats[(uint64_t)tile_v * a.rows + t0 + n] = make_float2(most, sum);
+        }
+    } else {
+        float column[P::I * 16];      // the bias gradient's sums over this lane's rows
+#pragma unroll
+        for (uint32_t i = 0; i < P::I * 16; ++i) column[i] = 0.0f;
+#pragma unroll
+        for (uint32_t j = 0; j < P::J; ++j) {
+            const uint32_t t = t0 + P::wave_n() + 32 * j + (lane & 31u);
+            HeadRow h = {0.0f, 0.0f, 0.0f, 0};
+            if (here[j]) h = a.row_info[t];
+            const bool none = nothing_arrives(h);
+            const uint32_t aim = target[j] - v_lane;
+#pragma unroll
+            for (uint32_t i = 0; i < P::I; ++i)
+#pragma unroll
+                for (uint32_t g = 0; g < 4; ++g) {
+                    const uint32_t o4 = 32 * i + 8 * g, v = v_lane + o4;
+                    f16 hi[4], lo[4];
+#pragma unroll
+                    for (uint32_t q = 0; q < 4; ++q) {
+                        float d = h.pull * power_of_e(z[i][j][4 * g + q] - h.lse);
+                        d -= o4 + q == aim ? h.push : 0.0f;
+                        if (none || o4 + q >= left) d = 0.0f;
+                        if (a.bias_parts) column[16 * i + 4 * g + q] += times_power(d, h.power - GRAD_TOP);
+                        halves_of(d, hi[q], lo[q]);
+                    }
+                    if (!here[j] || v - a.first >= a.grad_stride) continue;
+                    u32x2 o;
+                    o[0] = bits_of(hi[0], hi[1]);
+                    o[1] = bits_of(hi[2], hi[3]);
+                    *(u32x2 *)(a.grad[0] + t * a.grad_stride + (v - a.first)) = o;
+                    o[0] = bits_of(lo[0], lo[1]);
+                    o[1] = bits_of(lo[2], lo[3]);
+                    *(u32x2 *)(a.grad[1] + t * a.grad_stride + (v - a.first)) = o;
+                }
+        }
+        if (a.bias_parts) {
+            __syncthreads();
+            float(*const part)[M] = (float(*)[M])&lds;
+            // over 32 lanes: of every pair of lanes each takes half of the entries, until one or two are left
+            uint32_t entry = 0;
+#pragma unroll
+            for (uint32_t by = 1, left = P::I * 16; by < 32; by <<= 1) {
+                const bool upper = (lane & by) != 0;
+                const uint32_t keep = left > 1 ? left / 2 : 1;
+#pragma unroll
+                for (uint32_t k = 0; k < P::I * 8; ++k) {
+                    if (k >= keep) continue;
+                    const float mine = left > 1 && upper ? column[k + keep] : column[k], theirs = left > 1 && !upper ? column[k + keep] : column[k];
+                    column[k] = mine + __uint_as_float((uint32_t)__builtin_amdgcn_ds_bpermute((int)((lane ^ by) << 2), (int)__float_as_uint(theirs)));
+                }
+                entry += left > 1 && upper ? keep : 0u;
+                left = keep;
+            }
+#pragma unroll
+            for (uint32_t k = 0; k < (P::I > 2 ? P::I / 2 : 1); ++k)
+                part[wave % WAVES_N][P::wave_m() + 32 * ((entry + k) >> 4) + row_in_square((entry + k) & 15u) + 4 * half] = column[k];
+            __syncthreads();
+            for (uint32_t m = threadIdx.x; m < M; m += P::THREADS) {
+                const uint32_t v = v0 - a.first + m;
+                if (v >= a.grad_stride) continue;
+                float s = part[0][m];
+#pragma unroll
+                for (uint32_t w = 1; w < WAVES_N; ++w) s += part[w][m];
+                a.bias_parts[tile_t * a.grad_stride + v] = s;
+            }
+        }
+    }
+}
+
+// A row's lse and loss from its tiles' maxima and sums.  `apart` lanes a row (a power of two), 256 / apart rows.
+__global__ __launch_bounds__(256) void k_head_loss(const float2 *stats, const float *target_logit, Targets targets, uint32_t rows,
+                                                   uint32_t tiles, uint32_t apart, float *loss, float *lse)
+{
+    __shared__ float2 part[256];
+    const uint32_t per = 256 / apart, n = threadIdx.x % per, group = threadIdx.x / per;
+    const uint32_t t = blockIdx.x * per + n;
+    float most = -__builtin_inff(), sum = 0.0f;
+    if (t < rows) {
+        for (uint32_t i = group; i < tiles; i += apart) {
+            const float2 s = stats[(uint64_t)i * rows + t];
+            const float top = max(most, s.x), from = top == -__builtin_inff() ? 0.0f : top;
+            sum = sum * power_of_e(most - from) + s.y * power_of_e(s.x - from);
+            most = top;
+        }
+    }
+    part[threadIdx.x] = make_float2(most, sum);
+    __syncthreads();
+    if (group || t >= rows) return;
+    for (uint32_t i = 1; i < apart; ++i) {
+        const float2 s = part[i * per + n];
+        const float top = max(most, s.x), from = top == -__builtin_inff() ? 0.0f : top;
+        sum = sum * power_of_e(most - from) + s.y * power_of_e(s.x - from);
+        most = top;
+    }
+    const float l = most == -__builtin_inff() && sum == 0.0f ? most : most + logf(sum);
+    if (lse) lse[t] = l;
+    if (loss) loss[t] = target_of(targets, t) < targets.vocab ? l - target_logit[t] : 0.0f;
+}
+
+// ---------------------------------------------------------------------------
+// gradients
+// ---------------------------------------------------------------------------
+
+struct GradientArgs {
+    Side a, b;
+    uint32_t depth, split_depth, kind;      // the sum's length, and of a split of it
+    uint32_t m_tiles, n_tiles, splits;
+    uint32_t m, n;
+    float *out;              // whole: the result; otherwise splits x m x n of partial sums
+    uint64_t out_stride;
+    uint32_t add, whole;
+    const Scales *scales;    // whole: x's exponent comes off
+};
+
+// TURN_A: the first operand's k lies outside.  (The second's always does.)
+template <uint32_t M, uint32_t N, uint32_t WAVES_M, uint32_t WAVES_N, bool TURN_A>
+__global__ __launch_bounds__(WAVES_M *WAVES_N * 64, 2) void k_head_product(GradientArgs a)
+{
+    typedef Product<f16, M, N, WAVES_M, WAVES_N, TURN_A, true> P;
+    __shared__ __attribute__((aligned(16))) typename P::Lds lds;
+    const uint32_t at = tile_of_block(blockIdx.x, gridDim.x), tiles = a.m_tiles * a.n_tiles;
+    const uint32_t split = at / tiles, tile = at - split * tiles;
+    const uint32_t tile_m = tile / a.n_tiles, tile_n = tile - tile_m * a.n_tiles;
+    const uint32_t first = min(split * a.split_depth, a.depth), end = min(first + a.split_depth, a.depth);
+    typename P::Sums s;
+    P::run(lds, a.a, a.b, tile_m * M, tile_n * N, first, end, a.kind, s);
+    float *const out = a.out + (a.whole ? 0u : (uint64_t)split * a.m * a.out_stride);
+    const int e = a.whole ? -GRAD_TOP - a.scales->x : 0;
+#pragma unroll
+    for (uint32_t j = 0; j < P::J; ++j) {
+        const uint32_t n = tile_n * N + P::wave_n() + 32 * j + (lane_id() & 31u);
+        if (n >= a.n) continue;
+#pragma unroll
+        for (uint32_t i = 0; i < P::I; ++i)
+#pragma unroll
+            for (uint32_t r = 0; r < 16; ++r) {
+                const uint32_t m = tile_m * M + P::wave_m() + 32 * i + square_row(r);
+                if (m >= a.m) continue;
+                float *const p = out + m * a.out_stride + n;
+                const float v = times_power(s[i][j][r], e);
+                *p = a.add ? *p + v : v;
+            }
+    }
+}
+
+// dx: the splits' sums, times the row's power, W's taken off.
+template <class T>
+__global__ __launch_bounds__(256) void k_head_dx(const float *sums, uint32_t splits, uint32_t rows, uint32_t cols, const HeadRow *row_info,
+                                                 const Scales *scales, T *dx, uint64_t dx_stride)
+{
+    const uint64_t at = (uint64_t)blockIdx.x * 256 + threadIdx.x, pieces = (cols + 7) / 8;
+    const uint64_t row = at / pieces;
+    if (row >= rows) return;
+    const uint32_t c = (uint32_t)(at - row * pieces) * 8, n = live8(c, cols);
+    float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+    for (uint32_t s = 0; s < splits; ++s) {
+        float w[8];
+        load8_f32(sums + ((uint64_t)s * rows + row) * cols + c, n, w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] += w[i];
+    }
+    const int e = row_info[row].power - GRAD_TOP - (scales ? scales->w : 0);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = times_power(v[i], e);
+    store8(dx + row * dx_stride, c, n, v);
+}
+
+// dweight: the splits' sums, x's exponent taken off.
+__global__ __launch_bounds__(256) void k_head_dweight(const float *sums, uint32_t splits, uint32_t rows, uint32_t cols,
+                                                      const Scales *scales, float *out, uint64_t out_stride, uint32_t add)
+{
+    const uint64_t at = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+    const uint64_t row = at / cols;
+    if (row >= rows) return;
+    const uint32_t c = (uint32_t)(at - row * cols);
+    float v = 0.0f;
+    for (uint32_t s = 0; s < splits; ++s) v += sums[((uint64_t)s * rows + row) * cols + c];
+    if (splits) v = times_power(v, -GRAD_TOP - scales->x);
+    float *const p = out + row * out_stride + c;
+    *p = add ? *p + v : v;
+}
+
+__global__ __launch_bounds__(256) void k_head_dbias(const float *parts, uint32_t tiles, uint64_t stride, uint32_t count, float *out,
+                                                    uint32_t add)
+{
+    const uint32_t v = blockIdx.x * 256 + threadIdx.x;
+    if (v >= count) return;
+    float s = 0.0f;
+    for (uint32_t i = 0; i < tiles; ++i) s += parts[i * stride + v];
+    out[v] = add ? out[v] + s : s;
+}
+
+// ---------------------------------------------------------------------------
+// host side
+// ---------------------------------------------------------------------------
+
+enum { TILE_LARGE, TILE_SMALL, TILE_FEW };
+struct TileSize { uint32_t m, n; };
+static TileSize size_of(int tile) { return tile == TILE_LARGE ? TileSize{256, 256} : tile == TILE_SMALL ? TileSize{128, 128} : TileSize{128, 32}; }
+static uint32_t tiles_of(uint32_t n, uint32_t size) { return n ? (n - 1) / size + 1 : 0; }
+static int tile_for(uint32_t m, uint32_t n)
+{
+#ifdef DGS_HEAD_TILE      // (a CPU build that is to reach one kind on small matrices)
+    return DGS_HEAD_TILE;
+#endif
+    return (uint64_t)tiles_of(m, 256) * tiles_of(n, 256) >= 192 ? TILE_LARGE : TILE_SMALL;
+}
+static int logits_tile(uint32_t vocab, uint32_t rows) { return rows <= 32 ? TILE_FEW : tile_for(vocab, rows); }
+
+constexpr uint64_t PIECE_BYTES = 1ull << 30;      // of the logits' gradient, at a time
+
+struct HeadPlan {
+    bool back, wants_dx, wants_dw;
+    bool scale_x_rows, copy_x, copy_w, scale_w;      // which operands are copied, and how
+    uint32_t width;                                  // columns, up to a multiple of eight
+    uint32_t piece;                                  // entries at a time
+    uint32_t dx_splits, dw_splits;
+    int logits, dx_tile, dw_tile;
+    uint64_t bytes;
+    // sections
+    float2 *stats;
+    float *target_logit;
+    HeadRow *row_info;
+    Ranges ranges;
+    Scales *scales;
+    uint16_t *x[2], *x_weighed[2], *w[2], *grad[2];
+    float *bias_parts, *dx_sums, *dw_sums;
+};
+
+static bool straight_ok(const dgs_matrix &m, uint32_t cols)
+{
+    return cols % 8 == 0 && m.stride % 8 == 0 && aligned_to(m.data, 16);
+}
+static uint32_t splits_for(uint64_t tiles, uint32_t depth)
+{
+    uint64_t s = tiles ? 512 / tiles : 1;
+    if (s > depth / 512) s = depth / 512;
+    if (s > 16) s = 16;
+    return s < 1 ? 1u : (uint32_t)s;
+}
+
+static HeadPlan plan_of(const dgs_head_args &p, bool back)
+{
+    HeadPlan h = {};
+    h.back = back;
+    h.wants_dx = back && p.dx.data;
+    h.wants_dw = back && p.dweight;
+    h.width = (p.cols + 7) & ~7u;
+    const bool f32 = p.type == DGS_F32;
+    h.scale_x_rows = f32;
+    h.scale_w = f32 || (back && p.type == DGS_BF16 && h.wants_dx);
+    h.copy_x = !f32 && !straight_ok(p.x, p.cols);
+    h.copy_w = !f32 && !straight_ok(p.weight, p.cols);
+    h.logits = logits_tile(p.vocab, p.rows);
+    Sections s = {(uintptr_t)p.workspace, 0};
+    const uint64_t x_bytes = (uint64_t)p.rows * h.width * 2, w_bytes = (uint64_t)p.vocab * h.width * 2;
+    const TileSize tile = size_of(h.logits);
+    if (!back) {
+        h.stats = (float2 *)s.take((uint64_t)tiles_of(p.vocab, tile.m) * p.rows * sizeof(float2));
+        h.target_logit = (float *)s.take((uint64_t)p.rows * 4);
+    }
+    if (back || f32) {
+        h.ranges.row = (int *)s.take((uint64_t)p.rows * 4);
+        h.ranges.x = (int *)s.take(RANGE_BLOCKS * 4);
+        h.ranges.w = (int *)s.take(RANGE_BLOCKS * 4);
+        h.scales = (Scales *)s.take(sizeof(Scales));
+        if (!h.scale_w) h.ranges.w = nullptr;
+    }
+    if (f32 || h.copy_x) h.x[0] = (uint16_t *)s.take(x_bytes);
+    if (f32) h.x[1] = (uint16_t *)s.take(x_bytes);
+    if (f32 || h.copy_w) h.w[0] = (uint16_t *)s.take(w_bytes);
+    if (f32) h.w[1] = (uint16_t *)s.take(w_bytes);
+    if (back) {
+        h.row_info = (HeadRow *)s.take((uint64_t)p.rows * sizeof(HeadRow));
+        if (h.wants_dw) h.x_weighed[0] = (uint16_t *)s.take(x_bytes);
+        if (h.wants_dw && f32) h.x_weighed[1] = (uint16_t *)s.take(x_bytes);
+        // the logits' gradient: pieces of the vocabulary, whole tiles of it
+        uint64_t most = p.rows ? PIECE_BYTES / (4ull * p.rows) & ~255ull : p.vocab;
+        if (most < 256) most = 256;
+#ifdef DGS_HEAD_PIECE
+        most = DGS_HEAD_PIECE;
+#endif
+        h.piece = most < p.vocab ? (uint32_t)most : p.vocab;
+        const uint64_t stride = ((uint64_t)h.piece + 7) & ~7ull;
+        h.grad[0] = (uint16_t *)s.take(p.rows * stride * 2);
+        h.grad[1] = (uint16_t *)s.take(p.rows * stride * 2);
+        if (p.dbias) h.bias_parts = (float *)s.take(tiles_of(p.rows, tile.n) * stride * 4);
+        h.dx_tile = tile_for(p.rows, p.cols);
+        h.dw_tile = tile_for(h.piece, p.cols);
+        const TileSize x = size_of(h.dx_tile), w = size_of(h.dw_tile);
+        h.dx_splits = splits_for((uint64_t)tiles_of(p.rows, x.m) * tiles_of(p.cols, x.n), h.piece);
+        h.dw_splits = splits_for((uint64_t)tiles_of(h.piece, w.m) * tiles_of(p.cols, w.n), p.rows);
+        if (h.wants_dx) h.dx_sums = (float *)s.take((uint64_t)h.dx_splits * p.rows * p.cols * 4);
+        if (h.wants_dw && h.dw_splits > 1) h.dw_sums = (float *)s.take((uint64_t)h.dw_splits * h.piece * p.cols * 4);
+        if (h.scale_w && !f32) h.w[1] = (uint16_t *)s.take(w_bytes);      // (of bfloat16: W in half, for dx)
+    }
+    h.bytes = s.used ? s.used : 256;
+    return h;
+}
+
+template <class T, int KIND>
+static void copy(const dgs_matrix &m, uint32_t rows, uint32_t cols, uint16_t *hi, uint16_t *lo, const HeadPlan &h, hipStream_t st)
+{
+    if (rows == 0) return;
+    const uint32_t pieces = h.width / 8;
+    const uint64_t blocks = ((uint64_t)rows * pieces + 255) / 256;
+    hipLaunchKernelGGL((k_head_copy<T, KIND>), dim3((uint32_t)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, st, (const T *)m.data, m.stride,
+                       rows, cols, hi, lo, pieces, h.ranges, (const HeadRow *)h.row_info, h.scales);
+}
+
+template <class T> static void prepare(const dgs_head_args &p, const HeadPlan &h, const Targets &targets, hipStream_t st)
+{
+    constexpr bool f32 = __is_same(T, float);
+    if (h.back || f32)
+        hipLaunchKernelGGL(k_head_range<T>, dim3(2 * RANGE_BLOCKS), dim3(256), 0, st, (const T *)p.x.data, p.x.stride,
+                           (const T *)p.weight.data, p.weight.stride, p.rows, p.cols, targets, (const float *)p.lse, p.dloss, p.dlse,
+                           h.row_info, h.ranges);
+    if constexpr (f32) {
+        copy<T, COPY_ROWS>(p.x, p.rows, p.cols, h.x[0], h.x[1], h, st);
+        copy<T, COPY_ALL>(p.weight, p.vocab, p.cols, h.w[0], h.w[1], h, st);
+    } else {
+        if (h.copy_x) copy<T, COPY_PLAIN>(p.x, p.rows, p.cols, h.x[0], nullptr, h, st);
+        if (h.copy_w) copy<T, COPY_PLAIN>(p.weight, p.vocab, p.cols, h.w[0], nullptr, h, st);
+        if (h.scale_w) copy<T, COPY_ALL>(p.weight, p.vocab, p.cols, h.w[1], nullptr, h, st);
+    }
+    if (h.wants_dw) copy<T, COPY_WEIGHED>(p.x, p.rows, p.cols, h.x_weighed[0], h.x_weighed[1], h, st);
+}
+
+template <class E, bool BACK> static void logits(const LogitArgs &a, int tile, hipStream_t st)
+{
+    const dim3 grid(a.v_tiles * a.t_tiles);
+    if (tile == TILE_LARGE) hipLaunchKernelGGL((k_head_logits<E, 256, 256, 2, 4, BACK>), grid, dim3(512), 0, st, a);
+    else if (tile == TILE_SMALL) hipLaunchKernelGGL((k_head_logits<E, 128, 128, 2, 2, BACK>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((k_head_logits<E, 128, 32, 4, 1, BACK>), grid, dim3(256), 0, st, a);
+}
+template <bool BACK> static void logits(const LogitArgs &a, int type, int tile, hipStream_t st)
+{
+    if (type == DGS_BF16) logits<bf16, BACK>(a, tile, st);
+    else logits<f16, BACK>(a, tile, st);
+}
+template <bool TURN_A> static void product(const GradientArgs &a, int tile, hipStream_t st)
+{
+    const dim3 grid(a.m_tiles * a.n_tiles * a.splits);
+    if (tile == TILE_LARGE) hipLaunchKernelGGL((k_head_product<256, 256, 2, 4, TURN_A>), grid, dim3(512), 0, st, a);
+    else hipLaunchKernelGGL((k_head_product<128, 128, 2, 2, TURN_A>), grid, dim3(256), 0, st, a);
+}
+
+static LogitArgs logit_args(const dgs_head_args &p, const HeadPlan &h, const Targets &targets)
+{
+    LogitArgs a = {};
+    const bool f32 = p.type == DGS_F32;
+    const bool own_x = f32 || h.copy_x, own_w = f32 || h.copy_w;
+    a.x = Side{{own_x ? h.x[0] : (const uint16_t *)p.x.data, h.x[1]}, own_x ? h.width : p.x.stride, p.rows};
+    a.w = Side{{own_w ? h.w[0] : (const uint16_t *)p.weight.data, h.w[1]}, own_w ? h.width : p.weight.stride, p.vocab};
+    a.cols = p.cols;
+    a.kind = f32 ? BOTH_IN_TWO : ONE_PAIR;
+    a.rows = p.rows;
+    a.vocab = p.vocab;
+    a.t_tiles = tiles_of(p.rows, size_of(h.logits).n);
+    a.bias = p.bias;
+    a.targets = targets;
+    a.x_powers = f32 ? h.ranges.row : nullptr;
+    a.scales = h.scales;
+    return a;
+}
+
+// What both calls refuse.
+static int refused(const dgs_head_args &p, bool back)
+{
+    if (p.cols == 0 || p.vocab == 0 || !is_type(p.type) || (p.target_bytes != 4 && p.target_bytes != 8)) return DGS_EINVAL;
+    if (!matrix_ok(p.weight.data, p.weight.stride, p.cols, p.type) || !aligned_to(p.bias, 4)) return DGS_EINVAL;
+    if (p.rows) {
+        if (!matrix_ok(p.x.data, p.x.stride, p.cols, p.type) || !p.targets || !aligned_to(p.targets, p.target_bytes)) return DGS_EINVAL;
+        if (!aligned_to(p.loss, 4) || !p.lse || !aligned_to(p.lse, 4)) return DGS_EINVAL;
+        if (back && p.dx.data && !matrix_ok(p.dx.data, p.dx.stride, p.cols, p.type)) return DGS_EINVAL;
+    }
+    if (back && p.dweight && (p.dweight_stride < p.cols || p.dweight_stride >= (1ull << 32))) return DGS_EINVAL;
+    if (!aligned_to(p.dloss, 4) || !aligned_to(p.dlse, 4) || !aligned_to(p.dweight, 4) || !aligned_to(p.dbias, 4)) return DGS_EINVAL;
+    // (a tile's 256 rows are reached by 31 bits)
+    if (p.cols > (1u << 20) || p.x.stride >= (1u << 21) || p.weight.stride >= (1u << 21)) return DGS_ENOTSUP;
+    if (p.rows > (1u << 24) || p.vocab > (1u << 24)) return DGS_ENOTSUP;
+    return DGS_OK;
+}
+
+}  // namespace dgs
+
+using namespace dgs;
+
+extern "C" size_t dgs_head_workspace(const dgs_head_args *args, int backward)
+{
+    if (!args || refused(*args, backward != 0) != DGS_OK) return 0;
+    return (size_t)plan_of(*args, backward != 0).bytes;
+}
+
+extern "C" int dgs_head_forward(const dgs_head_args *args, void *hip_stream)
+{
+    if (!args) return DGS_EINVAL;
+    const dgs_head_args &p = *args;
+    const int rc = refused(p, false);
+    if (rc != DGS_OK) return rc;
+    if (p.rows == 0) return DGS_OK;
+    if (!p.workspace || !aligned_to(p.workspace, 16)) return DGS_EINVAL;
+    const HeadPlan h = plan_of(p, false);
+    if (p.workspace_bytes < h.bytes) return DGS_ENOMEM;
+    const hipStream_t st = (hipStream_t)hip_stream;
+    const Targets targets = {p.targets, p.target_bytes == 8, p.vocab};
+    if (p.type == DGS_F32) prepare<float>(p, h, targets, st);
+    else if (p.type == DGS_F16) prepare<f16>(p, h, targets, st);
+    else prepare<bf16>(p, h, targets, st);
+    LogitArgs a = logit_args(p, h, targets);
+    a.end = p.vocab;
+    a.v_tiles = tiles_of(p.vocab, size_of(h.logits).m);
+    a.stats = h.stats;
+    a.target_logit = h.target_logit;
+    logits<false>(a, p.type, h.logits, st);
+    const uint32_t apart = p.rows >= 2048 ? 8 : p.rows >= 64 ? 32 : 256;
+    hipLaunchKernelGGL(k_head_loss, dim3(tiles_of(p.rows, 256 / apart)), dim3(256), 0, st, (const float2 *)h.stats,
+                       (const float *)h.target_logit, targets, p.rows, a.v_tiles, apart, p.loss, p.lse);
+    return launched();
+}
+
+extern "C" int dgs_head_backward(const dgs_head_args *args, void *hip_stream)
+{
+    if (!args) return DGS_EINVAL;
+    const dgs_head_args &p = *args;
+    const int rc = refused(p, true);
+    if (rc != DGS_OK) return rc;
+    if (p.rows == 0) {      // (no sums: zeros, or what is there)
+        if (p.accumulate || (!p.dweight && !p.dbias)) return DGS_OK;
+        if (p.dweight)
+            hipLaunchKernelGGL(k_head_dweight, dim3((uint32_t)(((uint64_t)p.vocab * p.cols + 255) / 256)), dim3(256), 0, (hipStream_t)hip_stream,
+                               (const float *)nullptr, 0u, p.vocab, p.cols, (const Scales *)nullptr, p.dweight, p.dweight_stride, 0u);
+        if (p.dbias)
+            hipLaunchKernelGGL(k_head_dbias, dim3(tiles_of(p.vocab, 256)), dim3(256), 0, (hipStream_t)hip_stream, (const float *)nullptr, 0u,
+                               (uint64_t)0, p.vocab, p.dbias, 0u);
+        return launched();
+    }
+    if (!p.workspace || !aligned_to(p.workspace, 16)) return DGS_EINVAL;
+    const HeadPlan h = plan_of(p, true);
+    if (p.workspace_bytes < h.bytes) return DGS_ENOMEM;
+    const hipStream_t st = (hipStream_t)hip_stream;
+    const Targets targets = {p.targets, p.target_bytes == 8, p.vocab};
+    const bool f32 = p.type == DGS_F32;
+    if (p.type == DGS_F32) prepare<float>(p, h, targets, st);
+    else if (p.type == DGS_F16) prepare<f16>(p, h, targets, st);
+    else prepare<bf16>(p, h, targets, st);
+    const TileSize tile = size_of(h.logits), tx = size_of(h.dx_tile), tw = size_of(h.dw_tile);
+    const uint64_t stride = ((uint64_t)h.piece + 7) & ~7ull;
+    LogitArgs a = logit_args(p, h, targets);
+    a.row_info = h.row_info;
+    a.grad[0] = h.grad[0];
+    a.grad[1] = h.grad[1];
+    a.grad_stride = stride;
+    a.bias_parts = p.dbias ? h.bias_parts : nullptr;
+    for (uint32_t first = 0; first < p.vocab; first += h.piece) {
+        const uint32_t count = p.vocab - first < h.piece ? p.vocab - first : h.piece;
+        a.first = first;
+        a.end = first + count;
+        a.v_tiles = tiles_of(count, tile.m);
+        logits<true>(a, p.type, h.logits, st);
+        if (p.dbias)
+            hipLaunchKernelGGL(k_head_dbias, dim3(tiles_of(count, 256)), dim3(256), 0, st, (const float *)h.bias_parts,
+                               a.t_tiles, stride, count, p.dbias + first, (uint32_t)(p.accumulate != 0));
+        if (h.wants_dx) {
+            GradientArgs g = {};
+            const uint16_t *w = p.type == DGS_BF16 ? h.w[1] : a.w.part[0];
+            const uint64_t w_stride = p.type == DGS_BF16 ? h.width : a.w.stride;
+            g.a = Side{{h.grad[0], h.grad[1]}, stride, p.rows};
+            g.b = Side{{w + first * w_stride, f32 ? a.w.part[1] + first * w_stride : nullptr}, w_stride, p.cols};
+            g.depth = count;
+            g.splits = h.dx_splits;
+            g.split_depth = (tiles_of(count, PRODUCT_STEP) + g.splits - 1) / g.splits * PRODUCT_STEP;
+            g.kind = f32 ? BOTH_IN_TWO : p.type == DGS_F16 ? FIRST_IN_TWO : ONE_PAIR;
+            g.m = p.rows;
+            g.n = p.cols;
+            g.m_tiles = tiles_of(g.m, tx.m);
+            g.n_tiles = tiles_of(g.n, tx.n);
+            g.out = h.dx_sums;
+            g.out_stride = p.cols;
+            g.add = first != 0;
+            product<false>(g, h.dx_tile, st);
+        }
+        if (h.wants_dw) {
+            GradientArgs g = {};
+            g.a = Side{{h.grad[0], h.grad[1]}, stride, count};
+            g.b = Side{{h.x_weighed[0], h.x_weighed[1]}, h.width, p.cols};
+            g.depth = p.rows;
+            g.splits = h.dw_splits;
+            g.split_depth = (tiles_of(p.rows, PRODUCT_STEP) + g.splits - 1) / g.splits * PRODUCT_STEP;
+            g.kind = f32 ? BOTH_IN_TWO : FIRST_IN_TWO;
+            g.m = count;
+            g.n = p.cols;
+            g.m_tiles = tiles_of(g.m, tw.m);
+            g.n_tiles = tiles_of(g.n, tw.n);
+            g.whole = g.splits == 1;
+            g.out = g.whole ? p.dweight + first * p.dweight_stride : h.dw_sums;
+            g.out_stride = g.whole ? p.dweight_stride : p.cols;
+            g.add = g.whole && p.accumulate;
+            g.scales = h.scales;
+            product<true>(g, h.dw_tile, st);
+            if (h.dw_splits > 1)
+                hipLaunchKernelGGL(k_head_dweight, dim3((uint32_t)(((uint64_t)count * p.cols + 255) / 256)), dim3(256), 0, st,
+                                   (const float *)h.dw_sums, g.splits, count, p.cols, (const Scales *)h.scales,
+                                   p.dweight + first * p.dweight_stride, p.dweight_stride, (uint32_t)(p.accumulate != 0));
+        }
+    }
+    if (h.wants_dx) {
+        const uint64_t blocks = ((uint64_t)p.rows * ((p.cols + 7) / 8) + 255) / 256;
+        const dim3 grid((uint32_t)blocks);
+        const Scales *const sc = h.scale_w ? h.scales : nullptr;
+        if (f32) hipLaunchKernelGGL(k_head_dx<float>, grid, dim3(256), 0, st, (const float *)h.dx_sums, h.dx_splits, p.rows, p.cols, (const HeadRow *)h.row_info, sc, (float *)p.dx.data, p.dx.stride);
+        else if (p.type == DGS_F16) hipLaunchKernelGGL(k_head_dx<f16>, grid, dim3(256), 0, st, (const float *)h.dx_sums, h.dx_splits, p.rows, p.cols, (const HeadRow *)h.row_info, sc, (f16 *)p.dx.data, p.dx.stride);
+        else hipLaunchKernelGGL(k_head_dx<bf16>, grid, dim3(256), 0, st, (const float *)h.dx_sums, h.dx_splits, p.rows, p.cols, (const HeadRow *)h.row_info, sc, (bf16 *)p.dx.data, p.dx.stride);
+    }
+    return launched();
+}

@@ -1,0 +1,396 @@
+"""The output layer with its loss (blocks.Head) against plain computations in 64 bits.
+
+Tolerances.  A logit is a sum of `cols` products: exact for half and bfloat16, off by 2^-22 for fp32 (two operands in 22 bits each),
+and every fp32 addition by EPS = 2^-24 of what has been added up.  Z, the largest sum of a row's magnitudes, bounds that: logits are off by
+at most LOGIT = (cols + 8) EPS Z.  Exponentials and logarithms add a few EPS of their arguments (64 allowed): lse is off by LOGIT + 64 EPS
+(|lse| + 64), the loss by twice that.  The gradient of a logit, pull softmax - push onehot, is then off by at most e = 4 (LOGIT + 64 EPS 64)
+of its terms' magnitudes, and by 2^-22 (dx of bfloat16: 2^-11) where it is held in halves.  Products of it with W or x: that much of the
+sum of magnitudes, and EPS for every term of the sum (16 for the largest is far more than random signs leave; a sum over n terms is given
+n EPS).  A rounded result adds half a step of its type."""
+import pytest
+
+from paper_1910_10929_amd import blocks, dgs
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+DEV = "cuda:0"
+EPS = 2.0 ** -24
+F32, F16, BF16, D = torch.float32, torch.float16, torch.bfloat16, torch.float64
+HALF = {F32: 2.0 ** -24, F16: 2.0 ** -11, BF16: 2.0 ** -8}
+
+
+@pytest.fixture(scope="module", autouse=True)
+def built():
+    assert torch.cuda.is_available()
+    dgs.lib()
+
+
+class Case:
+    def __init__(self, rows, cols, vocab, dtype, bias=False, pad=0, shift=0, left_out=0.2, seed=0):
+        self.g = torch.Generator(device=DEV)
+        self.g.manual_seed(1000 * seed + rows + 7 * cols + 11 * vocab)
+        self.rows, self.cols, self.vocab, self.dtype = rows, cols, vocab, dtype
+        self.x, self.w = self.matrix(rows, cols, dtype, pad, shift), self.matrix(vocab, cols, dtype, pad, 0, 1.5 / cols ** 0.5)
+        self.bias = self.normal(vocab) * 0.5 if bias else None
+        self.targets = torch.randint(0, vocab, (rows,), device=DEV, generator=self.g)
+        out = torch.rand(rows, device=DEV, generator=self.g) < left_out
+        self.targets[out] = -100
+        self.dloss, self.dlse = self.normal(rows), 0.1 * self.normal(rows)
+
+    def normal(self, *shape):
+        return torch.randn(*shape, device=DEV, generator=self.g)
+
+    def matrix(self, rows, cols, dtype, pad=0, shift=0, scale=1.0):
+        n = rows * (cols + pad) + shift
+        t = torch.full((max(n, 1),), float("nan"), dtype=dtype, device=DEV)[shift:shift + rows * (cols + pad)].view(rows, cols + pad)[:, :cols]
+        t.copy_(self.normal(rows, cols) * scale)
+        return t
+
+    def head(self):
+        return blocks.Head(self.w, self.bias)
+
+    def exact(self, dloss=None, dlse=None):
+        """The definition in 64 bits, and beside each result how far it may be off."""
+        x, w = self.x.to(D), self.w.to(D)
+        z = x @ w.t()
+        size = (x.abs() @ w.abs().t())
+        if self.bias is not None:
+            z = z + self.bias.to(D)
+            size = size + torch.where(self.bias.isfinite(), self.bias.abs(), 0.0).to(D)
+        lse = torch.logsumexp(z, 1)
+        counts = (self.targets >= 0) & (self.targets < self.vocab)
+        at = torch.where(counts, self.targets.long(), 0)
+        loss = torch.where(counts, lse - z.gather(1, at[:, None])[:, 0], 0.0)
+        logit = (self.cols + 8) * EPS * size.amax(1)
+        if self.dtype == F32:
+            logit = logit + 2.0 ** -21 * size.amax(1)
+        tol_lse = logit + 64 * EPS * (lse.abs() + 64)
+        r = {"lse": (lse, tol_lse), "loss": (loss, torch.where(counts, 2 * tol_lse, 0.0))}
+        up = torch.where(counts, torch.ones(self.rows, dtype=D, device=DEV) if dloss is None else dloss.to(D), 0.0)
+        all_ = up + (0.0 if dlse is None else dlse.to(D))
+        p = torch.softmax(z, 1)
+        one = torch.zeros_like(p).scatter_(1, at[:, None], up[:, None])
+        dz = all_[:, None] * p - one
+        terms = all_.abs()[:, None] * p + one.abs()
+        e = 4 * (logit + 64 * EPS * 64)[:, None] + 2.0 ** -22
+        off = terms * e
+        short = off + (dz.abs() * 2.0 ** -11 if self.dtype == BF16 else 0.0)
+        dx = dz @ w
+        tol = short @ w.abs() + self.vocab * EPS * (dz.abs() @ w.abs()) + HALF[self.dtype] * dx.abs()
+        r["dx"] = (dx, tol + (2.0 ** -24 if self.dtype == F16 else 0.0))
+        r["dweight"] = (dz.t() @ x, off.t() @ x.abs() + (self.rows + 4) * EPS * (dz.abs().t() @ x.abs()))
+        r["dbias"] = (dz.sum(0), off.sum(0) + (self.rows + 4) * EPS * dz.abs().sum(0))
+        return r
+
+    def gradients(self, lse, dloss=None, dlse=None, **more):
+        dw, db = torch.full((self.vocab, self.cols), 7.0, device=DEV), torch.full((self.vocab,), 7.0, device=DEV)
+        dx = self.head().backward(self.x, self.targets, lse, dloss=dloss, dlse=dlse, dweight=dw, dbias=db, **more)
+        return {"dx": dx, "dweight": dw, "dbias": db}
+
+
+def assert_near(got, want, what):
+    value, tol = want
+    bad = ~((got.to(D) - value).abs() <= tol)
+    if bool(bad.any()):
+        i = int(bad.reshape(-1).nonzero()[0])
+        raise AssertionError(f"{what}: {int(bad.sum())} of {bad.numel()} off, first at {i}: {got.reshape(-1)[i].item()} != "
+                             f"{value.reshape(-1)[i].item()} within {tol.reshape(-1)[i].item()}")
+
+
+# rows, columns, entries, type, bias, padding, shift
+CASES = [
+    (1, 1, 1, F32, True, 0, 0), (1, 8, 2, BF16, False, 0, 0), (2, 7, 3, F16, True, 1, 1), (1, 768, 5000, BF16, False, 0, 0),
+    (1, 64, 70001, F16, True, 0, 0), (31, 64, 257, BF16, True, 8, 8), (32, 65, 256, F16, False, 0, 0), (33, 64, 255, F32, True, 3, 1),
+    (64, 72, 1000, BF16, True, 0, 3), (65, 128, 1001, F16, True, 8, 0), (127, 200, 513, F32, False, 0, 0), (128, 256, 512, BF16, False, 64, 0),
+    (129, 333, 1009, F32, True, 5, 0), (257, 1000, 2050, BF16, True, 0, 0), (300, 96, 12345, F16, True, 0, 0), (1000, 40, 64, BF16, True, 0, 0),
+    (3000, 24, 9, F32, True, 0, 0), (2049, 520, 4099, BF16, True, 0, 0), (2048, 512, 8192, F16, False, 0, 0), (5000, 64, 8000, BF16, False, 3, 0),
+]
+
+
+@pytest.mark.parametrize("case", CASES, ids=lambda c: f"{c[0]}x{c[1]}x{c[2]}-{str(c[3])[6:]}")
+def test_against_64_bits(case):
+    print(case, flush=True)
+    rows, cols, vocab, dtype, bias, pad, shift = case
+    c = Case(rows, cols, vocab, dtype, bias, pad, shift)
+    loss, lse = c.head().forward(c.x, c.targets)
+    want = c.exact(c.dloss, c.dlse)
+    assert_near(loss, want["loss"], "loss")
+    assert_near(lse, want["lse"], "lse")
+    assert bool((loss[c.targets < 0] == 0).all())
+    got = c.gradients(lse, c.dloss, c.dlse)
+    for k in ("dx", "dweight", "dbias"):
+        assert_near(got[k], want[k], k)
+    again = c.gradients(lse, c.dloss, c.dlse)
+    assert all(torch.equal(got[k], again[k]) for k in got)
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+def test_ones_arrive_where_nothing_is_given(dtype):
+    c = Case(70, 48, 300, dtype, True)
+    lse = c.head().forward(c.x, c.targets)[1]
+    want, got = c.exact(), c.gradients(lse)
+    for k in got:
+        assert_near(got[k], want[k], k)
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+def test_added_to_and_partly_asked_for(dtype):
+    """dweight in rows of a wider matrix and dbias are added to; what is not asked for is not computed, and the rest is the same."""
+    c = Case(90, 80, 400, dtype, True)
+    h, lse = c.head(), c.head().forward(c.x, c.targets.int())[1]
+    whole = c.gradients(lse, c.dloss)
+    room = torch.full((400, 87), 3.0, device=DEV)
+    dw, db = room[:, 4:84], torch.full((400,), -2.0, device=DEV)
+    before = dw.clone()
+    assert h.backward(c.x, c.targets.int(), lse, dloss=c.dloss, dweight=dw, dbias=db, need_dx=False, accumulate=True) is None
+    assert torch.equal(dw, before + whole["dweight"]) and torch.equal(db, whole["dbias"] - 2.0)
+    assert bool((room[:, :4] == 3.0).all()) and bool((room[:, 84:] == 3.0).all())
+    out = torch.zeros(90, 88, dtype=dtype, device=DEV)
+    dx = h.backward(c.x, c.targets, lse, dloss=c.dloss, dx=out[:, :80])
+    assert torch.equal(dx, whole["dx"]) and bool((out[:, 80:] == 0).all())
+    only = torch.empty(400, device=DEV)
+    h.backward(c.x, c.targets, lse, dloss=c.dloss, dbias=only, need_dx=False)
+    assert torch.equal(only, whole["dbias"])
+
+
+def test_no_rows():
+    h = blocks.Head(torch.zeros(20, 16, device=DEV))
+    x, t = torch.zeros(0, 16, device=DEV), torch.zeros(0, dtype=torch.int64, device=DEV)
+    loss, lse = h.forward(x, t)
+    assert loss.shape == lse.shape == (0,)
+    dw, db = torch.full((20, 16), 5.0, device=DEV), torch.full((20,), 5.0, device=DEV)
+    h.backward(x, t, lse, dweight=dw, dbias=db, accumulate=True)
+    assert bool((dw == 5).all()) and bool((db == 5).all())
+    assert h.backward(x, t, lse, dweight=dw, dbias=db).shape == (0, 16)
+    assert bool((dw == 0).all()) and bool((db == 0).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+def test_every_row_left_out(dtype):
+    c = Case(40, 64, 130, dtype, True, left_out=2.0)
+    loss, lse = c.head().forward(c.x, c.targets)
+    assert bool((loss == 0).all())
+    assert_near(lse, c.exact()["lse"], "lse")
+    assert all(bool((v == 0).all()) for v in c.gradients(lse).values())
+    # ... but for what arrives at lse
+    want, got = c.exact(None, c.dlse), c.gradients(lse, None, c.dlse)
+    for k in got:
+        assert_near(got[k], want[k], k)
+
+
+@pytest.mark.parametrize("target", [-1, -100, 130, 1000, 2 ** 31, -2 ** 31, 2 ** 40 + 5, 2 ** 63 - 1, -2 ** 63])
+def test_targets_outside_the_vocabulary(target):
+    c = Case(33, 64, 130, BF16, left_out=0.0)
+    c.targets[::3] = target
+    loss, lse = c.head().forward(c.x, c.targets)
+    assert bool((loss[::3] == 0).all()) and bool((loss[1::3] > 0).all())
+    dx = c.head().backward(c.x, c.targets, lse)
+    assert bool((dx[::3] == 0).all()) and bool((dx[1::3] != 0).any(1).all())
+    if -2 ** 31 <= target < 2 ** 31:
+        assert torch.equal(c.head().forward(c.x, c.targets.int())[0], loss)
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+def test_entries_taken_out(dtype):
+    """A bias of -infinity takes an entry out (rows of padding at the vocabulary's end); a target among them costs infinity."""
+    c = Case(50, 64, 700, dtype, True)
+    c.bias[640:] = -float("inf")
+    c.bias[3] = -float("inf")
+    c.targets[0], c.targets[1], c.targets[2:] = 690, 3, c.targets[2:].clamp(max=600)
+    c.targets[c.targets == 3] = 4
+    c.targets[1] = 3
+    loss, lse = c.head().forward(c.x, c.targets)
+    want = c.exact(c.dloss)
+    assert bool(loss[:2].isinf().all()) and bool(loss[2:].isfinite().all())
+    assert_near(lse, want["lse"], "lse")
+    assert_near(loss[2:], (want["loss"][0][2:], want["loss"][1][2:]), "loss")
+    got = c.gradients(lse, c.dloss)
+    for k in got:
+        assert_near(got[k], want[k], k)
+    assert bool((got["dweight"][650:690] == 0).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+def test_what_a_row_that_nothing_arrives_at_holds(dtype):
+    """Padding rows of infinities and NaN leave no gradient and disturb no other row."""
+    c = Case(70, 64, 300, dtype, True, left_out=0.0)
+    c.targets[::7] = -100
+    lse = c.head().forward(c.x, c.targets)[1]
+    clean = c.gradients(lse, c.dloss)
+    c.x[0] = float("nan")
+    c.x[7] = float("inf")
+    c.x[14, 3] = -float("inf")
+    c.x[21] = 3e38 if dtype != F16 else 65504.0
+    loss2, lse2 = c.head().forward(c.x, c.targets)
+    assert bool((loss2[::7] == 0).all()) and bool((lse2 == lse)[1:7].all())
+    got = c.gradients(lse2, c.dloss)
+    assert bool((got["dx"][::7] == 0).all())
+    for k in got:
+        assert torch.equal(got[k], clean[k]), k
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+def test_nan_stays_with_its_row(dtype):
+    """A row that counts and holds a NaN: its loss and dx are NaN, and the weights' gradients; other rows' losses are not."""
+    c = Case(40, 64, 300, dtype, left_out=0.0)
+    c.x[5, 7] = float("nan")
+    loss, lse = c.head().forward(c.x, c.targets)
+    assert bool(loss[5].isnan()) and int(loss.isnan().sum()) == 1
+    got = c.gradients(lse)
+    assert bool(got["dx"][5].isnan().all()) and int(got["dx"].isnan().any(1).sum()) == 1
+    assert bool(got["dweight"].isnan().all())
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+def test_rows_of_unlike_size(dtype):
+    """Incoming gradients and rows of x over many powers of two: every row's dx and the weights' gradient keep their precision."""
+    c = Case(64, 64, 300, dtype, left_out=0.0)
+    scale = torch.exp2(torch.arange(64, device=DEV).float().remainder(17) - 8)
+    c.x.mul_(0.1 * torch.exp2(torch.arange(64, device=DEV).float().remainder(5))[:, None])
+    dloss = c.dloss * (scale if dtype == F16 else scale ** 3)
+    lse = c.head().forward(c.x, c.targets)[1]
+    want, got = c.exact(dloss), c.gradients(lse, dloss)
+    for k in got:
+        assert_near(got[k], want[k], k)
+
+
+def test_confident_rows():
+    """Logits so far apart that softmax is 0 and 1."""
+    c = Case(40, 64, 300, F32, left_out=0.0)
+    c.x.mul_(200.0)
+    loss, lse = c.head().forward(c.x, c.targets)
+    want = c.exact(c.dloss)
+    assert_near(loss, want["loss"], "loss")
+    assert_near(lse, want["lse"], "lse")
+    assert bool((loss >= 0).all()) and bool(torch.isfinite(loss).all())
+
+
+def test_gradients_against_differences():
+    """Loss and penalty in 64 bits along random directions of x, W and the bias."""
+    c = Case(30, 40, 70, F32, True)
+    lse = c.head().forward(c.x, c.targets)[1]
+    got = c.gradients(lse, c.dloss, c.dlse)
+
+    def value(x, w, b):
+        z = x @ w.t() + b
+        l = torch.logsumexp(z, 1)
+        counts = c.targets >= 0
+        at = torch.where(counts, c.targets, 0)
+        return (torch.where(counts, l - z.gather(1, at[:, None])[:, 0], 0.0) * c.dloss + l * c.dlse).sum()
+
+    x, w, b = c.x.to(D), c.w.to(D), c.bias.to(D)
+    for _ in range(4):
+        u, v, t = c.normal(30, 40).to(D), c.normal(70, 40).to(D), c.normal(70).to(D)
+        h = 1e-4
+        diff = (value(x + h * u, w + h * v, b + h * t) - value(x - h * u, w - h * v, b - h * t)) / (2 * h)
+        slope = (got["dx"].to(D) * u).sum() + (got["dweight"].to(D) * v).sum() + (got["dbias"].to(D) * t).sum()
+        size = (got["dx"].to(D) * u).abs().sum() + (got["dweight"].to(D) * v).abs().sum() + (got["dbias"].to(D) * t).abs().sum()
+        # (the third derivative's share is of the order of h^2; the gradients' own error 2^-20 of the terms)
+        assert abs(float(diff - slope)) <= float(size) * (2.0 ** -18 + 100 * h * h)
+
+
+def test_weights_beyond_32_bits():
+    """A weight and its gradient whose last rows begin more than 2^32 bytes behind their first."""
+    vocab, cols, rows = 1_100_000, 2048, 8
+    if torch.cuda.mem_get_info()[0] < 60 << 30:
+        pytest.skip("needs 60 GB")
+    w = torch.zeros(vocab, cols, dtype=BF16, device=DEV)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(5)
+    tail = torch.randn(1000, cols, device=DEV, generator=g).to(BF16)
+    w[-1000:] = tail
+    x = torch.randn(rows, cols, device=DEV, generator=g).to(BF16)
+    t = torch.arange(vocab - 8, vocab, device=DEV)
+    h = blocks.Head(w)
+    loss, lse = h.forward(x, t)
+    z = x.to(D) @ tail.to(D).t()
+    want = torch.logsumexp(torch.cat([z, torch.zeros(rows, 1, dtype=D, device=DEV) + torch.log(torch.tensor(vocab - 1000.0, dtype=D))], 1), 1)
+    assert float((lse.to(D) - want).abs().max()) < 1e-3 and float((loss.to(D) - (want - z[:, -8:].diagonal())).abs().max()) < 2e-3
+    dw = torch.full((vocab, cols), float("nan"), device=DEV)
+    dx = h.backward(x, t, lse, dweight=dw)
+    dz = torch.exp(z - want[:, None])
+    dz[:, -8:] -= torch.eye(8, dtype=D, device=DEV)
+    assert float((dw[-1000:].to(D) - dz.t() @ x.to(D)).norm() / (dz.t() @ x.to(D)).norm()) < 1e-3
+    assert float((dx.to(D) - dz @ tail.to(D)).norm() / (dz @ tail.to(D)).norm()) < 5e-3
+    rest = torch.exp(-want) @ x.to(D)
+    # (logits of the others are 0 beside some of 100 and more: fp32 ends at 2^-149 a value, and what a half keeps of dz at 2^-39)
+    assert float((dw[12345].to(D) - rest).norm()) <= 1e-3 * float(rest.norm()) + 2.0 ** -39 * float(x.to(D).norm()) and bool(torch.isfinite(dw[::1000]).all())
+
+
+def test_another_stream_and_a_graph():
+    """On a side stream, and replayed from a graph with other work between, the same bits as eagerly; new inputs in a replay count."""
+    c = Case(300, 256, 2000, BF16, True)
+    h = c.head()
+
+    def step(out):
+        loss, lse = h.forward(c.x, c.targets, loss=out["loss"], lse=out["lse"])
+        h.backward(c.x, c.targets, lse, dloss=c.dloss, dx=out["dx"], dweight=out["dweight"], dbias=out["dbias"])
+
+    def fresh():
+        return {"loss": torch.zeros(300, device=DEV), "lse": torch.zeros(300, device=DEV), "dx": torch.zeros(300, 256, dtype=BF16, device=DEV),
+                "dweight": torch.zeros(2000, 256, device=DEV), "dbias": torch.zeros(2000, device=DEV)}
+
+    eager = fresh()
+    step(eager)
+    torch.cuda.synchronize()
+    side, other = torch.cuda.Stream(), fresh()
+    with torch.cuda.stream(side):
+        step(other)
+    side.synchronize()
+    assert all(torch.equal(eager[k], other[k]) for k in eager)
+    out, graph = fresh(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        step(out)
+    x0 = c.x.clone()
+    for replay in range(4):
+        for t in out.values():
+            t.fill_(float("nan"))
+        c.x.copy_(x0 if replay % 2 == 0 else -x0)
+        graph.replay()
+        torch.cuda.synchronize()
+        now = fresh()
+        step(now)
+        assert all(torch.equal(now[k], out[k]) for k in out), replay
+        assert torch.equal(out["dx"], eager["dx"]) == (replay % 2 == 0)
+        assert float(torch.randn(1000, device=DEV).sum()) != 0.0
+
+
+def test_two_streams_at_once():
+    """Calls side by side on two streams, each with a workspace of its own, and one after another in one workspace."""
+    a, b = Case(200, 128, 3000, BF16, True, seed=1), Case(333, 96, 1500, F16, seed=2)
+    alone = []
+    for c in (a, b):
+        lse = c.head().forward(c.x, c.targets)[1]
+        alone.append(dict(c.gradients(lse, c.dloss), lse=lse))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [None, None]
+    for _ in range(5):
+        for i, (c, s) in enumerate(zip((a, b), streams)):
+            with torch.cuda.stream(s):
+                lse = c.head().forward(c.x, c.targets)[1]
+                got[i] = dict(c.gradients(lse, c.dloss), lse=lse)
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(alone[i][k], got[i][k]) for k in got[i])
+    ws = torch.full((1 << 26,), 0xFF, dtype=torch.uint8, device=DEV)
+    for i, c in enumerate((a, b, a)):
+        lse = c.head().forward(c.x, c.targets, workspace=ws)[1]
+        now = dict(c.gradients(lse, c.dloss, workspace=ws), lse=lse)
+        assert all(torch.equal(alone[i % 2][k], now[k]) for k in now)
+    with pytest.raises(dgs.DgsError) as err:
+        a.head().forward(a.x, a.targets, workspace=ws[:1024])
+    assert err.value.code == dgs.DGS_ENOMEM
+    assert all(float(t.sum()) == 0.0 for t in [torch.zeros(3, device=DEV)])
+
+
+def test_refuses_what_is_elsewhere():
+    w = torch.zeros(50, 40, device=DEV)
+    h, x, t = blocks.Head(w), torch.zeros(6, 40, device=DEV), torch.zeros(6, dtype=torch.int64, device=DEV)
+    for call in (lambda: h.forward(x.cpu(), t), lambda: h.forward(x, t.cpu()), lambda: blocks.Head(w.cpu()), lambda: blocks.Head(w, torch.zeros(50)),
+                 lambda: h.backward(x, t, torch.zeros(6)), lambda: h.backward(x, t, torch.zeros(6, device=DEV), dweight=torch.zeros(50, 40))):
+        with pytest.raises(dgs.DgsError) as err:
+            call()
+        assert err.value.code == dgs.DGS_EINVAL
