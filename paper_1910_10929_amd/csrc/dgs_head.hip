@@ -19,7 +19,7 @@ namespace dgs {
 // operands
 // ---------------------------------------------------------------------------
 
-constexpr uint32_t RANGE_BLOCKS = 256;      // of rows, and as many of W
+constexpr uint32_t RANGE_BLOCKS = 1024;     // of rows, and as many of W
 constexpr int NO_RANGE = -100000;           // nothing but zeros
 constexpr int TOP = 15;                     // the largest magnitude of a scaled operand lies below 2^TOP
 constexpr int GRAD_TOP = 14;                // a row's logit gradients are at most 2 after division
@@ -159,7 +159,10 @@ __global__ __launch_bounds__(256) void k_head_copy(const T *from, uint64_t from_
     if constexpr (KIND == COPY_WEIGHED || KIND == COPY_ALL) {
         __shared__ int best[4];
         const int *const r = KIND == COPY_ALL ? ranges.w : ranges.x;
-        const int e = wave_max(r[threadIdx.x]);      // (as many as there are threads)
+        int most = NO_RANGE;
+#pragma unroll
+        for (uint32_t k = 0; k < RANGE_BLOCKS; k += 256) most = max(most, r[k + threadIdx.x]);
+        const int e = wave_max(most);
         if (lane_id() == 0) best[threadIdx.x >> 6] = e;
         __syncthreads();
         all = scale_of(max(max(best[0], best[1]), max(best[2], best[3])));
@@ -187,13 +190,8 @@ __global__ __launch_bounds__(256) void k_head_copy(const T *from, uint64_t from_
                 }
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                f16 a, b, c0, d;
-                halves_of(times_power(v[2 * i], e), a, b);
-                halves_of(times_power(v[2 * i + 1], e), c0, d);
-                h[i] = bits_of(a, c0);
-                l[i] = bits_of(b, d);
-            }
+            for (int i = 0; i < 8; ++i) v[i] = times_power(v[i], e);
+            halves8(v, h, l);
             *(u32x4 *)(hi + at * 8) = h;
             if (lo) *(u32x4 *)(lo + at * 8) = l;
         }
@@ -320,27 +318,23 @@ __global__ __launch_bounds__(WAVES_M *WAVES_N * 64, 2) void k_head_logits(LogitA
 #pragma unroll
             for (uint32_t i = 0; i < P::I; ++i)
 #pragma unroll
-                for (uint32_t g = 0; g < 4; ++g) {
-                    const uint32_t o4 = 32 * i + 8 * g, v = v_lane + o4;
-                    f16 hi[4], lo[4];
-#pragma unroll
-                    for (uint32_t q = 0; q < 4; ++q) {
-                        float d = h.pull * power_of_e(z[i][j][4 * g + q] - h.lse);
-                        d -= o4 + q == aim ? h.push : 0.0f;
-                        if (none || o4 + q >= left) d = 0.0f;
-                        if (a.bias_parts) column[16 * i + 4 * g + q] += times_power(d, h.power - GRAD_TOP);
-                        halves_of(d, hi[q], lo[q]);
-                    }
-                    if (!here[j] || v - a.first >= a.grad_stride) continue;
-                    u32x2 o;
-                    o[0] = bits_of(hi[0], hi[1]);
-                    o[1] = bits_of(hi[2], hi[3]);
-                    *(u32x2 *)(a.grad[0] + t * a.grad_stride + (v - a.first)) = o;
-                    o[0] = bits_of(lo[0], lo[1]);
-                    o[1] = bits_of(lo[2], lo[3]);
-                    *(u32x2 *)(a.grad[1] + t * a.grad_stride + (v - a.first)) = o;
+                for (uint32_t r = 0; r < 16; ++r) {
+                    const uint32_t o = 32 * i + row_in_square(r);
+                    float d = h.pull * power_of_e(z[i][j][r] - h.lse);
+                    d -= o == aim ? h.push : 0.0f;
+                    if (none || o >= left) d = 0.0f;
+                    if (a.bias_parts) column[16 * i + r] += times_power(d, h.power - GRAD_TOP);
+                    z[i][j][r] = d;
                 }
         }
+        P::by_columns(lds, z, [&](uint32_t m, uint32_t n, const float (&v)[8]) {
+            const uint32_t t = t0 + n, at_v = v0 - a.first + m;
+            if (t >= a.rows || at_v >= a.grad_stride) return;
+            u32x4 hi, lo;
+            halves8(v, hi, lo);
+            *(u32x4 *)(a.grad[0] + t * a.grad_stride + at_v) = hi;
+            *(u32x4 *)(a.grad[1] + t * a.grad_stride + at_v) = lo;
+        });
         if (a.bias_parts) {
             __syncthreads();
             float(*const part)[M] = (float(*)[M])&lds;
@@ -375,33 +369,38 @@ __global__ __launch_bounds__(WAVES_M *WAVES_N * 64, 2) void k_head_logits(LogitA
     }
 }
 
-// A row's lse and loss from its tiles' maxima and sums.  `apart` lanes a row (a power of two), 256 / apart rows.
+// Two parts of a row's sum of exponentials, each a maximum and the sum relative to it.
+__device__ __forceinline__ float2 joined(float2 a, float2 b)
+{
+    const float most = max(a.x, b.x), from = most == -__builtin_inff() ? 0.0f : most;
+    return make_float2(most, a.y * power_of_e(a.x - from) + b.y * power_of_e(b.x - from));
+}
+
+// A row's lse and loss from its tiles' parts.  `apart` lanes a row (a power of two), 256 / apart rows.
 __global__ __launch_bounds__(256) void k_head_loss(const float2 *stats, const float *target_logit, Targets targets, uint32_t rows,
                                                    uint32_t tiles, uint32_t apart, float *loss, float *lse)
 {
     __shared__ float2 part[256];
     const uint32_t per = 256 / apart, n = threadIdx.x % per, group = threadIdx.x / per;
-    const uint32_t t = blockIdx.x * per + n;
-    float most = -__builtin_inff(), sum = 0.0f;
-    if (t < rows) {
-        for (uint32_t i = group; i < tiles; i += apart) {
-            const float2 s = stats[(uint64_t)i * rows + t];
-            const float top = max(most, s.x), from = top == -__builtin_inff() ? 0.0f : top;
-            sum = sum * power_of_e(most - from) + s.y * power_of_e(s.x - from);
-            most = top;
-        }
+    const uint32_t t = blockIdx.x * per + n, row = min(t, rows - 1u);
+    float2 all = make_float2(-__builtin_inff(), 0.0f);
+    for (uint32_t i = group; i < tiles; i += 4 * apart) {
+        float2 s[4];
+#pragma unroll
+        for (uint32_t k = 0; k < 4; ++k) s[k] = stats[(uint64_t)min(i + k * apart, tiles - 1u) * rows + row];
+#pragma unroll
+        for (uint32_t k = 0; k < 4; ++k)
+            if (i + k * apart < tiles) all = joined(all, s[k]);
     }
-    part[threadIdx.x] = make_float2(most, sum);
-    __syncthreads();
+    part[threadIdx.x] = all;
+    for (uint32_t by = apart / 2; by; by >>= 1) {
+        __syncthreads();
+        if (group < by) part[threadIdx.x] = joined(part[threadIdx.x], part[threadIdx.x + by * per]);
+    }
     if (group || t >= rows) return;
-    for (uint32_t i = 1; i < apart; ++i) {
-        const float2 s = part[i * per + n];
-        const float top = max(most, s.x), from = top == -__builtin_inff() ? 0.0f : top;
-        sum = sum * power_of_e(most - from) + s.y * power_of_e(s.x - from);
-        most = top;
-    }
-    const float l = most == -__builtin_inff() && sum == 0.0f ? most : most + logf(sum);
-    if (lse) lse[t] = l;
+    all = part[threadIdx.x];
+    const float l = all.x == -__builtin_inff() && all.y == 0.0f ? all.x : all.x + logf(all.y);
+    lse[t] = l;
     if (loss) loss[t] = target_of(targets, t) < targets.vocab ? l - target_logit[t] : 0.0f;
 }
 
@@ -434,21 +433,20 @@ __global__ __launch_bounds__(WAVES_M *WAVES_N * 64, 2) void k_head_product(Gradi
     P::run(lds, a.a, a.b, tile_m * M, tile_n * N, first, end, a.kind, s);
     float *const out = a.out + (a.whole ? 0u : (uint64_t)split * a.m * a.out_stride);
     const int e = a.whole ? -GRAD_TOP - a.scales->x : 0;
+    float old[P::PASSES][8];
+    P::by_rows(lds, s, [&](uint32_t p, uint32_t row, uint32_t col) {
+        const uint32_t m = tile_m * M + row, n = tile_n * N + col, count = m < a.m ? live8(n, a.n) : 0u;
+        if (a.add && count) load8_f32(out + m * a.out_stride + n, count, old[p]);
+    }, [&](uint32_t p, uint32_t row, uint32_t col, float (&v)[8]) {
+        const uint32_t m = tile_m * M + row, n = tile_n * N + col, count = m < a.m ? live8(n, a.n) : 0u;
+        if (count == 0) return;
 #pragma unroll
-    for (uint32_t j = 0; j < P::J; ++j) {
-        const uint32_t n = tile_n * N + P::wave_n() + 32 * j + (lane_id() & 31u);
-        if (n >= a.n) continue;
-#pragma unroll
-        for (uint32_t i = 0; i < P::I; ++i)
-#pragma unroll
-            for (uint32_t r = 0; r < 16; ++r) {
-                const uint32_t m = tile_m * M + P::wave_m() + 32 * i + square_row(r);
-                if (m >= a.m) continue;
-                float *const p = out + m * a.out_stride + n;
-                const float v = times_power(s[i][j][r], e);
-                *p = a.add ? *p + v : v;
-            }
-    }
+        for (int k = 0; k < 8; ++k) {
+            v[k] = times_power(v[k], e);
+            if (a.add) v[k] += old[p][k];
+        }
+        store8(out + m * a.out_stride, n, count, v);
+    });
 }
 
 // dx: the splits' sums, times the row's power, W's taken off.

@@ -125,6 +125,14 @@ __global__ __launch_bounds__(256) void k_ortho_load(Matrices in, uint32_t rows, 
     }
 }
 
+__device__ __forceinline__ void put_halves(const Halves &to, uint64_t at, const float (&v)[8])
+{
+    u32x4 hi, lo;
+    halves8(v, hi, lo);
+    *(u32x4 *)(to.hi + at) = hi;
+    if (to.lo) *(u32x4 *)(to.lo + at) = lo;
+}
+
 struct SquareArgs {
     Halves x;                // both operands: rows of it by rows of it
     uint32_t depth, kind;
@@ -153,64 +161,40 @@ __global__ __launch_bounds__(WAVES_M *WAVES_N * 64, 2) void k_ortho_square(Squar
     const Side side = {{a.x.hi + which * a.x.size, a.x.lo ? a.x.lo + which * a.x.size : nullptr}, a.x.stride, a.size};
     typename P::Sums s;
     P::run(lds, side, side, tile_m * M, tile_n * M, 0, a.depth, a.kind, s);
-    const uint32_t half = lane_id() >> 5;
-    const uint64_t base = which * a.out.size;
+    const uint64_t base = which * a.out.size, from = which * a.gram.size;
     const int power = -12 - (a.log2_norm ? 2 * lift_of(a.log2_norm[which], a.growth) : 0);
+    u32x4 gram_hi[P::PASSES], gram_lo[P::PASSES];
+    // (the result's columns are a multiple of eight, those beyond its rows zeros)
+    P::by_rows(lds, s, [&](uint32_t p, uint32_t row, uint32_t col) {
+        if constexpr (POLY) {
+            const uint32_t m = tile_m * M + row, n = tile_n * M + col;
+            const u32x4 none = {0, 0, 0, 0};
+            gram_hi[p] = gram_lo[p] = none;
+            if (m < a.size && n < a.gram.stride) {
+                gram_hi[p] = *(const u32x4 *)(a.gram.hi + from + m * a.gram.stride + n);
+                if (a.gram.lo) gram_lo[p] = *(const u32x4 *)(a.gram.lo + from + m * a.gram.stride + n);
+            }
+        }
+    }, [&](uint32_t p, uint32_t row, uint32_t col, float (&v)[8], float *back) {
+        const uint32_t m = tile_m * M + row, n = tile_n * M + col;
 #pragma unroll
-    for (uint32_t j = 0; j < P::J; ++j) {
-        const uint32_t n = tile_n * M + P::wave_n() + 32 * j + (lane_id() & 31u);
-        if (n >= a.out.stride) continue;
-#pragma unroll
-        for (uint32_t i = 0; i < P::I; ++i)
-#pragma unroll
-            for (uint32_t g = 0; g < 4; ++g) {
-                const uint32_t m = tile_m * M + P::wave_m() + 32 * i + 8 * g + 4 * half;
-                if (m >= a.out.stride) continue;
-                float v[4];
-#pragma unroll
-                for (uint32_t q = 0; q < 4; ++q) v[q] = times_power(s[i][j][4 * g + q], power);
-                if constexpr (POLY) {
-                    u32x2 hi = {0, 0}, lo = {0, 0};
-                    const uint64_t from = which * a.gram.size + n * a.gram.stride + m;
-                    if (n < a.size) {
-                        hi = *(const u32x2 *)(a.gram.hi + from);
-                        if (a.gram.lo) lo = *(const u32x2 *)(a.gram.lo + from);
-                    }
-#pragma unroll
-                    for (uint32_t q = 0; q < 4; ++q) {
-                        const float gram = value_of((uint16_t)(hi[q >> 1] >> (16 * (q & 1)))) + value_of((uint16_t)(lo[q >> 1] >> (16 * (q & 1))));
-                        v[q] = a.b * gram + a.c * v[q];
-                        if (m + q == n) {
-                            if (n < a.size) a.diagonal[which * a.size + n] = a.a + v[q] * LEFT;
-                            v[q] = 0.0f;
-                        }
-                    }
-                }
-                f16 hi[4], lo[4];
-#pragma unroll
-                for (uint32_t q = 0; q < 4; ++q) halves_of(v[q], hi[q], lo[q]);
-                if (n < a.size) {
-                    u32x2 o;
-                    const uint64_t to = base + n * a.out.stride + m;
-                    o[0] = bits_of(hi[0], hi[1]);
-                    o[1] = bits_of(hi[2], hi[3]);
-                    *(u32x2 *)(a.out.hi + to) = o;
-                    if (a.out.lo) {
-                        o[0] = bits_of(lo[0], lo[1]);
-                        o[1] = bits_of(lo[2], lo[3]);
-                        *(u32x2 *)(a.out.lo + to) = o;
-                    }
-                }
-                if (tile_m == tile_n) continue;
-#pragma unroll
-                for (uint32_t q = 0; q < 4; ++q) {
-                    if (m + q >= a.size) continue;
-                    const uint64_t to = base + (m + q) * a.out.stride + n;
-                    a.out.hi[to] = half_bits(hi[q]);
-                    if (a.out.lo) a.out.lo[to] = half_bits(lo[q]);
+        for (uint32_t k = 0; k < 8; ++k) {
+            v[k] = times_power(v[k], power);
+            if constexpr (POLY) {
+                const float gram = value_of((uint16_t)(gram_hi[p][k >> 1] >> (16 * (k & 1)))) + value_of((uint16_t)(gram_lo[p][k >> 1] >> (16 * (k & 1))));
+                v[k] = a.b * gram + a.c * v[k];
+                if (n + k == m) {
+                    if (m < a.size) a.diagonal[which * a.size + m] = a.a + v[k] * LEFT;
+                    v[k] = 0.0f;
                 }
             }
-    }
+            back[k] = v[k];
+        }
+        if (m < a.size && n < a.out.stride) put_halves(a.out, base + m * a.out.stride + n, v);
+    }, [&](uint32_t row, uint32_t col, const float (&v)[8]) {      // the other side of the diagonal
+        const uint32_t m = tile_m * M + row, n = tile_n * M + col;
+        if (tile_m != tile_n && n < a.size && m < a.out.stride) put_halves(a.out, base + n * a.out.stride + m, v);
+    });
 }
 
 struct StepArgs {
@@ -221,20 +205,23 @@ struct StepArgs {
     const float *log2_norm;
     float growth, next_growth;
     // the last step
-    uint32_t turned, add;
-    int32_t out_type;
+    uint32_t add;
     float scale;
-    Matrices out;
 };
 
-template <class T> __device__ __forceinline__ void put(T *p, float v, uint32_t add)
+template <class T> __device__ __forceinline__ void put8(T *p, uint32_t count, float (&v)[8], float scale, uint32_t add)
 {
-    *p = from_float<T>(add ? to_float(*p) + v : v);
+    float old[8];
+    if (add) unpack8(load8((const T *)p, count), old);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = add ? old[k] + v[k] * scale : v[k] * scale;
+    store8(p, 0, count, v);
 }
 
 // X of the next step: its rows times the polynomial's diagonal, plus the product of the rest with it.
-template <uint32_t M, uint32_t N, uint32_t WAVES_M, uint32_t WAVES_N>
-__global__ __launch_bounds__(WAVES_M *WAVES_N * 64, 2) void k_ortho_step(StepArgs a)
+// T: the result's type in the last step, void in the others; TURNED: the result's rows are X's columns.
+template <uint32_t M, uint32_t N, uint32_t WAVES_M, uint32_t WAVES_N, class T, bool TURNED>
+__global__ __launch_bounds__(WAVES_M *WAVES_N * 64, 2) void k_ortho_step(StepArgs a, Matrices results)
 {
     typedef Product<f16, M, N, WAVES_M, WAVES_N, false, true> P;
     __shared__ __attribute__((aligned(16))) typename P::Lds lds;
@@ -248,36 +235,51 @@ __global__ __launch_bounds__(WAVES_M *WAVES_N * 64, 2) void k_ortho_step(StepArg
     P::run(lds, left, right, tile_m * M, tile_n * N, 0, a.rows, a.kind, s);
     // from how this X is held to how the next one is, or to the result
     const int lift = lift_of(a.log2_norm[which], a.growth);
-    const int power = a.next.hi ? lift_of(a.log2_norm[which], a.next_growth) - lift : -12 - lift;
+    const int power = __is_same(T, void) ? lift_of(a.log2_norm[which], a.next_growth) - lift : -12 - lift;
+    // a row of X's next, or of the result's
+    u32x4 hi[P::PASSES], lo[P::PASSES];
+    float d[P::PASSES];
+    auto look = [&](uint32_t p, uint32_t row, uint32_t col) {
+        const uint32_t m = tile_m * M + row, n = tile_n * N + col;
+        const bool in = m < a.rows && n < a.x.stride;
+        const uint64_t at = in ? m * a.x.stride + n : 0;
+        hi[p] = *(const u32x4 *)(x_hi + at);
+        lo[p] = *(const u32x4 *)(x_lo + at);
+        d[p] = a.diagonal[which * a.rows + (in ? m : 0)];
+    };
+    auto next = [&](uint32_t p, float (&v)[8]) {
 #pragma unroll
-    for (uint32_t i = 0; i < P::I; ++i)
-#pragma unroll
-        for (uint32_t r = 0; r < 16; ++r) {
-            const uint32_t m = tile_m * M + P::wave_m() + 32 * i + square_row(r);
-            if (m >= a.rows) continue;
-            const float d = a.diagonal[which * a.rows + m];
-#pragma unroll
-            for (uint32_t j = 0; j < P::J; ++j) {
-                const uint32_t n = tile_n * N + P::wave_n() + 32 * j + (lane_id() & 31u);
-                if (n >= a.x.stride) continue;
-                const uint64_t here = m * a.x.stride + n;
-                const float x = value_of(x_hi[here]) + value_of(x_lo[here]);
-                const float v = times_power(__builtin_fmaf(d, x, s[i][j][r] * LEFT), power);
-                if (a.next.hi) {
-                    f16 hi, lo;
-                    halves_of(v, hi, lo);
-                    a.next.hi[which * a.next.size + here] = half_bits(hi);
-                    a.next.lo[which * a.next.size + here] = half_bits(lo);
-                } else if (n < a.cols) {
-                    const uint64_t stride = a.out.stride[which], to = a.turned ? n * stride + m : m * stride + n;
-                    const float w = v * a.scale;
-                    void *const out = (void *)a.out.data[which];
-                    if (a.out_type == DGS_F32) put((float *)out + to, w, a.add);
-                    else if (a.out_type == DGS_F16) put((f16 *)out + to, w, a.add);
-                    else put((bf16 *)out + to, w, a.add);
-                }
-            }
+        for (uint32_t k = 0; k < 8; ++k) {
+            const float x = value_of((uint16_t)(hi[p][k >> 1] >> (16 * (k & 1)))) + value_of((uint16_t)(lo[p][k >> 1] >> (16 * (k & 1))));
+            v[k] = times_power(__builtin_fmaf(d[p], x, v[k] * LEFT), power);
         }
+    };
+    if constexpr (__is_same(T, void)) {
+        P::by_rows(lds, s, look, [&](uint32_t p, uint32_t row, uint32_t col, float (&v)[8]) {
+            const uint32_t m = tile_m * M + row, n = tile_n * N + col;
+            next(p, v);
+            if (m < a.rows && n < a.x.stride) put_halves(a.next, which * a.next.size + m * a.x.stride + n, v);
+        });
+    } else {
+        T *const out = (T *)results.data[which];
+        const uint64_t stride = results.stride[which];
+        if constexpr (TURNED) {
+            P::by_rows(lds, s, look, [&](uint32_t p, uint32_t, uint32_t, float (&v)[8], float *back) {
+                next(p, v);
+#pragma unroll
+                for (uint32_t k = 0; k < 8; ++k) back[k] = v[k];
+            }, [&](uint32_t row, uint32_t col, float (&v)[8]) {
+                const uint32_t m = tile_m * M + row, n = tile_n * N + col;
+                if (m < a.rows && n < a.cols) put8(out + n * stride + m, live8(m, a.rows), v, a.scale, a.add);
+            });
+        } else {
+            P::by_rows(lds, s, look, [&](uint32_t p, uint32_t row, uint32_t col, float (&v)[8]) {
+                const uint32_t m = tile_m * M + row, n = tile_n * N + col;
+                next(p, v);
+                if (m < a.rows && n < a.cols) put8(out + m * stride + n, live8(n, a.cols), v, a.scale, a.add);
+            });
+        }
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -334,6 +336,17 @@ template <class T> static void load_matrices(const Matrices &in, const dgs_ortho
     hipLaunchKernelGGL(k_ortho_norm<T>, dim3(NORM_PARTS, count), dim3(256), 0, st, in, p.rows, p.cols, o.norm);
     hipLaunchKernelGGL(k_ortho_load<T>, dim3((p.cols + 63) / 64 * ((p.rows + 63) / 64), count), dim3(256), 0, st, in, p.rows, p.cols,
                        (uint32_t)o.turned, (const double *)o.norm, p.eps, o.x[0], o.log2_norm);
+}
+
+template <class T, bool TURNED> static void launch_step(const StepArgs &s, const Matrices &out, bool large, dim3 grid, hipStream_t st)
+{
+    if (large) hipLaunchKernelGGL((k_ortho_step<256, 256, 2, 4, T, TURNED>), grid, dim3(512), 0, st, s, out);
+    else hipLaunchKernelGGL((k_ortho_step<128, 128, 2, 2, T, TURNED>), grid, dim3(256), 0, st, s, out);
+}
+template <class T> static void launch_last(const StepArgs &s, const Matrices &out, bool turned, bool large, dim3 grid, hipStream_t st)
+{
+    if (turned) launch_step<T, true>(s, out, large, grid, st);
+    else launch_step<T, false>(s, out, large, grid, st);
 }
 
 }  // namespace dgs
@@ -418,17 +431,16 @@ extern "C" int dgs_orthogonalise(const dgs_orthogonalise_args *args, void *hip_s
             s.log2_norm = o.log2_norm;
             s.growth = (float)step * grows;
             s.next_growth = s.growth + grows;
-            s.turned = o.turned;
             s.add = p.accumulate != 0;
-            s.out_type = p.out_type;
             s.scale = p.scale;
-            s.out = out;
             const uint32_t size = large_step ? 256 : 128;
             s.m_tiles = tiles(o.rows, size);
             s.n_tiles = tiles(o.cols, size);
             const dim3 all(s.m_tiles * s.n_tiles * count);
-            if (large_step) hipLaunchKernelGGL((k_ortho_step<256, 256, 2, 4>), all, dim3(512), 0, st, s);
-            else hipLaunchKernelGGL((k_ortho_step<128, 128, 2, 2>), all, dim3(256), 0, st, s);
+            if (step + 1 < p.steps) launch_step<void, false>(s, out, large_step, all, st);
+            else if (p.out_type == DGS_F32) launch_last<float>(s, out, o.turned, large_step, all, st);
+            else if (p.out_type == DGS_F16) launch_last<f16>(s, out, o.turned, large_step, all, st);
+            else launch_last<bf16>(s, out, o.turned, large_step, all, st);
         }
     }
     return launched();

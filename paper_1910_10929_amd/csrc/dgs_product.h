@@ -127,6 +127,10 @@ template <uint32_t WIDTH, bool TURNED, uint32_t WAVES> struct Staged {
     }
 };
 
+// Row of sum r of a lane in a 32 x 32 square, its column being lane % 32: row_in_square(r), plus 4 in the upper 32 lanes.
+__device__ __forceinline__ constexpr uint32_t row_in_square(uint32_t r) { return (r & 3u) + 8 * (r >> 2); }
+__device__ __forceinline__ uint32_t square_row(uint32_t r) { return row_in_square(r) + 4 * (lane_id() >> 5); }
+
 // The pairs of parts that a product goes over, two bits each: the first operand's part, and twice the second's.
 constexpr uint32_t ONE_PAIR = 0x1, FIRST_IN_TWO = 0x2, BOTH_IN_TWO = 0x3;
 __device__ __forceinline__ uint32_t pairs_of(uint32_t kind) { return kind == ONE_PAIR ? 1u : kind == FIRST_IN_TWO ? 2u : 3u; }
@@ -135,8 +139,14 @@ template <class E, uint32_t M, uint32_t N, uint32_t WAVES_M, uint32_t WAVES_N, b
     static constexpr uint32_t WAVES = WAVES_M * WAVES_N, THREADS = WAVES * 64, I = M / 32 / WAVES_M, J = N / 32 / WAVES_N;
     typedef Staged<M, TURN_A, WAVES> A;
     typedef Staged<N, TURN_B, WAVES> B;
-    struct Lds {
-        uint16_t a[2][M * PRODUCT_STEP], b[2][N * PRODUCT_STEP];
+    // Behind the sums, LDS takes a part of them from each wavefront (by_rows, by_columns).
+    static constexpr uint32_t ABOVE = I < 2 ? 1 : 2, ROW_PITCH = 32 * J + 4, COLUMN_PITCH = 32 * ABOVE + 4;
+    static constexpr uint32_t PART = 32 * ROW_PITCH > 32 * J * COLUMN_PITCH ? 32 * ROW_PITCH : 32 * J * COLUMN_PITCH;
+    union Lds {
+        struct {
+            uint16_t a[2][M * PRODUCT_STEP], b[2][N * PRODUCT_STEP];
+        };
+        float part[WAVES][PART];
     };
     typedef f32x16 Sums[I][J];
 
@@ -193,11 +203,134 @@ template <class E, uint32_t M, uint32_t N, uint32_t WAVES_M, uint32_t WAVES_N, b
             }
         }
     }
-};
 
-// Row of sum r of a lane in a 32 x 32 square, its column being lane % 32: row_in_square(r), plus 4 in the upper 32 lanes.
-__device__ __forceinline__ constexpr uint32_t row_in_square(uint32_t r) { return (r & 3u) + 8 * (r >> 2); }
-__device__ __forceinline__ uint32_t square_row(uint32_t r) { return row_in_square(r) + 4 * (lane_id() >> 5); }
+    // The lanes hold a column of a square each, four rows together.  Memory wants rows: the sums go through LDS, a wavefront's own
+    // part of it, and come back as eight values of a row.  look(p, m, n) for every p first (what has to be loaded, so that the loads are
+    // in flight together), then take(p, m, n, v), m and n in the tile.
+    static constexpr uint32_t PASSES = 2 * J;      // of by_rows, 32 rows
+    template <class Look, class Take> static __device__ __forceinline__ void by_rows(Lds &lds, const Sums &sums, Look look, Take take)
+    {
+        const uint32_t lane = lane_id(), wave = uniform(threadIdx.x >> 6), wm = wave_m(), wn = wave_n();
+        float *const mine = lds.part[wave];
+        __syncthreads();      // nobody reads operands any more
+#pragma unroll
+        for (uint32_t i = 0; i < I; ++i) {
+#pragma unroll
+            for (uint32_t p = 0; p < PASSES; ++p) {
+                const uint32_t at = p * 64 + lane;
+                look(p, wm + 32 * i + at / (4 * J), wn + at % (4 * J) * 8);
+            }
+#pragma unroll
+            for (uint32_t j = 0; j < J; ++j)
+#pragma unroll
+                for (uint32_t r = 0; r < 16; ++r) mine[square_row(r) * ROW_PITCH + 32 * j + (lane & 31u)] = sums[i][j][r];
+            meet();
+#pragma unroll
+            for (uint32_t p = 0; p < PASSES; ++p) {
+                const uint32_t at = p * 64 + lane, row = at / (4 * J), c = at % (4 * J) * 8;
+                float v[8];
+#pragma unroll
+                for (uint32_t k = 0; k < 2; ++k) {
+                    const f32x4 w = *(const f32x4 *)(mine + row * ROW_PITCH + c + 4 * k);
+                    v[4 * k] = w.x; v[4 * k + 1] = w.y; v[4 * k + 2] = w.z; v[4 * k + 3] = w.w;
+                }
+                take(p, wm + 32 * i + row, wn + c, v);
+            }
+            meet();
+        }
+    }
+    // The same where the values are wanted by columns too: take(p, m, n, v, back) leaves at `back` what turn(m, n, v) gets as eight values
+    // of a column, m to m + 7.
+    template <class Look, class Take, class Turn> static __device__ __forceinline__ void by_rows(Lds &lds, const Sums &sums, Look look, Take take, Turn turn)
+    {
+        const uint32_t lane = lane_id(), wave = uniform(threadIdx.x >> 6), wm = wave_m(), wn = wave_n();
+        float *const mine = lds.part[wave];
+        __syncthreads();
+#pragma unroll
+        for (uint32_t i = 0; i < I; ++i) {
+#pragma unroll
+            for (uint32_t p = 0; p < PASSES; ++p) {
+                const uint32_t at = p * 64 + lane;
+                look(p, wm + 32 * i + at / (4 * J), wn + at % (4 * J) * 8);
+            }
+#pragma unroll
+            for (uint32_t j = 0; j < J; ++j)
+#pragma unroll
+                for (uint32_t r = 0; r < 16; ++r) mine[square_row(r) * ROW_PITCH + 32 * j + (lane & 31u)] = sums[i][j][r];
+            meet();
+#pragma unroll
+            for (uint32_t p = 0; p < PASSES; ++p) {
+                const uint32_t at = p * 64 + lane, row = at / (4 * J), c = at % (4 * J) * 8;
+                float v[8], back[8];
+                float *const here = mine + row * ROW_PITCH + c;
+#pragma unroll
+                for (uint32_t k = 0; k < 2; ++k) {
+                    const f32x4 w = *(const f32x4 *)(here + 4 * k);
+                    v[4 * k] = w.x; v[4 * k + 1] = w.y; v[4 * k + 2] = w.z; v[4 * k + 3] = w.w;
+                }
+                take(p, wm + 32 * i + row, wn + c, v, back);
+#pragma unroll
+                for (uint32_t k = 0; k < 2; ++k) {
+                    f32x4 w;
+                    w.x = back[4 * k]; w.y = back[4 * k + 1]; w.z = back[4 * k + 2]; w.w = back[4 * k + 3];
+                    *(f32x4 *)(here + 4 * k) = w;
+                }
+            }
+            meet();
+#pragma unroll
+            for (uint32_t p = 0; p < PASSES; ++p) {
+                // four lanes a column, so that memory gets 32 values of it together
+                const uint32_t at = p * 64 + lane, col = at >> 2, row = (at & 3u) * 8;
+                float v[8];
+#pragma unroll
+                for (uint32_t k = 0; k < 8; ++k) v[k] = mine[(row + k) * ROW_PITCH + col];
+                turn(wm + 32 * i + row, wn + col, v);
+            }
+            meet();
+        }
+    }
+    // Eight values of a column, m to m + 7, in the same way: take(m, n, v).
+    template <class Take> static __device__ __forceinline__ void by_columns(Lds &lds, const Sums &sums, Take take)
+    {
+        const uint32_t lane = lane_id(), wave = uniform(threadIdx.x >> 6), wm = wave_m(), wn = wave_n();
+        float *const mine = lds.part[wave];
+        __syncthreads();
+#pragma unroll
+        for (uint32_t i = 0; i < I; i += ABOVE) {
+#pragma unroll
+            for (uint32_t above = 0; above < ABOVE; ++above)
+#pragma unroll
+                for (uint32_t j = 0; j < J; ++j)
+#pragma unroll
+                    for (uint32_t g = 0; g < 4; ++g) {
+                        f32x4 w;
+                        w.x = sums[i + above][j][4 * g]; w.y = sums[i + above][j][4 * g + 1];
+                        w.z = sums[i + above][j][4 * g + 2]; w.w = sums[i + above][j][4 * g + 3];
+                        *(f32x4 *)(mine + (32 * j + (lane & 31u)) * COLUMN_PITCH + 32 * above + square_row(4 * g)) = w;
+                    }
+            meet();
+#pragma unroll
+            for (uint32_t p = 0; p < 2 * J * ABOVE; ++p) {
+                const uint32_t at = p * 64 + lane, n = at / (4 * ABOVE), m = at % (4 * ABOVE) * 8;
+                float v[8];
+#pragma unroll
+                for (uint32_t k = 0; k < 2; ++k) {
+                    const f32x4 w = *(const f32x4 *)(mine + n * COLUMN_PITCH + m + 4 * k);
+                    v[4 * k] = w.x; v[4 * k + 1] = w.y; v[4 * k + 2] = w.z; v[4 * k + 3] = w.w;
+                }
+                take(wm + 32 * i + m, wn + n, v);
+            }
+            meet();
+        }
+    }
+    // What lanes of a wavefront have written to LDS is there for the others.
+    static __device__ __forceinline__ void meet()
+    {
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    }
+};
 
 // Workgroup `block` of `total`, of which neighbours go to different dies: every die gets a run of the tiles.
 __device__ __forceinline__ uint32_t tile_of_block(uint32_t block, uint32_t total)
@@ -218,6 +351,19 @@ __device__ __forceinline__ uint32_t bits_of(f16 a, f16 b)
     __builtin_memcpy(&x, &a, 2);
     __builtin_memcpy(&y, &b, 2);
     return x | (uint32_t)y << 16;
+}
+
+// Eight values as halves, in one part or two.
+__device__ __forceinline__ void halves8(const float (&v)[8], u32x4 &hi, u32x4 &lo)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f16 a, b, c, d;
+        halves_of(v[2 * i], a, b);
+        halves_of(v[2 * i + 1], c, d);
+        hi[i] = bits_of(a, c);
+        lo[i] = bits_of(b, d);
+    }
 }
 
 // Sections of a workspace, one after another, each from a multiple of 256 bytes behind its start on.  (Nothing is reached through
