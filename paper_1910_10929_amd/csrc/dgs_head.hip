@@ -150,51 +150,73 @@ enum CopyKind {
     COPY_ALL,        // ... all by the same power
 };
 
-// An operand in halves (in one part or two), scaled.  Eight columns a lane; columns up to the next multiple of eight are zeros.
-template <class T, int KIND>
-__global__ __launch_bounds__(256) void k_head_copy(const T *from, uint64_t from_stride, uint32_t rows, uint32_t cols, uint16_t *hi,
-                                                   uint16_t *lo, uint32_t pieces, Ranges ranges, const HeadRow *row_info, Scales *scales)
+struct CopyJob {
+    const void *from;
+    uint64_t stride;
+    uint16_t *hi, *lo;      // lo: absent where one part is wanted
+    uint32_t rows, blocks;
+    int32_t kind;
+};
+constexpr int COPY_JOBS = 4;
+struct CopyJobs {
+    CopyJob job[COPY_JOBS];
+    uint32_t count, cols, pieces;      // of every matrix: columns, and eights of them
+};
+
+// Operands in the form that the products read.  Eight columns a lane; columns up to the next multiple of eight are zeros.  Bound by memory:
+// a bfloat16 W of 32768 x 4096 into halves, 537 MB, 85 us (6.3 TB/s, part of it from cache).
+template <class T>
+__global__ __launch_bounds__(256) void k_head_copy(CopyJobs jobs, Ranges ranges, const HeadRow *row_info, Scales *scales)
 {
+    __shared__ int best[4];
+    uint32_t block = blockIdx.x, which = 0;
+    CopyJob j = jobs.job[0];
+#pragma unroll
+    for (int i = 1; i < COPY_JOBS; ++i)
+        if (which + 1 < jobs.count && block >= j.blocks) {
+            block -= j.blocks;
+            j = jobs.job[i];
+            which = i;
+        }
     int all = 0;
-    if constexpr (KIND == COPY_WEIGHED || KIND == COPY_ALL) {
-        __shared__ int best[4];
-        const int *const r = KIND == COPY_ALL ? ranges.w : ranges.x;
+    if (j.kind == COPY_WEIGHED || j.kind == COPY_ALL) {
+        const int *const r = j.kind == COPY_ALL ? ranges.w : ranges.x;
         int most = NO_RANGE;
 #pragma unroll
         for (uint32_t k = 0; k < RANGE_BLOCKS; k += 256) most = max(most, r[k + threadIdx.x]);
-        const int e = wave_max(most);
-        if (lane_id() == 0) best[threadIdx.x >> 6] = e;
+        most = wave_max(most);
+        if (lane_id() == 0) best[threadIdx.x >> 6] = most;
         __syncthreads();
         all = scale_of(max(max(best[0], best[1]), max(best[2], best[3])));
-        if (blockIdx.x == 0 && threadIdx.x == 0) (KIND == COPY_ALL ? scales->w : scales->x) = all;
+        if (block == 0 && threadIdx.x == 0) (j.kind == COPY_ALL ? scales->w : scales->x) = all;
     }
-    const uint64_t step = (uint64_t)gridDim.x * 256, end = (uint64_t)rows * pieces;
-    for (uint64_t at = (uint64_t)blockIdx.x * 256 + threadIdx.x; at < end; at += step) {
-        const uint32_t row = (uint32_t)(at / pieces), c = (uint32_t)(at - (uint64_t)row * pieces) * 8;
-        const Raw8<T> raw = load8(from + row * from_stride + c, live8(c, cols));
+    const uint64_t step = (uint64_t)j.blocks * 256, end = (uint64_t)j.rows * jobs.pieces;
+    for (uint64_t at = (uint64_t)block * 256 + threadIdx.x; at < end; at += step) {
+        const uint32_t row = (uint32_t)(at / jobs.pieces), c = (uint32_t)(at - (uint64_t)row * jobs.pieces) * 8;
+        const Raw8<T> raw = load8((const T *)j.from + row * j.stride + c, live8(c, jobs.cols));
         u32x4 h, l;
-        if constexpr (KIND == COPY_PLAIN) {
+        if (j.kind == COPY_PLAIN) {
             __builtin_memcpy(&h, &raw, 16);
-            *(u32x4 *)(hi + at * 8) = h;
-        } else {
-            int e = all;
-            float v[8];
-            unpack8(raw, v);
-            if constexpr (KIND == COPY_ROWS) e = scale_of(ranges.row[row]);
-            if constexpr (KIND == COPY_WEIGHED) {
-                const HeadRow h = row_info[row];
-                e = all + h.power;
-                if (nothing_arrives(h)) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) v[i] = 0.0f;
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = times_power(v[i], e);
-            halves8(v, h, l);
-            *(u32x4 *)(hi + at * 8) = h;
-            if (lo) *(u32x4 *)(lo + at * 8) = l;
+            *(u32x4 *)(j.hi + at * 8) = h;
+            continue;
         }
+        int e = all;
+        float v[8];
+        unpack8(raw, v);
+        if (j.kind == COPY_ROWS) e = scale_of(ranges.row[row]);
+        if (j.kind == COPY_WEIGHED) {
+            const HeadRow r = row_info[row];
+            e = all + r.power;
+            if (nothing_arrives(r)) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = 0.0f;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = times_power(v[i], e);
+        halves8(v, h, l);
+        *(u32x4 *)(j.hi + at * 8) = h;
+        if (j.lo) *(u32x4 *)(j.lo + at * 8) = l;
     }
 }
 
@@ -222,13 +244,13 @@ struct LogitArgs {
 };
 
 // Entries (m) and rows (n) of a tile.
-template <class E, uint32_t M, uint32_t N, uint32_t WAVES_M, uint32_t WAVES_N, bool BACK>
-__global__ __launch_bounds__(WAVES_M *WAVES_N * 64, 2) void k_head_logits(LogitArgs a)
+template <class E, uint32_t M, uint32_t N, uint32_t WAVES_M, uint32_t WAVES_N, uint32_t STAGES, bool BACK>
+__global__ __launch_bounds__(WAVES_M *WAVES_N * 64, WAVES_M *WAVES_N > 4 || STAGES < 4 ? 2 : 1) void k_head_logits(LogitArgs a)
 {
-    typedef Product<E, M, N, WAVES_M, WAVES_N, false, false> P;
+    typedef Product<E, M, N, WAVES_M, WAVES_N, false, false, STAGES, M == 256 && N == 128 ? 32 : PRODUCT_STEP> P;
     __shared__ __attribute__((aligned(16))) typename P::Lds lds;
-    const uint32_t at = tile_of_block(blockIdx.x, gridDim.x);
-    const uint32_t tile_v = at / a.t_tiles, tile_t = at - tile_v * a.t_tiles;
+    const TilePlace place = place_of_tile(tile_of_block(blockIdx.x, gridDim.x), a.v_tiles, a.t_tiles);
+    const uint32_t tile_v = place.m, tile_t = place.n;
     const uint32_t v0 = a.first + tile_v * M, t0 = tile_t * N;
     typename P::Sums z;
     P::run(lds, a.w, a.x, v0, t0, 0, a.cols, a.kind, z);
@@ -420,14 +442,15 @@ struct GradientArgs {
 };
 
 // TURN_A: the first operand's k lies outside.  (The second's always does.)
-template <uint32_t M, uint32_t N, uint32_t WAVES_M, uint32_t WAVES_N, bool TURN_A>
-__global__ __launch_bounds__(WAVES_M *WAVES_N * 64, 2) void k_head_product(GradientArgs a)
+template <uint32_t M, uint32_t N, uint32_t WAVES_M, uint32_t WAVES_N, uint32_t STAGES, bool TURN_A>
+__global__ __launch_bounds__(WAVES_M *WAVES_N * 64, WAVES_M *WAVES_N > 4 || STAGES < 4 ? 2 : 1) void k_head_product(GradientArgs a)
 {
-    typedef Product<f16, M, N, WAVES_M, WAVES_N, TURN_A, true> P;
+    typedef Product<f16, M, N, WAVES_M, WAVES_N, TURN_A, true, STAGES, M == 256 && N == 128 ? 32 : PRODUCT_STEP> P;
     __shared__ __attribute__((aligned(16))) typename P::Lds lds;
     const uint32_t at = tile_of_block(blockIdx.x, gridDim.x), tiles = a.m_tiles * a.n_tiles;
-    const uint32_t split = at / tiles, tile = at - split * tiles;
-    const uint32_t tile_m = tile / a.n_tiles, tile_n = tile - tile_m * a.n_tiles;
+    const uint32_t split = at / tiles;
+    const TilePlace place = place_of_tile(at - split * tiles, a.m_tiles, a.n_tiles);
+    const uint32_t tile_m = place.m, tile_n = place.n;
     const uint32_t first = min(split * a.split_depth, a.depth), end = min(first + a.split_depth, a.depth);
     typename P::Sums s;
     P::run(lds, a.a, a.b, tile_m * M, tile_n * N, first, end, a.kind, s);
@@ -486,13 +509,24 @@ __global__ __launch_bounds__(256) void k_head_dweight(const float *sums, uint32_
     *p = add ? *p + v : v;
 }
 
+// dbias: the tiles' sums, 64 entries to a workgroup, four lanes each.
 __global__ __launch_bounds__(256) void k_head_dbias(const float *parts, uint32_t tiles, uint64_t stride, uint32_t count, float *out,
                                                     uint32_t add)
 {
-    const uint32_t v = blockIdx.x * 256 + threadIdx.x;
-    if (v >= count) return;
+    __shared__ float sums[256];
+    const uint32_t v = blockIdx.x * 64 + (threadIdx.x & 63u), at = min(v, count - 1u);
     float s = 0.0f;
-    for (uint32_t i = 0; i < tiles; ++i) s += parts[i * stride + v];
+    for (uint32_t i = threadIdx.x >> 6; i < tiles; i += 32) {
+        float w[8];
+#pragma unroll
+        for (uint32_t k = 0; k < 8; ++k) w[k] = parts[min(i + 4 * k, tiles - 1u) * stride + at];
+#pragma unroll
+        for (uint32_t k = 0; k < 8; ++k) s += i + 4 * k < tiles ? w[k] : 0.0f;
+    }
+    sums[threadIdx.x] = s;
+    __syncthreads();
+    if (threadIdx.x >= 64 || v >= count) return;
+    s = (s + sums[threadIdx.x + 64]) + (sums[threadIdx.x + 128] + sums[threadIdx.x + 192]);
     out[v] = add ? out[v] + s : s;
 }
 
@@ -500,18 +534,41 @@ __global__ __launch_bounds__(256) void k_head_dbias(const float *parts, uint32_t
 // host side
 // ---------------------------------------------------------------------------
 
-enum { TILE_LARGE, TILE_SMALL, TILE_FEW };
+enum { TILE_FEW = PRODUCT_TILES };      // 128 entries, 32 rows
 struct TileSize { uint32_t m, n; };
-static TileSize size_of(int tile) { return tile == TILE_LARGE ? TileSize{256, 256} : tile == TILE_SMALL ? TileSize{128, 128} : TileSize{128, 32}; }
-static uint32_t tiles_of(uint32_t n, uint32_t size) { return n ? (n - 1) / size + 1 : 0; }
-static int tile_for(uint32_t m, uint32_t n)
+static TileSize size_of(int tile) { return tile == TILE_FEW ? TileSize{128, 32} : TileSize{tile_high(tile), tile_wide(tile)}; }
+static uint32_t steps_of(uint32_t depth, uint32_t kind) { return tiles_of(depth, PRODUCT_STEP) * (kind == ONE_PAIR ? 1 : kind == FIRST_IN_TWO ? 2 : 3); }
+static int logits_tile(uint32_t vocab, uint32_t rows, uint32_t steps)
 {
-#ifdef DGS_HEAD_TILE      // (a CPU build that is to reach one kind on small matrices)
-    return DGS_HEAD_TILE;
-#endif
-    return (uint64_t)tiles_of(m, 256) * tiles_of(n, 256) >= 192 ? TILE_LARGE : TILE_SMALL;
+    if (rows <= 32) return TILE_FEW;
+    float us = 0.0f;
+    return product_tile([=](uint32_t high, uint32_t wide) { return (uint64_t)tiles_of(vocab, high) * tiles_of(rows, wide); }, steps, false, us);
 }
-static int logits_tile(uint32_t vocab, uint32_t rows) { return rows <= 32 ? TILE_FEW : tile_for(vocab, rows); }
+// A gradient's product: its tile, and how many splits of the sum are added up by a launch of their own.
+struct ProductPlan {
+    int tile;
+    uint32_t splits, split_depth, kind;
+};
+static ProductPlan product_plan(uint32_t m, uint32_t n, uint32_t depth, uint32_t kind, bool tall)
+{
+    ProductPlan best = {};
+    float least = 0.0f;
+    // (at least four steps to a split; a split's sums are written and read)
+    const uint32_t steps = depth ? tiles_of(depth, PRODUCT_STEP) : 1u, most = steps / 4 > 16 ? 16 : steps / 4 < 1 ? 1 : steps / 4;
+    for (uint32_t s = 1; s <= most; ++s) {
+        const uint32_t each = (steps + s - 1) / s;
+        if ((steps + each - 1) / each != s) continue;
+        float us = 0.0f;
+        const int tile = product_tile([=](uint32_t high, uint32_t wide) { return (uint64_t)tiles_of(m, high) * tiles_of(n, wide) * s; },
+                                      steps_of(each * PRODUCT_STEP, kind), tall, us);
+        if (s > 1) us += 3.0f + (float)s * (float)m * (float)n * 8.0f / 4.5e6f;
+        if (least == 0.0f || us < least) {
+            least = us;
+            best = ProductPlan{tile, s, each * PRODUCT_STEP, kind};
+        }
+    }
+    return best;
+}
 
 constexpr uint64_t PIECE_BYTES = 1ull << 30;      // of the logits' gradient, at a time
 
@@ -520,8 +577,8 @@ struct HeadPlan {
     bool scale_x_rows, copy_x, copy_w, scale_w;      // which operands are copied, and how
     uint32_t width;                                  // columns, up to a multiple of eight
     uint32_t piece;                                  // entries at a time
-    uint32_t dx_splits, dw_splits;
-    int logits, dx_tile, dw_tile;
+    int logits;
+    ProductPlan dx, dw;
     uint64_t bytes;
     // sections
     float2 *stats;
@@ -537,14 +594,6 @@ static bool straight_ok(const dgs_matrix &m, uint32_t cols)
 {
     return cols % 8 == 0 && m.stride % 8 == 0 && aligned_to(m.data, 16);
 }
-static uint32_t splits_for(uint64_t tiles, uint32_t depth)
-{
-    uint64_t s = tiles ? 512 / tiles : 1;
-    if (s > depth / 512) s = depth / 512;
-    if (s > 16) s = 16;
-    return s < 1 ? 1u : (uint32_t)s;
-}
-
 static HeadPlan plan_of(const dgs_head_args &p, bool back)
 {
     HeadPlan h = {};
@@ -557,7 +606,7 @@ static HeadPlan plan_of(const dgs_head_args &p, bool back)
     h.scale_w = f32 || (back && p.type == DGS_BF16 && h.wants_dx);
     h.copy_x = !f32 && !straight_ok(p.x, p.cols);
     h.copy_w = !f32 && !straight_ok(p.weight, p.cols);
-    h.logits = logits_tile(p.vocab, p.rows);
+    h.logits = logits_tile(p.vocab, p.rows, steps_of(p.cols, f32 ? BOTH_IN_TWO : ONE_PAIR));
     Sections s = {(uintptr_t)p.workspace, 0};
     const uint64_t x_bytes = (uint64_t)p.rows * h.width * 2, w_bytes = (uint64_t)p.vocab * h.width * 2;
     const TileSize tile = size_of(h.logits);
@@ -591,27 +640,14 @@ static HeadPlan plan_of(const dgs_head_args &p, bool back)
         h.grad[0] = (uint16_t *)s.take(p.rows * stride * 2);
         h.grad[1] = (uint16_t *)s.take(p.rows * stride * 2);
         if (p.dbias) h.bias_parts = (float *)s.take(tiles_of(p.rows, tile.n) * stride * 4);
-        h.dx_tile = tile_for(p.rows, p.cols);
-        h.dw_tile = tile_for(h.piece, p.cols);
-        const TileSize x = size_of(h.dx_tile), w = size_of(h.dw_tile);
-        h.dx_splits = splits_for((uint64_t)tiles_of(p.rows, x.m) * tiles_of(p.cols, x.n), h.piece);
-        h.dw_splits = splits_for((uint64_t)tiles_of(h.piece, w.m) * tiles_of(p.cols, w.n), p.rows);
-        if (h.wants_dx) h.dx_sums = (float *)s.take((uint64_t)h.dx_splits * p.rows * p.cols * 4);
-        if (h.wants_dw && h.dw_splits > 1) h.dw_sums = (float *)s.take((uint64_t)h.dw_splits * h.piece * p.cols * 4);
+        h.dx = product_plan(p.rows, p.cols, h.piece, f32 ? BOTH_IN_TWO : p.type == DGS_F16 ? FIRST_IN_TWO : ONE_PAIR, false);
+        h.dw = product_plan(h.piece, p.cols, p.rows, f32 ? BOTH_IN_TWO : FIRST_IN_TWO, true);
+        if (h.wants_dx) h.dx_sums = (float *)s.take((uint64_t)h.dx.splits * p.rows * p.cols * 4);
+        if (h.wants_dw && h.dw.splits > 1) h.dw_sums = (float *)s.take((uint64_t)h.dw.splits * h.piece * p.cols * 4);
         if (h.scale_w && !f32) h.w[1] = (uint16_t *)s.take(w_bytes);      // (of bfloat16: W in half, for dx)
     }
     h.bytes = s.used ? s.used : 256;
     return h;
-}
-
-template <class T, int KIND>
-static void copy(const dgs_matrix &m, uint32_t rows, uint32_t cols, uint16_t *hi, uint16_t *lo, const HeadPlan &h, hipStream_t st)
-{
-    if (rows == 0) return;
-    const uint32_t pieces = h.width / 8;
-    const uint64_t blocks = ((uint64_t)rows * pieces + 255) / 256;
-    hipLaunchKernelGGL((k_head_copy<T, KIND>), dim3((uint32_t)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, st, (const T *)m.data, m.stride,
-                       rows, cols, hi, lo, pieces, h.ranges, (const HeadRow *)h.row_info, h.scales);
 }
 
 template <class T> static void prepare(const dgs_head_args &p, const HeadPlan &h, const Targets &targets, hipStream_t st)
@@ -621,23 +657,35 @@ template <class T> static void prepare(const dgs_head_args &p, const HeadPlan &h
         hipLaunchKernelGGL(k_head_range<T>, dim3(2 * RANGE_BLOCKS), dim3(256), 0, st, (const T *)p.x.data, p.x.stride,
                            (const T *)p.weight.data, p.weight.stride, p.rows, p.cols, targets, (const float *)p.lse, p.dloss, p.dlse,
                            h.row_info, h.ranges);
-    if constexpr (f32) {
-        copy<T, COPY_ROWS>(p.x, p.rows, p.cols, h.x[0], h.x[1], h, st);
-        copy<T, COPY_ALL>(p.weight, p.vocab, p.cols, h.w[0], h.w[1], h, st);
+    CopyJobs jobs = {};
+    jobs.cols = p.cols;
+    jobs.pieces = h.width / 8;
+    uint32_t blocks = 0;
+    auto job = [&](const dgs_matrix &m, uint32_t rows, int kind, uint16_t *hi, uint16_t *lo) {
+        const uint64_t n = ((uint64_t)rows * jobs.pieces + 255) / 256;
+        const uint32_t b = n < 4096 ? (uint32_t)n : 4096u;
+        jobs.job[jobs.count++] = CopyJob{m.data, m.stride, hi, lo, rows, b, kind};
+        blocks += b;
+    };
+    if (f32) {
+        job(p.x, p.rows, COPY_ROWS, h.x[0], h.x[1]);
+        job(p.weight, p.vocab, COPY_ALL, h.w[0], h.w[1]);
     } else {
-        if (h.copy_x) copy<T, COPY_PLAIN>(p.x, p.rows, p.cols, h.x[0], nullptr, h, st);
-        if (h.copy_w) copy<T, COPY_PLAIN>(p.weight, p.vocab, p.cols, h.w[0], nullptr, h, st);
-        if (h.scale_w) copy<T, COPY_ALL>(p.weight, p.vocab, p.cols, h.w[1], nullptr, h, st);
+        if (h.copy_x) job(p.x, p.rows, COPY_PLAIN, h.x[0], nullptr);
+        if (h.copy_w) job(p.weight, p.vocab, COPY_PLAIN, h.w[0], nullptr);
+        if (h.scale_w) job(p.weight, p.vocab, COPY_ALL, h.w[1], nullptr);
     }
-    if (h.wants_dw) copy<T, COPY_WEIGHED>(p.x, p.rows, p.cols, h.x_weighed[0], h.x_weighed[1], h, st);
+    if (h.wants_dw) job(p.x, p.rows, COPY_WEIGHED, h.x_weighed[0], h.x_weighed[1]);
+    if (blocks) hipLaunchKernelGGL(k_head_copy<T>, dim3(blocks), dim3(256), 0, st, jobs, h.ranges, (const HeadRow *)h.row_info, h.scales);
 }
 
 template <class E, bool BACK> static void logits(const LogitArgs &a, int tile, hipStream_t st)
 {
     const dim3 grid(a.v_tiles * a.t_tiles);
-    if (tile == TILE_LARGE) hipLaunchKernelGGL((k_head_logits<E, 256, 256, 2, 4, BACK>), grid, dim3(512), 0, st, a);
-    else if (tile == TILE_SMALL) hipLaunchKernelGGL((k_head_logits<E, 128, 128, 2, 2, BACK>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((k_head_logits<E, 128, 32, 4, 1, BACK>), grid, dim3(256), 0, st, a);
+    if (tile == TILE_256) hipLaunchKernelGGL((k_head_logits<E, 256, 256, 2, 4, 2, BACK>), grid, dim3(512), 0, st, a);
+    else if (tile == TILE_128) hipLaunchKernelGGL((k_head_logits<E, 128, 128, 2, 2, 2, BACK>), grid, dim3(256), 0, st, a);
+    else if (tile == TILE_64) hipLaunchKernelGGL((k_head_logits<E, 64, 64, 2, 2, 4, BACK>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((k_head_logits<E, 128, 32, 4, 1, 4, BACK>), grid, dim3(256), 0, st, a);
 }
 template <bool BACK> static void logits(const LogitArgs &a, int type, int tile, hipStream_t st)
 {
@@ -647,8 +695,10 @@ template <bool BACK> static void logits(const LogitArgs &a, int type, int tile, 
 template <bool TURN_A> static void product(const GradientArgs &a, int tile, hipStream_t st)
 {
     const dim3 grid(a.m_tiles * a.n_tiles * a.splits);
-    if (tile == TILE_LARGE) hipLaunchKernelGGL((k_head_product<256, 256, 2, 4, TURN_A>), grid, dim3(512), 0, st, a);
-    else hipLaunchKernelGGL((k_head_product<128, 128, 2, 2, TURN_A>), grid, dim3(256), 0, st, a);
+    if (tile == TILE_256) hipLaunchKernelGGL((k_head_product<256, 256, 2, 4, 2, TURN_A>), grid, dim3(512), 0, st, a);
+    else if (tile == TILE_TALL) hipLaunchKernelGGL((k_head_product<256, 128, 2, 2, 3, TURN_A>), grid, dim3(256), 0, st, a);
+    else if (tile == TILE_128) hipLaunchKernelGGL((k_head_product<128, 128, 2, 2, 2, TURN_A>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((k_head_product<64, 64, 2, 2, 4, TURN_A>), grid, dim3(256), 0, st, a);
 }
 
 static LogitArgs logit_args(const dgs_head_args &p, const HeadPlan &h, const Targets &targets)
@@ -737,7 +787,7 @@ extern "C" int dgs_head_backward(const dgs_head_args *args, void *hip_stream)
             hipLaunchKernelGGL(k_head_dweight, dim3((uint32_t)(((uint64_t)p.vocab * p.cols + 255) / 256)), dim3(256), 0, (hipStream_t)hip_stream,
                                (const float *)nullptr, 0u, p.vocab, p.cols, (const Scales *)nullptr, p.dweight, p.dweight_stride, 0u);
         if (p.dbias)
-            hipLaunchKernelGGL(k_head_dbias, dim3(tiles_of(p.vocab, 256)), dim3(256), 0, (hipStream_t)hip_stream, (const float *)nullptr, 0u,
+            hipLaunchKernelGGL(k_head_dbias, dim3(tiles_of(p.vocab, 64)), dim3(256), 0, (hipStream_t)hip_stream, (const float *)nullptr, 0u,
                                (uint64_t)0, p.vocab, p.dbias, 0u);
         return launched();
     }
@@ -750,7 +800,7 @@ extern "C" int dgs_head_backward(const dgs_head_args *args, void *hip_stream)
     if (p.type == DGS_F32) prepare<float>(p, h, targets, st);
     else if (p.type == DGS_F16) prepare<f16>(p, h, targets, st);
     else prepare<bf16>(p, h, targets, st);
-    const TileSize tile = size_of(h.logits), tx = size_of(h.dx_tile), tw = size_of(h.dw_tile);
+    const TileSize tile = size_of(h.logits), tx = size_of(h.dx.tile), tw = size_of(h.dw.tile);
     const uint64_t stride = ((uint64_t)h.piece + 7) & ~7ull;
     LogitArgs a = logit_args(p, h, targets);
     a.row_info = h.row_info;
@@ -765,7 +815,7 @@ extern "C" int dgs_head_backward(const dgs_head_args *args, void *hip_stream)
         a.v_tiles = tiles_of(count, tile.m);
         logits<true>(a, p.type, h.logits, st);
         if (p.dbias)
-            hipLaunchKernelGGL(k_head_dbias, dim3(tiles_of(count, 256)), dim3(256), 0, st, (const float *)h.bias_parts,
+            hipLaunchKernelGGL(k_head_dbias, dim3(tiles_of(count, 64)), dim3(256), 0, st, (const float *)h.bias_parts,
                                a.t_tiles, stride, count, p.dbias + first, (uint32_t)(p.accumulate != 0));
         if (h.wants_dx) {
             GradientArgs g = {};
@@ -774,9 +824,9 @@ extern "C" int dgs_head_backward(const dgs_head_args *args, void *hip_stream)
             g.a = Side{{h.grad[0], h.grad[1]}, stride, p.rows};
             g.b = Side{{w + first * w_stride, f32 ? a.w.part[1] + first * w_stride : nullptr}, w_stride, p.cols};
             g.depth = count;
-            g.splits = h.dx_splits;
-            g.split_depth = (tiles_of(count, PRODUCT_STEP) + g.splits - 1) / g.splits * PRODUCT_STEP;
-            g.kind = f32 ? BOTH_IN_TWO : p.type == DGS_F16 ? FIRST_IN_TWO : ONE_PAIR;
+            g.splits = h.dx.splits;
+            g.split_depth = h.dx.split_depth;
+            g.kind = h.dx.kind;
             g.m = p.rows;
             g.n = p.cols;
             g.m_tiles = tiles_of(g.m, tx.m);
@@ -784,16 +834,16 @@ extern "C" int dgs_head_backward(const dgs_head_args *args, void *hip_stream)
             g.out = h.dx_sums;
             g.out_stride = p.cols;
             g.add = first != 0;
-            product<false>(g, h.dx_tile, st);
+            product<false>(g, h.dx.tile, st);
         }
         if (h.wants_dw) {
             GradientArgs g = {};
             g.a = Side{{h.grad[0], h.grad[1]}, stride, count};
             g.b = Side{{h.x_weighed[0], h.x_weighed[1]}, h.width, p.cols};
             g.depth = p.rows;
-            g.splits = h.dw_splits;
-            g.split_depth = (tiles_of(p.rows, PRODUCT_STEP) + g.splits - 1) / g.splits * PRODUCT_STEP;
-            g.kind = f32 ? BOTH_IN_TWO : FIRST_IN_TWO;
+            g.splits = h.dw.splits;
+            g.split_depth = h.dw.split_depth;
+            g.kind = h.dw.kind;
             g.m = count;
             g.n = p.cols;
             g.m_tiles = tiles_of(g.m, tw.m);
@@ -803,8 +853,8 @@ extern "C" int dgs_head_backward(const dgs_head_args *args, void *hip_stream)
             g.out_stride = g.whole ? p.dweight_stride : p.cols;
             g.add = g.whole && p.accumulate;
             g.scales = h.scales;
-            product<true>(g, h.dw_tile, st);
-            if (h.dw_splits > 1)
+            product<true>(g, h.dw.tile, st);
+            if (h.dw.splits > 1)
                 hipLaunchKernelGGL(k_head_dweight, dim3((uint32_t)(((uint64_t)count * p.cols + 255) / 256)), dim3(256), 0, st,
                                    (const float *)h.dw_sums, g.splits, count, p.cols, (const Scales *)h.scales,
                                    p.dweight + first * p.dweight_stride, p.dweight_stride, (uint32_t)(p.accumulate != 0));
@@ -814,9 +864,9 @@ extern "C" int dgs_head_backward(const dgs_head_args *args, void *hip_stream)
         const uint64_t blocks = ((uint64_t)p.rows * ((p.cols + 7) / 8) + 255) / 256;
         const dim3 grid((uint32_t)blocks);
         const Scales *const sc = h.scale_w ? h.scales : nullptr;
-        if (f32) hipLaunchKernelGGL(k_head_dx<float>, grid, dim3(256), 0, st, (const float *)h.dx_sums, h.dx_splits, p.rows, p.cols, (const HeadRow *)h.row_info, sc, (float *)p.dx.data, p.dx.stride);
-        else if (p.type == DGS_F16) hipLaunchKernelGGL(k_head_dx<f16>, grid, dim3(256), 0, st, (const float *)h.dx_sums, h.dx_splits, p.rows, p.cols, (const HeadRow *)h.row_info, sc, (f16 *)p.dx.data, p.dx.stride);
-        else hipLaunchKernelGGL(k_head_dx<bf16>, grid, dim3(256), 0, st, (const float *)h.dx_sums, h.dx_splits, p.rows, p.cols, (const HeadRow *)h.row_info, sc, (bf16 *)p.dx.data, p.dx.stride);
+        if (f32) hipLaunchKernelGGL(k_head_dx<float>, grid, dim3(256), 0, st, (const float *)h.dx_sums, h.dx.splits, p.rows, p.cols, (const HeadRow *)h.row_info, sc, (float *)p.dx.data, p.dx.stride);
+        else if (p.type == DGS_F16) hipLaunchKernelGGL(k_head_dx<f16>, grid, dim3(256), 0, st, (const float *)h.dx_sums, h.dx.splits, p.rows, p.cols, (const HeadRow *)h.row_info, sc, (f16 *)p.dx.data, p.dx.stride);
+        else hipLaunchKernelGGL(k_head_dx<bf16>, grid, dim3(256), 0, st, (const float *)h.dx_sums, h.dx.splits, p.rows, p.cols, (const HeadRow *)h.row_info, sc, (bf16 *)p.dx.data, p.dx.stride);
     }
     return launched();
 }

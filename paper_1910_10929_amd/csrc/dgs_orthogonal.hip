@@ -16,7 +16,7 @@ namespace dgs {
 
 constexpr float HELD = 4096.0f, LEFT = 1.0f / HELD;      // X, A and B are held times 2^12
 constexpr uint32_t ORTHO_AT_ONCE = 32;      // matrices of a launch
-constexpr uint32_t NORM_PARTS = 64;
+constexpr uint32_t NORM_PARTS = 256;      // at most
 
 struct Matrices {
     const void *data[ORTHO_AT_ONCE];
@@ -64,7 +64,7 @@ __global__ __launch_bounds__(256) void k_ortho_norm(Matrices in, uint32_t rows, 
     const T *const m = (const T *)in.data[which];
     const uint64_t stride = in.stride[which], pieces = (cols + 7) / 8, end = pieces * rows;
     double s = 0.0;
-    for (uint64_t at = blockIdx.x * 256 + threadIdx.x; at < end; at += NORM_PARTS * 256) {
+    for (uint64_t at = blockIdx.x * 256 + threadIdx.x; at < end; at += gridDim.x * 256) {
         const uint64_t row = at / pieces;
         const uint32_t c = (uint32_t)(at - row * pieces) * 8;
         float v[8];
@@ -78,21 +78,24 @@ __global__ __launch_bounds__(256) void k_ortho_norm(Matrices in, uint32_t rows, 
         if (threadIdx.x < by) sums[threadIdx.x] += sums[threadIdx.x + by];
         __syncthreads();
     }
-    if (threadIdx.x == 0) parts[which * NORM_PARTS + blockIdx.x] = sums[0];
+    if (threadIdx.x == 0) parts[which * gridDim.x + blockIdx.x] = sums[0];
 }
 
 // X from G, 64 x 64 of it to a workgroup, turned where that makes it wide.  Columns up to a multiple of eight are zeros.
 template <class T>
-__global__ __launch_bounds__(256) void k_ortho_load(Matrices in, uint32_t rows, uint32_t cols, uint32_t turned, const double *parts,
+__global__ __launch_bounds__(256) void k_ortho_load(Matrices in, uint32_t rows, uint32_t cols, uint32_t turned, const double *parts, uint32_t norm_parts,
                                                     float eps, Halves x, float *log2_norm)
 {
     __shared__ double norm[NORM_PARTS];
     __shared__ float tile[64][65];
     const uint32_t which = blockIdx.y, across = (cols + 63) / 64;
-    if (threadIdx.x < NORM_PARTS) norm[threadIdx.x] = parts[which * NORM_PARTS + threadIdx.x];
+    norm[threadIdx.x] = threadIdx.x < norm_parts ? parts[which * norm_parts + threadIdx.x] : 0.0;
+    for (uint32_t by = NORM_PARTS / 2; by; by >>= 1) {
+        __syncthreads();
+        if (threadIdx.x < by) norm[threadIdx.x] += norm[threadIdx.x + by];
+    }
     __syncthreads();
-    double sum = 0.0;
-    for (uint32_t i = 0; i < NORM_PARTS; ++i) sum += norm[i];
+    const double sum = norm[0];
     const double length = sqrt(sum), whole = length + (double)eps;
     const float log2_of = sum > 0.0 ? (float)(log2(length) - log2(whole)) : 0.0f;
     const double by = ldexp((double)HELD, lift_of(log2_of, 0.0f)) / whole;
@@ -147,10 +150,10 @@ struct SquareArgs {
 };
 
 // The symmetric product of X with itself (POLY: of A with itself, from which the polynomial is made).
-template <uint32_t M, uint32_t WAVES_M, uint32_t WAVES_N, bool POLY>
-__global__ __launch_bounds__(WAVES_M *WAVES_N * 64, 2) void k_ortho_square(SquareArgs a)
+template <uint32_t M, uint32_t WAVES_M, uint32_t WAVES_N, uint32_t STAGES, bool POLY>
+__global__ __launch_bounds__(WAVES_M *WAVES_N * 64, WAVES_M *WAVES_N > 4 || STAGES < 4 ? 2 : 1) void k_ortho_square(SquareArgs a)
 {
-    typedef Product<f16, M, M, WAVES_M, WAVES_N, false, false> P;
+    typedef Product<f16, M, M, WAVES_M, WAVES_N, false, false, STAGES> P;
     __shared__ __attribute__((aligned(16))) typename P::Lds lds;
     // tiles on and below the diagonal, row by row
     const uint32_t count = a.tiles * (a.tiles + 1) / 2;
@@ -220,19 +223,20 @@ template <class T> __device__ __forceinline__ void put8(T *p, uint32_t count, fl
 
 // X of the next step: its rows times the polynomial's diagonal, plus the product of the rest with it.
 // T: the result's type in the last step, void in the others; TURNED: the result's rows are X's columns.
-template <uint32_t M, uint32_t N, uint32_t WAVES_M, uint32_t WAVES_N, class T, bool TURNED>
-__global__ __launch_bounds__(WAVES_M *WAVES_N * 64, 2) void k_ortho_step(StepArgs a, Matrices results)
+template <uint32_t M, uint32_t WAVES_M, uint32_t WAVES_N, uint32_t STAGES, class T, bool TURNED>
+__global__ __launch_bounds__(WAVES_M *WAVES_N * 64, WAVES_M *WAVES_N > 4 || STAGES < 4 ? 2 : 1) void k_ortho_step(StepArgs a, Matrices results)
 {
-    typedef Product<f16, M, N, WAVES_M, WAVES_N, false, true> P;
+    typedef Product<f16, M, M, WAVES_M, WAVES_N, false, true, STAGES> P;
     __shared__ __attribute__((aligned(16))) typename P::Lds lds;
     const uint32_t count = a.m_tiles * a.n_tiles;
     const uint32_t all = tile_of_block(blockIdx.x, gridDim.x), which = all / count, at = all - which * count;
-    const uint32_t tile_m = at / a.n_tiles, tile_n = at - tile_m * a.n_tiles;
+    const TilePlace place = place_of_tile(at, a.m_tiles, a.n_tiles);
+    const uint32_t tile_m = place.m, tile_n = place.n;
     const uint16_t *const x_hi = a.x.hi + which * a.x.size, *const x_lo = a.x.lo + which * a.x.size;
     const Side left = {{a.poly.hi + which * a.poly.size, a.poly.lo ? a.poly.lo + which * a.poly.size : nullptr}, a.poly.stride, a.rows};
     const Side right = {{x_hi, x_lo}, a.x.stride, a.cols};
     typename P::Sums s;
-    P::run(lds, left, right, tile_m * M, tile_n * N, 0, a.rows, a.kind, s);
+    P::run(lds, left, right, tile_m * M, tile_n * M, 0, a.rows, a.kind, s);
     // from how this X is held to how the next one is, or to the result
     const int lift = lift_of(a.log2_norm[which], a.growth);
     const int power = __is_same(T, void) ? lift_of(a.log2_norm[which], a.next_growth) - lift : -12 - lift;
@@ -240,7 +244,7 @@ __global__ __launch_bounds__(WAVES_M *WAVES_N * 64, 2) void k_ortho_step(StepArg
     u32x4 hi[P::PASSES], lo[P::PASSES];
     float d[P::PASSES];
     auto look = [&](uint32_t p, uint32_t row, uint32_t col) {
-        const uint32_t m = tile_m * M + row, n = tile_n * N + col;
+        const uint32_t m = tile_m * M + row, n = tile_n * M + col;
         const bool in = m < a.rows && n < a.x.stride;
         const uint64_t at = in ? m * a.x.stride + n : 0;
         hi[p] = *(const u32x4 *)(x_hi + at);
@@ -256,7 +260,7 @@ __global__ __launch_bounds__(WAVES_M *WAVES_N * 64, 2) void k_ortho_step(StepArg
     };
     if constexpr (__is_same(T, void)) {
         P::by_rows(lds, s, look, [&](uint32_t p, uint32_t row, uint32_t col, float (&v)[8]) {
-            const uint32_t m = tile_m * M + row, n = tile_n * N + col;
+            const uint32_t m = tile_m * M + row, n = tile_n * M + col;
             next(p, v);
             if (m < a.rows && n < a.x.stride) put_halves(a.next, which * a.next.size + m * a.x.stride + n, v);
         });
@@ -269,12 +273,12 @@ __global__ __launch_bounds__(WAVES_M *WAVES_N * 64, 2) void k_ortho_step(StepArg
 #pragma unroll
                 for (uint32_t k = 0; k < 8; ++k) back[k] = v[k];
             }, [&](uint32_t row, uint32_t col, float (&v)[8]) {
-                const uint32_t m = tile_m * M + row, n = tile_n * N + col;
+                const uint32_t m = tile_m * M + row, n = tile_n * M + col;
                 if (m < a.rows && n < a.cols) put8(out + n * stride + m, live8(m, a.rows), v, a.scale, a.add);
             });
         } else {
             P::by_rows(lds, s, look, [&](uint32_t p, uint32_t row, uint32_t col, float (&v)[8]) {
-                const uint32_t m = tile_m * M + row, n = tile_n * N + col;
+                const uint32_t m = tile_m * M + row, n = tile_n * M + col;
                 next(p, v);
                 if (m < a.rows && n < a.cols) put8(out + m * stride + n, live8(n, a.cols), v, a.scale, a.add);
             });
@@ -333,20 +337,32 @@ static int ortho_refused(const dgs_orthogonalise_args &p)
 
 template <class T> static void load_matrices(const Matrices &in, const dgs_orthogonalise_args &p, const OrthoPlan &o, uint32_t count, hipStream_t st)
 {
-    hipLaunchKernelGGL(k_ortho_norm<T>, dim3(NORM_PARTS, count), dim3(256), 0, st, in, p.rows, p.cols, o.norm);
+    // (a workgroup for every 64 KB or so of halves, and as few as there are work)
+    const uint64_t work = (uint64_t)p.rows * ((p.cols + 7) / 8) / 2048 + 1;
+    const uint32_t parts = work < NORM_PARTS ? (uint32_t)work : NORM_PARTS;
+    hipLaunchKernelGGL(k_ortho_norm<T>, dim3(parts, count), dim3(256), 0, st, in, p.rows, p.cols, o.norm);
     hipLaunchKernelGGL(k_ortho_load<T>, dim3((p.cols + 63) / 64 * ((p.rows + 63) / 64), count), dim3(256), 0, st, in, p.rows, p.cols,
-                       (uint32_t)o.turned, (const double *)o.norm, p.eps, o.x[0], o.log2_norm);
+                       (uint32_t)o.turned, (const double *)o.norm, parts, p.eps, o.x[0], o.log2_norm);
 }
 
-template <class T, bool TURNED> static void launch_step(const StepArgs &s, const Matrices &out, bool large, dim3 grid, hipStream_t st)
+template <class T, bool TURNED> static void launch_step(const StepArgs &s, const Matrices &out, int tile, uint32_t count, hipStream_t st)
 {
-    if (large) hipLaunchKernelGGL((k_ortho_step<256, 256, 2, 4, T, TURNED>), grid, dim3(512), 0, st, s, out);
-    else hipLaunchKernelGGL((k_ortho_step<128, 128, 2, 2, T, TURNED>), grid, dim3(256), 0, st, s, out);
+    const dim3 grid(s.m_tiles * s.n_tiles * count);
+    if (tile == TILE_256) hipLaunchKernelGGL((k_ortho_step<256, 2, 4, 2, T, TURNED>), grid, dim3(512), 0, st, s, out);
+    else if (tile == TILE_128) hipLaunchKernelGGL((k_ortho_step<128, 2, 2, 2, T, TURNED>), grid, dim3(256), 0, st, s, out);
+    else hipLaunchKernelGGL((k_ortho_step<64, 2, 2, 4, T, TURNED>), grid, dim3(256), 0, st, s, out);
 }
-template <class T> static void launch_last(const StepArgs &s, const Matrices &out, bool turned, bool large, dim3 grid, hipStream_t st)
+template <bool POLY> static void launch_square(const SquareArgs &a, int tile, uint32_t count, hipStream_t st)
 {
-    if (turned) launch_step<T, true>(s, out, large, grid, st);
-    else launch_step<T, false>(s, out, large, grid, st);
+    const dim3 grid(a.tiles * (a.tiles + 1) / 2 * count);
+    if (tile == TILE_256) hipLaunchKernelGGL((k_ortho_square<256, 2, 4, 2, POLY>), grid, dim3(512), 0, st, a);
+    else if (tile == TILE_128) hipLaunchKernelGGL((k_ortho_square<128, 2, 2, 2, POLY>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((k_ortho_square<64, 2, 2, 4, POLY>), grid, dim3(256), 0, st, a);
+}
+template <class T> static void launch_last(const StepArgs &s, const Matrices &out, bool turned, int tile, uint32_t count, hipStream_t st)
+{
+    if (turned) launch_step<T, true>(s, out, tile, count, st);
+    else launch_step<T, false>(s, out, tile, count, st);
 }
 
 }  // namespace dgs
@@ -387,28 +403,25 @@ extern "C" int dgs_orthogonalise(const dgs_orthogonalise_args *args, void *hip_s
         else if (p.type == DGS_F16) load_matrices<f16>(in, p, o, count, st);
         else load_matrices<bf16>(in, p, o, count, st);
         const uint32_t kind = o.two ? BOTH_IN_TWO : ONE_PAIR;
-        auto tiles = [](uint32_t n, uint32_t size) { return (n - 1) / size + 1; };
-        const uint32_t t256 = tiles(o.rows, 256);
-        bool large_square = (uint64_t)t256 * (t256 + 1) / 2 * count >= 192;
-        bool large_step = (uint64_t)t256 * tiles(o.cols, 256) * count >= 192;
-#ifdef DGS_ORTHO_LARGE      // (a CPU build that is to reach one kind on small matrices)
-        large_square = large_step = DGS_ORTHO_LARGE;
-#endif
+        const uint32_t pairs = o.two ? 3 : 1;
+        auto half_of = [&](uint32_t size, uint32_t) { const uint64_t t = tiles_of(o.rows, size); return t * (t + 1) / 2 * count; };
+        auto all_of = [&](uint32_t high, uint32_t wide) { return (uint64_t)tiles_of(o.rows, high) * tiles_of(o.cols, wide) * count; };
+        const uint32_t long_steps = tiles_of(o.cols, PRODUCT_STEP) * pairs, short_steps = tiles_of(o.rows, PRODUCT_STEP) * pairs;
+        float us[3] = {};
+        const int gram_tile = product_tile(half_of, long_steps, false, us[0]), poly_tile = product_tile(half_of, short_steps, false, us[1]),
+                  step_tile = product_tile(all_of, short_steps, false, us[2]);
         const float grows = p.a != 0.0f ? log2f(fabsf(p.a)) : 0.0f;
-        const uint32_t side = tiles(o.rows, large_square ? 256 : 128);
         for (uint32_t step = 0; step < p.steps; ++step) {
             SquareArgs g = {};
             g.x = o.x[step & 1u];
             g.depth = o.cols;
             g.kind = kind;
             g.size = o.rows;
-            g.tiles = side;
+            g.tiles = tiles_of(o.rows, tile_high(gram_tile));
             g.out = o.gram;
             g.log2_norm = o.log2_norm;
             g.growth = (float)step * grows;
-            const dim3 grid(side * (side + 1) / 2 * count);
-            if (large_square) hipLaunchKernelGGL((k_ortho_square<256, 2, 4, false>), grid, dim3(512), 0, st, g);
-            else hipLaunchKernelGGL((k_ortho_square<128, 2, 2, false>), grid, dim3(256), 0, st, g);
+            launch_square<false>(g, gram_tile, count, st);
             g.x = o.gram;
             g.log2_norm = nullptr;
             g.depth = o.rows;
@@ -418,8 +431,8 @@ extern "C" int dgs_orthogonalise(const dgs_orthogonalise_args *args, void *hip_s
             g.a = p.a;
             g.b = p.b;
             g.c = p.c;
-            if (large_square) hipLaunchKernelGGL((k_ortho_square<256, 2, 4, true>), grid, dim3(512), 0, st, g);
-            else hipLaunchKernelGGL((k_ortho_square<128, 2, 2, true>), grid, dim3(256), 0, st, g);
+            g.tiles = tiles_of(o.rows, tile_high(poly_tile));
+            launch_square<true>(g, poly_tile, count, st);
             StepArgs s = {};
             s.poly = o.poly;
             s.x = o.x[step & 1u];
@@ -433,14 +446,12 @@ extern "C" int dgs_orthogonalise(const dgs_orthogonalise_args *args, void *hip_s
             s.next_growth = s.growth + grows;
             s.add = p.accumulate != 0;
             s.scale = p.scale;
-            const uint32_t size = large_step ? 256 : 128;
-            s.m_tiles = tiles(o.rows, size);
-            s.n_tiles = tiles(o.cols, size);
-            const dim3 all(s.m_tiles * s.n_tiles * count);
-            if (step + 1 < p.steps) launch_step<void, false>(s, out, large_step, all, st);
-            else if (p.out_type == DGS_F32) launch_last<float>(s, out, o.turned, large_step, all, st);
-            else if (p.out_type == DGS_F16) launch_last<f16>(s, out, o.turned, large_step, all, st);
-            else launch_last<bf16>(s, out, o.turned, large_step, all, st);
+            s.m_tiles = tiles_of(o.rows, tile_high(step_tile));
+            s.n_tiles = tiles_of(o.cols, tile_high(step_tile));
+            if (step + 1 < p.steps) launch_step<void, false>(s, out, step_tile, count, st);
+            else if (p.out_type == DGS_F32) launch_last<float>(s, out, o.turned, step_tile, count, st);
+            else if (p.out_type == DGS_F16) launch_last<f16>(s, out, o.turned, step_tile, count, st);
+            else launch_last<bf16>(s, out, o.turned, step_tile, count, st);
         }
     }
     return launched();

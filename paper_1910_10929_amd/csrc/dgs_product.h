@@ -19,7 +19,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));      // eight 16-bit values of a lane
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-constexpr uint32_t NOWHERE = 0x80000000u;      // an offset beyond every buffer
+constexpr uint32_t NOWHERE = 0x80000000u, ANYWHERE = 0x7FFFFFFFu;      // an offset beyond every buffer, and the largest buffer
 
 #ifdef DGS_HOST_EMULATION
 }  // namespace dgs
@@ -46,25 +46,28 @@ __device__ __forceinline__ u32x2 read_turned(const uint16_t *p)
     return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)p));
 }
 
-// Memory that a workgroup's loads start from.
+// Memory that a workgroup's loads start from, and how much of it there is: beyond it they get zeros.
 typedef i32x4 Window;
-__device__ __forceinline__ Window window_at(const void *p)
+__device__ __forceinline__ Window window_at(const void *p, uint32_t bytes)
 {
     const uint64_t a = (uint64_t)p;
     Window w;
     w.x = (int)uniform((uint32_t)a);
     w.y = (int)(uniform((uint32_t)(a >> 32)) & 0xFFFFu);
-    w.z = (int)0x7FFFFFFF;
+    w.z = (int)uniform(bytes);
     w.w = 0x00020000;
     return w;
 }
-// 16 bytes from `offset` on into LDS: lane l's at `to` + 16 l.  Nothing waits; loads_done() does.
-__device__ __forceinline__ void load_to_lds(Window w, uint32_t offset, uint16_t *to)
+// Where in LDS a wavefront's loads go.
+typedef uint32_t LdsPlace;
+__device__ __forceinline__ LdsPlace lds_place(uint16_t *p) { return uniform((uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint16_t *)p); }
+// 16 bytes from `offset` on into LDS: lane l's `behind` + 16 l bytes behind `to`.  Nothing waits; loads_meet() does.
+__device__ __forceinline__ void load_to_lds(Window w, uint32_t offset, LdsPlace to, uint32_t behind)
 {
-    const uint32_t at = uniform((uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint16_t *)to);
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at), "v"(offset), "s"(w) : "memory");
+    asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(w), "s"(behind) : "memory", "scc");
 }
-template <int LEFT> __device__ __forceinline__ void loads_done() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory"); }
+// Every wavefront's loads but its last LEFT have arrived, and what was read before has been.
+template <int LEFT> __device__ __forceinline__ void loads_meet() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory"); }
 #endif
 
 // One side of a product.
@@ -74,19 +77,20 @@ struct Side {
     uint32_t size;        // m or n
 };
 
-constexpr uint32_t PRODUCT_STEP = 64;
+constexpr uint32_t PRODUCT_STEP = 64;      // of k, staged at a time
 
 // Loads of one operand: WIDTH of its m (or n) and a step of k, by WAVES wavefronts.
-template <uint32_t WIDTH, bool TURNED, uint32_t WAVES> struct Staged {
-    static constexpr uint32_t LOADS = WIDTH * PRODUCT_STEP / 8 / 64 / WAVES;
+template <uint32_t WIDTH, bool TURNED, uint32_t WAVES, uint32_t STEP> struct Staged {
+    static constexpr uint32_t LOADS = WIDTH * STEP / 8 / 64 / WAVES;
     // turned: pieces of a row (its columns m), exchanged so that the four rows that 32 lanes read 64 bytes of lie in different
     // banks; straight: pieces of a row (its k), exchanged so that 16 rows' pieces of the same k do
-    static constexpr uint32_t PIECES = TURNED ? WIDTH / 8 : PRODUCT_STEP / 8;
+    static constexpr uint32_t PIECES = TURNED ? WIDTH / 8 : STEP / 8;
     static __device__ __forceinline__ uint32_t at(uint32_t row, uint32_t piece)
     {
-        return row * PIECES * 8 + ((TURNED ? piece ^ ((row & 3u) << 2) : piece ^ ((row >> 1) & 7u)) << 3);
+        return row * PIECES * 8 + ((!TURNED ? piece ^ (PIECES == 8 ? (row >> 1) & 7u : (row >> 2) & 3u) : PIECES == 8 ? piece ^ ((row & 2u) << 1) : piece ^ ((row & 3u) << 2)) << 3);
     }
-    uint32_t offset[LOADS], k[LOADS];
+    uint32_t offset[LOADS], k;      // (straight: the k that a lane loads is the same in all its loads)
+    Window from;
 
     __device__ __forceinline__ void plan(const Side &s, uint32_t first)
     {
@@ -97,16 +101,24 @@ template <uint32_t WIDTH, bool TURNED, uint32_t WAVES> struct Staged {
             const uint32_t piece = ((at(row, slot % PIECES) >> 3) % PIECES);      // (an exchange undoes itself)
             const uint32_t outer = TURNED ? first + piece * 8 : first + row;
             offset[i] = outer < s.size ? (uint32_t)(row * s.stride + piece * 8) * 2u : NOWHERE;
-            k[i] = TURNED ? row : piece * 8;
+            if (i == 0) k = piece * 8;
         }
     }
-    __device__ __forceinline__ void load(const Side &s, uint32_t part, uint32_t first, uint32_t k0, uint32_t k_end, uint16_t *lds) const
+    // Where a step's loads are from; `left` of k are there.  (Turned: a row of k that is not there lies beyond the window.)
+    __device__ __forceinline__ void step(const Side &s, uint32_t part, uint32_t first, uint32_t k0, uint32_t left)
     {
-        const uint32_t wave = uniform(threadIdx.x >> 6);
-        const Window w = window_at((part ? s.part[1] : s.part[0]) + (TURNED ? k0 * s.stride + first : first * s.stride + k0));
-#pragma unroll
-        for (uint32_t i = 0; i < LOADS; ++i) load_to_lds(w, k0 + k[i] < k_end ? offset[i] : NOWHERE, lds + (i * WAVES + wave) * 512);
+        const uint64_t bytes = TURNED ? left * s.stride * 2u : (uint64_t)ANYWHERE;
+        from = window_at((part ? s.part[1] : s.part[0]) + (TURNED ? k0 * s.stride + first : first * s.stride + k0),
+                         bytes < ANYWHERE ? (uint32_t)bytes : ANYWHERE);
+        inside = k < left;
     }
+    bool inside;
+    // (`lds`: this wavefront's place in the first stage)
+    __device__ __forceinline__ void load(uint32_t i, LdsPlace lds, uint32_t stage) const
+    {
+        load_to_lds(from, TURNED || inside ? offset[i] : NOWHERE, lds, stage * (WIDTH * STEP * 2) + i * WAVES * 1024);
+    }
+    static_assert(LOADS > 0 && (TURNED || WAVES * 64 / PIECES % 16 == 0), "whole loads, of one k");
     // The operand of one matrix instruction: 32 of m from `m` on, k from 16 s to 16 s + 15.
     static __device__ __forceinline__ u32x4 fragment(const uint16_t *lds, uint32_t m, uint32_t s)
     {
@@ -135,18 +147,26 @@ __device__ __forceinline__ uint32_t square_row(uint32_t r) { return row_in_squar
 constexpr uint32_t ONE_PAIR = 0x1, FIRST_IN_TWO = 0x2, BOTH_IN_TWO = 0x3;
 __device__ __forceinline__ uint32_t pairs_of(uint32_t kind) { return kind == ONE_PAIR ? 1u : kind == FIRST_IN_TWO ? 2u : 3u; }
 
-template <class E, uint32_t M, uint32_t N, uint32_t WAVES_M, uint32_t WAVES_N, bool TURN_A, bool TURN_B> struct Product {
+// Nothing is moved across this by the compiler, which would put LDS reads right before what waits for them.
+__device__ __forceinline__ void in_order()
+{
+#ifndef DGS_HOST_EMULATION
+    __builtin_amdgcn_sched_barrier(0);
+#endif
+}
+
+template <class E, uint32_t M, uint32_t N, uint32_t WAVES_M, uint32_t WAVES_N, bool TURN_A, bool TURN_B, uint32_t STAGES, uint32_t STEP = PRODUCT_STEP> struct Product {
     static constexpr uint32_t WAVES = WAVES_M * WAVES_N, THREADS = WAVES * 64, I = M / 32 / WAVES_M, J = N / 32 / WAVES_N;
-    typedef Staged<M, TURN_A, WAVES> A;
-    typedef Staged<N, TURN_B, WAVES> B;
+    typedef Staged<M, TURN_A, WAVES, STEP> A;
+    typedef Staged<N, TURN_B, WAVES, STEP> B;
     // Behind the sums, LDS takes a part of them from each wavefront (by_rows, by_columns).
     static constexpr uint32_t ABOVE = I < 2 ? 1 : 2, ROW_PITCH = 32 * J + 4, COLUMN_PITCH = 32 * ABOVE + 4;
     static constexpr uint32_t PART = 32 * ROW_PITCH > 32 * J * COLUMN_PITCH ? 32 * ROW_PITCH : 32 * J * COLUMN_PITCH;
     union Lds {
         struct {
-            uint16_t a[2][M * PRODUCT_STEP], b[2][N * PRODUCT_STEP];
+            uint16_t a[STAGES][M * STEP], b[STAGES][N * STEP];
         };
-        float part[WAVES][PART];
+        __attribute__((aligned(16))) float part[WAVES][PART];
     };
     typedef f32x16 Sums[I][J];
 
@@ -168,40 +188,75 @@ template <class E, uint32_t M, uint32_t N, uint32_t WAVES_M, uint32_t WAVES_N, b
             for (uint32_t j = 0; j < J; ++j)
 #pragma unroll
                 for (uint32_t r = 0; r < 16; ++r) sums[i][j][r] = 0.0f;
-        const uint32_t per_pair = k_end > k_first ? (k_end - k_first + PRODUCT_STEP - 1) / PRODUCT_STEP : 0u;
-        const uint32_t steps = per_pair * pairs_of(kind);
+        const uint32_t per_pair = k_end > k_first ? (k_end - k_first + STEP - 1) / STEP : 0u;
+        const uint32_t pairs = pairs_of(kind), steps = per_pair * pairs;
+        if (steps == 0) return;
         const uint32_t wm = wave_m(), wn = wave_n();
-        uint32_t next = 0, next_k = k_first, pair = 0;      // what is loaded next
-        auto load = [&](uint32_t buf) {
+        // what is loaded next; behind the last step nothing, in as many loads
+        uint32_t next = 0, next_k = k_first, pair = 0, to = 0;
+        auto next_step = [&]() {
             // pairs: first with first, second with first, first with second
-            la.load(a, pair == 1, m0, next_k, k_end, lds.a[buf]);
-            lb.load(b, pair == 2, n0, next_k, k_end, lds.b[buf]);
-            next_k += PRODUCT_STEP;
+            const uint32_t left = pair < pairs ? k_end - next_k : 0u;
+            la.step(a, pair == 1 && pairs > 1, m0, next_k, left);
+            lb.step(b, pair == 2 && pairs > 2, n0, next_k, left);
+            next_k += STEP;
             if (++next == per_pair) {
                 next = 0;
                 next_k = k_first;
                 ++pair;
             }
         };
-        if (steps) load(0);
-        for (uint32_t step = 0; step < steps; ++step) {
-            const uint32_t buf = step & 1u;
-            loads_done<0>();
-            __syncthreads();      // this step has arrived, and nobody reads the one before any more
-            if (step + 1 < steps) load(buf ^ 1u);
+        constexpr uint32_t EACH = A::LOADS + B::LOADS, SLICES = STEP / 16, READS = I + J, SQUARES = I * J;
+        const uint32_t wave = uniform(threadIdx.x >> 6);
+        const LdsPlace place_a = lds_place(lds.a[0] + wave * 512), place_b = lds_place(lds.b[0] + wave * 512);
+        auto load = [&](uint32_t l) {
+            if (l < A::LOADS) la.load(l, place_a, to);
+            else lb.load(l - A::LOADS, place_b, to);
+        };
+        u32x4 fa[2][I], fb[2][J];
+        auto read = [&](uint32_t stage, uint32_t s, uint32_t r) {
+            if (r < J) fb[s & 1][r] = B::fragment(lds.b[stage], wn + 32 * r, s);
+            else fa[s & 1][r - J] = A::fragment(lds.a[stage], wm + 32 * (r - J), s);
+        };
+        // A slice of 16 k: its matrix instructions, and between them the reads of the next slice's operands (early: they have to be there when
+        // this one ends) and, in a step's last slice, the loads of the step after next.  The order is as written.
+        auto slice = [&](uint32_t s, uint32_t read_stage, bool loads) {
 #pragma unroll
-            for (uint32_t s = 0; s < PRODUCT_STEP / 16; ++s) {
-                u32x4 fa[I], fb[J];
+            for (uint32_t q = 0; q < SQUARES; ++q) {
+                sums[q / J][q % J] = matrix_unit_of<E>(fa[s & 1][q / J], fb[s & 1][q % J], sums[q / J][q % J]);
+                in_order();
+                constexpr uint32_t FEW = SQUARES >= 2 * READS ? 1 : SQUARES >= READS ? 1 : (READS + SQUARES - 1) / SQUARES;
 #pragma unroll
-                for (uint32_t j = 0; j < J; ++j) fb[j] = B::fragment(lds.b[buf], wn + 32 * j, s);
+                for (uint32_t r = q * FEW; r < (q + 1) * FEW; ++r)
+                    if (r < READS) read(read_stage, (s + 1) % SLICES, r);
+                if (loads) {
 #pragma unroll
-                for (uint32_t i = 0; i < I; ++i) fa[i] = A::fragment(lds.a[buf], wm + 32 * i, s);
-#pragma unroll
-                for (uint32_t i = 0; i < I; ++i)
-#pragma unroll
-                    for (uint32_t j = 0; j < J; ++j) sums[i][j] = matrix_unit_of<E>(fa[i], fb[j], sums[i][j]);
+                    for (uint32_t l = q * EACH / SQUARES; l < (q + 1) * EACH / SQUARES; ++l) load(l);
+                }
+                in_order();
             }
+        };
+#pragma unroll
+        for (uint32_t s = 0; s < STAGES; ++s) {
+            next_step();
+#pragma unroll
+            for (uint32_t l = 0; l < EACH; ++l) load(l);
+            to = (to + 1) % STAGES;
         }
+        loads_meet<(STAGES - 1) * EACH>();
+#pragma unroll
+        for (uint32_t r = 0; r < READS; ++r) read(0, 0, r);
+        for (uint32_t step = 0, stage = 0; step < steps; ++step) {
+#pragma unroll
+            for (uint32_t s = 0; s + 1 < SLICES; ++s) slice(s, stage, false);
+            next_step();
+            // this wavefront has read all of the step, and the next one has arrived: everybody's part of it
+            loads_meet<(STAGES - 2) * EACH>();
+            const uint32_t following = (stage + 1) % STAGES;
+            slice(SLICES - 1, following, true);
+            to = stage = following;
+        }
+        loads_meet<0>();      // (the loads of nothing)
     }
 
     // The lanes hold a column of a square each, four rows together.  Memory wants rows: the sums go through LDS, a wavefront's own
@@ -338,6 +393,15 @@ __device__ __forceinline__ uint32_t tile_of_block(uint32_t block, uint32_t total
     const uint32_t die = block & 7u;
     return die * (total >> 3) + min(die, total & 7u) + (block >> 3);
 }
+constexpr uint32_t TILE_BAND = 4;
+// Tile `at` of m_tiles x n_tiles: bands of TILE_BAND rows of tiles, column by column, so that the 32 tiles that a die works on at a time
+// are about as many high as wide and share what they load in its L2.
+struct TilePlace { uint32_t m, n; };
+__device__ __forceinline__ TilePlace place_of_tile(uint32_t at, uint32_t m_tiles, uint32_t n_tiles)
+{
+    const uint32_t band = at / (TILE_BAND * n_tiles), first = band * TILE_BAND, high = min(m_tiles - first, TILE_BAND), in = at - first * n_tiles;
+    return TilePlace{first + in % high, in / high};
+}
 
 // A value in two halves (22 bits).
 __device__ __forceinline__ void halves_of(float v, f16 &hi, f16 &lo)
@@ -378,5 +442,52 @@ struct Sections {
         return p;
     }
 };
+
+// ---------------------------------------------------------------------------
+// host side: which tile
+// ---------------------------------------------------------------------------
+
+// 256 x 256 to eight wavefronts, one workgroup to a compute unit; 256 x 128 (steps of 32), 128 x 128 and 64 x 64 to four, two
+// workgroups to a compute unit.
+enum ProductTile { TILE_256, TILE_TALL, TILE_128, TILE_64, PRODUCT_TILES };
+static inline uint32_t tile_high(int tile) { return tile <= TILE_TALL ? 256 : tile == TILE_128 ? 128 : 64; }
+static inline uint32_t tile_wide(int tile) { return tile == TILE_256 ? 256 : tile == TILE_64 ? 64 : 128; }
+static inline uint32_t tiles_of(uint32_t n, uint32_t size) { return n ? (n - 1) / size + 1 : 0; }
+
+// Microseconds that `tiles` tiles of `steps` steps of 64 k take: what a tile takes besides its steps, and for a step with every
+// compute unit's places taken and with one workgroup to a compute unit at most, as timed.  (4096 x 4096 squares on and below the
+// diagonal, 64 steps: 256 x 256 110 us, 128 x 128 114, 64 x 64 170; four of 1024 x 1024, 192 steps: 230, 128, 141; five of 333 x 333, 48
+// steps: 66, 33, 17; 30522 x 768 turned, 256 steps: 256 x 256 882, 256 x 128 775, 128 x 128 845.)
+static inline float tile_time(int tile, uint64_t tiles, uint32_t steps)
+{
+    static constexpr struct { float besides, full, one; uint32_t places; } cost[PRODUCT_TILES] = {
+        {10.0f, 1.9f, 1.2f, 256}, {6.0f, 2.0f, 1.0f, 512}, {5.0f, 1.12f, 0.66f, 512}, {3.5f, 0.5f, 0.3f, 512}};
+    const auto &c = cost[tile];
+    const uint64_t rounds = tiles / c.places, rest = tiles % c.places;
+    float us = (float)rounds * (c.besides + c.full * (float)steps);
+    if (rest) {
+        // (one to a compute unit: the clock falls as more of the chip multiplies)
+        const float step = rest > 256 ? c.full : c.places > 256 ? c.one : c.one + (c.full - c.one) * (float)rest / 256.0f;
+        us += c.besides + step * (float)steps;
+    }
+    return us;
+}
+// The tile that should take the least time; tiles(high, wide): how many of them there are.  `tall`: whether TILE_TALL is there.
+template <class Tiles> static int product_tile(Tiles tiles, uint32_t steps, bool tall, float &least)
+{
+    int best = TILE_256;
+    for (int t = 0; t < PRODUCT_TILES; ++t) {
+#ifdef DGS_PRODUCT_TILE      // (a CPU build that is to reach one kind on small matrices)
+        if (t != (DGS_PRODUCT_TILE == TILE_TALL && !tall ? TILE_128 : DGS_PRODUCT_TILE)) continue;
+#endif
+        if (t == TILE_TALL && !tall) continue;
+        const float us = tile_time(t, tiles(tile_high(t), tile_wide(t)), steps);
+        if (least == 0.0f || us < least) {
+            least = us;
+            best = t;
+        }
+    }
+    return best;
+}
 
 }  // namespace dgs

@@ -37,14 +37,16 @@ template <class E> static f32x16 matrix_unit_of(u32x4 a, u32x4 b, f32x16 c)
     return c;
 }
 
-typedef const char *Window;
-static inline Window window_at(const void *p) { return (const char *)p; }
-static inline void load_to_lds(Window w, uint32_t offset, uint16_t *to)
+struct Window { const char *p; uint32_t bytes; };
+static inline Window window_at(const void *p, uint32_t bytes) { return Window{(const char *)p, bytes}; }
+typedef uint16_t *LdsPlace;
+static inline LdsPlace lds_place(uint16_t *p) { return p; }
+static inline void load_to_lds(Window w, uint32_t offset, LdsPlace to, uint32_t behind)
 {
-    char *const p = (char *)to + 16 * (threadIdx.x & 63u);
-    if (offset >= 0x7FFFFFFFu) memset(p, 0, 16);
-    else memcpy(p, w + offset, 16);
+    char *const p = (char *)to + behind + 16 * (threadIdx.x & 63u);
+    if (offset >= w.bytes) memset(p, 0, 16);
+    else memcpy(p, w.p + offset, 16);
 }
-template <int LEFT> static inline void loads_done() {}
+template <int LEFT> static inline void loads_meet() { __syncthreads(); }
 
 }  // namespace dgs

@@ -13,8 +13,8 @@ EMU = os.path.join(HERE, "emu")
 CLANG = os.environ.get("DGS_HOST_CLANG", "/opt/rocm/llvm/bin/clang++")
 FLAGS = ["-std=c++17", "-O1", "-g", f"-I{EMU}", "-ffp-contract=off", "-fsanitize=address,undefined", "-fno-sanitize-recover=all",
          "-Wno-unknown-attributes", "-Wno-unused-function", "-Wno-array-compare", "-Wno-pass-failed"]
-# the library as it is, and with its largest tiles and smallest pieces of the vocabulary taken at any size
-BUILDS = {"": [], "large": ["-DDGS_HEAD_TILE=0", "-DDGS_HEAD_PIECE=256", "-DDGS_ORTHO_LARGE=1"]}
+# the library as it is, and with one kind of tile, and small pieces of the vocabulary, taken at any size
+BUILDS = {"": [], **{f"tile{t}": [f"-DDGS_PRODUCT_TILE={t}", "-DDGS_HEAD_PIECE=256"] for t in range(4)}}
 
 
 @pytest.fixture(scope="module")
@@ -36,7 +36,7 @@ def programs(tmp_path_factory):
 
 def test_head_kernels_on_the_cpu_under_asan_ubsan(programs):
     env = dict(os.environ, ASAN_OPTIONS="detect_leaks=0:detect_stack_use_after_return=0")
-    runs = [("", "head"), ("", "large"), ("", "ortho"), ("large", "large"), ("large", "ortho")]
+    runs = [("", "head"), ("", "large"), ("", "ortho")] + [(f"tile{t}", what) for t in range(4) for what in ("large", "ortho")]
     procs = [(run, subprocess.Popen([programs[run[0]], run[1]], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, env=env)) for run in runs]
     try:
         for run, p in procs:
