@@ -243,6 +243,13 @@ struct LogitArgs {
     float *bias_parts;               // t_tiles x grad_stride
 };
 
+// Two parts of a row's sum of exponentials, each a maximum and the sum relative to it.
+__device__ __forceinline__ float2 joined(float2 a, float2 b)
+{
+    const float most = max(a.x, b.x), from = most == -__builtin_inff() ? 0.0f : most;
+    return make_float2(most, a.y * power_of_e(a.x - from) + b.y * power_of_e(b.x - from));
+}
+
 // Entries (m) and rows (n) of a tile.
 template <class E, uint32_t M, uint32_t N, uint32_t WAVES_M, uint32_t WAVES_N, uint32_t STAGES, bool BACK>
 __global__ __launch_bounds__(WAVES_M *WAVES_N * 64, WAVES_M *WAVES_N > 4 || STAGES < 4 ? 2 : 1) void k_head_logits(LogitArgs a)
@@ -252,11 +259,17 @@ __global__ __launch_bounds__(WAVES_M *WAVES_N * 64, WAVES_M *WAVES_N > 4 || STAG
     const TilePlace place = place_of_tile(tile_of_block(blockIdx.x, gridDim.x), a.v_tiles, a.t_tiles);
     const uint32_t tile_v = place.m, tile_t = place.n;
     const uint32_t v0 = a.first + tile_v * M, t0 = tile_t * N;
+    __shared__ __attribute__((aligned(16))) float bias[M];
+    if (a.bias) {      // (read behind the product's barriers)
+        for (uint32_t m = threadIdx.x; m < M; m += P::THREADS) bias[m] = a.bias[min(v0 + m, a.end - 1u)];
+    }
     typename P::Sums z;
     P::run(lds, a.w, a.x, v0, t0, 0, a.cols, a.kind, z);
 
     const uint32_t lane = lane_id(), half = lane >> 5, wave = uniform(threadIdx.x >> 6);
-    const uint32_t v_wave = v0 + P::wave_m();
+    // this lane's first entry of the tile; the others are row_in_square(r) + 32 i behind it, `left` of them are there
+    const uint32_t v_lane = v0 + P::wave_m() + 4 * half, left = a.end - min(v_lane, a.end);
+    const bool edge = v0 + M > a.end;
     uint32_t target[P::J];
     bool here[P::J];
 #pragma unroll
@@ -272,39 +285,54 @@ __global__ __launch_bounds__(WAVES_M *WAVES_N * 64, WAVES_M *WAVES_N > 4 || STAG
                 for (uint32_t r = 0; r < 16; ++r) z[i][j][r] = times_power(z[i][j][r], e);
         }
     }
-    // this lane's first entry of the tile; the others are row_in_square(r) + 32 i behind it
-    const uint32_t v_lane = v_wave + 4 * half, left = a.end - min(v_lane, a.end);
     if (a.bias) {
 #pragma unroll
         for (uint32_t i = 0; i < P::I; ++i)
 #pragma unroll
-            for (uint32_t r = 0; r < 16; ++r) {
-                const uint32_t o = 32 * i + row_in_square(r);
-                const float b = o < left ? a.bias[v_lane + o] : 0.0f;
+            for (uint32_t g = 0; g < 4; ++g) {
+                const f32x4 b = *(const f32x4 *)(bias + P::wave_m() + 32 * i + 8 * g + 4 * half);
 #pragma unroll
-                for (uint32_t j = 0; j < P::J; ++j) z[i][j][r] += b;
+                for (uint32_t j = 0; j < P::J; ++j) {
+                    z[i][j][4 * g] += b.x;
+                    z[i][j][4 * g + 1] += b.y;
+                    z[i][j][4 * g + 2] += b.z;
+                    z[i][j][4 * g + 3] += b.w;
+                }
             }
     }
     if constexpr (!BACK) {
         __syncthreads();      // nobody reads operands any more
         float2(*const part)[N] = (float2(*)[N])&lds;
-#pragma unroll
-        for (uint32_t j = 0; j < P::J; ++j) {
-            const uint32_t n = P::wave_n() + 32 * j + (lane & 31u), t = t0 + n;
-            float most = -__builtin_inff(), sum = 0.0f, hit = 0.0f;
-            const uint32_t aim = target[j] - v_lane;      // (where the target lies, if it lies here)
-            bool found = false;
+        if (edge) {
 #pragma unroll
             for (uint32_t i = 0; i < P::I; ++i)
 #pragma unroll
-                for (uint32_t r = 0; r < 16; ++r) {
-                    const uint32_t o = 32 * i + row_in_square(r);
-                    z[i][j][r] = o < left ? z[i][j][r] : -__builtin_inff();
-                    most = max(most, z[i][j][r]);
-                    hit = o == aim ? z[i][j][r] : hit;
-                    found |= o == aim;
-                }
-            if (found && here[j]) a.target_logit[t] = hit;
+                for (uint32_t j = 0; j < P::J; ++j)
+#pragma unroll
+                    for (uint32_t r = 0; r < 16; ++r) z[i][j][r] = 32 * i + row_in_square(r) < left ? z[i][j][r] : -__builtin_inff();
+        }
+#pragma unroll
+        for (uint32_t j = 0; j < P::J; ++j) {
+            const uint32_t n = P::wave_n() + 32 * j + (lane & 31u), t = t0 + n;
+            const uint32_t aim = target[j] - v_lane;      // (where the target lies, if it lies here)
+            if (ballot64(aim < 32 * P::I)) {
+                float hit = 0.0f;
+                bool found = false;
+#pragma unroll
+                for (uint32_t i = 0; i < P::I; ++i)
+#pragma unroll
+                    for (uint32_t r = 0; r < 16; ++r) {
+                        const bool is = 32 * i + row_in_square(r) == aim;
+                        hit = is ? z[i][j][r] : hit;
+                        found |= is;
+                    }
+                if (found && here[j]) a.target_logit[t] = hit;
+            }
+            float most = -__builtin_inff(), sum = 0.0f;
+#pragma unroll
+            for (uint32_t i = 0; i < P::I; ++i)
+#pragma unroll
+                for (uint32_t r = 0; r < 16; ++r) most = max(most, z[i][j][r]);
             most = max(most, other_half(most));
             const float from = most == -__builtin_inff() ? 0.0f : most;
 #pragma unroll
@@ -317,37 +345,40 @@ __global__ __launch_bounds__(WAVES_M *WAVES_N * 64, WAVES_M *WAVES_N > 4 || STAG
         __syncthreads();
         for (uint32_t n = threadIdx.x; n < N; n += P::THREADS) {
             if (t0 + n >= a.rows) continue;
-            float most = part[0][n].x;
+            float2 all = part[0][n];
 #pragma unroll
-            for (uint32_t w = 1; w < WAVES_M; ++w) most = max(most, part[w][n].x);
-            const float from = most == -__builtin_inff() ? 0.0f : most;
-            float sum = 0.0f;
-#pragma unroll
-            for (uint32_t w = 0; w < WAVES_M; ++w) sum += part[w][n].y * power_of_e(part[w][n].x - from);
-            a.stats[(uint64_t)tile_v * a.rows + t0 + n] = make_float2(most, sum);
+            for (uint32_t w = 1; w < WAVES_M; ++w) all = joined(all, part[w][n]);
+            a.stats[(uint64_t)tile_v * a.rows + t0 + n] = all;
         }
     } else {
-        float column[P::I * 16];      // the bias gradient's sums over this lane's rows
-#pragma unroll
-        for (uint32_t i = 0; i < P::I * 16; ++i) column[i] = 0.0f;
+        float weight[P::J];      // what the bias gradient takes of a row
 #pragma unroll
         for (uint32_t j = 0; j < P::J; ++j) {
             const uint32_t t = t0 + P::wave_n() + 32 * j + (lane & 31u);
             HeadRow h = {0.0f, 0.0f, 0.0f, 0};
             if (here[j]) h = a.row_info[t];
+            weight[j] = times_power(1.0f, h.power - GRAD_TOP);
+            // what is not there counts as a logit of -infinity; so does all of a row that nothing arrives at, whatever its logits are
             const bool none = nothing_arrives(h);
+            const uint32_t there = none ? 0u : left;
+            if (none) h.lse = 0.0f;
             const uint32_t aim = target[j] - v_lane;
+            if (edge || ballot64(none)) {
+#pragma unroll
+                for (uint32_t i = 0; i < P::I; ++i)
+#pragma unroll
+                    for (uint32_t r = 0; r < 16; ++r) z[i][j][r] = 32 * i + row_in_square(r) < there ? z[i][j][r] : -__builtin_inff();
+            }
 #pragma unroll
             for (uint32_t i = 0; i < P::I; ++i)
 #pragma unroll
-                for (uint32_t r = 0; r < 16; ++r) {
-                    const uint32_t o = 32 * i + row_in_square(r);
-                    float d = h.pull * power_of_e(z[i][j][r] - h.lse);
-                    d -= o == aim ? h.push : 0.0f;
-                    if (none || o >= left) d = 0.0f;
-                    if (a.bias_parts) column[16 * i + r] += times_power(d, h.power - GRAD_TOP);
-                    z[i][j][r] = d;
-                }
+                for (uint32_t r = 0; r < 16; ++r) z[i][j][r] = h.pull * power_of_e(z[i][j][r] - h.lse);
+            if (ballot64(aim < 32 * P::I)) {
+#pragma unroll
+                for (uint32_t i = 0; i < P::I; ++i)
+#pragma unroll
+                    for (uint32_t r = 0; r < 16; ++r) z[i][j][r] -= 32 * i + row_in_square(r) == aim ? h.push : 0.0f;
+            }
         }
         P::by_columns(lds, z, [&](uint32_t m, uint32_t n, const float (&v)[8]) {
             const uint32_t t = t0 + n, at_v = v0 - a.first + m;
@@ -360,6 +391,13 @@ __global__ __launch_bounds__(WAVES_M *WAVES_N * 64, WAVES_M *WAVES_N > 4 || STAG
         if (a.bias_parts) {
             __syncthreads();
             float(*const part)[M] = (float(*)[M])&lds;
+            float column[P::I * 16];      // the bias gradient's sums over this lane's rows
+#pragma unroll
+            for (uint32_t k = 0; k < P::I * 16; ++k) {
+                column[k] = z[k / 16][0][k % 16] * weight[0];
+#pragma unroll
+                for (uint32_t j = 1; j < P::J; ++j) column[k] = __builtin_fmaf(z[k / 16][j][k % 16], weight[j], column[k]);
+            }
             // over 32 lanes: of every pair of lanes each takes half of the entries, until one or two are left
             uint32_t entry = 0;
 #pragma unroll
@@ -389,13 +427,6 @@ __global__ __launch_bounds__(WAVES_M *WAVES_N * 64, WAVES_M *WAVES_N > 4 || STAG
             }
         }
     }
-}
-
-// Two parts of a row's sum of exponentials, each a maximum and the sum relative to it.
-__device__ __forceinline__ float2 joined(float2 a, float2 b)
-{
-    const float most = max(a.x, b.x), from = most == -__builtin_inff() ? 0.0f : most;
-    return make_float2(most, a.y * power_of_e(a.x - from) + b.y * power_of_e(b.x - from));
 }
 
 // A row's lse and loss from its tiles' parts.  `apart` lanes a row (a power of two), 256 / apart rows.
@@ -553,16 +584,15 @@ static ProductPlan product_plan(uint32_t m, uint32_t n, uint32_t depth, uint32_t
 {
     ProductPlan best = {};
     float least = 0.0f;
-    // (at least four steps to a split; a split's sums are written and read)
-    const uint32_t steps = depth ? tiles_of(depth, PRODUCT_STEP) : 1u, most = steps / 4 > 16 ? 16 : steps / 4 < 1 ? 1 : steps / 4;
+    const uint32_t steps = depth ? tiles_of(depth, PRODUCT_STEP) : 1u, most = splits_tried(steps, 16);
     for (uint32_t s = 1; s <= most; ++s) {
         const uint32_t each = (steps + s - 1) / s;
         if ((steps + each - 1) / each != s) continue;
         float us = 0.0f;
         const int tile = product_tile([=](uint32_t high, uint32_t wide) { return (uint64_t)tiles_of(m, high) * tiles_of(n, wide) * s; },
                                       steps_of(each * PRODUCT_STEP, kind), tall, us);
-        if (s > 1) us += 3.0f + (float)s * (float)m * (float)n * 8.0f / 4.5e6f;
-        if (least == 0.0f || us < least) {
+        if (s > 1) us += 3.0f + (float)s * (float)m * (float)n * 8.0f / 4.5e6f;      // (a split's sums are written and read)
+        if (least == 0.0f || us < least || MOST_SPLITS) {
             least = us;
             best = ProductPlan{tile, s, each * PRODUCT_STEP, kind};
         }

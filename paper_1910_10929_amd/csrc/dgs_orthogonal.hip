@@ -140,6 +140,9 @@ struct SquareArgs {
     Halves x;                // both operands: rows of it by rows of it
     uint32_t depth, kind;
     uint32_t size, tiles;    // of the result, and tiles along a side
+    uint32_t count;          // matrices
+    uint32_t split_depth;    // of a split of the sum; as long as it is for a single one
+    float *sums;             // with several: size x out.stride for each split and matrix, on and below the diagonal
     const float *log2_norm;  // of each X at the start; absent: nothing was lifted
     float growth;            // of X since
     Halves out;              // lo: absent where products take the first halves
@@ -149,6 +152,45 @@ struct SquareArgs {
     float a, b, c;
 };
 
+// What becomes of a row's eight sums from column n on: A, or the polynomial without its diagonal.
+template <bool POLY>
+__device__ __forceinline__ void finish8(const SquareArgs &a, uint32_t which, uint32_t m, uint32_t n, int power, const u32x4 &gram_hi,
+                                        const u32x4 &gram_lo, float (&v)[8])
+{
+#pragma unroll
+    for (uint32_t k = 0; k < 8; ++k) {
+        v[k] = times_power(v[k], power);
+        if constexpr (POLY) {
+            const float gram = value_of((uint16_t)(gram_hi[k >> 1] >> (16 * (k & 1)))) + value_of((uint16_t)(gram_lo[k >> 1] >> (16 * (k & 1))));
+            v[k] = a.b * gram + a.c * v[k];
+        }
+    }
+    if constexpr (POLY) {
+        if (n <= m && m < n + 8) {
+#pragma unroll
+            for (uint32_t k = 0; k < 8; ++k)
+                if (n + k == m) {
+                    if (m < a.size) a.diagonal[which * a.size + m] = a.a + v[k] * LEFT;
+                    v[k] = 0.0f;
+                }
+        }
+    }
+}
+// A's row m, columns n to n + 7.
+__device__ __forceinline__ void gram8(const SquareArgs &a, uint64_t from, uint32_t m, uint32_t n, u32x4 &hi, u32x4 &lo)
+{
+    const u32x4 none = {0, 0, 0, 0};
+    hi = lo = none;
+    if (m < a.size && n < a.gram.stride) {
+        hi = *(const u32x4 *)(a.gram.hi + from + m * a.gram.stride + n);
+        if (a.gram.lo) lo = *(const u32x4 *)(a.gram.lo + from + m * a.gram.stride + n);
+    }
+}
+__device__ __forceinline__ int power_of_sums(const SquareArgs &a, uint32_t which)
+{
+    return -12 - (a.log2_norm ? 2 * lift_of(a.log2_norm[which], a.growth) : 0);
+}
+
 // The symmetric product of X with itself (POLY: of A with itself, from which the polynomial is made).
 template <uint32_t M, uint32_t WAVES_M, uint32_t WAVES_N, uint32_t STAGES, bool POLY>
 __global__ __launch_bounds__(WAVES_M *WAVES_N * 64, WAVES_M *WAVES_N > 4 || STAGES < 4 ? 2 : 1) void k_ortho_square(SquareArgs a)
@@ -157,47 +199,89 @@ __global__ __launch_bounds__(WAVES_M *WAVES_N * 64, WAVES_M *WAVES_N > 4 || STAG
     __shared__ __attribute__((aligned(16))) typename P::Lds lds;
     // tiles on and below the diagonal, row by row
     const uint32_t count = a.tiles * (a.tiles + 1) / 2;
-    const uint32_t all = tile_of_block(blockIdx.x, gridDim.x), which = all / count, at = all - which * count;
+    const uint32_t all = tile_of_block(blockIdx.x, gridDim.x), each = all / count, at = all - each * count;
+    const uint32_t split = each / a.count, which = each - split * a.count;
     uint32_t tile_m = 0, passed = 0;
     while (passed + tile_m + 1 <= at) passed += ++tile_m;
     const uint32_t tile_n = at - passed;
     const Side side = {{a.x.hi + which * a.x.size, a.x.lo ? a.x.lo + which * a.x.size : nullptr}, a.x.stride, a.size};
+    const uint32_t first = split * a.split_depth;
     typename P::Sums s;
-    P::run(lds, side, side, tile_m * M, tile_n * M, 0, a.depth, a.kind, s);
+    P::run(lds, side, side, tile_m * M, tile_n * M, first, min(first + a.split_depth, a.depth), a.kind, s);
+    if (a.sums) {
+        float *const sums = a.sums + (uint64_t)each * a.size * a.out.stride;
+        P::by_rows(lds, s, [&](uint32_t, uint32_t, uint32_t) {}, [&](uint32_t, uint32_t row, uint32_t col, float (&v)[8]) {
+            const uint32_t m = tile_m * M + row, n = tile_n * M + col;
+            if (m >= a.size || n >= a.out.stride) return;
+            f32x4 w;
+            w.x = v[0]; w.y = v[1]; w.z = v[2]; w.w = v[3];
+            *(f32x4 *)(sums + m * a.out.stride + n) = w;
+            w.x = v[4]; w.y = v[5]; w.z = v[6]; w.w = v[7];
+            *(f32x4 *)(sums + m * a.out.stride + n + 4) = w;
+        });
+        return;
+    }
     const uint64_t base = which * a.out.size, from = which * a.gram.size;
-    const int power = -12 - (a.log2_norm ? 2 * lift_of(a.log2_norm[which], a.growth) : 0);
+    const int power = power_of_sums(a, which);
     u32x4 gram_hi[P::PASSES], gram_lo[P::PASSES];
     // (the result's columns are a multiple of eight, those beyond its rows zeros)
     P::by_rows(lds, s, [&](uint32_t p, uint32_t row, uint32_t col) {
-        if constexpr (POLY) {
-            const uint32_t m = tile_m * M + row, n = tile_n * M + col;
-            const u32x4 none = {0, 0, 0, 0};
-            gram_hi[p] = gram_lo[p] = none;
-            if (m < a.size && n < a.gram.stride) {
-                gram_hi[p] = *(const u32x4 *)(a.gram.hi + from + m * a.gram.stride + n);
-                if (a.gram.lo) gram_lo[p] = *(const u32x4 *)(a.gram.lo + from + m * a.gram.stride + n);
-            }
-        }
+        if constexpr (POLY) gram8(a, from, tile_m * M + row, tile_n * M + col, gram_hi[p], gram_lo[p]);
     }, [&](uint32_t p, uint32_t row, uint32_t col, float (&v)[8], float *back) {
         const uint32_t m = tile_m * M + row, n = tile_n * M + col;
+        finish8<POLY>(a, which, m, n, power, gram_hi[p], gram_lo[p], v);
 #pragma unroll
-        for (uint32_t k = 0; k < 8; ++k) {
-            v[k] = times_power(v[k], power);
-            if constexpr (POLY) {
-                const float gram = value_of((uint16_t)(gram_hi[p][k >> 1] >> (16 * (k & 1)))) + value_of((uint16_t)(gram_lo[p][k >> 1] >> (16 * (k & 1))));
-                v[k] = a.b * gram + a.c * v[k];
-                if (n + k == m) {
-                    if (m < a.size) a.diagonal[which * a.size + m] = a.a + v[k] * LEFT;
-                    v[k] = 0.0f;
-                }
-            }
-            back[k] = v[k];
-        }
+        for (uint32_t k = 0; k < 8; ++k) back[k] = v[k];
         if (m < a.size && n < a.out.stride) put_halves(a.out, base + m * a.out.stride + n, v);
     }, [&](uint32_t row, uint32_t col, const float (&v)[8]) {      // the other side of the diagonal
         const uint32_t m = tile_m * M + row, n = tile_n * M + col;
         if (tile_m != tile_n && n < a.size && m < a.out.stride) put_halves(a.out, base + n * a.out.stride + m, v);
     });
+}
+
+// The same from several splits' sums: 64 x 64 of the result, on or below the diagonal, to a workgroup.
+template <bool POLY> __global__ __launch_bounds__(256) void k_ortho_join(SquareArgs a, uint32_t splits, uint32_t tiles)
+{
+    __shared__ float turned[64][65];
+    const uint32_t count = tiles * (tiles + 1) / 2;
+    const uint32_t which = blockIdx.x / count, at = blockIdx.x - which * count;
+    uint32_t tile_m = 0, passed = 0;
+    while (passed + tile_m + 1 <= at) passed += ++tile_m;
+    const uint32_t tile_n = at - passed;
+    const uint64_t base = which * a.out.size, from = which * a.gram.size, apart = (uint64_t)a.count * a.size * a.out.stride;
+    const int power = power_of_sums(a, which);
+    const uint32_t c = (threadIdx.x & 7u) * 8, n = tile_n * 64 + c;
+    const bool column = n < a.out.stride;
+#pragma unroll
+    for (uint32_t i = 0; i < 64; i += 32) {
+        const uint32_t r = i + (threadIdx.x >> 3), m = tile_m * 64 + r;
+        float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+        u32x4 hi = {0, 0, 0, 0}, lo = hi;
+        if constexpr (POLY) gram8(a, from, m, n, hi, lo);
+        if (m < a.size && column) {
+            const float *const p = a.sums + ((uint64_t)which * a.size + m) * a.out.stride + n;
+            for (uint32_t s = 0; s < splits; ++s) {
+                const f32x4 x = *(const f32x4 *)(p + s * apart), y = *(const f32x4 *)(p + s * apart + 4);
+                v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
+                v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
+            }
+            finish8<POLY>(a, which, m, n, power, hi, lo, v);
+            put_halves(a.out, base + m * a.out.stride + n, v);
+        }
+#pragma unroll
+        for (uint32_t k = 0; k < 8; ++k) turned[r][c + k] = v[k];
+    }
+    __syncthreads();
+    if (tile_m == tile_n) return;
+#pragma unroll
+    for (uint32_t i = 0; i < 64; i += 32) {
+        const uint32_t r = i + (threadIdx.x >> 3), row = tile_n * 64 + r, col = tile_m * 64 + c;
+        if (row >= a.size || col >= a.out.stride) continue;
+        float v[8];
+#pragma unroll
+        for (uint32_t k = 0; k < 8; ++k) v[k] = turned[c + k][r];
+        put_halves(a.out, base + row * a.out.stride + col, v);
+    }
 }
 
 struct StepArgs {
@@ -290,12 +374,38 @@ __global__ __launch_bounds__(WAVES_M *WAVES_N * 64, WAVES_M *WAVES_N > 4 || STAG
 // host side
 // ---------------------------------------------------------------------------
 
+// A symmetric product's tile, and how many splits of its sum another launch adds up.
+struct SquarePlan {
+    int tile;
+    uint32_t splits, split_depth;
+};
+static SquarePlan square_plan(uint32_t size, uint32_t depth, uint32_t pairs, uint32_t count)
+{
+    SquarePlan best = {};
+    float least = 0.0f;
+    const uint32_t steps = tiles_of(depth, PRODUCT_STEP), most = splits_tried(steps, 8);
+    for (uint32_t s = 1; s <= most; ++s) {
+        const uint32_t each = (steps + s - 1) / s;
+        if ((steps + each - 1) / each != s) continue;
+        float us = 0.0f;
+        const int tile = product_tile([=](uint32_t high, uint32_t) { const uint64_t t = tiles_of(size, high); return t * (t + 1) / 2 * count * s; },
+                                      each * pairs, false, us);
+        // (the sums of half the square and more are written and read)
+        if (s > 1) us += 6.0f + (float)s * (float)count * (float)size * (float)size * 5.0f / 4.5e6f;
+        if (least == 0.0f || us < least || MOST_SPLITS) {
+            least = us;
+            best = SquarePlan{tile, s, each * PRODUCT_STEP};
+        }
+    }
+    return best;
+}
 struct OrthoPlan {
     uint32_t rows, cols, at_once;      // of X, and matrices of a launch
     bool turned, two;
     Halves x[2], gram, poly;
     double *norm;
-    float *diagonal, *log2_norm;
+    float *diagonal, *log2_norm, *sums;
+    SquarePlan square, poly_square;      // of X with itself, of A with itself
     uint64_t bytes;
 };
 static OrthoPlan ortho_plan(const dgs_orthogonalise_args &p)
@@ -324,6 +434,10 @@ static OrthoPlan ortho_plan(const dgs_orthogonalise_args &p)
     o.norm = (double *)s.take(sizeof(double) * NORM_PARTS * o.at_once);
     o.diagonal = (float *)s.take(4ull * o.rows * o.at_once);
     o.log2_norm = (float *)s.take(4ull * o.at_once);
+    o.square = square_plan(o.rows, o.cols, o.two ? 3 : 1, o.at_once);
+    o.poly_square = square_plan(o.rows, o.rows, o.two ? 3 : 1, o.at_once);
+    const uint32_t splits = o.square.splits > o.poly_square.splits ? o.square.splits : o.poly_square.splits;
+    if (splits > 1) o.sums = (float *)s.take(4ull * splits * o.at_once * o.rows * small);
     o.bytes = s.used;
     return o;
 }
@@ -352,12 +466,20 @@ template <class T, bool TURNED> static void launch_step(const StepArgs &s, const
     else if (tile == TILE_128) hipLaunchKernelGGL((k_ortho_step<128, 2, 2, 2, T, TURNED>), grid, dim3(256), 0, st, s, out);
     else hipLaunchKernelGGL((k_ortho_step<64, 2, 2, 4, T, TURNED>), grid, dim3(256), 0, st, s, out);
 }
-template <bool POLY> static void launch_square(const SquareArgs &a, int tile, uint32_t count, hipStream_t st)
+template <bool POLY> static void launch_square(SquareArgs a, const SquarePlan &plan, float *sums, hipStream_t st)
 {
-    const dim3 grid(a.tiles * (a.tiles + 1) / 2 * count);
+    a.tiles = tiles_of(a.size, tile_high(plan.tile));
+    a.split_depth = plan.split_depth;
+    a.sums = plan.splits > 1 ? sums : nullptr;
+    const int tile = plan.tile;
+    const dim3 grid(a.tiles * (a.tiles + 1) / 2 * a.count * plan.splits);
     if (tile == TILE_256) hipLaunchKernelGGL((k_ortho_square<256, 2, 4, 2, POLY>), grid, dim3(512), 0, st, a);
     else if (tile == TILE_128) hipLaunchKernelGGL((k_ortho_square<128, 2, 2, 2, POLY>), grid, dim3(256), 0, st, a);
     else hipLaunchKernelGGL((k_ortho_square<64, 2, 2, 4, POLY>), grid, dim3(256), 0, st, a);
+    if (plan.splits > 1) {
+        const uint32_t tiles = tiles_of(a.size, 64);
+        hipLaunchKernelGGL(k_ortho_join<POLY>, dim3(tiles * (tiles + 1) / 2 * a.count), dim3(256), 0, st, a, plan.splits, tiles);
+    }
 }
 template <class T> static void launch_last(const StepArgs &s, const Matrices &out, bool turned, int tile, uint32_t count, hipStream_t st)
 {
@@ -403,13 +525,9 @@ extern "C" int dgs_orthogonalise(const dgs_orthogonalise_args *args, void *hip_s
         else if (p.type == DGS_F16) load_matrices<f16>(in, p, o, count, st);
         else load_matrices<bf16>(in, p, o, count, st);
         const uint32_t kind = o.two ? BOTH_IN_TWO : ONE_PAIR;
-        const uint32_t pairs = o.two ? 3 : 1;
-        auto half_of = [&](uint32_t size, uint32_t) { const uint64_t t = tiles_of(o.rows, size); return t * (t + 1) / 2 * count; };
-        auto all_of = [&](uint32_t high, uint32_t wide) { return (uint64_t)tiles_of(o.rows, high) * tiles_of(o.cols, wide) * count; };
-        const uint32_t long_steps = tiles_of(o.cols, PRODUCT_STEP) * pairs, short_steps = tiles_of(o.rows, PRODUCT_STEP) * pairs;
-        float us[3] = {};
-        const int gram_tile = product_tile(half_of, long_steps, false, us[0]), poly_tile = product_tile(half_of, short_steps, false, us[1]),
-                  step_tile = product_tile(all_of, short_steps, false, us[2]);
+        float us = 0.0f;
+        const int step_tile = product_tile([&](uint32_t high, uint32_t wide) { return (uint64_t)tiles_of(o.rows, high) * tiles_of(o.cols, wide) * count; },
+                                           tiles_of(o.rows, PRODUCT_STEP) * (o.two ? 3u : 1u), false, us);
         const float grows = p.a != 0.0f ? log2f(fabsf(p.a)) : 0.0f;
         for (uint32_t step = 0; step < p.steps; ++step) {
             SquareArgs g = {};
@@ -417,11 +535,11 @@ extern "C" int dgs_orthogonalise(const dgs_orthogonalise_args *args, void *hip_s
             g.depth = o.cols;
             g.kind = kind;
             g.size = o.rows;
-            g.tiles = tiles_of(o.rows, tile_high(gram_tile));
+            g.count = count;
             g.out = o.gram;
             g.log2_norm = o.log2_norm;
             g.growth = (float)step * grows;
-            launch_square<false>(g, gram_tile, count, st);
+            launch_square<false>(g, o.square, o.sums, st);
             g.x = o.gram;
             g.log2_norm = nullptr;
             g.depth = o.rows;
@@ -431,8 +549,7 @@ extern "C" int dgs_orthogonalise(const dgs_orthogonalise_args *args, void *hip_s
             g.a = p.a;
             g.b = p.b;
             g.c = p.c;
-            g.tiles = tiles_of(o.rows, tile_high(poly_tile));
-            launch_square<true>(g, poly_tile, count, st);
+            launch_square<true>(g, o.poly_square, o.sums, st);
             StepArgs s = {};
             s.poly = o.poly;
             s.x = o.x[step & 1u];

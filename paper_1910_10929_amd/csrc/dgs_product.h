@@ -418,15 +418,18 @@ __device__ __forceinline__ uint32_t bits_of(f16 a, f16 b)
 }
 
 // Eight values as halves, in one part or two.
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef f16 f16x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ void halves8(const float (&v)[8], u32x4 &hi, u32x4 &lo)
 {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        f16 a, b, c, d;
-        halves_of(v[2 * i], a, b);
-        halves_of(v[2 * i + 1], c, d);
-        hi[i] = bits_of(a, c);
-        lo[i] = bits_of(b, d);
+        const f32x2 w = {v[2 * i], v[2 * i + 1]};
+        const f16x2 h = __builtin_convertvector(w, f16x2);
+        const f32x2 left = {w.x - (float)h.x, w.y - (float)h.y};
+        const f16x2 l = __builtin_convertvector(left, f16x2);
+        hi[i] = __builtin_bit_cast(uint32_t, h);
+        lo[i] = __builtin_bit_cast(uint32_t, l);
     }
 }
 
@@ -489,5 +492,19 @@ template <class Tiles> static int product_tile(Tiles tiles, uint32_t steps, bool
     }
     return best;
 }
+
+// How many splits of a sum of `steps` steps are tried: four steps each at least, `most` splits.  (A CPU build may ask for a number.)
+static inline uint32_t splits_tried(uint32_t steps, uint32_t most)
+{
+#ifdef DGS_PRODUCT_SPLITS
+    return steps < DGS_PRODUCT_SPLITS ? steps : DGS_PRODUCT_SPLITS;
+#endif
+    return steps / 4 > most ? most : steps / 4 < 1 ? 1u : steps / 4;
+}
+#ifdef DGS_PRODUCT_SPLITS
+constexpr bool MOST_SPLITS = true;      // the last number that is tried
+#else
+constexpr bool MOST_SPLITS = false;     // the one with the least time
+#endif
 
 }  // namespace dgs

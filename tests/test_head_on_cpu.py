@@ -13,8 +13,8 @@ EMU = os.path.join(HERE, "emu")
 CLANG = os.environ.get("DGS_HOST_CLANG", "/opt/rocm/llvm/bin/clang++")
 FLAGS = ["-std=c++17", "-O1", "-g", f"-I{EMU}", "-ffp-contract=off", "-fsanitize=address,undefined", "-fno-sanitize-recover=all",
          "-Wno-unknown-attributes", "-Wno-unused-function", "-Wno-array-compare", "-Wno-pass-failed"]
-# the library as it is, and with one kind of tile, and small pieces of the vocabulary, taken at any size
-BUILDS = {"": [], **{f"tile{t}": [f"-DDGS_PRODUCT_TILE={t}", "-DDGS_HEAD_PIECE=256"] for t in range(4)}}
+# the library as it is, and with one kind of tile, small pieces of the vocabulary and split sums taken at any size
+BUILDS = {"": [], **{f"tile{t}": [f"-DDGS_PRODUCT_TILE={t}", "-DDGS_HEAD_PIECE=256", f"-DDGS_PRODUCT_SPLITS={1 + t % 3}"] for t in range(4)}}
 
 
 @pytest.fixture(scope="module")
