@@ -252,7 +252,7 @@ __device__ __forceinline__ float2 joined(float2 a, float2 b)
 
 // Entries (m) and rows (n) of a tile.
 template <class E, uint32_t M, uint32_t N, uint32_t WAVES_M, uint32_t WAVES_N, uint32_t STAGES, bool BACK>
-__global__ __launch_bounds__(WAVES_M *WAVES_N * 64, WAVES_M *WAVES_N > 4 || STAGES < 4 ? 2 : 1) void k_head_logits(LogitArgs a)
+__global__ __launch_bounds__(WAVES_M *WAVES_N * 64, 2) void k_head_logits(LogitArgs a)
 {
     typedef Product<E, M, N, WAVES_M, WAVES_N, false, false, STAGES, M == 256 && N == 128 ? 32 : PRODUCT_STEP> P;
     __shared__ __attribute__((aligned(16))) typename P::Lds lds;
@@ -474,7 +474,7 @@ struct GradientArgs {
 
 // TURN_A: the first operand's k lies outside.  (The second's always does.)
 template <uint32_t M, uint32_t N, uint32_t WAVES_M, uint32_t WAVES_N, uint32_t STAGES, bool TURN_A>
-__global__ __launch_bounds__(WAVES_M *WAVES_N * 64, WAVES_M *WAVES_N > 4 || STAGES < 4 ? 2 : 1) void k_head_product(GradientArgs a)
+__global__ __launch_bounds__(WAVES_M *WAVES_N * 64, 2) void k_head_product(GradientArgs a)
 {
     typedef Product<f16, M, N, WAVES_M, WAVES_N, TURN_A, true, STAGES, M == 256 && N == 128 ? 32 : PRODUCT_STEP> P;
     __shared__ __attribute__((aligned(16))) typename P::Lds lds;
@@ -483,15 +483,17 @@ __global__ __launch_bounds__(WAVES_M *WAVES_N * 64, WAVES_M *WAVES_N > 4 || STAG
     const TilePlace place = place_of_tile(at - split * tiles, a.m_tiles, a.n_tiles);
     const uint32_t tile_m = place.m, tile_n = place.n;
     const uint32_t first = min(split * a.split_depth, a.depth), end = min(first + a.split_depth, a.depth);
-    typename P::Sums s;
-    P::run(lds, a.a, a.b, tile_m * M, tile_n * N, first, end, a.kind, s);
     float *const out = a.out + (a.whole ? 0u : (uint64_t)split * a.m * a.out_stride);
-    const int e = a.whole ? -GRAD_TOP - a.scales->x : 0;
     float old[P::PASSES][8];
-    P::by_rows(lds, s, [&](uint32_t p, uint32_t row, uint32_t col) {
+    auto look = [&](uint32_t p, uint32_t row, uint32_t col) {
         const uint32_t m = tile_m * M + row, n = tile_n * N + col, count = m < a.m ? live8(n, a.n) : 0u;
         if (a.add && count) load8_f32(out + m * a.out_stride + n, count, old[p]);
-    }, [&](uint32_t p, uint32_t row, uint32_t col, float (&v)[8]) {
+    };
+    P::look_early(look);
+    typename P::Sums s;
+    P::run(lds, a.a, a.b, tile_m * M, tile_n * N, first, end, a.kind, s);
+    const int e = a.whole ? -GRAD_TOP - a.scales->x : 0;
+    P::by_rows(lds, s, look, [&](uint32_t p, uint32_t row, uint32_t col, float (&v)[8]) {
         const uint32_t m = tile_m * M + row, n = tile_n * N + col, count = m < a.m ? live8(n, a.n) : 0u;
         if (count == 0) return;
 #pragma unroll
@@ -573,14 +575,14 @@ static int logits_tile(uint32_t vocab, uint32_t rows, uint32_t steps)
 {
     if (rows <= 32) return TILE_FEW;
     float us = 0.0f;
-    return product_tile([=](uint32_t high, uint32_t wide) { return (uint64_t)tiles_of(vocab, high) * tiles_of(rows, wide); }, steps, false, us);
+    return product_tile([=](uint32_t high, uint32_t wide) { return (uint64_t)tiles_of(vocab, high) * tiles_of(rows, wide); }, steps, TILE_256, us);
 }
 // A gradient's product: its tile, and how many splits of the sum are added up by a launch of their own.
 struct ProductPlan {
     int tile;
     uint32_t splits, split_depth, kind;
 };
-static ProductPlan product_plan(uint32_t m, uint32_t n, uint32_t depth, uint32_t kind, bool tall)
+static ProductPlan product_plan(uint32_t m, uint32_t n, uint32_t depth, uint32_t kind, int more)
 {
     ProductPlan best = {};
     float least = 0.0f;
@@ -590,7 +592,7 @@ static ProductPlan product_plan(uint32_t m, uint32_t n, uint32_t depth, uint32_t
         if ((steps + each - 1) / each != s) continue;
         float us = 0.0f;
         const int tile = product_tile([=](uint32_t high, uint32_t wide) { return (uint64_t)tiles_of(m, high) * tiles_of(n, wide) * s; },
-                                      steps_of(each * PRODUCT_STEP, kind), tall, us);
+                                      steps_of(each * PRODUCT_STEP, kind), more, us);
         if (s > 1) us += 3.0f + (float)s * (float)m * (float)n * 8.0f / 4.5e6f;      // (a split's sums are written and read)
         if (least == 0.0f || us < least || MOST_SPLITS) {
             least = us;
@@ -670,8 +672,8 @@ static HeadPlan plan_of(const dgs_head_args &p, bool back)
         h.grad[0] = (uint16_t *)s.take(p.rows * stride * 2);
         h.grad[1] = (uint16_t *)s.take(p.rows * stride * 2);
         if (p.dbias) h.bias_parts = (float *)s.take(tiles_of(p.rows, tile.n) * stride * 4);
-        h.dx = product_plan(p.rows, p.cols, h.piece, f32 ? BOTH_IN_TWO : p.type == DGS_F16 ? FIRST_IN_TWO : ONE_PAIR, false);
-        h.dw = product_plan(h.piece, p.cols, p.rows, f32 ? BOTH_IN_TWO : FIRST_IN_TWO, true);
+        h.dx = product_plan(p.rows, p.cols, h.piece, f32 ? BOTH_IN_TWO : p.type == DGS_F16 ? FIRST_IN_TWO : ONE_PAIR, TILE_256);
+        h.dw = product_plan(h.piece, p.cols, p.rows, f32 ? BOTH_IN_TWO : FIRST_IN_TWO, TILE_TALL);
         if (h.wants_dx) h.dx_sums = (float *)s.take((uint64_t)h.dx.splits * p.rows * p.cols * 4);
         if (h.wants_dw && h.dw.splits > 1) h.dw_sums = (float *)s.take((uint64_t)h.dw.splits * h.piece * p.cols * 4);
         if (h.scale_w && !f32) h.w[1] = (uint16_t *)s.take(w_bytes);      // (of bfloat16: W in half, for dx)
@@ -715,7 +717,7 @@ template <class E, bool BACK> static void logits(const LogitArgs &a, int tile, h
     if (tile == TILE_256) hipLaunchKernelGGL((k_head_logits<E, 256, 256, 2, 4, 2, BACK>), grid, dim3(512), 0, st, a);
     else if (tile == TILE_128) hipLaunchKernelGGL((k_head_logits<E, 128, 128, 2, 2, 2, BACK>), grid, dim3(256), 0, st, a);
     else if (tile == TILE_64) hipLaunchKernelGGL((k_head_logits<E, 64, 64, 2, 2, 4, BACK>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((k_head_logits<E, 128, 32, 4, 1, 4, BACK>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((k_head_logits<E, 128, 32, 4, 1, 3, BACK>), grid, dim3(256), 0, st, a);
 }
 template <bool BACK> static void logits(const LogitArgs &a, int type, int tile, hipStream_t st)
 {

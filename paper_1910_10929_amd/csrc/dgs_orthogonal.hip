@@ -55,6 +55,14 @@ __device__ __forceinline__ uint16_t half_bits(f16 h)
     return b;
 }
 
+__device__ __forceinline__ void put_halves(const Halves &to, uint64_t at, const float (&v)[8])
+{
+    u32x4 hi, lo;
+    halves8(v, hi, lo);
+    *(u32x4 *)(to.hi + at) = hi;
+    if (to.lo) *(u32x4 *)(to.lo + at) = lo;
+}
+
 // Sums of squares, NORM_PARTS a matrix.
 template <class T>
 __global__ __launch_bounds__(256) void k_ortho_norm(Matrices in, uint32_t rows, uint32_t cols, double *parts)
@@ -103,37 +111,32 @@ __global__ __launch_bounds__(256) void k_ortho_load(Matrices in, uint32_t rows, 
     const T *const m = (const T *)in.data[which];
     const uint64_t stride = in.stride[which];
     const uint32_t r0 = blockIdx.x / across * 64, c0 = blockIdx.x % across * 64;      // of G
-    const uint32_t c = c0 + (threadIdx.x & 63u);
-    for (uint32_t i = threadIdx.x >> 6; i < 64; i += 4) {
-        const uint32_t r = r0 + i;
-        tile[i][threadIdx.x & 63u] = r < rows && c < cols ? (float)((double)to_float(m[r * stride + c]) * by) : 0.0f;
+    const uint32_t c = (threadIdx.x & 7u) * 8, n = live8(c0 + c, cols);
+    Raw8<T> raw[2];
+#pragma unroll
+    for (uint32_t i = 0; i < 2; ++i) {
+        const uint32_t r = r0 + 32 * i + (threadIdx.x >> 3);
+        raw[i] = load8(m + (r < rows && n ? r * stride + c0 + c : 0u), r < rows ? n : 0u);
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < 2; ++i) {
+        float v[8];
+        unpack8(raw[i], v);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) tile[32 * i + (threadIdx.x >> 3)][c + k] = (float)((double)v[k] * by);
     }
     __syncthreads();
     const uint32_t x_rows = turned ? cols : rows;
     const uint32_t first_row = turned ? c0 : r0, first_col = turned ? r0 : c0;
-    for (uint32_t at = threadIdx.x; at < 64 * 16; at += 256) {
-        const uint32_t i = at >> 4, q = (at & 15u) * 4;
-        if (first_row + i >= x_rows || first_col + q >= x.stride) continue;
-        f16 hi[4], lo[4];
 #pragma unroll
-        for (uint32_t k = 0; k < 4; ++k) halves_of(turned ? tile[q + k][i] : tile[i][q + k], hi[k], lo[k]);
-        const uint64_t to = which * x.size + (first_row + i) * x.stride + first_col + q;
-        u32x2 o;
-        o[0] = bits_of(hi[0], hi[1]);
-        o[1] = bits_of(hi[2], hi[3]);
-        *(u32x2 *)(x.hi + to) = o;
-        o[0] = bits_of(lo[0], lo[1]);
-        o[1] = bits_of(lo[2], lo[3]);
-        *(u32x2 *)(x.lo + to) = o;
+    for (uint32_t at = threadIdx.x; at < 64 * 8; at += 256) {
+        const uint32_t i = at >> 3, q = (at & 7u) * 8;
+        if (first_row + i >= x_rows || first_col + q >= x.stride) continue;
+        float v[8];
+#pragma unroll
+        for (uint32_t k = 0; k < 8; ++k) v[k] = turned ? tile[q + k][i] : tile[i][q + k];
+        put_halves(x, which * x.size + (first_row + i) * x.stride + first_col + q, v);
     }
-}
-
-__device__ __forceinline__ void put_halves(const Halves &to, uint64_t at, const float (&v)[8])
-{
-    u32x4 hi, lo;
-    halves8(v, hi, lo);
-    *(u32x4 *)(to.hi + at) = hi;
-    if (to.lo) *(u32x4 *)(to.lo + at) = lo;
 }
 
 struct SquareArgs {
@@ -193,7 +196,7 @@ __device__ __forceinline__ int power_of_sums(const SquareArgs &a, uint32_t which
 
 // The symmetric product of X with itself (POLY: of A with itself, from which the polynomial is made).
 template <uint32_t M, uint32_t WAVES_M, uint32_t WAVES_N, uint32_t STAGES, bool POLY>
-__global__ __launch_bounds__(WAVES_M *WAVES_N * 64, WAVES_M *WAVES_N > 4 || STAGES < 4 ? 2 : 1) void k_ortho_square(SquareArgs a)
+__global__ __launch_bounds__(WAVES_M *WAVES_N * 64, M == 192 ? 1 : 2) void k_ortho_square(SquareArgs a)
 {
     typedef Product<f16, M, M, WAVES_M, WAVES_N, false, false, STAGES> P;
     __shared__ __attribute__((aligned(16))) typename P::Lds lds;
@@ -206,6 +209,12 @@ __global__ __launch_bounds__(WAVES_M *WAVES_N * 64, WAVES_M *WAVES_N > 4 || STAG
     const uint32_t tile_n = at - passed;
     const Side side = {{a.x.hi + which * a.x.size, a.x.lo ? a.x.lo + which * a.x.size : nullptr}, a.x.stride, a.size};
     const uint32_t first = split * a.split_depth;
+    const uint64_t base = which * a.out.size, from = which * a.gram.size;
+    u32x4 gram_hi[P::PASSES], gram_lo[P::PASSES];
+    auto look = [&](uint32_t p, uint32_t row, uint32_t col) {
+        if constexpr (POLY) gram8(a, from, tile_m * M + row, tile_n * M + col, gram_hi[p], gram_lo[p]);
+    };
+    P::look_early(look);
     typename P::Sums s;
     P::run(lds, side, side, tile_m * M, tile_n * M, first, min(first + a.split_depth, a.depth), a.kind, s);
     if (a.sums) {
@@ -221,13 +230,9 @@ __global__ __launch_bounds__(WAVES_M *WAVES_N * 64, WAVES_M *WAVES_N > 4 || STAG
         });
         return;
     }
-    const uint64_t base = which * a.out.size, from = which * a.gram.size;
     const int power = power_of_sums(a, which);
-    u32x4 gram_hi[P::PASSES], gram_lo[P::PASSES];
     // (the result's columns are a multiple of eight, those beyond its rows zeros)
-    P::by_rows(lds, s, [&](uint32_t p, uint32_t row, uint32_t col) {
-        if constexpr (POLY) gram8(a, from, tile_m * M + row, tile_n * M + col, gram_hi[p], gram_lo[p]);
-    }, [&](uint32_t p, uint32_t row, uint32_t col, float (&v)[8], float *back) {
+    P::by_rows(lds, s, look, [&](uint32_t p, uint32_t row, uint32_t col, float (&v)[8], float *back) {
         const uint32_t m = tile_m * M + row, n = tile_n * M + col;
         finish8<POLY>(a, which, m, n, power, gram_hi[p], gram_lo[p], v);
 #pragma unroll
@@ -308,7 +313,7 @@ template <class T> __device__ __forceinline__ void put8(T *p, uint32_t count, fl
 // X of the next step: its rows times the polynomial's diagonal, plus the product of the rest with it.
 // T: the result's type in the last step, void in the others; TURNED: the result's rows are X's columns.
 template <uint32_t M, uint32_t WAVES_M, uint32_t WAVES_N, uint32_t STAGES, class T, bool TURNED>
-__global__ __launch_bounds__(WAVES_M *WAVES_N * 64, WAVES_M *WAVES_N > 4 || STAGES < 4 ? 2 : 1) void k_ortho_step(StepArgs a, Matrices results)
+__global__ __launch_bounds__(WAVES_M *WAVES_N * 64, 2) void k_ortho_step(StepArgs a, Matrices results)
 {
     typedef Product<f16, M, M, WAVES_M, WAVES_N, false, true, STAGES> P;
     __shared__ __attribute__((aligned(16))) typename P::Lds lds;
@@ -319,11 +324,6 @@ __global__ __launch_bounds__(WAVES_M *WAVES_N * 64, WAVES_M *WAVES_N > 4 || STAG
     const uint16_t *const x_hi = a.x.hi + which * a.x.size, *const x_lo = a.x.lo + which * a.x.size;
     const Side left = {{a.poly.hi + which * a.poly.size, a.poly.lo ? a.poly.lo + which * a.poly.size : nullptr}, a.poly.stride, a.rows};
     const Side right = {{x_hi, x_lo}, a.x.stride, a.cols};
-    typename P::Sums s;
-    P::run(lds, left, right, tile_m * M, tile_n * M, 0, a.rows, a.kind, s);
-    // from how this X is held to how the next one is, or to the result
-    const int lift = lift_of(a.log2_norm[which], a.growth);
-    const int power = __is_same(T, void) ? lift_of(a.log2_norm[which], a.next_growth) - lift : -12 - lift;
     // a row of X's next, or of the result's
     u32x4 hi[P::PASSES], lo[P::PASSES];
     float d[P::PASSES];
@@ -335,6 +335,12 @@ __global__ __launch_bounds__(WAVES_M *WAVES_N * 64, WAVES_M *WAVES_N > 4 || STAG
         lo[p] = *(const u32x4 *)(x_lo + at);
         d[p] = a.diagonal[which * a.rows + (in ? m : 0)];
     };
+    P::look_early(look);
+    typename P::Sums s;
+    P::run(lds, left, right, tile_m * M, tile_n * M, 0, a.rows, a.kind, s);
+    // from how this X is held to how the next one is, or to the result
+    const int lift = lift_of(a.log2_norm[which], a.growth);
+    const int power = __is_same(T, void) ? lift_of(a.log2_norm[which], a.next_growth) - lift : -12 - lift;
     auto next = [&](uint32_t p, float (&v)[8]) {
 #pragma unroll
         for (uint32_t k = 0; k < 8; ++k) {
@@ -389,7 +395,7 @@ static SquarePlan square_plan(uint32_t size, uint32_t depth, uint32_t pairs, uin
         if ((steps + each - 1) / each != s) continue;
         float us = 0.0f;
         const int tile = product_tile([=](uint32_t high, uint32_t) { const uint64_t t = tiles_of(size, high); return t * (t + 1) / 2 * count * s; },
-                                      each * pairs, false, us);
+                                      each * pairs, TILE_192, us);
         // (the sums of half the square and more are written and read)
         if (s > 1) us += 6.0f + (float)s * (float)count * (float)size * (float)size * 5.0f / 4.5e6f;
         if (least == 0.0f || us < least || MOST_SPLITS) {
@@ -474,6 +480,7 @@ template <bool POLY> static void launch_square(SquareArgs a, const SquarePlan &p
     const int tile = plan.tile;
     const dim3 grid(a.tiles * (a.tiles + 1) / 2 * a.count * plan.splits);
     if (tile == TILE_256) hipLaunchKernelGGL((k_ortho_square<256, 2, 4, 2, POLY>), grid, dim3(512), 0, st, a);
+    else if (tile == TILE_192) hipLaunchKernelGGL((k_ortho_square<192, 2, 2, 2, POLY>), grid, dim3(256), 0, st, a);
     else if (tile == TILE_128) hipLaunchKernelGGL((k_ortho_square<128, 2, 2, 2, POLY>), grid, dim3(256), 0, st, a);
     else hipLaunchKernelGGL((k_ortho_square<64, 2, 2, 4, POLY>), grid, dim3(256), 0, st, a);
     if (plan.splits > 1) {
@@ -527,7 +534,7 @@ extern "C" int dgs_orthogonalise(const dgs_orthogonalise_args *args, void *hip_s
         const uint32_t kind = o.two ? BOTH_IN_TWO : ONE_PAIR;
         float us = 0.0f;
         const int step_tile = product_tile([&](uint32_t high, uint32_t wide) { return (uint64_t)tiles_of(o.rows, high) * tiles_of(o.cols, wide) * count; },
-                                           tiles_of(o.rows, PRODUCT_STEP) * (o.two ? 3u : 1u), false, us);
+                                           tiles_of(o.rows, PRODUCT_STEP) * (o.two ? 3u : 1u), TILE_256, us);
         const float grows = p.a != 0.0f ? log2f(fabsf(p.a)) : 0.0f;
         for (uint32_t step = 0; step < p.steps; ++step) {
             SquareArgs g = {};

@@ -262,7 +262,18 @@ template <class E, uint32_t M, uint32_t N, uint32_t WAVES_M, uint32_t WAVES_N, b
     // The lanes hold a column of a square each, four rows together.  Memory wants rows: the sums go through LDS, a wavefront's own
     // part of it, and come back as eight values of a row.  look(p, m, n) for every p first (what has to be loaded, so that the loads are
     // in flight together), then take(p, m, n, v), m and n in the tile.
+    // (Where a wavefront has 32 rows alone, look_early() is called before the sums are taken, and by_rows looks no more.)
     static constexpr uint32_t PASSES = 2 * J;      // of by_rows, 32 rows
+    template <class Look> static __device__ __forceinline__ void look_early(Look look)
+    {
+        if constexpr (I == 1) {
+#pragma unroll
+            for (uint32_t p = 0; p < PASSES; ++p) {
+                const uint32_t at = p * 64 + lane_id();
+                look(p, wave_m() + at / (4 * J), wave_n() + at % (4 * J) * 8);
+            }
+        }
+    }
     template <class Look, class Take> static __device__ __forceinline__ void by_rows(Lds &lds, const Sums &sums, Look look, Take take)
     {
         const uint32_t lane = lane_id(), wave = uniform(threadIdx.x >> 6), wm = wave_m(), wn = wave_n();
@@ -270,10 +281,12 @@ template <class E, uint32_t M, uint32_t N, uint32_t WAVES_M, uint32_t WAVES_N, b
         __syncthreads();      // nobody reads operands any more
 #pragma unroll
         for (uint32_t i = 0; i < I; ++i) {
+            if constexpr (I > 1) {
 #pragma unroll
-            for (uint32_t p = 0; p < PASSES; ++p) {
-                const uint32_t at = p * 64 + lane;
-                look(p, wm + 32 * i + at / (4 * J), wn + at % (4 * J) * 8);
+                for (uint32_t p = 0; p < PASSES; ++p) {
+                    const uint32_t at = p * 64 + lane;
+                    look(p, wm + 32 * i + at / (4 * J), wn + at % (4 * J) * 8);
+                }
             }
 #pragma unroll
             for (uint32_t j = 0; j < J; ++j)
@@ -303,10 +316,12 @@ template <class E, uint32_t M, uint32_t N, uint32_t WAVES_M, uint32_t WAVES_N, b
         __syncthreads();
 #pragma unroll
         for (uint32_t i = 0; i < I; ++i) {
+            if constexpr (I > 1) {
 #pragma unroll
-            for (uint32_t p = 0; p < PASSES; ++p) {
-                const uint32_t at = p * 64 + lane;
-                look(p, wm + 32 * i + at / (4 * J), wn + at % (4 * J) * 8);
+                for (uint32_t p = 0; p < PASSES; ++p) {
+                    const uint32_t at = p * 64 + lane;
+                    look(p, wm + 32 * i + at / (4 * J), wn + at % (4 * J) * 8);
+                }
             }
 #pragma unroll
             for (uint32_t j = 0; j < J; ++j)
@@ -450,11 +465,11 @@ struct Sections {
 // host side: which tile
 // ---------------------------------------------------------------------------
 
-// 256 x 256 to eight wavefronts, one workgroup to a compute unit; 256 x 128 (steps of 32), 128 x 128 and 64 x 64 to four, two
-// workgroups to a compute unit.
-enum ProductTile { TILE_256, TILE_TALL, TILE_128, TILE_64, PRODUCT_TILES };
-static inline uint32_t tile_high(int tile) { return tile <= TILE_TALL ? 256 : tile == TILE_128 ? 128 : 64; }
-static inline uint32_t tile_wide(int tile) { return tile == TILE_256 ? 256 : tile == TILE_64 ? 64 : 128; }
+// 256 x 256 to eight wavefronts and 192 x 192 to four, one workgroup to a compute unit; 256 x 128 (steps of 32), 128 x 128 and
+// 64 x 64 to four, two workgroups to a compute unit.
+enum ProductTile { TILE_256, TILE_TALL, TILE_192, TILE_128, TILE_64, PRODUCT_TILES };
+static inline uint32_t tile_high(int tile) { return tile <= TILE_TALL ? 256 : tile == TILE_192 ? 192 : tile == TILE_128 ? 128 : 64; }
+static inline uint32_t tile_wide(int tile) { return tile == TILE_TALL ? 128 : tile_high(tile); }
 static inline uint32_t tiles_of(uint32_t n, uint32_t size) { return n ? (n - 1) / size + 1 : 0; }
 
 // Microseconds that `tiles` tiles of `steps` steps of 64 k take: what a tile takes besides its steps, and for a step with every
@@ -464,7 +479,7 @@ static inline uint32_t tiles_of(uint32_t n, uint32_t size) { return n ? (n - 1) 
 static inline float tile_time(int tile, uint64_t tiles, uint32_t steps)
 {
     static constexpr struct { float besides, full, one; uint32_t places; } cost[PRODUCT_TILES] = {
-        {10.0f, 1.9f, 1.2f, 256}, {6.0f, 2.0f, 1.0f, 512}, {5.0f, 1.12f, 0.66f, 512}, {3.5f, 0.5f, 0.3f, 512}};
+        {10.0f, 1.9f, 1.2f, 256}, {6.0f, 2.0f, 1.0f, 512}, {8.0f, 1.2f, 0.85f, 256}, {5.0f, 1.12f, 0.66f, 512}, {3.5f, 0.5f, 0.3f, 512}};
     const auto &c = cost[tile];
     const uint64_t rounds = tiles / c.places, rest = tiles % c.places;
     float us = (float)rounds * (c.besides + c.full * (float)steps);
@@ -475,15 +490,16 @@ static inline float tile_time(int tile, uint64_t tiles, uint32_t steps)
     }
     return us;
 }
-// The tile that should take the least time; tiles(high, wide): how many of them there are.  `tall`: whether TILE_TALL is there.
-template <class Tiles> static int product_tile(Tiles tiles, uint32_t steps, bool tall, float &least)
+// The tile that should take the least time; tiles(high, wide): how many of them there are.  `more`: TILE_TALL or TILE_192 where that
+// is there too.
+template <class Tiles> static int product_tile(Tiles tiles, uint32_t steps, int more, float &least)
 {
     int best = TILE_256;
     for (int t = 0; t < PRODUCT_TILES; ++t) {
 #ifdef DGS_PRODUCT_TILE      // (a CPU build that is to reach one kind on small matrices)
-        if (t != (DGS_PRODUCT_TILE == TILE_TALL && !tall ? TILE_128 : DGS_PRODUCT_TILE)) continue;
+        if (t != ((DGS_PRODUCT_TILE == TILE_TALL || DGS_PRODUCT_TILE == TILE_192) && more != DGS_PRODUCT_TILE ? TILE_128 : DGS_PRODUCT_TILE)) continue;
 #endif
-        if (t == TILE_TALL && !tall) continue;
+        if ((t == TILE_TALL || t == TILE_192) && t != more) continue;
         const float us = tile_time(t, tiles(tile_high(t), tile_wide(t)), steps);
         if (least == 0.0f || us < least) {
             least = us;

@@ -14,7 +14,7 @@ CLANG = os.environ.get("DGS_HOST_CLANG", "/opt/rocm/llvm/bin/clang++")
 FLAGS = ["-std=c++17", "-O1", "-g", f"-I{EMU}", "-ffp-contract=off", "-fsanitize=address,undefined", "-fno-sanitize-recover=all",
          "-Wno-unknown-attributes", "-Wno-unused-function", "-Wno-array-compare", "-Wno-pass-failed"]
 # the library as it is, and with one kind of tile, small pieces of the vocabulary and split sums taken at any size
-BUILDS = {"": [], **{f"tile{t}": [f"-DDGS_PRODUCT_TILE={t}", "-DDGS_HEAD_PIECE=256", f"-DDGS_PRODUCT_SPLITS={1 + t % 3}"] for t in range(4)}}
+BUILDS = {"": [], **{f"tile{t}": [f"-DDGS_PRODUCT_TILE={t}", "-DDGS_HEAD_PIECE=256", f"-DDGS_PRODUCT_SPLITS={1 + t % 3}"] for t in range(5)}}
 
 
 @pytest.fixture(scope="module")
@@ -36,7 +36,7 @@ def programs(tmp_path_factory):
 
 def test_head_kernels_on_the_cpu_under_asan_ubsan(programs):
     env = dict(os.environ, ASAN_OPTIONS="detect_leaks=0:detect_stack_use_after_return=0")
-    runs = [("", "head"), ("", "large"), ("", "ortho")] + [(f"tile{t}", what) for t in range(4) for what in ("large", "ortho")]
+    runs = [("", "head"), ("", "large"), ("", "ortho")] + [(f"tile{t}", "large") for t in (0, 1, 3, 4)] + [(f"tile{t}", "ortho") for t in (0, 2, 3, 4)]
     procs = [(run, subprocess.Popen([programs[run[0]], run[1]], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, env=env)) for run in runs]
     try:
         for run, p in procs:
