@@ -19,7 +19,11 @@ namespace dgs {
 // operands
 // ---------------------------------------------------------------------------
 
-constexpr uint32_t RANGE_BLOCKS = 1024;     // of rows, and as many of W
+#ifdef DGS_HOST_EMULATION
+constexpr uint32_t RANGE_BLOCKS = 256;
+#else
+constexpr uint32_t RANGE_BLOCKS = 1024;      // of rows, and as many of W
+#endif
 constexpr int NO_RANGE = -100000;           // nothing but zeros
 constexpr int TOP = 15;                     // the largest magnitude of a scaled operand lies below 2^TOP
 constexpr int GRAD_TOP = 14;                // a row's logit gradients are at most 2 after division
@@ -250,11 +254,205 @@ __device__ __forceinline__ float2 joined(float2 a, float2 b)
     return make_float2(most, a.y * power_of_e(a.x - from) + b.y * power_of_e(b.x - from));
 }
 
-// Entries (m) and rows (n) of a tile.
-template <class E, uint32_t M, uint32_t N, uint32_t WAVES_M, uint32_t WAVES_N, uint32_t STAGES, bool BACK>
-__global__ __launch_bounds__(WAVES_M *WAVES_N * 64, 2) void k_head_logits(LogitArgs a)
+// ---------------------------------------------------------------------------
+// few rows
+// ---------------------------------------------------------------------------
+// Up to 32 rows are one square's columns, and every call is a pass or two over W: what counts is to read it once, as it is.  A
+// workgroup takes 32 entries, its fragments straight from memory (any alignment, any type; fp32 in three bfloat16 parts, whose six
+// largest products leave 2^-23 of a product out): a copy of W in another form would move it twice more.  Its wavefronts take the
+// columns in turn, so that enough loads are in flight where W has few rows.
+
+constexpr uint32_t FEW_ROWS = 32, FEW_WAVES = 4;
+
+// Eight values in three parts, each taken off the rest by truncation: exact but for the smallest numbers.
+__device__ __forceinline__ void three_parts(const float (&v)[8], u32x4 (&part)[3])
 {
-    typedef Product<E, M, N, WAVES_M, WAVES_N, false, false, STAGES, M == 256 && N == 128 ? 32 : PRODUCT_STEP> P;
+    float left[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) left[i] = v[i];
+#pragma unroll
+    for (int p = 0; p < 3; ++p) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            part[p][i] = (__float_as_uint(left[2 * i]) >> 16) | (__float_as_uint(left[2 * i + 1]) & 0xFFFF0000u);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) left[i] -= __uint_as_float(__float_as_uint(left[i]) & 0xFFFF0000u);
+    }
+}
+
+template <class T> __device__ __forceinline__ void multiply8(const Raw8<T> &a, const Raw8<T> &b, f32x16 &sums)
+{
+    if constexpr (sizeof(T) == 4) {
+        float v[8];
+        u32x4 x[3], y[3];
+        unpack8(a, v);
+        three_parts(v, x);
+        unpack8(b, v);
+        three_parts(v, y);
+#pragma unroll
+        for (int all = 2; all >= 0; --all)
+#pragma unroll
+            for (int i = 0; i <= all; ++i) sums = matrix_unit_of<bf16>(x[i], y[all - i], sums);
+    } else {
+        u32x4 x, y;
+        __builtin_memcpy(&x, &a, 16);
+        __builtin_memcpy(&y, &b, 16);
+        sums = matrix_unit_of<T>(x, y, sums);
+    }
+}
+
+// 32 rows of w by 32 of x, over all columns; the first wavefront gets the sums.  (Rows beyond the last are the last.)
+template <class T>
+__device__ __forceinline__ void few_sums(const Side &w, uint32_t w_first, const Side &x, uint32_t cols, float (&part)[FEW_WAVES - 1][16][64],
+                                         f32x16 &sums)
+{
+    constexpr uint32_t EACH = sizeof(T) == 4 ? 4 : 8, CHUNK = 16 * EACH, TURN = FEW_WAVES * CHUNK;
+    const uint32_t lane = lane_id(), wave = uniform(threadIdx.x >> 6), behind = 8 * (lane >> 5);
+    const T *const pw = (const T *)w.part[0] + min(w_first + (lane & 31u), w.size - 1u) * w.stride;
+    const T *const px = (const T *)x.part[0] + min(lane & 31u, x.size - 1u) * x.stride;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) sums[r] = 0.0f;
+    Raw8<T> a[2][EACH], b[2][EACH];
+    auto fetch = [&](int to, uint32_t k) {
+#pragma unroll
+        for (uint32_t i = 0; i < EACH; ++i) {
+            a[to][i] = load8(pw + k + 16 * i + behind, 8);
+            b[to][i] = load8(px + k + 16 * i + behind, 8);
+        }
+    };
+    auto multiply = [&](int from) {
+#pragma unroll
+        for (uint32_t i = 0; i < EACH; ++i) multiply8<T>(a[from][i], b[from][i], sums);
+    };
+    const uint32_t whole = cols / CHUNK * CHUNK, first = wave * CHUNK;
+    if (first < whole) fetch(0, first);
+    for (uint32_t k = first; k < whole; k += 2 * TURN) {
+        if (k + TURN < whole) fetch(1, k + TURN);
+        multiply(0);
+        if (k + TURN < whole) {
+            if (k + 2 * TURN < whole) fetch(0, k + 2 * TURN);
+            multiply(1);
+        }
+    }
+    for (uint32_t k = whole + 16 * wave; k < cols; k += 16 * FEW_WAVES) {
+        const uint32_t c = k + behind, n = live8(c, cols);
+        multiply8<T>(load8(pw + (n ? c : 0u), n), load8(px + (n ? c : 0u), n), sums);
+    }
+    if (wave) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) part[wave - 1][r][lane] = sums[r];
+    }
+    __syncthreads();
+    if (wave == 0) {
+#pragma unroll
+        for (uint32_t i = 0; i < FEW_WAVES - 1; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sums[r] += part[i][r][lane];
+    }
+}
+
+// dx of few rows, a part of it: sums over `chunk` entries, in fp32, of the logits' gradient (both halves) and W as it is.  256 columns to a
+// workgroup, four a lane, its wavefronts taking 32 entries in turn, of which the gradient is in LDS.
+constexpr uint32_t FEW_BLOCK = 32;
+template <class T> __device__ __forceinline__ void load4(const T *p, uint32_t n, float (&v)[4])
+{
+    if (n >= 4) {
+        T t[4];
+        if constexpr (sizeof(T) == 4) {
+            const f32x4_any q = *(const f32x4_any *)p;
+            __builtin_memcpy(t, &q, 16);
+        } else {
+            const u32x2_any q = *(const u32x2_any *)p;
+            __builtin_memcpy(t, &q, 8);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = to_float(t[i]);
+    } else {
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) v[i] = i < n ? to_float(p[i]) : 0.0f;
+    }
+}
+template <class T, uint32_t ROWS>
+__global__ __launch_bounds__(FEW_WAVES * 64) void k_head_few_dx(const T *w, uint64_t w_stride, uint32_t count, uint32_t cols, const uint16_t *hi,
+                                                                const uint16_t *lo, uint64_t grad_stride, uint32_t rows, uint32_t chunk,
+                                                                float *sums, uint32_t add)
+{
+    constexpr uint32_t AHEAD = 8;
+    __shared__ union {
+        __attribute__((aligned(16))) float grad[FEW_WAVES][FEW_BLOCK][ROWS];
+        float part[FEW_WAVES / 2][ROWS * 4][64];
+    } lds;
+    const uint32_t lane = lane_id(), wave = uniform(threadIdx.x >> 6), c = blockIdx.x * 256 + lane * 4, n = c < cols ? min(4u, cols - c) : 0u;
+    const uint32_t first = blockIdx.y * chunk, end = min(first + chunk, count);
+    float (*const grad)[ROWS] = lds.grad[wave];
+    float s[ROWS][4];
+#pragma unroll
+    for (uint32_t t = 0; t < ROWS; ++t) s[t][0] = s[t][1] = s[t][2] = s[t][3] = 0.0f;
+    for (uint32_t turn = first; turn < end; turn += FEW_WAVES * FEW_BLOCK) {
+        const uint32_t v0 = turn + wave * FEW_BLOCK;
+        __syncthreads();
+#pragma unroll
+        for (uint32_t t = 0; t < ROWS; t += 2) {
+            const uint32_t row = t + (lane >> 5), v = v0 + (lane & 31u);
+            const bool in = row < rows && v < end;
+            const uint64_t at = in ? row * grad_stride + v : 0u;
+            grad[lane & 31u][row] = in ? half_value(hi[at]) + half_value(lo[at]) : 0.0f;
+        }
+        __syncthreads();
+        for (uint32_t v = 0; v < FEW_BLOCK && v0 + v < end; v += AHEAD) {
+            float x[AHEAD][4];
+#pragma unroll
+            for (uint32_t i = 0; i < AHEAD; ++i) {
+                const bool in = v0 + v + i < end;      // (beyond the end the gradient is 0, and W is not read)
+                load4(w + (n && in ? (v0 + v + i) * w_stride + c : 0u), in ? n : 0u, x[i]);
+            }
+#pragma unroll
+            for (uint32_t i = 0; i < AHEAD; ++i)
+#pragma unroll
+                for (uint32_t t = 0; t < ROWS; t += 4) {
+                    const f32x4 g = *(const f32x4 *)&grad[v + i][t];
+                    const float q[4] = {g.x, g.y, g.z, g.w};
+#pragma unroll
+                    for (uint32_t k = 0; k < 4; ++k)
+#pragma unroll
+                        for (uint32_t e = 0; e < 4; ++e) s[t + k][e] = __builtin_fmaf(q[k], x[i][e], s[t + k][e]);
+                }
+        }
+    }
+    // the wavefronts' sums, by halves
+#pragma unroll
+    for (uint32_t by = FEW_WAVES / 2; by; by >>= 1) {
+        __syncthreads();
+        if (wave >= by && wave < 2 * by) {
+#pragma unroll
+            for (uint32_t t = 0; t < ROWS; ++t)
+#pragma unroll
+                for (uint32_t e = 0; e < 4; ++e) lds.part[wave - by][4 * t + e][lane] = s[t][e];
+        }
+        __syncthreads();
+        if (wave < by) {
+#pragma unroll
+            for (uint32_t t = 0; t < ROWS; ++t)
+#pragma unroll
+                for (uint32_t e = 0; e < 4; ++e) s[t][e] += lds.part[wave][4 * t + e][lane];
+        }
+    }
+    if (wave) return;
+#pragma unroll
+    for (uint32_t t = 0; t < ROWS; ++t) {
+        if (t >= rows) continue;
+        float *const to = sums + ((uint64_t)blockIdx.y * rows + t) * cols + c;
+#pragma unroll
+        for (uint32_t e = 0; e < 4; ++e)
+            if (e < n) to[e] = add ? to[e] + s[t][e] : s[t][e];
+    }
+}
+
+// Entries (m) and rows (n) of a tile.  E: the operands' type as they are staged; STAGES = 0: as they are read, a square to a wavefront.
+template <class E, uint32_t M, uint32_t N, uint32_t WAVES_M, uint32_t WAVES_N, uint32_t STAGES, bool BACK>
+__global__ __launch_bounds__(STAGES ? WAVES_M *WAVES_N * 64 : FEW_WAVES * 64, 2) void k_head_logits(LogitArgs a)
+{
+    typedef Product<E, M, N, WAVES_M, WAVES_N, false, false, STAGES, PRODUCT_STEP> P;
     __shared__ __attribute__((aligned(16))) typename P::Lds lds;
     const TilePlace place = place_of_tile(tile_of_block(blockIdx.x, gridDim.x), a.v_tiles, a.t_tiles);
     const uint32_t tile_v = place.m, tile_t = place.n;
@@ -264,7 +462,13 @@ __global__ __launch_bounds__(WAVES_M *WAVES_N * 64, 2) void k_head_logits(LogitA
         for (uint32_t m = threadIdx.x; m < M; m += P::THREADS) bias[m] = a.bias[min(v0 + m, a.end - 1u)];
     }
     typename P::Sums z;
-    P::run(lds, a.w, a.x, v0, t0, 0, a.cols, a.kind, z);
+    if constexpr (STAGES == 0) {
+        __shared__ float part[FEW_WAVES - 1][16][64];
+        few_sums<E>(a.w, v0, a.x, a.cols, part, z[0][0]);
+        if (threadIdx.x >= 64) return;      // (the rest is a wavefront's work)
+    } else {
+        P::run(lds, a.w, a.x, v0, t0, 0, a.cols, a.kind, z);
+    }
 
     const uint32_t lane = lane_id(), half = lane >> 5, wave = uniform(threadIdx.x >> 6);
     // this lane's first entry of the tile; the others are row_in_square(r) + 32 i behind it, `left` of them are there
@@ -301,7 +505,7 @@ __global__ __launch_bounds__(WAVES_M *WAVES_N * 64, 2) void k_head_logits(LogitA
             }
     }
     if constexpr (!BACK) {
-        __syncthreads();      // nobody reads operands any more
+        P::sync();      // nobody reads operands any more
         float2(*const part)[N] = (float2(*)[N])&lds;
         if (edge) {
 #pragma unroll
@@ -342,7 +546,7 @@ __global__ __launch_bounds__(WAVES_M *WAVES_N * 64, 2) void k_head_logits(LogitA
             sum += other_half(sum);
             if (half == 0) part[wave / WAVES_N][n] = make_float2(most, sum);
         }
-        __syncthreads();
+        P::sync();
         for (uint32_t n = threadIdx.x; n < N; n += P::THREADS) {
             if (t0 + n >= a.rows) continue;
             float2 all = part[0][n];
@@ -389,7 +593,7 @@ __global__ __launch_bounds__(WAVES_M *WAVES_N * 64, 2) void k_head_logits(LogitA
             *(u32x4 *)(a.grad[1] + t * a.grad_stride + at_v) = lo;
         });
         if (a.bias_parts) {
-            __syncthreads();
+            P::sync();
             float(*const part)[M] = (float(*)[M])&lds;
             float column[P::I * 16];      // the bias gradient's sums over this lane's rows
 #pragma unroll
@@ -416,7 +620,7 @@ __global__ __launch_bounds__(WAVES_M *WAVES_N * 64, 2) void k_head_logits(LogitA
 #pragma unroll
             for (uint32_t k = 0; k < (P::I > 2 ? P::I / 2 : 1); ++k)
                 part[wave % WAVES_N][P::wave_m() + 32 * ((entry + k) >> 4) + row_in_square((entry + k) & 15u) + 4 * half] = column[k];
-            __syncthreads();
+            P::sync();
             for (uint32_t m = threadIdx.x; m < M; m += P::THREADS) {
                 const uint32_t v = v0 - a.first + m;
                 if (v >= a.grad_stride) continue;
@@ -484,43 +688,64 @@ __global__ __launch_bounds__(WAVES_M *WAVES_N * 64, 2) void k_head_product(Gradi
     const uint32_t tile_m = place.m, tile_n = place.n;
     const uint32_t first = min(split * a.split_depth, a.depth), end = min(first + a.split_depth, a.depth);
     float *const out = a.out + (a.whole ? 0u : (uint64_t)split * a.m * a.out_stride);
-    float old[P::PASSES][8];
-    auto look = [&](uint32_t p, uint32_t row, uint32_t col) {
-        const uint32_t m = tile_m * M + row, n = tile_n * N + col, count = m < a.m ? live8(n, a.n) : 0u;
-        if (a.add && count) load8_f32(out + m * a.out_stride + n, count, old[p]);
-    };
-    P::look_early(look);
     typename P::Sums s;
     P::run(lds, a.a, a.b, tile_m * M, tile_n * N, first, end, a.kind, s);
     const int e = a.whole ? -GRAD_TOP - a.scales->x : 0;
-    P::by_rows(lds, s, look, [&](uint32_t p, uint32_t row, uint32_t col, float (&v)[8]) {
-        const uint32_t m = tile_m * M + row, n = tile_n * N + col, count = m < a.m ? live8(n, a.n) : 0u;
-        if (count == 0) return;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            v[k] = times_power(v[k], e);
-            if (a.add) v[k] += old[p][k];
+    f32x4 old[2 * P::PASSES];
+    P::by_fours(lds, s, [&](uint32_t p, uint32_t row, uint32_t col) {
+        const uint32_t m = tile_m * M + row, n = tile_n * N + col;
+        if (a.add && m < a.m && n + 4 <= a.n) old[p] = *(const f32x4_any *)(out + m * a.out_stride + n);
+    }, [&](uint32_t p, uint32_t row, uint32_t col, const f32x4 &v) {
+        const uint32_t m = tile_m * M + row, n = tile_n * N + col;
+        if (m >= a.m || n >= a.n) return;
+        float *const to = out + m * a.out_stride + n;
+        f32x4_any w;
+        w.x = times_power(v.x, e); w.y = times_power(v.y, e); w.z = times_power(v.z, e); w.w = times_power(v.w, e);
+        if (n + 4 <= a.n) {
+            if (a.add) w += old[p];
+            __builtin_nontemporal_store(w, (f32x4_any *)to);
+        } else {
+            to[0] = a.add ? to[0] + w.x : w.x;
+            if (n + 1 < a.n) to[1] = a.add ? to[1] + w.y : w.y;
+            if (n + 2 < a.n) to[2] = a.add ? to[2] + w.z : w.z;
         }
-        store8(out + m * a.out_stride, n, count, v);
     });
 }
 
-// dx: the splits' sums, times the row's power, W's taken off.
-template <class T>
+// dx: the splits' sums, times the row's power, W's taken off.  Eight columns a lane; GROUPS lanes take the splits in turn.
+template <class T, uint32_t GROUPS>
 __global__ __launch_bounds__(256) void k_head_dx(const float *sums, uint32_t splits, uint32_t rows, uint32_t cols, const HeadRow *row_info,
                                                  const Scales *scales, T *dx, uint64_t dx_stride)
 {
-    const uint64_t at = (uint64_t)blockIdx.x * 256 + threadIdx.x, pieces = (cols + 7) / 8;
+    constexpr uint32_t PER = 256 / GROUPS;
+    __shared__ float part[GROUPS][8][PER];
+    const uint32_t place = threadIdx.x % PER, group = threadIdx.x / PER;
+    const uint64_t at = (uint64_t)blockIdx.x * PER + place, pieces = (cols + 7) / 8;
     const uint64_t row = at / pieces;
-    if (row >= rows) return;
-    const uint32_t c = (uint32_t)(at - row * pieces) * 8, n = live8(c, cols);
+    const uint32_t c = (uint32_t)(at - row * pieces) * 8, n = row < rows ? live8(c, cols) : 0u;
     float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-    for (uint32_t s = 0; s < splits; ++s) {
-        float w[8];
-        load8_f32(sums + ((uint64_t)s * rows + row) * cols + c, n, w);
+    const uint64_t apart = (uint64_t)rows * cols;
+    const float *const p = sums + (n ? row * cols + c : 0u);
+    for (uint32_t s = group; s < splits; s += 4 * GROUPS) {
+        float w[4][8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] += w[i];
+        for (uint32_t k = 0; k < 4; ++k) load8_f32(p + min(s + k * GROUPS, splits - 1u) * apart, n, w[k]);
+#pragma unroll
+        for (uint32_t k = 0; k < 4; ++k)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] += s + k * GROUPS < splits ? w[k][i] : 0.0f;
     }
+    if constexpr (GROUPS > 1) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) part[group][i][place] = v[i];
+        __syncthreads();
+        if (group) return;
+#pragma unroll
+        for (uint32_t g = 1; g < GROUPS; ++g)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] += part[g][i][place];
+    }
+    if (n == 0) return;
     const int e = row_info[row].power - GRAD_TOP - (scales ? scales->w : 0);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = times_power(v[i], e);
@@ -567,13 +792,12 @@ __global__ __launch_bounds__(256) void k_head_dbias(const float *parts, uint32_t
 // host side
 // ---------------------------------------------------------------------------
 
-enum { TILE_FEW = PRODUCT_TILES };      // 128 entries, 32 rows
+enum { TILE_FEW = PRODUCT_TILES, TILE_DIRECT };      // 128 entries, 32 rows; 32 entries, 32 rows, as they are
 struct TileSize { uint32_t m, n; };
-static TileSize size_of(int tile) { return tile == TILE_FEW ? TileSize{128, 32} : TileSize{tile_high(tile), tile_wide(tile)}; }
+static TileSize size_of(int tile) { return tile == TILE_FEW ? TileSize{128, FEW_ROWS} : tile == TILE_DIRECT ? TileSize{32, FEW_ROWS} : TileSize{tile_high(tile), tile_wide(tile)}; }
 static uint32_t steps_of(uint32_t depth, uint32_t kind) { return tiles_of(depth, PRODUCT_STEP) * (kind == ONE_PAIR ? 1 : kind == FIRST_IN_TWO ? 2 : 3); }
 static int logits_tile(uint32_t vocab, uint32_t rows, uint32_t steps)
 {
-    if (rows <= 32) return TILE_FEW;
     float us = 0.0f;
     return product_tile([=](uint32_t high, uint32_t wide) { return (uint64_t)tiles_of(vocab, high) * tiles_of(rows, wide); }, steps, TILE_256, us);
 }
@@ -606,7 +830,8 @@ constexpr uint64_t PIECE_BYTES = 1ull << 30;      // of the logits' gradient, at
 
 struct HeadPlan {
     bool back, wants_dx, wants_dw;
-    bool scale_x_rows, copy_x, copy_w, scale_w;      // which operands are copied, and how
+    bool few, direct, few_dx;        // rows of one square; whose logits, whose dx are taken of W as it is
+    bool split, copy_x, copy_w, scale_w;      // which operands are copied, and how
     uint32_t width;                                  // columns, up to a multiple of eight
     uint32_t piece;                                  // entries at a time
     int logits;
@@ -634,11 +859,17 @@ static HeadPlan plan_of(const dgs_head_args &p, bool back)
     h.wants_dw = back && p.dweight;
     h.width = (p.cols + 7) & ~7u;
     const bool f32 = p.type == DGS_F32;
-    h.scale_x_rows = f32;
-    h.scale_w = f32 || (back && p.type == DGS_BF16 && h.wants_dx);
-    h.copy_x = !f32 && !straight_ok(p.x, p.cols);
-    h.copy_w = !f32 && !straight_ok(p.weight, p.cols);
-    h.logits = logits_tile(p.vocab, p.rows, steps_of(p.cols, f32 ? BOTH_IN_TWO : ONE_PAIR));
+    const bool staged = straight_ok(p.x, p.cols) && straight_ok(p.weight, p.cols);
+    h.few = p.rows <= FEW_ROWS;
+    h.direct = h.few && (f32 || !staged);
+    // (dx alone, bfloat16 W of 32000 x 4096, by few_dx and by the matrix units from a copy of W: 8 rows 140 and 267 us, 16 rows 206 and 287,
+    // 32 rows 360 and 278; of 32000 x 1024 16 rows 67 and 67)
+    h.few_dx = h.few && (f32 || p.rows <= 16);
+    h.split = f32 && !h.few;
+    h.scale_w = h.split || (p.type == DGS_BF16 && h.wants_dx && !h.few_dx);
+    h.copy_x = !f32 && !h.few && !straight_ok(p.x, p.cols);
+    h.copy_w = !f32 && !straight_ok(p.weight, p.cols) && (!h.few || (p.type == DGS_F16 && h.wants_dx && !h.few_dx));
+    h.logits = h.direct ? TILE_DIRECT : h.few ? TILE_FEW : logits_tile(p.vocab, p.rows, steps_of(p.cols, f32 ? BOTH_IN_TWO : ONE_PAIR));
     Sections s = {(uintptr_t)p.workspace, 0};
     const uint64_t x_bytes = (uint64_t)p.rows * h.width * 2, w_bytes = (uint64_t)p.vocab * h.width * 2;
     const TileSize tile = size_of(h.logits);
@@ -646,17 +877,17 @@ static HeadPlan plan_of(const dgs_head_args &p, bool back)
         h.stats = (float2 *)s.take((uint64_t)tiles_of(p.vocab, tile.m) * p.rows * sizeof(float2));
         h.target_logit = (float *)s.take((uint64_t)p.rows * 4);
     }
-    if (back || f32) {
+    if (back || h.split) {
         h.ranges.row = (int *)s.take((uint64_t)p.rows * 4);
         h.ranges.x = (int *)s.take(RANGE_BLOCKS * 4);
         h.ranges.w = (int *)s.take(RANGE_BLOCKS * 4);
         h.scales = (Scales *)s.take(sizeof(Scales));
         if (!h.scale_w) h.ranges.w = nullptr;
     }
-    if (f32 || h.copy_x) h.x[0] = (uint16_t *)s.take(x_bytes);
-    if (f32) h.x[1] = (uint16_t *)s.take(x_bytes);
-    if (f32 || h.copy_w) h.w[0] = (uint16_t *)s.take(w_bytes);
-    if (f32) h.w[1] = (uint16_t *)s.take(w_bytes);
+    if (h.split || h.copy_x) h.x[0] = (uint16_t *)s.take(x_bytes);
+    if (h.split) h.x[1] = (uint16_t *)s.take(x_bytes);
+    if (h.split || h.copy_w) h.w[0] = (uint16_t *)s.take(w_bytes);
+    if (h.split) h.w[1] = (uint16_t *)s.take(w_bytes);
     if (back) {
         h.row_info = (HeadRow *)s.take((uint64_t)p.rows * sizeof(HeadRow));
         if (h.wants_dw) h.x_weighed[0] = (uint16_t *)s.take(x_bytes);
@@ -672,7 +903,13 @@ static HeadPlan plan_of(const dgs_head_args &p, bool back)
         h.grad[0] = (uint16_t *)s.take(p.rows * stride * 2);
         h.grad[1] = (uint16_t *)s.take(p.rows * stride * 2);
         if (p.dbias) h.bias_parts = (float *)s.take(tiles_of(p.rows, tile.n) * stride * 4);
-        h.dx = product_plan(p.rows, p.cols, h.piece, f32 ? BOTH_IN_TWO : p.type == DGS_F16 ? FIRST_IN_TWO : ONE_PAIR, TILE_256);
+        if (h.few_dx) {
+            // a turn of the wavefronts' blocks at least, about 2048 workgroups, at most 128 sums a value
+            const uint32_t turn = FEW_WAVES * FEW_BLOCK, across = tiles_of(p.cols, 256);
+            const uint32_t most = across > 16 ? (across > 2048 ? 1u : 2048 / across) : 128u;
+            const uint32_t each = tiles_of(tiles_of(h.piece, most), turn) * turn;
+            h.dx = ProductPlan{0, tiles_of(h.piece, each), each, 0};
+        } else h.dx = product_plan(p.rows, p.cols, h.piece, f32 ? BOTH_IN_TWO : p.type == DGS_F16 ? FIRST_IN_TWO : ONE_PAIR, TILE_256);
         h.dw = product_plan(h.piece, p.cols, p.rows, f32 ? BOTH_IN_TWO : FIRST_IN_TWO, TILE_TALL);
         if (h.wants_dx) h.dx_sums = (float *)s.take((uint64_t)h.dx.splits * p.rows * p.cols * 4);
         if (h.wants_dw && h.dw.splits > 1) h.dw_sums = (float *)s.take((uint64_t)h.dw.splits * h.piece * p.cols * 4);
@@ -684,8 +921,7 @@ static HeadPlan plan_of(const dgs_head_args &p, bool back)
 
 template <class T> static void prepare(const dgs_head_args &p, const HeadPlan &h, const Targets &targets, hipStream_t st)
 {
-    constexpr bool f32 = __is_same(T, float);
-    if (h.back || f32)
+    if (h.back || h.split)
         hipLaunchKernelGGL(k_head_range<T>, dim3(2 * RANGE_BLOCKS), dim3(256), 0, st, (const T *)p.x.data, p.x.stride,
                            (const T *)p.weight.data, p.weight.stride, p.rows, p.cols, targets, (const float *)p.lse, p.dloss, p.dlse,
                            h.row_info, h.ranges);
@@ -699,7 +935,7 @@ template <class T> static void prepare(const dgs_head_args &p, const HeadPlan &h
         jobs.job[jobs.count++] = CopyJob{m.data, m.stride, hi, lo, rows, b, kind};
         blocks += b;
     };
-    if (f32) {
+    if (h.split) {
         job(p.x, p.rows, COPY_ROWS, h.x[0], h.x[1]);
         job(p.weight, p.vocab, COPY_ALL, h.w[0], h.w[1]);
     } else {
@@ -721,6 +957,13 @@ template <class E, bool BACK> static void logits(const LogitArgs &a, int tile, h
 }
 template <bool BACK> static void logits(const LogitArgs &a, int type, int tile, hipStream_t st)
 {
+    if (tile == TILE_DIRECT) {
+        const dim3 grid(a.v_tiles * a.t_tiles);
+        if (type == DGS_F32) hipLaunchKernelGGL((k_head_logits<float, 32, 32, 1, 1, 0, BACK>), grid, dim3(FEW_WAVES * 64), 0, st, a);
+        else if (type == DGS_F16) hipLaunchKernelGGL((k_head_logits<f16, 32, 32, 1, 1, 0, BACK>), grid, dim3(FEW_WAVES * 64), 0, st, a);
+        else hipLaunchKernelGGL((k_head_logits<bf16, 32, 32, 1, 1, 0, BACK>), grid, dim3(FEW_WAVES * 64), 0, st, a);
+        return;
+    }
     if (type == DGS_BF16) logits<bf16, BACK>(a, tile, st);
     else logits<f16, BACK>(a, tile, st);
 }
@@ -728,16 +971,50 @@ template <bool TURN_A> static void product(const GradientArgs &a, int tile, hipS
 {
     const dim3 grid(a.m_tiles * a.n_tiles * a.splits);
     if (tile == TILE_256) hipLaunchKernelGGL((k_head_product<256, 256, 2, 4, 2, TURN_A>), grid, dim3(512), 0, st, a);
-    else if (tile == TILE_TALL) hipLaunchKernelGGL((k_head_product<256, 128, 2, 2, 3, TURN_A>), grid, dim3(256), 0, st, a);
+    else if (tile == TILE_TALL) {
+        if constexpr (TURN_A) hipLaunchKernelGGL((k_head_product<256, 128, 2, 2, 3, TURN_A>), grid, dim3(256), 0, st, a);
+    }
     else if (tile == TILE_128) hipLaunchKernelGGL((k_head_product<128, 128, 2, 2, 2, TURN_A>), grid, dim3(256), 0, st, a);
     else hipLaunchKernelGGL((k_head_product<64, 64, 2, 2, 4, TURN_A>), grid, dim3(256), 0, st, a);
+}
+
+template <class T, uint32_t ROWS>
+static void few_dx_of(const dgs_head_args &p, const HeadPlan &h, uint32_t first, uint32_t count, uint64_t stride, hipStream_t st)
+{
+    hipLaunchKernelGGL((k_head_few_dx<T, ROWS>), dim3(tiles_of(p.cols, 256), h.dx.splits), dim3(FEW_WAVES * 64), 0, st,
+                       (const T *)p.weight.data + first * p.weight.stride, p.weight.stride, count, p.cols, (const uint16_t *)h.grad[0],
+                       (const uint16_t *)h.grad[1], stride, p.rows, h.dx.split_depth, h.dx_sums, (uint32_t)(first != 0));
+}
+template <class T> static void few_dx_by_rows(const dgs_head_args &p, const HeadPlan &h, uint32_t first, uint32_t count, uint64_t stride, hipStream_t st)
+{
+    if (p.rows <= 4) few_dx_of<T, 4>(p, h, first, count, stride, st);
+    else if (p.rows <= 8) few_dx_of<T, 8>(p, h, first, count, stride, st);
+    else if (p.rows <= 16) few_dx_of<T, 16>(p, h, first, count, stride, st);
+    else if constexpr (__is_same(T, float)) few_dx_of<T, FEW_ROWS>(p, h, first, count, stride, st);
+}
+static void few_dx(const dgs_head_args &p, const HeadPlan &h, uint32_t first, uint32_t count, uint64_t stride, hipStream_t st)
+{
+    if (p.type == DGS_F32) few_dx_by_rows<float>(p, h, first, count, stride, st);
+    else if (p.type == DGS_F16) few_dx_by_rows<f16>(p, h, first, count, stride, st);
+    else few_dx_by_rows<bf16>(p, h, first, count, stride, st);
+}
+
+template <class T> static void finish_dx(const dgs_head_args &p, const HeadPlan &h, const Scales *scales, hipStream_t st)
+{
+    const uint64_t pieces = (uint64_t)p.rows * ((p.cols + 7) / 8);
+    if (h.dx.splits > 16)
+        hipLaunchKernelGGL((k_head_dx<T, 8>), dim3((uint32_t)((pieces + 31) / 32)), dim3(256), 0, st, (const float *)h.dx_sums, h.dx.splits,
+                           p.rows, p.cols, (const HeadRow *)h.row_info, scales, (T *)p.dx.data, p.dx.stride);
+    else
+        hipLaunchKernelGGL((k_head_dx<T, 1>), dim3((uint32_t)((pieces + 255) / 256)), dim3(256), 0, st, (const float *)h.dx_sums, h.dx.splits,
+                           p.rows, p.cols, (const HeadRow *)h.row_info, scales, (T *)p.dx.data, p.dx.stride);
 }
 
 static LogitArgs logit_args(const dgs_head_args &p, const HeadPlan &h, const Targets &targets)
 {
     LogitArgs a = {};
     const bool f32 = p.type == DGS_F32;
-    const bool own_x = f32 || h.copy_x, own_w = f32 || h.copy_w;
+    const bool own_x = h.split || h.copy_x, own_w = h.split || (h.copy_w && !h.direct);
     a.x = Side{{own_x ? h.x[0] : (const uint16_t *)p.x.data, h.x[1]}, own_x ? h.width : p.x.stride, p.rows};
     a.w = Side{{own_w ? h.w[0] : (const uint16_t *)p.weight.data, h.w[1]}, own_w ? h.width : p.weight.stride, p.vocab};
     a.cols = p.cols;
@@ -747,7 +1024,7 @@ static LogitArgs logit_args(const dgs_head_args &p, const HeadPlan &h, const Tar
     a.t_tiles = tiles_of(p.rows, size_of(h.logits).n);
     a.bias = p.bias;
     a.targets = targets;
-    a.x_powers = f32 ? h.ranges.row : nullptr;
+    a.x_powers = h.split ? h.ranges.row : nullptr;
     a.scales = h.scales;
     return a;
 }
@@ -849,10 +1126,12 @@ extern "C" int dgs_head_backward(const dgs_head_args *args, void *hip_stream)
         if (p.dbias)
             hipLaunchKernelGGL(k_head_dbias, dim3(tiles_of(count, 64)), dim3(256), 0, st, (const float *)h.bias_parts,
                                a.t_tiles, stride, count, p.dbias + first, (uint32_t)(p.accumulate != 0));
-        if (h.wants_dx) {
+        if (h.wants_dx && h.few_dx) {
+            few_dx(p, h, first, count, stride, st);
+        } else if (h.wants_dx) {
             GradientArgs g = {};
-            const uint16_t *w = p.type == DGS_BF16 ? h.w[1] : a.w.part[0];
-            const uint64_t w_stride = p.type == DGS_BF16 ? h.width : a.w.stride;
+            const uint16_t *w = p.type == DGS_BF16 ? h.w[1] : h.copy_w ? h.w[0] : a.w.part[0];
+            const uint64_t w_stride = p.type == DGS_BF16 || h.copy_w ? h.width : a.w.stride;
             g.a = Side{{h.grad[0], h.grad[1]}, stride, p.rows};
             g.b = Side{{w + first * w_stride, f32 ? a.w.part[1] + first * w_stride : nullptr}, w_stride, p.cols};
             g.depth = count;
@@ -893,12 +1172,10 @@ extern "C" int dgs_head_backward(const dgs_head_args *args, void *hip_stream)
         }
     }
     if (h.wants_dx) {
-        const uint64_t blocks = ((uint64_t)p.rows * ((p.cols + 7) / 8) + 255) / 256;
-        const dim3 grid((uint32_t)blocks);
         const Scales *const sc = h.scale_w ? h.scales : nullptr;
-        if (f32) hipLaunchKernelGGL(k_head_dx<float>, grid, dim3(256), 0, st, (const float *)h.dx_sums, h.dx.splits, p.rows, p.cols, (const HeadRow *)h.row_info, sc, (float *)p.dx.data, p.dx.stride);
-        else if (p.type == DGS_F16) hipLaunchKernelGGL(k_head_dx<f16>, grid, dim3(256), 0, st, (const float *)h.dx_sums, h.dx.splits, p.rows, p.cols, (const HeadRow *)h.row_info, sc, (f16 *)p.dx.data, p.dx.stride);
-        else hipLaunchKernelGGL(k_head_dx<bf16>, grid, dim3(256), 0, st, (const float *)h.dx_sums, h.dx.splits, p.rows, p.cols, (const HeadRow *)h.row_info, sc, (bf16 *)p.dx.data, p.dx.stride);
+        if (f32) finish_dx<float>(p, h, sc, st);
+        else if (p.type == DGS_F16) finish_dx<f16>(p, h, sc, st);
+        else finish_dx<bf16>(p, h, sc, st);
     }
     return launched();
 }

@@ -42,19 +42,6 @@ __device__ __forceinline__ float times_power(float v, int e)
     return __builtin_amdgcn_ldexpf(v, e);
 #endif
 }
-__device__ __forceinline__ float value_of(uint16_t bits)
-{
-    f16 h;
-    __builtin_memcpy(&h, &bits, 2);
-    return (float)h;
-}
-__device__ __forceinline__ uint16_t half_bits(f16 h)
-{
-    uint16_t b;
-    __builtin_memcpy(&b, &h, 2);
-    return b;
-}
-
 __device__ __forceinline__ void put_halves(const Halves &to, uint64_t at, const float (&v)[8])
 {
     u32x4 hi, lo;
@@ -164,7 +151,7 @@ __device__ __forceinline__ void finish8(const SquareArgs &a, uint32_t which, uin
     for (uint32_t k = 0; k < 8; ++k) {
         v[k] = times_power(v[k], power);
         if constexpr (POLY) {
-            const float gram = value_of((uint16_t)(gram_hi[k >> 1] >> (16 * (k & 1)))) + value_of((uint16_t)(gram_lo[k >> 1] >> (16 * (k & 1))));
+            const float gram = half_value((uint16_t)(gram_hi[k >> 1] >> (16 * (k & 1)))) + half_value((uint16_t)(gram_lo[k >> 1] >> (16 * (k & 1))));
             v[k] = a.b * gram + a.c * v[k];
         }
     }
@@ -344,7 +331,7 @@ __global__ __launch_bounds__(WAVES_M *WAVES_N * 64, 2) void k_ortho_step(StepArg
     auto next = [&](uint32_t p, float (&v)[8]) {
 #pragma unroll
         for (uint32_t k = 0; k < 8; ++k) {
-            const float x = value_of((uint16_t)(hi[p][k >> 1] >> (16 * (k & 1)))) + value_of((uint16_t)(lo[p][k >> 1] >> (16 * (k & 1))));
+            const float x = half_value((uint16_t)(hi[p][k >> 1] >> (16 * (k & 1)))) + half_value((uint16_t)(lo[p][k >> 1] >> (16 * (k & 1))));
             v[k] = times_power(__builtin_fmaf(d[p], x, v[k] * LEFT), power);
         }
     };

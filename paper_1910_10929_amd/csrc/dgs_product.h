@@ -278,7 +278,7 @@ template <class E, uint32_t M, uint32_t N, uint32_t WAVES_M, uint32_t WAVES_N, b
     {
         const uint32_t lane = lane_id(), wave = uniform(threadIdx.x >> 6), wm = wave_m(), wn = wave_n();
         float *const mine = lds.part[wave];
-        __syncthreads();      // nobody reads operands any more
+        sync();      // nobody reads operands any more
 #pragma unroll
         for (uint32_t i = 0; i < I; ++i) {
             if constexpr (I > 1) {
@@ -307,13 +307,40 @@ template <class E, uint32_t M, uint32_t N, uint32_t WAVES_M, uint32_t WAVES_N, b
             meet();
         }
     }
+    // The same, four values at a time, for results of four bytes: a load or store of the wavefront is whole rows of 32 J values.
+    template <class Look, class Take> static __device__ __forceinline__ void by_fours(Lds &lds, const Sums &sums, Look look, Take take)
+    {
+        const uint32_t lane = lane_id(), wave = uniform(threadIdx.x >> 6), wm = wave_m(), wn = wave_n();
+        float *const mine = lds.part[wave];
+        sync();
+#pragma unroll
+        for (uint32_t i = 0; i < I; ++i) {
+#pragma unroll
+            for (uint32_t p = 0; p < 2 * PASSES; ++p) {
+                const uint32_t at = p * 64 + lane;
+                look(p, wm + 32 * i + at / (8 * J), wn + at % (8 * J) * 4);
+            }
+#pragma unroll
+            for (uint32_t j = 0; j < J; ++j)
+#pragma unroll
+                for (uint32_t r = 0; r < 16; ++r) mine[square_row(r) * ROW_PITCH + 32 * j + (lane & 31u)] = sums[i][j][r];
+            meet();
+#pragma unroll
+            for (uint32_t p = 0; p < 2 * PASSES; ++p) {
+                const uint32_t at = p * 64 + lane, row = at / (8 * J), c = at % (8 * J) * 4;
+                f32x4 v = *(const f32x4 *)(mine + row * ROW_PITCH + c);
+                take(p, wm + 32 * i + row, wn + c, v);
+            }
+            meet();
+        }
+    }
     // The same where the values are wanted by columns too: take(p, m, n, v, back) leaves at `back` what turn(m, n, v) gets as eight values
     // of a column, m to m + 7.
     template <class Look, class Take, class Turn> static __device__ __forceinline__ void by_rows(Lds &lds, const Sums &sums, Look look, Take take, Turn turn)
     {
         const uint32_t lane = lane_id(), wave = uniform(threadIdx.x >> 6), wm = wave_m(), wn = wave_n();
         float *const mine = lds.part[wave];
-        __syncthreads();
+        sync();
 #pragma unroll
         for (uint32_t i = 0; i < I; ++i) {
             if constexpr (I > 1) {
@@ -364,7 +391,7 @@ template <class E, uint32_t M, uint32_t N, uint32_t WAVES_M, uint32_t WAVES_N, b
     {
         const uint32_t lane = lane_id(), wave = uniform(threadIdx.x >> 6), wm = wave_m(), wn = wave_n();
         float *const mine = lds.part[wave];
-        __syncthreads();
+        sync();
 #pragma unroll
         for (uint32_t i = 0; i < I; i += ABOVE) {
 #pragma unroll
@@ -393,6 +420,12 @@ template <class E, uint32_t M, uint32_t N, uint32_t WAVES_M, uint32_t WAVES_N, b
             meet();
         }
     }
+    // The tile's wavefronts meet (one alone needs no barrier, which others of its workgroup that have ended would not reach).
+    static __device__ __forceinline__ void sync()
+    {
+        if constexpr (WAVES == 1) meet();
+        else __syncthreads();
+    }
     // What lanes of a wavefront have written to LDS is there for the others.
     static __device__ __forceinline__ void meet()
     {
@@ -418,21 +451,14 @@ __device__ __forceinline__ TilePlace place_of_tile(uint32_t at, uint32_t m_tiles
     return TilePlace{first + in % high, in / high};
 }
 
-// A value in two halves (22 bits).
-__device__ __forceinline__ void halves_of(float v, f16 &hi, f16 &lo)
+__device__ __forceinline__ float half_value(uint16_t bits)
 {
-    hi = (f16)v;
-    lo = (f16)(v - (float)hi);
-}
-__device__ __forceinline__ uint32_t bits_of(f16 a, f16 b)
-{
-    uint16_t x, y;
-    __builtin_memcpy(&x, &a, 2);
-    __builtin_memcpy(&y, &b, 2);
-    return x | (uint32_t)y << 16;
+    f16 h;
+    __builtin_memcpy(&h, &bits, 2);
+    return (float)h;
 }
 
-// Eight values as halves, in one part or two.
+// Eight values as halves, in two parts (22 bits of each).
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef f16 f16x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ void halves8(const float (&v)[8], u32x4 &hi, u32x4 &lo)

@@ -240,12 +240,21 @@ int main(int, char **argv)
             head(type, 140, 72, 129, 8, 8, true, false, true);
         }
         head(2, 32, 136, 260, 0, 0, false, true, false);
+        // few rows, operands as they are: whole chunks and what is left of them, any alignment
+        for (int type = 0; type < 3; ++type) {
+            head(type, 5, 300, 140, 1, 1, true, true, true);
+            head(type, 17, 129, 70, 3, 0, true, false, false);
+            head(type, 32, 257, 45, 0, 1, false, true, false);
+        }
         head(2, 0, 16, 9, 0, 0, true, true, false);
         head(1, 0, 16, 9, 0, 0, true, true, true);
     } else if (what == "large") {
         head(2, 270, 72, 300, 0, 0, true, true, false);
         head(1, 257, 64, 257, 8, 0, false, true, true);
         head(0, 30, 40, 520, 0, 0, true, true, false);
+    } else if (what == "tiles") {
+        ortho(0, 0, 2, 133, 40, 1, 2, false);
+        ortho(2, 2, 1, 130, 140, 0, 1, true);
     } else {
         for (int out = 0; out < 3; ++out) {
             ortho(0, out, 1, 1, 1, 0, 5, false);
