@@ -394,3 +394,51 @@ def test_refuses_what_is_elsewhere():
         with pytest.raises(dgs.DgsError) as err:
             call()
         assert err.value.code == dgs.DGS_EINVAL
+
+
+# rows, columns, entries, type, padding, shift: few rows, whose operands are read as they are
+FEW = [(1, 3, 40, F32, 0, 1), (2, 130, 33, F32, 1, 0), (9, 64, 31, F32, 0, 0), (17, 1000, 65, F32, 3, 1), (32, 257, 400, F32, 0, 0),
+       (4, 515, 100, BF16, 2, 1), (16, 1025, 700, BF16, 0, 0), (17, 300, 129, BF16, 1, 0), (32, 77, 1000, BF16, 5, 1), (5, 129, 64, F16, 0, 1),
+       (16, 640, 333, F16, 1, 0), (20, 121, 257, F16, 0, 0), (32, 2049, 90, F16, 0, 3)]
+
+
+@pytest.mark.parametrize("case", FEW, ids=lambda c: f"{c[0]}x{c[1]}x{c[2]}-{str(c[3])[6:]}")
+def test_few_rows(case):
+    print(case, flush=True)
+    rows, cols, vocab, dtype, pad, shift = case
+    c = Case(rows, cols, vocab, dtype, True, pad, shift)
+    loss, lse = c.head().forward(c.x, c.targets)
+    want = c.exact(c.dloss, c.dlse)
+    got = dict(c.gradients(lse, c.dloss, c.dlse), loss=loss, lse=lse)
+    for k in got:
+        assert_near(got[k], want[k], k)
+    # a row's loss does not depend on the rows beside it
+    alone = c.head().forward(c.x[-1:], c.targets[-1:])[1]
+    assert_near(alone, (want["lse"][0][-1:], want["lse"][1][-1:]), "alone")
+
+
+def test_sums_of_many_splits_over_pieces():
+    """The logits' gradient in several pieces of the vocabulary: rows of which a piece holds 256 entries at a time."""
+    rows, cols, vocab = 1_100_000, 8, 600
+    c = Case(rows, cols, vocab, BF16, True, left_out=0.1)
+    lse = c.head().forward(c.x, c.targets)[1]
+    got = c.gradients(lse)
+    some = slice(0, rows, 1000)
+    part = Case(1, cols, vocab, BF16)
+    part.rows, part.x, part.w, part.bias, part.targets = rows // 1000, c.x[some][:rows // 1000], c.w, c.bias, c.targets[some][:rows // 1000]
+    want = part.exact()
+    assert_near(lse[some][:rows // 1000], want["lse"], "lse")
+    assert_near(got["dx"][some][:rows // 1000], want["dx"], "dx")
+    dw, db = torch.zeros(vocab, cols, dtype=D, device=DEV), torch.zeros(vocab, dtype=D, device=DEV)
+    size = torch.zeros(vocab, cols, dtype=D, device=DEV)
+    for lo in range(0, rows, 100_000):
+        x, t = c.x[lo:lo + 100_000].to(D), c.targets[lo:lo + 100_000]
+        z = torch.softmax(x @ c.w.to(D).t() + c.bias.to(D), 1)
+        up = (t >= 0).to(D)
+        z.mul_(up[:, None]).scatter_add_(1, t.clamp(min=0)[:, None], -up[:, None])
+        dw += z.t() @ x
+        db += z.sum(0)
+        size += z.abs().t() @ x.abs()
+    # (sums of a million terms of random sign: 2^-24 sqrt(n) of them and what each is off by, 2^-18)
+    assert bool(((got["dweight"].to(D) - dw).abs() <= size * 2.0 ** -17).all())
+    assert float((got["dbias"].to(D) - db).abs().max()) <= rows * 2.0 ** -18
