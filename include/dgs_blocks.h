@@ -1,7 +1,8 @@
 /*
  * libdgs, training blocks -- the memory-bound part of a transformer worker's step, around the hot path of dgs.h: what lies
  * between two blocks (norm, gate, residual sum, norm), the 8-bit checkpoints that the forward pass keeps for the backward
- * pass, and the gradients that are read from them.  Parameters and their gradients are fp32, as in the flat buffers of
+ * pass, and the gradients that are read from them; and what lies behind the last block: the output layer with its loss, and
+ * updates orthogonalised before they are sent.  Parameters and their gradients are fp32, as in the flat buffers of
  * dgs.h, and gradients can be added to what such a buffer holds.
  *
  * Conventions as in dgs.h: the caller owns every device buffer; a call enqueues its work on `hip_stream` (a hipStream_t,
@@ -175,8 +176,8 @@ int dgs_checkpoint_weight_grad(const dgs_weight_grad_args *args /*host*/, void *
  * Logits are not kept: the backward pass computes them again, a piece of the vocabulary at a time.
  *
  * x, weight and dx have `type`; bias, loss, lse, dweight and dbias are fp32.  Sums, exponentials and statistics are fp32, of
- * products that are exact (DGS_F32: x and W in 22 bits).  dz is held in 22 bits, 11 for a dx of 16 bits.  Of the operands of
- * the gradients' products, magnitudes below 2^-39 of the largest (of W; of x times its row's gradients) are lost.  A bias of
+ * products that are exact (DGS_F32: x and W in 22 bits).  dz is held in 22 bits, of which a dx of DGS_BF16 takes 11 (of at
+ * most 16 rows all).  Of the operands of the gradients' products, magnitudes below 2^-39 of the largest (of W; of x times its row's gradients) are lost.  A bias of
  * -infinity takes an entry out; where all of them are out, and where logits are infinite or NaN, lse is what the formula gives or NaN.
  * A row that nothing arrives at (dloss and dlse 0) leaves no gradient, whatever it holds.
  *

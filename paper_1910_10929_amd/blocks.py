@@ -2,7 +2,8 @@
 
 The memory-bound part of a transformer worker's step, around `dgs.Context`: the edge between two blocks (norm of
 the branch, gate, residual sum, norm of the stream) with its gradients, 8-bit checkpoints of activations, and the gradient of
-a linear layer read from the checkpoint of its input.  Parameters and their gradients are fp32 vectors and matrices -- slices
+a linear layer read from the checkpoint of its input; and the end of that step: the output layer with its loss and gradients,
+and updates of weight matrices orthogonalised.  Parameters and their gradients are fp32 vectors and matrices -- slices
 of the flat buffers that `dgs.Context` works on -- and gradients can be added to what is there.
 
 Matrices are 2-d tensors whose columns are contiguous; rows may be any distance apart.  Work is enqueued on torch's

@@ -7,8 +7,8 @@
 //
 // Numbers.  Sums, statistics and exponentials are fp32.  Logits are products of the operands as they are (bfloat16, half;
 // fp32 in two halves, 22 bits).  The gradient of the logits is divided by a power of two for each row (at least the larger
-// of the incoming gradients) and held in two halves, 22 bits of each value; dx of 16-bit types takes the first, 11 bits
-// where the result is rounded to 8 or 11, dweight, in fp32, both.  The other operand of these products is W or x in half,
+// of the incoming gradients) and held in two halves, 22 bits of each value; dx in bfloat16 takes the first, 11 bits
+// where the result is rounded to 8, everything else both.  The other operand of these products is W or x in half,
 // scaled by powers of two so that the largest magnitude lies below 2^15: a bfloat16 value is exact there down to 2^-31 of the
 // largest, and what is lost of smaller ones is below 2^-39 of it.  x carries the rows' powers of two.
 #include "dgs_product.h"
@@ -89,7 +89,8 @@ __device__ __forceinline__ uint32_t target_of(const Targets &t, uint32_t row)
     return min(((const uint32_t *)t.at)[row], t.vocab);
 }
 
-// Exponents of x, row by row, and of W; in a backward pass what the rows need besides.  A wavefront a row.
+// Exponents of x, row by row, and of W; in a backward pass what the rows need besides.  A wavefront a row.  Bound by memory: x of
+// 8192 x 4096 and W of 32768 x 4096 in bfloat16, 336 MB, 57 us (5.9 TB/s, part of it from cache).
 template <class T>
 __global__ __launch_bounds__(256) void k_head_range(const T *x, uint64_t x_stride, const T *w, uint64_t w_stride, uint32_t rows,
                                                     uint32_t cols, Targets targets, const float *lse, const float *dloss,
@@ -168,7 +169,7 @@ struct CopyJobs {
 };
 
 // Operands in the form that the products read.  Eight columns a lane; columns up to the next multiple of eight are zeros.  Bound by memory:
-// a bfloat16 W of 32768 x 4096 into halves, 537 MB, 85 us (6.3 TB/s, part of it from cache).
+// a bfloat16 W of 32768 x 4096 and x of 8192 x 4096 into halves, 671 MB, 107 us (6.3 TB/s, part of it from cache).
 template <class T>
 __global__ __launch_bounds__(256) void k_head_copy(CopyJobs jobs, Ranges ranges, const HeadRow *row_info, Scales *scales)
 {
@@ -449,6 +450,9 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void k_head_few_dx(const T *w, uint
 }
 
 // Entries (m) and rows (n) of a tile.  E: the operands' type as they are staged; STAGES = 0: as they are read, a square to a wavefront.
+// Bound by the matrix units: of 8192 x 4096 x 32768 (2.2 TFLOP, bfloat16) 1695 us, 1297 TFLOP/s, with the gradient's halves written
+// (1.1 GB) 1835; of 8192 x 768 x 30522 376 and 527, since 12 steps a tile hide less of its epilogue.  One row of 768 columns: by W's reading,
+// 47 MB in 10.3 us.  No branch in the epilogue but for tiles at the edge or with a target: with them 16384 x 768 x 30522 760 us, without 671.
 template <class E, uint32_t M, uint32_t N, uint32_t WAVES_M, uint32_t WAVES_N, uint32_t STAGES, bool BACK>
 __global__ __launch_bounds__(STAGES ? WAVES_M *WAVES_N * 64 : FEW_WAVES * 64, 2) void k_head_logits(LogitArgs a)
 {
@@ -633,7 +637,8 @@ __global__ __launch_bounds__(STAGES ? WAVES_M *WAVES_N * 64 : FEW_WAVES * 64, 2)
     }
 }
 
-// A row's lse and loss from its tiles' parts.  `apart` lanes a row (a power of two), 256 / apart rows.
+// A row's lse and loss from its tiles' parts (8 bytes each: 3 to 7 us, most of it the launch).
+// `apart` lanes a row (a power of two), 256 / apart rows.
 __global__ __launch_bounds__(256) void k_head_loss(const float2 *stats, const float *target_logit, Targets targets, uint32_t rows,
                                                    uint32_t tiles, uint32_t apart, float *loss, float *lse)
 {
@@ -676,7 +681,9 @@ struct GradientArgs {
     const Scales *scales;    // whole: x's exponent comes off
 };
 
-// TURN_A: the first operand's k lies outside.  (The second's always does.)
+// dx (of a piece's entries) and dweight (TURN_A: the first operand's k lies outside; the second's always does).  Bound by the matrix units:
+// of 8192 x 4096 x 32768, dx 1695 us (1297 TFLOP/s), dweight, of two halves, 3518 (1250).  Of 8192 x 768 x 30522 dx 374 and dweight 726:
+// 256 x 128, two workgroups to a compute unit, so that one's epilogue overlaps the other's product; 256 x 256 takes 882.
 template <uint32_t M, uint32_t N, uint32_t WAVES_M, uint32_t WAVES_N, uint32_t STAGES, bool TURN_A>
 __global__ __launch_bounds__(WAVES_M *WAVES_N * 64, 2) void k_head_product(GradientArgs a)
 {
@@ -712,7 +719,8 @@ __global__ __launch_bounds__(WAVES_M *WAVES_N * 64, 2) void k_head_product(Gradi
     });
 }
 
-// dx: the splits' sums, times the row's power, W's taken off.  Eight columns a lane; GROUPS lanes take the splits in turn.
+// dx: the splits' sums, times the row's power, W's taken off.  Eight columns a lane; GROUPS lanes take the splits in turn.  Bound by
+// memory: 8192 x 4096 of one sum into bfloat16, 201 MB, 36 us (5.6 TB/s).
 template <class T, uint32_t GROUPS>
 __global__ __launch_bounds__(256) void k_head_dx(const float *sums, uint32_t splits, uint32_t rows, uint32_t cols, const HeadRow *row_info,
                                                  const Scales *scales, T *dx, uint64_t dx_stride)

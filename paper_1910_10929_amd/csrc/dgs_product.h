@@ -87,7 +87,7 @@ template <uint32_t WIDTH, bool TURNED, uint32_t WAVES, uint32_t STEP> struct Sta
     static constexpr uint32_t PIECES = TURNED ? WIDTH / 8 : STEP / 8;
     static __device__ __forceinline__ uint32_t at(uint32_t row, uint32_t piece)
     {
-        return row * PIECES * 8 + ((!TURNED ? piece ^ (PIECES == 8 ? (row >> 1) & 7u : (row >> 2) & 3u) : PIECES == 8 ? piece ^ ((row & 2u) << 1) : piece ^ ((row & 3u) << 2)) << 3);
+        return row * PIECES * 8 + ((!TURNED ? piece ^ ((row >> 1) & 7u) : PIECES == 8 ? piece ^ ((row & 2u) << 1) : piece ^ ((row & 3u) << 2)) << 3);
     }
     uint32_t offset[LOADS], k;      // (straight: the k that a lane loads is the same in all its loads)
     Window from;
@@ -118,6 +118,7 @@ template <uint32_t WIDTH, bool TURNED, uint32_t WAVES, uint32_t STEP> struct Sta
     {
         load_to_lds(from, TURNED || inside ? offset[i] : NOWHERE, lds, stage * (WIDTH * STEP * 2) + i * WAVES * 1024);
     }
+    static_assert(TURNED || PIECES == 8, "the exchange is of eight pieces");
     static_assert(LOADS > 0 && (TURNED || WAVES * 64 / PIECES % 16 == 0), "whole loads, of one k");
     // The operand of one matrix instruction: 32 of m from `m` on, k from 16 s to 16 s + 15.
     static __device__ __forceinline__ u32x4 fragment(const uint16_t *lds, uint32_t m, uint32_t s)
@@ -500,7 +501,7 @@ static inline uint32_t tiles_of(uint32_t n, uint32_t size) { return n ? (n - 1) 
 
 // Microseconds that `tiles` tiles of `steps` steps of 64 k take: what a tile takes besides its steps, and for a step with every
 // compute unit's places taken and with one workgroup to a compute unit at most, as timed.  (4096 x 4096 squares on and below the
-// diagonal, 64 steps: 256 x 256 110 us, 128 x 128 114, 64 x 64 170; four of 1024 x 1024, 192 steps: 230, 128, 141; five of 333 x 333, 48
+// diagonal, 64 steps: 256 x 256 110 us, 192 x 192 91, 128 x 128 114, 64 x 64 170; four of 1024 x 1024, 192 steps: 230, 128, 141; five of 333 x 333, 48
 // steps: 66, 33, 17; 30522 x 768 turned, 256 steps: 256 x 256 882, 256 x 128 775, 128 x 128 845.)
 static inline float tile_time(int tile, uint64_t tiles, uint32_t steps)
 {
