@@ -177,15 +177,17 @@ int dgs_checkpoint_weight_grad(const dgs_weight_grad_args *args /*host*/, void *
  *
  * x, weight and dx have `type`; bias, loss, lse, dweight and dbias are fp32.  Sums, exponentials and statistics are fp32, of
  * products that are exact (DGS_F32: x and W in 22 bits).  dz is held in 22 bits, of which a dx of DGS_BF16 takes 11 (of at
- * most 16 rows all).  Of the operands of the gradients' products, magnitudes below 2^-39 of the largest (of W; of x times its row's gradients) are lost.  A bias of
- * -infinity takes an entry out; where all of them are out, and where logits are infinite or NaN, lse is what the formula gives or NaN.
+ * most 16 rows all).  Of the operands of the gradients' products, magnitudes below 2^-39 of the largest (of W; of x times its
+ * row's gradients) are lost.  A bias of -infinity takes an entry out; where all of them are out, and where logits are infinite or
+ * NaN, lse is what the formula gives or NaN.
  * A row that nothing arrives at (dloss and dlse 0) leaves no gradient, whatever it holds.
  *
  *   forward    reads x, weight, bias, targets; writes loss (or NULL) and lse.
  *   backward   reads those and lse; writes dx, dweight (rows dweight_stride apart) and dbias, each or none of them.
  *              accumulate != 0: dweight and dbias are added to.
  * Outputs overlap nothing.  workspace: at least dgs_head_workspace() bytes for the same arguments (of the pointers their
- * alignment counts), 16-byte aligned; as above.  More than 2^20 columns, 2^24 rows or entries, or strides of 2^21: DGS_ENOTSUP.
+ * alignment counts), 16-byte aligned; as above.  More than 2^20 columns, 2^24 rows or entries, 2^34
+ * values of x or 2^38 logits, or strides of 2^21: DGS_ENOTSUP.
  */
 typedef struct dgs_head_args {
     uint32_t rows, cols, vocab;

@@ -760,19 +760,25 @@ __global__ __launch_bounds__(256) void k_head_dx(const float *sums, uint32_t spl
     store8(dx + row * dx_stride, c, n, v);
 }
 
-// dweight: the splits' sums, x's exponent taken off.
+// dweight: the splits' sums, x's exponent taken off (no splits: zeros).
+constexpr uint32_t DWEIGHT_BLOCKS = 1u << 16;      // at most
 __global__ __launch_bounds__(256) void k_head_dweight(const float *sums, uint32_t splits, uint32_t rows, uint32_t cols,
                                                       const Scales *scales, float *out, uint64_t out_stride, uint32_t add)
 {
-    const uint64_t at = (uint64_t)blockIdx.x * 256 + threadIdx.x;
-    const uint64_t row = at / cols;
-    if (row >= rows) return;
-    const uint32_t c = (uint32_t)(at - row * cols);
-    float v = 0.0f;
-    for (uint32_t s = 0; s < splits; ++s) v += sums[((uint64_t)s * rows + row) * cols + c];
-    if (splits) v = times_power(v, -GRAD_TOP - scales->x);
-    float *const p = out + row * out_stride + c;
-    *p = add ? *p + v : v;
+    const uint64_t end = (uint64_t)rows * cols;
+    for (uint64_t at = blockIdx.x * 256 + threadIdx.x; at < end; at += gridDim.x * 256) {
+        const uint64_t row = at / cols;
+        float v = 0.0f;
+        for (uint32_t s = 0; s < splits; ++s) v += sums[s * end + at];
+        if (splits) v = times_power(v, -GRAD_TOP - scales->x);
+        float *const p = out + row * out_stride + (at - row * cols);
+        *p = add ? *p + v : v;
+    }
+}
+static uint32_t dweight_blocks(uint32_t rows, uint32_t cols)
+{
+    const uint64_t n = ((uint64_t)rows * cols + 255) / 256;
+    return n < DWEIGHT_BLOCKS ? (uint32_t)n : DWEIGHT_BLOCKS;
 }
 
 // dbias: the tiles' sums, 64 entries to a workgroup, four lanes each.
@@ -1052,6 +1058,8 @@ static int refused(const dgs_head_args &p, bool back)
     // (a tile's 256 rows are reached by 31 bits)
     if (p.cols > (1u << 20) || p.x.stride >= (1u << 21) || p.weight.stride >= (1u << 21)) return DGS_ENOTSUP;
     if (p.rows > (1u << 24) || p.vocab > (1u << 24)) return DGS_ENOTSUP;
+    // (a launch has less than 2^32 lanes: a lane for 128 logits, for eight values of dx)
+    if ((uint64_t)p.rows * p.vocab > (1ull << 38) || (uint64_t)p.rows * p.cols > (1ull << 34)) return DGS_ENOTSUP;
     return DGS_OK;
 }
 
@@ -1101,7 +1109,7 @@ extern "C" int dgs_head_backward(const dgs_head_args *args, void *hip_stream)
     if (p.rows == 0) {      // (no sums: zeros, or what is there)
         if (p.accumulate || (!p.dweight && !p.dbias)) return DGS_OK;
         if (p.dweight)
-            hipLaunchKernelGGL(k_head_dweight, dim3((uint32_t)(((uint64_t)p.vocab * p.cols + 255) / 256)), dim3(256), 0, (hipStream_t)hip_stream,
+            hipLaunchKernelGGL(k_head_dweight, dim3(dweight_blocks(p.vocab, p.cols)), dim3(256), 0, (hipStream_t)hip_stream,
                                (const float *)nullptr, 0u, p.vocab, p.cols, (const Scales *)nullptr, p.dweight, p.dweight_stride, 0u);
         if (p.dbias)
             hipLaunchKernelGGL(k_head_dbias, dim3(tiles_of(p.vocab, 64)), dim3(256), 0, (hipStream_t)hip_stream, (const float *)nullptr, 0u,
@@ -1174,7 +1182,7 @@ extern "C" int dgs_head_backward(const dgs_head_args *args, void *hip_stream)
             g.scales = h.scales;
             product<true>(g, h.dw.tile, st);
             if (h.dw.splits > 1)
-                hipLaunchKernelGGL(k_head_dweight, dim3((uint32_t)(((uint64_t)count * p.cols + 255) / 256)), dim3(256), 0, st,
+                hipLaunchKernelGGL(k_head_dweight, dim3(dweight_blocks(count, p.cols)), dim3(256), 0, st,
                                    (const float *)h.dw_sums, g.splits, count, p.cols, (const Scales *)h.scales,
                                    p.dweight + first * p.dweight_stride, p.dweight_stride, (uint32_t)(p.accumulate != 0));
         }

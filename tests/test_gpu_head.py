@@ -154,6 +154,14 @@ def test_added_to_and_partly_asked_for(dtype):
     assert torch.equal(only, whole["dbias"])
 
 
+def test_no_rows_of_a_large_weight():      # (more values than the launch has lanes)
+    dw = torch.full((4100, 4200), float("nan"), device=DEV)
+    h = blocks.Head(torch.zeros(4100, 4100, device=DEV, dtype=BF16))
+    x, t = torch.zeros(0, 4100, device=DEV, dtype=BF16), torch.zeros(0, dtype=torch.int32, device=DEV)
+    h.backward(x, t, torch.zeros(0, device=DEV), dweight=dw[:, :4100], need_dx=False)
+    assert bool((dw[:, :4100] == 0).all()) and bool(dw[:, 4100:].isnan().all())
+
+
 def test_no_rows():
     h = blocks.Head(torch.zeros(20, 16, device=DEV))
     x, t = torch.zeros(0, 16, device=DEV), torch.zeros(0, dtype=torch.int64, device=DEV)

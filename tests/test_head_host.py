@@ -30,6 +30,7 @@ BOTH = [
     (EINVAL, dict(work=0)), (EINVAL, dict(work=P + 8)), (ENOMEM, dict(bytes=100)),
     (ENOTSUP, dict(cols=(1 << 20) + 8, xs=1 << 21, ws=1 << 21, dxs=1 << 21, dws=1 << 21)), (ENOTSUP, dict(xs=1 << 21)), (ENOTSUP, dict(ws=1 << 21)),
     (ENOTSUP, dict(rows=(1 << 24) + 1)), (ENOTSUP, dict(vocab=(1 << 24) + 1)),
+    (ENOTSUP, dict(rows=1 << 20, vocab=(1 << 18) + 1)), (ENOTSUP, dict(rows=1 << 24, cols=1032, xs=1032, ws=1032, dxs=1032, dws=1032)),
 ]
 
 
