@@ -12,6 +12,7 @@ anything is enqueued.  Nothing here is recorded by autograd.  There is no CPU fa
 """
 from __future__ import annotations
 
+import collections
 import ctypes
 import functools
 import struct
@@ -558,7 +559,7 @@ def orthogonalise(updates, out=None, steps=5, coefficients=(3.4445, -4.7750, 2.0
     """Updates of weight matrices -- one matrix, or a list of matrices of one shape and type -- with their singular vectors kept
     and their singular values taken near 1 by Newton-Schulz products; see dgs_orthogonalise in the header.  Of each: X = G / (|G| + eps),
     `steps` times X = a X + (b A + c A^2) X with A = X X^T (of the smaller side), then out = scale X, or with `accumulate` out + scale X.
-    `out`: as `updates`, of any one of the three types, or new ones of the updates' type; may be the updates themselves.  fp32 and half
+    `out`: as `updates`, of any one of the three types, or new ones of the updates' type; each may be its own update.  fp32 and half
     results take 22 bits of the operands to the products, bfloat16 ones 11."""
     one = isinstance(updates, torch.Tensor)
     given = [updates] if one else list(updates)
@@ -585,7 +586,7 @@ def orthogonalise(updates, out=None, steps=5, coefficients=(3.4445, -4.7750, 2.0
     if outs is None:
         outs = [torch.empty((rows, cols), dtype=first.dtype, device=first.device) for _ in given]
     out_kind = _type(outs[0], "out")
-    if not 1 <= steps <= 1000 or len(coefficients) != 3:
+    if not isinstance(steps, int) or not 1 <= steps <= 1000 or len(coefficients) != 3:
         _refuse("steps: 1 to 1000; coefficients: three")
     places, out_places = [], []
     for g, o in zip(given, outs):
@@ -595,6 +596,9 @@ def orthogonalise(updates, out=None, steps=5, coefficients=(3.4445, -4.7750, 2.0
         out_places += _matrix(o, rows, cols, device, "out")
     if len(set(out_places[::2])) != len(outs):
         _refuse("out: one matrix twice")
+    given_at = collections.Counter(places[::2])
+    if any(given_at[o] > (o == i) for i, o in zip(places[::2], out_places[::2])):
+        _refuse("out: lies over another update than its own")
     table = struct.pack(f"@{2 * len(places)}Q", *places, *out_places)
     table = ctypes.create_string_buffer(table, len(table))
     at = ctypes.addressof(table)

@@ -175,14 +175,16 @@ def test_orthogonalise_hands_over(calls):
 
 
 def test_orthogonalise_refuses(calls):
-    g = torch.zeros(30, 20)
+    g, other = torch.zeros(30, 20), torch.zeros(30, 20)
     bad = [
         lambda: blocks.orthogonalise(g[0]), lambda: blocks.orthogonalise(g.double()), lambda: blocks.orthogonalise([g, g[:20]]),
         lambda: blocks.orthogonalise([g, g.half()]), lambda: blocks.orthogonalise(g, accumulate=True), lambda: blocks.orthogonalise([g], g),
         lambda: blocks.orthogonalise([g, g], [g]), lambda: blocks.orthogonalise(g, g.t()), lambda: blocks.orthogonalise(g, steps=0),
         lambda: blocks.orthogonalise(g, coefficients=(1.0, 2.0)), lambda: blocks.orthogonalise(g.t()), lambda: blocks.orthogonalise(g[:0]),
         lambda: blocks.orthogonalise([g, g.clone()], [g.clone(), g.half()]), lambda: blocks.orthogonalise(g, g.to(torch.int32)),
-        lambda: blocks.orthogonalise([g, g.clone()], [torch.zeros(30, 20)] * 2),
+        lambda: blocks.orthogonalise([g, g.clone()], [torch.zeros(30, 20)] * 2), lambda: blocks.orthogonalise(g, steps=2.5),
+        lambda: blocks.orthogonalise([g, other], [other, g]), lambda: blocks.orthogonalise([g, other], [torch.zeros(30, 20), g]),
+        lambda: blocks.orthogonalise([g, g], [g, other]),
     ]
     for i, call in enumerate(bad):
         with pytest.raises(dgs.DgsError) as err:
