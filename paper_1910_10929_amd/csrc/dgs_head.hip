@@ -861,9 +861,10 @@ struct HeadPlan {
     float *bias_parts, *dx_sums, *dw_sums;
 };
 
-static bool straight_ok(const dgs_matrix &m, uint32_t cols)
+// Whether a product's loads take the matrix as it is: in pieces of 16 bytes, and (a tile's 256 rows reached by 31 bits) rows not too far apart.
+static bool straight_ok(const dgs_matrix &m, uint32_t rows, uint32_t cols)
 {
-    return cols % 8 == 0 && m.stride % 8 == 0 && aligned_to(m.data, 16);
+    return cols % 8 == 0 && aligned_to(m.data, 16) && (rows == 1 || (m.stride % 8 == 0 && m.stride < (1u << 21)));
 }
 static HeadPlan plan_of(const dgs_head_args &p, bool back)
 {
@@ -873,7 +874,7 @@ static HeadPlan plan_of(const dgs_head_args &p, bool back)
     h.wants_dw = back && p.dweight;
     h.width = (p.cols + 7) & ~7u;
     const bool f32 = p.type == DGS_F32;
-    const bool staged = straight_ok(p.x, p.cols) && straight_ok(p.weight, p.cols);
+    const bool staged = straight_ok(p.x, p.rows, p.cols) && straight_ok(p.weight, p.vocab, p.cols);
     h.few = p.rows <= FEW_ROWS;
     h.direct = h.few && (f32 || !staged);
     // (dx alone, bfloat16 W of 32000 x 4096, by few_dx and by the matrix units from a copy of W: 8 rows 140 and 267 us, 16 rows 206 and 287,
@@ -881,8 +882,8 @@ static HeadPlan plan_of(const dgs_head_args &p, bool back)
     h.few_dx = h.few && (f32 || p.rows <= 16);
     h.split = f32 && !h.few;
     h.scale_w = h.split || (p.type == DGS_BF16 && h.wants_dx && !h.few_dx);
-    h.copy_x = !f32 && !h.few && !straight_ok(p.x, p.cols);
-    h.copy_w = !f32 && !straight_ok(p.weight, p.cols) && (!h.few || (p.type == DGS_F16 && h.wants_dx && !h.few_dx));
+    h.copy_x = !f32 && !h.few && !straight_ok(p.x, p.rows, p.cols);
+    h.copy_w = !f32 && !straight_ok(p.weight, p.vocab, p.cols) && (!h.few || (p.type == DGS_F16 && h.wants_dx && !h.few_dx));
     h.logits = h.direct ? TILE_DIRECT : h.few ? TILE_FEW : logits_tile(p.vocab, p.rows, steps_of(p.cols, f32 ? BOTH_IN_TWO : ONE_PAIR));
     Sections s = {(uintptr_t)p.workspace, 0};
     const uint64_t x_bytes = (uint64_t)p.rows * h.width * 2, w_bytes = (uint64_t)p.vocab * h.width * 2;
@@ -1055,9 +1056,7 @@ static int refused(const dgs_head_args &p, bool back)
     }
     if (back && p.dweight && (p.dweight_stride < p.cols || p.dweight_stride >= (1ull << 32))) return DGS_EINVAL;
     if (!aligned_to(p.dloss, 4) || !aligned_to(p.dlse, 4) || !aligned_to(p.dweight, 4) || !aligned_to(p.dbias, 4)) return DGS_EINVAL;
-    // (a tile's 256 rows are reached by 31 bits)
-    if (p.cols > (1u << 20) || p.x.stride >= (1u << 21) || p.weight.stride >= (1u << 21)) return DGS_ENOTSUP;
-    if (p.rows > (1u << 24) || p.vocab > (1u << 24)) return DGS_ENOTSUP;
+    if (p.cols > (1u << 20) || p.rows > (1u << 24) || p.vocab > (1u << 24)) return DGS_ENOTSUP;
     // (a launch has less than 2^32 lanes: a lane for 128 logits, for eight values of dx)
     if ((uint64_t)p.rows * p.vocab > (1ull << 38) || (uint64_t)p.rows * p.cols > (1ull << 34)) return DGS_ENOTSUP;
     return DGS_OK;

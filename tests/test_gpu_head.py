@@ -425,6 +425,34 @@ def test_few_rows(case):
     assert_near(alone, (want["lse"][0][-1:], want["lse"][1][-1:]), "alone")
 
 
+@pytest.mark.parametrize("rows", [1, 5, 32, 70])
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+def test_rows_far_apart(rows, dtype):      # the last token of each of a batch's sequences
+    c = Case(rows, 72, 300, dtype, True)
+    far = torch.empty(rows, 1 << 21, dtype=dtype, device=DEV)
+    far[:, -72:] = c.x
+    c.x = far[:, -72:]
+    loss, lse = c.head().forward(c.x, c.targets)
+    want = c.exact(c.dloss, c.dlse)
+    got = dict(c.gradients(lse, c.dloss, c.dlse), loss=loss, lse=lse)
+    for k in got:
+        assert_near(got[k], want[k], k)
+
+
+@pytest.mark.parametrize("rows", [3, 70])
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+def test_entries_far_apart(rows, dtype):
+    c = Case(rows, 72, 130, dtype, True)
+    far = torch.empty(130, (1 << 21) + 8, dtype=dtype, device=DEV)
+    far[:, :72] = c.w
+    c.w = far[:, :72]
+    loss, lse = c.head().forward(c.x, c.targets)
+    want = c.exact(c.dloss, c.dlse)
+    got = dict(c.gradients(lse, c.dloss, c.dlse), loss=loss, lse=lse)
+    for k in got:
+        assert_near(got[k], want[k], k)
+
+
 def test_sums_of_many_splits_over_pieces():
     """The logits' gradient in several pieces of the vocabulary: rows of which a piece holds 256 entries at a time."""
     rows, cols, vocab = 1_100_000, 8, 600

@@ -28,7 +28,7 @@ BOTH = [
     (EINVAL, dict(x=0)), (EINVAL, dict(x=P + 1)), (EINVAL, dict(xs=95)), (EINVAL, dict(w=0)), (EINVAL, dict(ws=95)), (EINVAL, dict(w=P + 1)),
     (EINVAL, dict(bias=P + 2)), (EINVAL, dict(targets=0)), (EINVAL, dict(targets=P + 4)), (EINVAL, dict(lse=0)), (EINVAL, dict(lse=P + 1)),
     (EINVAL, dict(work=0)), (EINVAL, dict(work=P + 8)), (ENOMEM, dict(bytes=100)),
-    (ENOTSUP, dict(cols=(1 << 20) + 8, xs=1 << 21, ws=1 << 21, dxs=1 << 21, dws=1 << 21)), (ENOTSUP, dict(xs=1 << 21)), (ENOTSUP, dict(ws=1 << 21)),
+    (ENOTSUP, dict(cols=(1 << 20) + 8, xs=1 << 21, ws=1 << 21, dxs=1 << 21, dws=1 << 21)), (EINVAL, dict(xs=1 << 32)), (EINVAL, dict(ws=1 << 32)),
     (ENOTSUP, dict(rows=(1 << 24) + 1)), (ENOTSUP, dict(vocab=(1 << 24) + 1)),
     (ENOTSUP, dict(rows=1 << 20, vocab=(1 << 18) + 1)), (ENOTSUP, dict(rows=1 << 24, cols=1032, xs=1032, ws=1032, dxs=1032, dws=1032)),
 ]
@@ -67,7 +67,9 @@ def test_workspace_sizes():
     assert need(1, **dict(big, rows=1 << 20, vocab=1 << 17)) < (1 << 33) + (1 << 28) + (1 << 20) * 768 * 16
     # a matrix that is not laid out in pieces of sixteen bytes is copied
     assert need(0, **dict(big, w=P + 2)) >= need(0, **big) + 30522 * 768 * 2
-    assert need(0, **dict(big, ws=769)) == need(0, **dict(big, w=P + 2))
+    assert need(0, **dict(big, ws=769)) == need(0, **dict(big, w=P + 2)) == need(0, **dict(big, ws=1 << 21))
+    assert need(0, **dict(big, xs=1 << 31)) >= need(0, **big) + 8192 * 768 * 2
+    assert need(0, **dict(big, rows=1, xs=1 << 31)) == need(0, **dict(big, rows=1))
 
 
 ORTHO = dict(count=2, rows=40, cols=50, steps=5, type=0, out=0, accumulate=0, reserved=0, a=3.4, b=-4.8, c=2.0, eps=1e-7, scale=1.0,
