@@ -681,15 +681,17 @@ struct GradientArgs {
     const Scales *scales;    // whole: x's exponent comes off
 };
 
-// dx (of a piece's entries) and dweight (TURN_A: the first operand's k lies outside; the second's always does).  Bound by the matrix units:
+// A tile of dx (of a piece's entries) or dweight (TURN_A: the first operand's k lies outside; the second's always does).  Bound by the matrix units:
 // of 8192 x 4096 x 32768, dx 1695 us (1297 TFLOP/s), dweight, of two halves, 3518 (1250).  Of 8192 x 768 x 30522 dx 374 and dweight 726:
 // 256 x 128, two workgroups to a compute unit, so that one's epilogue overlaps the other's product; 256 x 256 takes 882.
-template <uint32_t M, uint32_t N, uint32_t WAVES_M, uint32_t WAVES_N, uint32_t STAGES, bool TURN_A>
-__global__ __launch_bounds__(WAVES_M *WAVES_N * 64, 2) void k_head_product(GradientArgs a)
-{
+template <uint32_t M, uint32_t N, uint32_t WAVES_M, uint32_t WAVES_N, uint32_t STAGES, bool TURN_A> struct GradientTile {
     typedef Product<f16, M, N, WAVES_M, WAVES_N, TURN_A, true, STAGES, M == 256 && N == 128 ? 32 : PRODUCT_STEP> P;
-    __shared__ __attribute__((aligned(16))) typename P::Lds lds;
-    const uint32_t at = tile_of_block(blockIdx.x, gridDim.x), tiles = a.m_tiles * a.n_tiles;
+    static __device__ __forceinline__ void run(typename P::Lds &lds, const GradientArgs &a, uint32_t at);
+};
+template <uint32_t M, uint32_t N, uint32_t WAVES_M, uint32_t WAVES_N, uint32_t STAGES, bool TURN_A>
+__device__ __forceinline__ void GradientTile<M, N, WAVES_M, WAVES_N, STAGES, TURN_A>::run(typename P::Lds &lds, const GradientArgs &a, uint32_t at)
+{
+    const uint32_t tiles = a.m_tiles * a.n_tiles;
     const uint32_t split = at / tiles;
     const TilePlace place = place_of_tile(at - split * tiles, a.m_tiles, a.n_tiles);
     const uint32_t tile_m = place.m, tile_n = place.n;
@@ -717,6 +719,61 @@ __global__ __launch_bounds__(WAVES_M *WAVES_N * 64, 2) void k_head_product(Gradi
             if (n + 2 < a.n) to[2] = a.add ? to[2] + w.z : w.z;
         }
     });
+}
+
+template <uint32_t M, uint32_t N, uint32_t WAVES_M, uint32_t WAVES_N, uint32_t STAGES, bool TURN_A>
+__global__ __launch_bounds__(WAVES_M *WAVES_N * 64, 2) void k_head_product(GradientArgs a)
+{
+    typedef GradientTile<M, N, WAVES_M, WAVES_N, STAGES, TURN_A> G;
+    __shared__ __attribute__((aligned(16))) typename G::P::Lds lds;
+    G::run(lds, a, tile_of_block(blockIdx.x, gridDim.x));
+}
+
+struct BiasArgs {
+    const float *parts;      // tiles x stride
+    uint32_t tiles, count, add;
+    uint64_t stride;
+    float *out;
+};
+// dbias: the tiles' sums, 64 entries to a workgroup, four lanes each.
+__device__ __forceinline__ void sum_bias(const BiasArgs &a, uint32_t block, float *sums)
+{
+    const uint32_t v = block * 64 + (threadIdx.x & 63u), at = min(v, a.count - 1u);
+    float s = 0.0f;
+    for (uint32_t i = threadIdx.x >> 6; i < a.tiles; i += 32) {
+        float w[8];
+#pragma unroll
+        for (uint32_t k = 0; k < 8; ++k) w[k] = a.parts[min(i + 4 * k, a.tiles - 1u) * a.stride + at];
+#pragma unroll
+        for (uint32_t k = 0; k < 8; ++k) s += i + 4 * k < a.tiles ? w[k] : 0.0f;
+    }
+    sums[threadIdx.x] = s;
+    __syncthreads();
+    if (threadIdx.x >= 64 || v >= a.count) return;
+    s = (s + sums[threadIdx.x + 64]) + (sums[threadIdx.x + 128] + sums[threadIdx.x + 192]);
+    a.out[v] = a.add ? a.out[v] + s : s;
+}
+__global__ __launch_bounds__(256) void k_head_dbias(BiasArgs a)
+{
+    __shared__ float sums[256];
+    sum_bias(a, blockIdx.x, sums);
+}
+
+// Gradients of little work in one launch: tiles of dweight, tiles of dx, and the bias gradient's sums.  Bound by the latency of few steps, so
+// that one beside the other costs little: 300 x 333 x 1009 of fp32 9.4 us, in three launches 8.4, 8.3 and 1.3 and what lies between them.
+__global__ __launch_bounds__(256, 2) void k_head_gradients(GradientArgs dw, GradientArgs dx, BiasArgs bias, uint32_t dw_blocks, uint32_t dx_blocks)
+{
+    typedef GradientTile<64, 64, 2, 2, 4, true> W;
+    typedef GradientTile<64, 64, 2, 2, 4, false> X;
+    __shared__ __attribute__((aligned(16))) union {
+        typename W::P::Lds w;
+        typename X::P::Lds x;
+        float sums[256];
+    } lds;
+    const uint32_t block = blockIdx.x;
+    if (block < dw_blocks) W::run(lds.w, dw, tile_of_block(block, dw_blocks));
+    else if (block < dw_blocks + dx_blocks) X::run(lds.x, dx, tile_of_block(block - dw_blocks, dx_blocks));
+    else sum_bias(bias, block - dw_blocks - dx_blocks, lds.sums);
 }
 
 // dx: the splits' sums, times the row's power, W's taken off.  Eight columns a lane; GROUPS lanes take the splits in turn.  Bound by
@@ -779,27 +836,6 @@ static uint32_t dweight_blocks(uint32_t rows, uint32_t cols)
 {
     const uint64_t n = ((uint64_t)rows * cols + 255) / 256;
     return n < DWEIGHT_BLOCKS ? (uint32_t)n : DWEIGHT_BLOCKS;
-}
-
-// dbias: the tiles' sums, 64 entries to a workgroup, four lanes each.
-__global__ __launch_bounds__(256) void k_head_dbias(const float *parts, uint32_t tiles, uint64_t stride, uint32_t count, float *out,
-                                                    uint32_t add)
-{
-    __shared__ float sums[256];
-    const uint32_t v = blockIdx.x * 64 + (threadIdx.x & 63u), at = min(v, count - 1u);
-    float s = 0.0f;
-    for (uint32_t i = threadIdx.x >> 6; i < tiles; i += 32) {
-        float w[8];
-#pragma unroll
-        for (uint32_t k = 0; k < 8; ++k) w[k] = parts[min(i + 4 * k, tiles - 1u) * stride + at];
-#pragma unroll
-        for (uint32_t k = 0; k < 8; ++k) s += i + 4 * k < tiles ? w[k] : 0.0f;
-    }
-    sums[threadIdx.x] = s;
-    __syncthreads();
-    if (threadIdx.x >= 64 || v >= count) return;
-    s = (s + sums[threadIdx.x + 64]) + (sums[threadIdx.x + 128] + sums[threadIdx.x + 192]);
-    out[v] = add ? out[v] + s : s;
 }
 
 // ---------------------------------------------------------------------------
@@ -1111,8 +1147,8 @@ extern "C" int dgs_head_backward(const dgs_head_args *args, void *hip_stream)
             hipLaunchKernelGGL(k_head_dweight, dim3(dweight_blocks(p.vocab, p.cols)), dim3(256), 0, (hipStream_t)hip_stream,
                                (const float *)nullptr, 0u, p.vocab, p.cols, (const Scales *)nullptr, p.dweight, p.dweight_stride, 0u);
         if (p.dbias)
-            hipLaunchKernelGGL(k_head_dbias, dim3(tiles_of(p.vocab, 64)), dim3(256), 0, (hipStream_t)hip_stream, (const float *)nullptr, 0u,
-                               (uint64_t)0, p.vocab, p.dbias, 0u);
+            hipLaunchKernelGGL(k_head_dbias, dim3(tiles_of(p.vocab, 64)), dim3(256), 0, (hipStream_t)hip_stream,
+                               BiasArgs{nullptr, 0, p.vocab, 0, 0, p.dbias});
         return launched();
     }
     if (!p.workspace || !aligned_to(p.workspace, 16)) return DGS_EINVAL;
@@ -1126,6 +1162,7 @@ extern "C" int dgs_head_backward(const dgs_head_args *args, void *hip_stream)
     else prepare<bf16>(p, h, targets, st);
     const TileSize tile = size_of(h.logits), tx = size_of(h.dx.tile), tw = size_of(h.dw.tile);
     const uint64_t stride = ((uint64_t)h.piece + 7) & ~7ull;
+    const bool together = h.wants_dx && !h.few_dx && h.wants_dw && h.dx.tile == TILE_64 && h.dw.tile == TILE_64;
     LogitArgs a = logit_args(p, h, targets);
     a.row_info = h.row_info;
     a.grad[0] = h.grad[0];
@@ -1138,13 +1175,13 @@ extern "C" int dgs_head_backward(const dgs_head_args *args, void *hip_stream)
         a.end = first + count;
         a.v_tiles = tiles_of(count, tile.m);
         logits<true>(a, p.type, h.logits, st);
-        if (p.dbias)
-            hipLaunchKernelGGL(k_head_dbias, dim3(tiles_of(count, 64)), dim3(256), 0, st, (const float *)h.bias_parts,
-                               a.t_tiles, stride, count, p.dbias + first, (uint32_t)(p.accumulate != 0));
+        const BiasArgs bias = {h.bias_parts, a.t_tiles, count, (uint32_t)(p.accumulate != 0), stride, p.dbias ? p.dbias + first : nullptr};
+        if (p.dbias && !together) hipLaunchKernelGGL(k_head_dbias, dim3(tiles_of(count, 64)), dim3(256), 0, st, bias);
+        GradientArgs dx = {};
         if (h.wants_dx && h.few_dx) {
             few_dx(p, h, first, count, stride, st);
         } else if (h.wants_dx) {
-            GradientArgs g = {};
+            GradientArgs &g = dx;
             const uint16_t *w = p.type == DGS_BF16 ? h.w[1] : h.copy_w ? h.w[0] : a.w.part[0];
             const uint64_t w_stride = p.type == DGS_BF16 || h.copy_w ? h.width : a.w.stride;
             g.a = Side{{h.grad[0], h.grad[1]}, stride, p.rows};
@@ -1160,7 +1197,7 @@ extern "C" int dgs_head_backward(const dgs_head_args *args, void *hip_stream)
             g.out = h.dx_sums;
             g.out_stride = p.cols;
             g.add = first != 0;
-            product<false>(g, h.dx.tile, st);
+            if (!together) product<false>(g, h.dx.tile, st);
         }
         if (h.wants_dw) {
             GradientArgs g = {};
@@ -1179,7 +1216,11 @@ extern "C" int dgs_head_backward(const dgs_head_args *args, void *hip_stream)
             g.out_stride = g.whole ? p.dweight_stride : p.cols;
             g.add = g.whole && p.accumulate;
             g.scales = h.scales;
-            product<true>(g, h.dw.tile, st);
+            if (together) {
+                const uint32_t dw_blocks = g.m_tiles * g.n_tiles * g.splits, dx_blocks = dx.m_tiles * dx.n_tiles * dx.splits;
+                hipLaunchKernelGGL(k_head_gradients, dim3(dw_blocks + dx_blocks + (p.dbias ? tiles_of(count, 64) : 0u)), dim3(256), 0, st, g, dx,
+                                   bias, dw_blocks, dx_blocks);
+            } else product<true>(g, h.dw.tile, st);
             if (h.dw.splits > 1)
                 hipLaunchKernelGGL(k_head_dweight, dim3(dweight_blocks(count, p.cols)), dim3(256), 0, st,
                                    (const float *)h.dw_sums, g.splits, count, p.cols, (const Scales *)h.scales,

@@ -17,6 +17,11 @@ namespace dgs {
 constexpr float HELD = 4096.0f, LEFT = 1.0f / HELD;      // X, A and B are held times 2^12
 constexpr uint32_t ORTHO_AT_ONCE = 32;      // matrices of a launch
 constexpr uint32_t NORM_PARTS = 256;      // at most
+#ifdef DGS_HOST_EMULATION
+constexpr uint32_t SMALL = 1u << 10;
+#else
+constexpr uint32_t SMALL = 1u << 14;      // values of a matrix whose norm has no launch of its own (128 x 128: 6.2 us, in two launches 3.6 and 4.2)
+#endif
 
 struct Matrices {
     const void *data[ORTHO_AT_ONCE];
@@ -50,24 +55,28 @@ __device__ __forceinline__ void put_halves(const Halves &to, uint64_t at, const 
     if (to.lo) *(u32x4 *)(to.lo + at) = lo;
 }
 
+// A lane's sum of squares: of eight columns at a time, from the `at`-th eight on, `step` further each turn.
+template <class T> __device__ __forceinline__ double squares(const T *m, uint64_t stride, uint32_t rows, uint32_t cols, uint32_t at, uint32_t step)
+{
+    const uint32_t pieces = (cols + 7) / 8, end = pieces * rows;      // (at most 2^29)
+    double s = 0.0;
+    for (; at < end; at += step) {
+        const uint32_t row = at / pieces, c = (at - row * pieces) * 8;
+        float v[8];
+        unpack8(load8(m + row * stride + c, live8(c, cols)), v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s += (double)v[i] * (double)v[i];
+    }
+    return s;
+}
+
 // Sums of squares, at most NORM_PARTS a matrix.  Bound by memory: twelve of 2304 x 768 in fp32, 85 MB, 15.4 us (5.5 TB/s).
 template <class T>
 __global__ __launch_bounds__(256) void k_ortho_norm(Matrices in, uint32_t rows, uint32_t cols, double *parts)
 {
     __shared__ double sums[256];
     const uint32_t which = blockIdx.y;
-    const T *const m = (const T *)in.data[which];
-    const uint64_t stride = in.stride[which], pieces = (cols + 7) / 8, end = pieces * rows;
-    double s = 0.0;
-    for (uint64_t at = blockIdx.x * 256 + threadIdx.x; at < end; at += gridDim.x * 256) {
-        const uint64_t row = at / pieces;
-        const uint32_t c = (uint32_t)(at - row * pieces) * 8;
-        float v[8];
-        unpack8(load8(m + row * stride + c, live8(c, cols)), v);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) s += (double)v[i] * (double)v[i];
-    }
-    sums[threadIdx.x] = s;
+    sums[threadIdx.x] = squares((const T *)in.data[which], in.stride[which], rows, cols, blockIdx.x * 256 + threadIdx.x, gridDim.x * 256);
     __syncthreads();
     for (uint32_t by = 128; by; by >>= 1) {
         if (threadIdx.x < by) sums[threadIdx.x] += sums[threadIdx.x + by];
@@ -77,7 +86,8 @@ __global__ __launch_bounds__(256) void k_ortho_norm(Matrices in, uint32_t rows, 
 }
 
 // X from G, 64 x 64 of it to a workgroup, turned where that makes it wide.  Columns up to a multiple of eight are zeros.
-// Bound by memory: twelve of 2304 x 768, 85 MB read and as many written, 32 us (5.3 TB/s).
+// Bound by memory: twelve of 2304 x 768, 85 MB read and as many written, 32 us (5.3 TB/s).  norm_parts = 0: every workgroup takes the norm
+// of its matrix itself.
 template <class T>
 __global__ __launch_bounds__(256) void k_ortho_load(Matrices in, uint32_t rows, uint32_t cols, uint32_t turned, const double *parts, uint32_t norm_parts,
                                                     float eps, Halves x, float *log2_norm)
@@ -85,7 +95,10 @@ __global__ __launch_bounds__(256) void k_ortho_load(Matrices in, uint32_t rows, 
     __shared__ double norm[NORM_PARTS];
     __shared__ float tile[64][65];
     const uint32_t which = blockIdx.y, across = (cols + 63) / 64;
-    norm[threadIdx.x] = threadIdx.x < norm_parts ? parts[which * norm_parts + threadIdx.x] : 0.0;
+    const T *const m = (const T *)in.data[which];
+    const uint64_t stride = in.stride[which];
+    if (norm_parts == 0) norm[threadIdx.x] = squares(m, stride, rows, cols, threadIdx.x, NORM_PARTS);
+    else norm[threadIdx.x] = threadIdx.x < norm_parts ? parts[which * norm_parts + threadIdx.x] : 0.0;
     for (uint32_t by = NORM_PARTS / 2; by; by >>= 1) {
         __syncthreads();
         if (threadIdx.x < by) norm[threadIdx.x] += norm[threadIdx.x + by];
@@ -96,8 +109,6 @@ __global__ __launch_bounds__(256) void k_ortho_load(Matrices in, uint32_t rows, 
     const float log2_of = sum > 0.0 ? (float)(log2(length) - log2(whole)) : 0.0f;
     const double by = ldexp((double)HELD, lift_of(log2_of, 0.0f)) / whole;
     if (blockIdx.x == 0 && threadIdx.x == 0) log2_norm[which] = log2_of;
-    const T *const m = (const T *)in.data[which];
-    const uint64_t stride = in.stride[which];
     const uint32_t r0 = blockIdx.x / across * 64, c0 = blockIdx.x % across * 64;      // of G
     const uint32_t c = (threadIdx.x & 7u) * 8, n = live8(c0 + c, cols);
     Raw8<T> raw[2];
@@ -450,8 +461,8 @@ template <class T> static void load_matrices(const Matrices &in, const dgs_ortho
 {
     // (a workgroup for every 64 KB or so of halves, and as few as there are work)
     const uint64_t work = (uint64_t)p.rows * ((p.cols + 7) / 8) / 2048 + 1;
-    const uint32_t parts = work < NORM_PARTS ? (uint32_t)work : NORM_PARTS;
-    hipLaunchKernelGGL(k_ortho_norm<T>, dim3(parts, count), dim3(256), 0, st, in, p.rows, p.cols, o.norm);
+    const uint32_t parts = (uint64_t)p.rows * p.cols <= SMALL ? 0u : work < NORM_PARTS ? (uint32_t)work : NORM_PARTS;
+    if (parts) hipLaunchKernelGGL(k_ortho_norm<T>, dim3(parts, count), dim3(256), 0, st, in, p.rows, p.cols, o.norm);
     hipLaunchKernelGGL(k_ortho_load<T>, dim3((p.cols + 63) / 64 * ((p.rows + 63) / 64), count), dim3(256), 0, st, in, p.rows, p.cols,
                        (uint32_t)o.turned, (const double *)o.norm, parts, p.eps, o.x[0], o.log2_norm);
 }
