@@ -3,7 +3,7 @@
 //     X = a X + (b A + c A^2) X
 //
 // which leaves G's singular vectors and takes its singular values towards 1 (X^T in place of X where rows outnumber columns, so
-// that A is the smaller square).  Three launches a step: the two symmetric products, of which tiles on and below the diagonal
+// that A is the smaller square).  Matrices of up to 128 x 128 take one launch, others three a step: the two symmetric products, of which tiles on and below the diagonal
 // are computed and stored twice, and the product with X.
 //
 // Numbers.  Sums are fp32, the norm's in 64 bits.  Between the products X is held in two halves (22 bits), times 2^12.  The
@@ -20,7 +20,7 @@ constexpr uint32_t NORM_PARTS = 256;      // at most
 #ifdef DGS_HOST_EMULATION
 constexpr uint32_t SMALL = 1u << 10;
 #else
-constexpr uint32_t SMALL = 1u << 14;      // values of a matrix whose norm has no launch of its own (128 x 128: 6.2 us, in two launches 3.6 and 4.2)
+constexpr uint32_t SMALL = 1u << 14;      // values of a matrix whose norm has no launch of its own (2^14 of them: 6.2 us, in two launches 3.6 and 4.2)
 #endif
 
 struct Matrices {
@@ -378,6 +378,158 @@ __global__ __launch_bounds__(WAVES_M *WAVES_N * 64, 2) void k_ortho_step(StepArg
     }
 }
 
+// Matrices of up to S x S, whole: a workgroup each, all steps in one launch.  A lane keeps its values of X and A in fp32; what the products
+// read of them lies in LDS in halves, transposed, so that the four rows that a lane has together are written together (A and the polynomial are
+// symmetric).  Bound by latency: 96 matrix instructions a wavefront at most between barriers.  A square of 32 x 32 to a wavefront, so that
+// four of them share a SIMD at 128 x 128: five steps of one in fp32 74 us (four wavefronts with four squares each: 102; in launches of their own, 16 of
+// them: 98); 64 x 64 31 (81); 32 of 128 x 128 in bfloat16 46 (89); 200 of 48 x 48 in fp32 245 (563).
+struct SmallArgs {
+    uint32_t rows, cols, turned, type, out_type;      // of G
+    uint32_t steps, kind, add;
+    float a, b, c, eps, scale, grows;
+};
+__device__ __forceinline__ float value_at(const void *p, uint64_t at, uint32_t type)
+{
+    return type == DGS_F32 ? ((const float *)p)[at] : type == DGS_F16 ? to_float(((const f16 *)p)[at]) : to_float(((const bf16 *)p)[at]);
+}
+__device__ __forceinline__ void put_value(void *p, uint64_t at, uint32_t type, float v)
+{
+    if (type == DGS_F32) ((float *)p)[at] = v;
+    else if (type == DGS_F16) ((f16 *)p)[at] = from_float<f16>(v);
+    else ((bf16 *)p)[at] = from_float<bf16>(v);
+}
+template <uint32_t S> struct Small {
+    static constexpr uint32_t SIDE = S / 32, THREADS = SIDE * SIDE * 64, PITCH = S + 8;      // (4 banks more than a multiple of 32)
+    typedef uint16_t Part[S][PITCH];
+
+    // A wavefront has a square of 32 x 32.
+    static __device__ __forceinline__ uint32_t wave_m() { return uniform(threadIdx.x >> 6) / SIDE * 32; }
+    static __device__ __forceinline__ uint32_t wave_n() { return uniform(threadIdx.x >> 6) % SIDE * 32; }
+
+    // Values as halves, transposed; `two`: what the first half leaves, too.
+    static __device__ __forceinline__ void put(Part *to, const f32x16 &v, bool two)
+    {
+        const uint32_t n = wave_n() + (lane_id() & 31u);
+#pragma unroll
+        for (uint32_t g = 0; g < 4; ++g) {
+            const uint32_t m = wave_m() + square_row(4 * g);
+            u32x2 hi, lo;
+#pragma unroll
+            for (uint32_t k = 0; k < 2; ++k) {
+                const f32x2 w = {v[4 * g + 2 * k], v[4 * g + 2 * k + 1]};
+                const f16x2 h = __builtin_convertvector(w, f16x2);
+                const f32x2 left = {w.x - (float)h.x, w.y - (float)h.y};
+                hi[k] = __builtin_bit_cast(uint32_t, h);
+                lo[k] = __builtin_bit_cast(uint32_t, __builtin_convertvector(left, f16x2));
+            }
+            *(u32x2 *)&to[0][n][m] = hi;
+            if (two) *(u32x2 *)&to[1][n][m] = lo;
+        }
+    }
+    // 32 rows from `first` on of an operand, k from 16 s on: k inside (TURNED: outside).
+    template <bool TURNED> static __device__ __forceinline__ u32x4 fragment(const Part &p, uint32_t first, uint32_t s)
+    {
+        const uint32_t lane = lane_id();
+        if constexpr (!TURNED) return *(const u32x4 *)&p[first + (lane & 31u)][16 * s + 8 * (lane >> 5)];
+        const uint32_t k = 16 * s + ((lane >> 5) << 3) + ((lane & 15u) >> 2), c = first + ((lane >> 4) & 1u) * 16 + (lane & 3u) * 4;
+        const u32x2 x = read_turned(&p[k][c]), y = read_turned(&p[k + 4][c]);
+        return u32x4{x.x, x.y, y.x, y.y};
+    }
+    template <bool TURNED> static __device__ __forceinline__ f32x16 product(const Part *a, const Part *b, uint32_t depth, uint32_t kind)
+    {
+        f32x16 c;
+#pragma unroll
+        for (uint32_t r = 0; r < 16; ++r) c[r] = 0.0f;
+        const uint32_t slices = (depth + 15) / 16;
+        for (uint32_t pair = 0; pair < pairs_of(kind); ++pair) {
+            const Part &pa = a[pair == 1], &pb = b[pair == 2];
+#pragma unroll 4
+            for (uint32_t s = 0; s < slices; ++s)
+                c = matrix_unit_of<f16>(fragment<TURNED>(pa, wave_m(), s), fragment<TURNED>(pb, wave_n(), s), c);
+        }
+        return c;
+    }
+};
+template <uint32_t S> __global__ __launch_bounds__(Small<S>::THREADS, 1) void k_ortho_small(SmallArgs a, Matrices in, Matrices results)
+{
+    typedef Small<S> P;
+    __shared__ __attribute__((aligned(16))) typename P::Part x_lds[2], square[2];
+    __shared__ float diagonal[S];
+    __shared__ double norm[P::THREADS];
+    const uint32_t which = blockIdx.x;
+    const uint32_t x_rows = a.turned ? a.cols : a.rows, x_cols = a.turned ? a.rows : a.cols;
+    const bool two = a.kind != ONE_PAIR;
+    // this lane's column, and its rows, of X; rows 4 g to 4 g + 3 of its sixteen lie together
+    const uint32_t n = P::wave_n() + (lane_id() & 31u);
+    uint32_t m[16];
+#pragma unroll
+    for (uint32_t r = 0; r < 16; ++r) m[r] = P::wave_m() + square_row(r);
+    f32x16 x, v, gram;
+    const void *const from = in.data[which];
+    const uint64_t stride = in.stride[which];
+    double sum = 0.0;
+#pragma unroll
+    for (uint32_t r = 0; r < 16; ++r) {
+        const bool here = m[r] < x_rows && n < x_cols;
+        x[r] = here ? value_at(from, a.turned ? n * stride + m[r] : m[r] * stride + n, a.type) : 0.0f;
+        sum += (double)x[r] * (double)x[r];
+    }
+    norm[threadIdx.x] = sum;
+    for (uint32_t by = P::THREADS / 2; by; by >>= 1) {
+        __syncthreads();
+        if (threadIdx.x < by) norm[threadIdx.x] += norm[threadIdx.x + by];
+    }
+    __syncthreads();
+    const double length = sqrt(norm[0]), whole = length + (double)a.eps;
+    const float log2_norm = norm[0] > 0.0 ? (float)(log2(length) - log2(whole)) : 0.0f;
+    int lift = lift_of(log2_norm, 0.0f);
+    const double by = ldexp((double)HELD, lift) / whole;
+#pragma unroll
+    for (uint32_t r = 0; r < 16; ++r) x[r] = m[r] < x_rows && n < x_cols ? (float)((double)x[r] * by) : 0.0f;
+    float growth = 0.0f;
+    for (uint32_t step = 0; step < a.steps; ++step) {
+        P::put(x_lds, x, two);
+        __syncthreads();
+        gram = P::template product<true>(x_lds, x_lds, x_cols, a.kind);
+        // (A as the products read it, in the polynomial too: near 1 what its rounding does to b A and c A^2 cancels but for a fifth)
+#pragma unroll
+        for (uint32_t r = 0; r < 16; ++r) {
+            gram[r] = times_power(gram[r], -12 - 2 * lift);
+            if (!two) gram[r] = to_float(from_float<f16>(gram[r]));
+        }
+        P::put(square, gram, two);
+        __syncthreads();
+        v = P::template product<false>(square, square, x_rows, a.kind);
+        __syncthreads();      // (A has been read)
+#pragma unroll
+        for (uint32_t r = 0; r < 16; ++r) {
+            v[r] = a.b * gram[r] + a.c * times_power(v[r], -12);
+            if (m[r] == n) {
+                diagonal[n] = a.a + v[r] * LEFT;
+                v[r] = 0.0f;
+            }
+        }
+        P::put(square, v, two);
+        __syncthreads();
+        v = P::template product<false>(square, x_lds, x_rows, a.kind);
+        growth += a.grows;
+        const int next_lift = step + 1 < a.steps ? lift_of(log2_norm, growth) : -12;
+#pragma unroll
+        for (uint32_t r = 0; r < 16; ++r) x[r] = times_power(__builtin_fmaf(diagonal[m[r]], x[r], v[r] * LEFT), next_lift - lift);
+        lift = next_lift;
+        __syncthreads();      // (X and the polynomial have been read)
+    }
+    if (n >= x_cols) return;
+    void *const to = (void *)results.data[which];
+    const uint64_t out_stride = results.stride[which];
+#pragma unroll
+    for (uint32_t r = 0; r < 16; ++r) {
+        if (m[r] >= x_rows) continue;
+        const uint64_t at = a.turned ? n * out_stride + m[r] : m[r] * out_stride + n;
+        put_value(to, at, a.out_type, a.add ? value_at(to, at, a.out_type) + x[r] * a.scale : x[r] * a.scale);
+    }
+}
+
 // ---------------------------------------------------------------------------
 // host side
 // ---------------------------------------------------------------------------
@@ -407,6 +559,12 @@ static SquarePlan square_plan(uint32_t size, uint32_t depth, uint32_t pairs, uin
     }
     return best;
 }
+// Matrices up to this side take one launch for all of their steps.  (A CPU build that splits products is there for the others.)
+#ifdef DGS_PRODUCT_SPLITS
+constexpr uint32_t SMALL_SIDE = 0;
+#else
+constexpr uint32_t SMALL_SIDE = 128;
+#endif
 struct OrthoPlan {
     uint32_t rows, cols, at_once;      // of X, and matrices of a launch
     bool turned, two;
@@ -521,6 +679,8 @@ extern "C" int dgs_orthogonalise(const dgs_orthogonalise_args *args, void *hip_s
     const OrthoPlan o = ortho_plan(p);
     if (p.workspace_bytes < o.bytes) return DGS_ENOMEM;
     const hipStream_t st = (hipStream_t)hip_stream;
+    const float grows = p.a != 0.0f ? log2f(fabsf(p.a)) : 0.0f;
+    const uint32_t kind = o.two ? BOTH_IN_TWO : ONE_PAIR;
     for (uint32_t first = 0; first < p.count; first += o.at_once) {
         const uint32_t count = p.count - first < o.at_once ? p.count - first : o.at_once;
         Matrices in = {}, out = {};
@@ -530,14 +690,19 @@ extern "C" int dgs_orthogonalise(const dgs_orthogonalise_args *args, void *hip_s
             out.data[i] = p.out[first + i].data;
             out.stride[i] = p.out[first + i].stride;
         }
+        if (o.cols <= SMALL_SIDE) {
+            const SmallArgs a = {p.rows, p.cols, (uint32_t)o.turned, (uint32_t)p.type, (uint32_t)p.out_type, p.steps, kind, (uint32_t)(p.accumulate != 0),
+                                 p.a, p.b, p.c, p.eps, p.scale, grows};
+            if (o.cols <= 64) hipLaunchKernelGGL(k_ortho_small<64>, dim3(count), dim3(Small<64>::THREADS), 0, st, a, in, out);
+            else hipLaunchKernelGGL(k_ortho_small<128>, dim3(count), dim3(Small<128>::THREADS), 0, st, a, in, out);
+            continue;
+        }
         if (p.type == DGS_F32) load_matrices<float>(in, p, o, count, st);
         else if (p.type == DGS_F16) load_matrices<f16>(in, p, o, count, st);
         else load_matrices<bf16>(in, p, o, count, st);
-        const uint32_t kind = o.two ? BOTH_IN_TWO : ONE_PAIR;
         float us = 0.0f;
         const int step_tile = product_tile([&](uint32_t high, uint32_t wide) { return (uint64_t)tiles_of(o.rows, high) * tiles_of(o.cols, wide) * count; },
                                            tiles_of(o.rows, PRODUCT_STEP) * (o.two ? 3u : 1u), TILE_256, us);
-        const float grows = p.a != 0.0f ? log2f(fabsf(p.a)) : 0.0f;
         for (uint32_t step = 0; step < p.steps; ++step) {
             SquareArgs g = {};
             g.x = o.x[step & 1u];

@@ -261,6 +261,11 @@ int main(int, char **argv)
             ortho(out, out, 3, 5, 70, 0, 5, true);
             ortho(2 - out, out, 2, 133, 40, 1, 5, false);
             ortho(0, out, 1, 130, 140, 0, 2, false);
+            // whole matrices to a workgroup
+            ortho(out, out, 2, 100, 77, 3, 3, false);
+            ortho(2 - out, out, 1, 128, 128, 0, 1, true);
+            ortho(0, out, 2, 64, 33, 1, 4, false);
+            ortho(out, out, 1, 17, 129, 0, 2, false);
         }
     }
     printf("%llu values as expected\n", (unsigned long long)checks);

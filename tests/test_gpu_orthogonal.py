@@ -139,6 +139,31 @@ def test_scaled_and_added(dtype, rows, cols):
     assert bool((room[:, :2] == 0).all()) and bool((room[:, 2 + cols:] == 0).all())
 
 
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("rows, cols", [(1, 128), (128, 1), (31, 97), (64, 65), (65, 64), (128, 127), (128, 129), (129, 128), (16, 16)])
+def test_small_sides(rows, cols, dtype):
+    m = Make(rows + 5 * cols)
+    g = m.matrix(rows, cols, dtype, "gradient", 3, 1)
+    assert_near(blocks.orthogonalise(g), g, dtype)
+
+
+def test_many_small_ones():      # more than a launch takes, some of them zeros or not finite
+    m = Make(9)
+    given = [m.matrix(20, 48) for _ in range(70)]
+    given[5].zero_()
+    given[40][3, 7] = float("inf")
+    given[69][0, 0] = float("nan")
+    kept = [g.clone() for g in given]
+    out = blocks.orthogonalise(given, given)
+    for i, g in enumerate(kept):
+        if i in (40, 69):
+            assert bool(out[i].isnan().all())
+        elif i == 5:
+            assert bool((out[i] == 0).all())
+        else:
+            assert_near(out[i], g, F32)
+
+
 @pytest.mark.parametrize("steps", [1, 2, 3, 7])
 def test_steps(steps):
     g = Make(5).matrix(96, 150)

@@ -13,14 +13,15 @@ EMU = os.path.join(HERE, "emu")
 CLANG = os.environ.get("DGS_HOST_CLANG", "/opt/rocm/llvm/bin/clang++")
 FLAGS = ["-std=c++17", "-O1", "-g", f"-I{EMU}", "-ffp-contract=off", "-fsanitize=address,undefined", "-fno-sanitize-recover=all",
          "-Wno-unknown-attributes", "-Wno-unused-function", "-Wno-array-compare", "-Wno-pass-failed"]
-# the library as it is, and with one kind of tile (256 x 256, 256 x 128, 192 x 192, 128 x 128; small matrices take 64 x 64 by
-# themselves), small pieces of the vocabulary and split sums taken at any size: of which kernels, and what is run
+# the library as it is, and with one kind of tile (256 x 256, 256 x 128, 192 x 192, 128 x 128, 64 x 64: small
+# products take that by themselves, small updates a launch for all their steps), small pieces of the vocabulary and split sums taken at any size: of which kernels, and what is run
 BUILDS = {
     "": ([], ("dgs_head", "dgs_orthogonal"), ("head", "large", "ortho")),
     "0": (["-DDGS_PRODUCT_SPLITS=1"], ("dgs_head", "dgs_orthogonal"), ("large", "tiles")),
     "1": (["-DDGS_PRODUCT_SPLITS=2"], ("dgs_head",), ("large",)),
     "2": (["-DDGS_PRODUCT_SPLITS=3"], ("dgs_orthogonal",), ("tiles",)),
     "3": (["-DDGS_PRODUCT_SPLITS=3"], ("dgs_head", "dgs_orthogonal"), ("large", "tiles")),
+    "4": (["-DDGS_PRODUCT_SPLITS=1"], ("dgs_orthogonal",), ("ortho",)),
 }
 
 
