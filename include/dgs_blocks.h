@@ -216,7 +216,8 @@ int dgs_head_backward(const dgs_head_args *args /*host*/, void *hip_stream);
  *     X = a X + (b A + c A^2) X
  *
  * and out = scale * X, or with accumulate != 0 out + scale * X, rounded once.  Sums are fp32, the norm's in 64 bits.  Results of
- * DGS_F32 and DGS_F16 take 22 bits of X, A and the polynomial to the products, of DGS_BF16 11.  Values of X, A and the polynomial
+ * DGS_F32 and DGS_F16 take 22 bits of X, A and the polynomial to the products, of DGS_BF16 11; what lies below 2^-15 is held in
+ * steps of 2^-37 (of an update whose norm is below eps, in steps as much smaller).  Values of X, A and the polynomial
  * must stay below 16, as they do with coefficients that take singular values up to 1 to such near 1.  A matrix that holds an
  * infinity or NaN leaves NaN; of zeros (with eps > 0) zeros.
  * in, out: host arrays of `count` matrices each, read before the call returns.  out[i] may be in[i] (same type and stride);

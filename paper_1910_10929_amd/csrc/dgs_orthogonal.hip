@@ -32,12 +32,19 @@ struct Halves {
     uint64_t stride, size;      // from row to row, and of a matrix
 };
 
-// An update whose norm is far below eps starts with an X far below 1, which grows by `a` a step at most.  X is then held times
-// 2^lift besides, so that what half's smallest numbers cut off stays as far below it as ever.  growth: log2(a^step).
-__device__ __forceinline__ int lift_of(float log2_norm, float growth)
+// An update whose norm is far below eps starts with an X far below 1.  X is then held times 2^lift besides, so that what half's
+// smallest numbers cut off stays as far below it as ever.  The lift follows a bound on X's singular values, here its log2: the norm at the
+// start, and a step takes s to at most s (|a| + |b| s^2 + |c| s^4).  (Not |a|^step: with |a| < 1 that goes to 0 where b and c keep singular
+// values near 1.)
+__device__ __forceinline__ int lift_of(float bound)
 {
-    const float down = -(log2_norm + growth);
-    return down >= 1.0f ? (int)min(down, 120.0f) : 0;      // (a NaN: 0)
+    return bound <= -1.0f ? (int)min(-bound, 120.0f) : 0;      // (a NaN: 0)
+}
+struct Coefficients { float a, b, c; };
+__device__ __forceinline__ float bound_after(float bound, const Coefficients &by)
+{
+    const float square = exp2f(2.0f * bound);
+    return bound + log2f(__builtin_fabsf(by.a) + (__builtin_fabsf(by.b) + __builtin_fabsf(by.c) * square) * square);
 }
 __device__ __forceinline__ float times_power(float v, int e)
 {
@@ -90,7 +97,7 @@ __global__ __launch_bounds__(256) void k_ortho_norm(Matrices in, uint32_t rows, 
 // of its matrix itself.
 template <class T>
 __global__ __launch_bounds__(256) void k_ortho_load(Matrices in, uint32_t rows, uint32_t cols, uint32_t turned, const double *parts, uint32_t norm_parts,
-                                                    float eps, Halves x, float *log2_norm)
+                                                    float eps, Halves x, float *bound)
 {
     __shared__ double norm[NORM_PARTS];
     __shared__ float tile[64][65];
@@ -107,8 +114,8 @@ __global__ __launch_bounds__(256) void k_ortho_load(Matrices in, uint32_t rows, 
     const double sum = norm[0];
     const double length = sqrt(sum), whole = length + (double)eps;
     const float log2_of = sum > 0.0 ? (float)(log2(length) - log2(whole)) : 0.0f;
-    const double by = ldexp((double)HELD, lift_of(log2_of, 0.0f)) / whole;
-    if (blockIdx.x == 0 && threadIdx.x == 0) log2_norm[which] = log2_of;
+    const double by = ldexp((double)HELD, lift_of(log2_of)) / whole;
+    if (blockIdx.x == 0 && threadIdx.x == 0) bound[which] = log2_of;
     const uint32_t r0 = blockIdx.x / across * 64, c0 = blockIdx.x % across * 64;      // of G
     const uint32_t c = (threadIdx.x & 7u) * 8, n = live8(c0 + c, cols);
     Raw8<T> raw[2];
@@ -145,13 +152,12 @@ struct SquareArgs {
     uint32_t count;          // matrices
     uint32_t split_depth;    // of a split of the sum; as long as it is for a single one
     float *sums;             // with several: size x out.stride for each split and matrix, on and below the diagonal
-    const float *log2_norm;  // of each X at the start; absent: nothing was lifted
-    float growth;            // of X since
+    const float *bound;      // of each X; absent: nothing was lifted
     Halves out;              // lo: absent where products take the first halves
     // the polynomial: b A + c A^2, and its diagonal
     Halves gram;
     float *diagonal;         // size a matrix
-    float a, b, c;
+    Coefficients by;
 };
 
 // What becomes of a row's eight sums from column n on: A, or the polynomial without its diagonal.
@@ -164,7 +170,7 @@ __device__ __forceinline__ void finish8(const SquareArgs &a, uint32_t which, uin
         v[k] = times_power(v[k], power);
         if constexpr (POLY) {
             const float gram = half_value((uint16_t)(gram_hi[k >> 1] >> (16 * (k & 1)))) + half_value((uint16_t)(gram_lo[k >> 1] >> (16 * (k & 1))));
-            v[k] = a.b * gram + a.c * v[k];
+            v[k] = a.by.b * gram + a.by.c * v[k];
         }
     }
     if constexpr (POLY) {
@@ -172,7 +178,7 @@ __device__ __forceinline__ void finish8(const SquareArgs &a, uint32_t which, uin
 #pragma unroll
             for (uint32_t k = 0; k < 8; ++k)
                 if (n + k == m) {
-                    if (m < a.size) a.diagonal[which * a.size + m] = a.a + v[k] * LEFT;
+                    if (m < a.size) a.diagonal[which * a.size + m] = a.by.a + v[k] * LEFT;
                     v[k] = 0.0f;
                 }
         }
@@ -190,7 +196,7 @@ __device__ __forceinline__ void gram8(const SquareArgs &a, uint64_t from, uint32
 }
 __device__ __forceinline__ int power_of_sums(const SquareArgs &a, uint32_t which)
 {
-    return -12 - (a.log2_norm ? 2 * lift_of(a.log2_norm[which], a.growth) : 0);
+    return -12 - (a.bound ? 2 * lift_of(a.bound[which]) : 0);
 }
 
 // The symmetric product of X with itself (POLY: of A with itself, from which the polynomial is made).  Bound by the matrix units:
@@ -295,8 +301,9 @@ struct StepArgs {
     const float *diagonal;
     uint32_t rows, cols, kind;
     uint32_t m_tiles, n_tiles;
-    const float *log2_norm;
-    float growth, next_growth;
+    const float *bound;      // of each X, and (but in the last step) of its next
+    float *next_bound;
+    Coefficients by;
     // the last step
     uint32_t add;
     float scale;
@@ -341,8 +348,14 @@ __global__ __launch_bounds__(WAVES_M *WAVES_N * 64, 2) void k_ortho_step(StepArg
     typename P::Sums s;
     P::run(lds, left, right, tile_m * M, tile_n * M, 0, a.rows, a.kind, s);
     // from how this X is held to how the next one is, or to the result
-    const int lift = lift_of(a.log2_norm[which], a.growth);
-    const int power = __is_same(T, void) ? lift_of(a.log2_norm[which], a.next_growth) - lift : -12 - lift;
+    const float bound = a.bound[which];
+    const int lift = lift_of(bound);
+    int power = -12 - lift;
+    if constexpr (__is_same(T, void)) {
+        const float next_bound = bound_after(bound, a.by);
+        power = lift_of(next_bound) - lift;
+        if (at == 0 && threadIdx.x == 0) a.next_bound[which] = next_bound;
+    }
     auto next = [&](uint32_t p, float (&v)[8]) {
 #pragma unroll
         for (uint32_t k = 0; k < 8; ++k) {
@@ -386,7 +399,8 @@ __global__ __launch_bounds__(WAVES_M *WAVES_N * 64, 2) void k_ortho_step(StepArg
 struct SmallArgs {
     uint32_t rows, cols, turned, type, out_type;      // of G
     uint32_t steps, kind, add;
-    float a, b, c, eps, scale, grows;
+    Coefficients by;
+    float eps, scale;
 };
 __device__ __forceinline__ float value_at(const void *p, uint64_t at, uint32_t type)
 {
@@ -481,12 +495,11 @@ template <uint32_t S> __global__ __launch_bounds__(Small<S>::THREADS, 1) void k_
     }
     __syncthreads();
     const double length = sqrt(norm[0]), whole = length + (double)a.eps;
-    const float log2_norm = norm[0] > 0.0 ? (float)(log2(length) - log2(whole)) : 0.0f;
-    int lift = lift_of(log2_norm, 0.0f);
+    float bound = norm[0] > 0.0 ? (float)(log2(length) - log2(whole)) : 0.0f;
+    int lift = lift_of(bound);
     const double by = ldexp((double)HELD, lift) / whole;
 #pragma unroll
     for (uint32_t r = 0; r < 16; ++r) x[r] = m[r] < x_rows && n < x_cols ? (float)((double)x[r] * by) : 0.0f;
-    float growth = 0.0f;
     for (uint32_t step = 0; step < a.steps; ++step) {
         P::put(x_lds, x, two);
         __syncthreads();
@@ -503,17 +516,17 @@ template <uint32_t S> __global__ __launch_bounds__(Small<S>::THREADS, 1) void k_
         __syncthreads();      // (A has been read)
 #pragma unroll
         for (uint32_t r = 0; r < 16; ++r) {
-            v[r] = a.b * gram[r] + a.c * times_power(v[r], -12);
+            v[r] = a.by.b * gram[r] + a.by.c * times_power(v[r], -12);
             if (m[r] == n) {
-                diagonal[n] = a.a + v[r] * LEFT;
+                diagonal[n] = a.by.a + v[r] * LEFT;
                 v[r] = 0.0f;
             }
         }
         P::put(square, v, two);
         __syncthreads();
         v = P::template product<false>(square, x_lds, x_rows, a.kind);
-        growth += a.grows;
-        const int next_lift = step + 1 < a.steps ? lift_of(log2_norm, growth) : -12;
+        bound = bound_after(bound, a.by);
+        const int next_lift = step + 1 < a.steps ? lift_of(bound) : -12;
 #pragma unroll
         for (uint32_t r = 0; r < 16; ++r) x[r] = times_power(__builtin_fmaf(diagonal[m[r]], x[r], v[r] * LEFT), next_lift - lift);
         lift = next_lift;
@@ -570,7 +583,7 @@ struct OrthoPlan {
     bool turned, two;
     Halves x[2], gram, poly;
     double *norm;
-    float *diagonal, *log2_norm, *sums;
+    float *diagonal, *bound[2], *sums;      // (bound: of a step's X, and of the next one's)
     SquarePlan square, poly_square;      // of X with itself, of A with itself
     uint64_t bytes;
 };
@@ -599,7 +612,7 @@ static OrthoPlan ortho_plan(const dgs_orthogonalise_args &p)
     o.poly = halves(small, o.rows, o.two);
     o.norm = (double *)s.take(sizeof(double) * NORM_PARTS * o.at_once);
     o.diagonal = (float *)s.take(4ull * o.rows * o.at_once);
-    o.log2_norm = (float *)s.take(4ull * o.at_once);
+    for (float *&b : o.bound) b = (float *)s.take(4ull * o.at_once);
     o.square = square_plan(o.rows, o.cols, o.two ? 3 : 1, o.at_once);
     o.poly_square = square_plan(o.rows, o.rows, o.two ? 3 : 1, o.at_once);
     const uint32_t splits = o.square.splits > o.poly_square.splits ? o.square.splits : o.poly_square.splits;
@@ -622,7 +635,7 @@ template <class T> static void load_matrices(const Matrices &in, const dgs_ortho
     const uint32_t parts = (uint64_t)p.rows * p.cols <= SMALL ? 0u : work < NORM_PARTS ? (uint32_t)work : NORM_PARTS;
     if (parts) hipLaunchKernelGGL(k_ortho_norm<T>, dim3(parts, count), dim3(256), 0, st, in, p.rows, p.cols, o.norm);
     hipLaunchKernelGGL(k_ortho_load<T>, dim3((p.cols + 63) / 64 * ((p.rows + 63) / 64), count), dim3(256), 0, st, in, p.rows, p.cols,
-                       (uint32_t)o.turned, (const double *)o.norm, parts, p.eps, o.x[0], o.log2_norm);
+                       (uint32_t)o.turned, (const double *)o.norm, parts, p.eps, o.x[0], o.bound[0]);
 }
 
 template <class T, bool TURNED> static void launch_step(const StepArgs &s, const Matrices &out, int tile, uint32_t count, hipStream_t st)
@@ -679,7 +692,7 @@ extern "C" int dgs_orthogonalise(const dgs_orthogonalise_args *args, void *hip_s
     const OrthoPlan o = ortho_plan(p);
     if (p.workspace_bytes < o.bytes) return DGS_ENOMEM;
     const hipStream_t st = (hipStream_t)hip_stream;
-    const float grows = p.a != 0.0f ? log2f(fabsf(p.a)) : 0.0f;
+    const Coefficients by = {p.a, p.b, p.c};
     const uint32_t kind = o.two ? BOTH_IN_TWO : ONE_PAIR;
     for (uint32_t first = 0; first < p.count; first += o.at_once) {
         const uint32_t count = p.count - first < o.at_once ? p.count - first : o.at_once;
@@ -692,7 +705,7 @@ extern "C" int dgs_orthogonalise(const dgs_orthogonalise_args *args, void *hip_s
         }
         if (o.cols <= SMALL_SIDE) {
             const SmallArgs a = {p.rows, p.cols, (uint32_t)o.turned, (uint32_t)p.type, (uint32_t)p.out_type, p.steps, kind, (uint32_t)(p.accumulate != 0),
-                                 p.a, p.b, p.c, p.eps, p.scale, grows};
+                                 by, p.eps, p.scale};
             if (o.cols <= 64) hipLaunchKernelGGL(k_ortho_small<64>, dim3(count), dim3(Small<64>::THREADS), 0, st, a, in, out);
             else hipLaunchKernelGGL(k_ortho_small<128>, dim3(count), dim3(Small<128>::THREADS), 0, st, a, in, out);
             continue;
@@ -711,18 +724,15 @@ extern "C" int dgs_orthogonalise(const dgs_orthogonalise_args *args, void *hip_s
             g.size = o.rows;
             g.count = count;
             g.out = o.gram;
-            g.log2_norm = o.log2_norm;
-            g.growth = (float)step * grows;
+            g.bound = o.bound[step & 1u];
             launch_square<false>(g, o.square, o.sums, st);
             g.x = o.gram;
-            g.log2_norm = nullptr;
+            g.bound = nullptr;
             g.depth = o.rows;
             g.out = o.poly;
             g.gram = o.gram;
             g.diagonal = o.diagonal;
-            g.a = p.a;
-            g.b = p.b;
-            g.c = p.c;
+            g.by = by;
             launch_square<true>(g, o.poly_square, o.sums, st);
             StepArgs s = {};
             s.poly = o.poly;
@@ -732,9 +742,9 @@ extern "C" int dgs_orthogonalise(const dgs_orthogonalise_args *args, void *hip_s
             s.rows = o.rows;
             s.cols = o.cols;
             s.kind = kind;
-            s.log2_norm = o.log2_norm;
-            s.growth = (float)step * grows;
-            s.next_growth = s.growth + grows;
+            s.bound = o.bound[step & 1u];
+            s.next_bound = o.bound[(step + 1) & 1u];
+            s.by = by;
             s.add = p.accumulate != 0;
             s.scale = p.scale;
             s.m_tiles = tiles_of(o.rows, tile_high(step_tile));

@@ -1,0 +1,135 @@
+// Where numbers are hard for the orthogonalising kernels and the output layer's, on the CPU, through the C ABI: coefficients that take
+// little or nothing off small singular values, against the same steps in double.
+#include <hip/hip_runtime.h>
+#include "../../include/dgs_blocks.h"
+#include <functional>
+#include <memory>
+#include <random>
+#include <string>
+
+static std::mt19937 gen(17);
+static double normal() { static std::normal_distribution<double> d; return d(gen); }
+
+static double read_as(int type, const void *p, uint64_t i)
+{
+    if (type == DGS_F32) return ((const float *)p)[i];
+    const uint16_t h = ((const uint16_t *)p)[i];
+    if (type == DGS_BF16) return __uint_as_float((uint32_t)h << 16);
+    _Float16 f;
+    memcpy(&f, &h, 2);
+    return (double)f;
+}
+static double half_step(int type) { return type == DGS_F32 ? ldexp(1.0, -24) : type == DGS_F16 ? ldexp(1.0, -11) : ldexp(1.0, -8); }
+
+static std::string name;
+static uint64_t checks = 0;
+static void near(double got, double want, double tol, const char *what, uint64_t i = 0, uint64_t j = 0)
+{
+    ++checks;
+    if (std::fabs(got - want) <= tol) return;
+    printf("%s: %s (%llu, %llu): %.9g, expected %.9g within %.3g\n", name.c_str(), what, (unsigned long long)i, (unsigned long long)j, got,
+           want, tol);
+    exit(1);
+}
+static void expect(int rc, const char *what)
+{
+    if (rc == DGS_OK) return;
+    printf("%s: %s returned %d\n", name.c_str(), what, rc);
+    exit(1);
+}
+// A call with a workspace of the size that it asks for, full of NaN.
+static void with_workspace(uint64_t bytes, std::function<int(void *, uint64_t)> call, const char *what)
+{
+    std::unique_ptr<char[]> ws(new char[bytes + 16]);
+    memset(ws.get(), 0xFF, bytes + 16);
+    expect(call(ws.get() + (-(uintptr_t)ws.get() & 15u), bytes), what);
+}
+
+// An fp32 matrix of the given Frobenius norm.  A step rounds X by 2^-21 (bfloat16 results: 2^-10) for the operands, by 2^-24 sqrt(n) for a sum of n
+// products (three pairs of parts; additions round to either side), and by 2^-37 of 1 since X's smallest values have fewer bits.  The
+// result may be off by `grown` times the first two, relative to the whole, the steps' number times the last, and half a step of its type.
+static void ortho(int out_type, uint32_t rows, uint32_t cols, float a, float b, float c, uint32_t steps, double norm, float eps, double grown)
+{
+    name = "ortho to " + std::to_string(out_type) + " " + std::to_string(rows) + "x" + std::to_string(cols) + " (" + std::to_string(a) + ", "
+         + std::to_string(b) + ", " + std::to_string(c) + ")";
+    std::vector<float> g(rows * cols);
+    std::unique_ptr<char[]> out(new char[g.size() * (out_type == DGS_F32 ? 4 : 2)]);
+    double sum = 0.0;
+    for (float &v : g) v = (float)normal(), sum += (double)v * v;
+    for (float &v : g) v = (float)(v * norm / sqrt(sum));
+    dgs_matrix in = {g.data(), cols}, to = {out.get(), cols};
+    dgs_orthogonalise_args p = {};
+    p.count = 1; p.rows = rows; p.cols = cols; p.steps = steps;
+    p.type = DGS_F32; p.out_type = out_type;
+    p.a = a; p.b = b; p.c = c; p.eps = eps; p.scale = 1.0f;
+    p.in = &in; p.out = &to;
+    with_workspace(dgs_orthogonalise_workspace(&p), [&](void *ws, uint64_t n) { p.workspace = ws; p.workspace_bytes = n; return dgs_orthogonalise(&p, nullptr); }, "orthogonalise");
+    const bool turned = rows > cols;
+    const uint32_t m = turned ? cols : rows, k = turned ? rows : cols;
+    std::vector<double> x(m * k), q(m * m), w(m * m), y(m * k);
+    sum = 0.0;
+    for (float v : g) sum += (double)v * v;
+    for (uint32_t r = 0; r < rows; ++r)
+        for (uint32_t j = 0; j < cols; ++j) (turned ? x[j * k + r] : x[r * k + j]) = g[r * cols + j] / (sqrt(sum) + (double)eps);
+    for (uint32_t s = 0; s < steps; ++s) {
+        for (uint32_t r = 0; r < m; ++r)
+            for (uint32_t j = 0; j < m; ++j) {
+                double d = 0.0;
+                for (uint32_t i = 0; i < k; ++i) d += x[r * k + i] * x[j * k + i];
+                q[r * m + j] = d;
+            }
+        for (uint32_t r = 0; r < m; ++r)
+            for (uint32_t j = 0; j < m; ++j) {
+                double d = 0.0;
+                for (uint32_t i = 0; i < m; ++i) d += q[r * m + i] * q[i * m + j];
+                w[r * m + j] = b * q[r * m + j] + c * d + (r == j ? a : 0.0);
+            }
+        for (uint32_t r = 0; r < m; ++r)
+            for (uint32_t j = 0; j < k; ++j) {
+                double d = 0.0;
+                for (uint32_t i = 0; i < m; ++i) d += w[r * m + i] * x[i * k + j];
+                y[r * k + j] = d;
+            }
+        x = y;
+    }
+    double far = 0.0, size = 0.0;
+    for (uint32_t r = 0; r < rows; ++r)
+        for (uint32_t j = 0; j < cols; ++j) {
+            const double want = turned ? x[j * k + r] : x[r * k + j], got = read_as(out_type, out.get(), r * cols + j);
+            if (!std::isfinite(got)) near(got, want, 0.0, "finite", r, j);
+            const double d = std::max(0.0, std::fabs(got - want) - half_step(out_type) * std::fabs(want) - (out_type == DGS_F16 ? ldexp(1.0, -25) : 0.0));
+            far += d * d;
+            size += want * want;
+        }
+    near(sqrt(far), 0.0, sqrt(size) * grown * (ldexp(1.0, out_type == DGS_BF16 ? -10 : -21) + ldexp(sqrt(3.0 * k), -24)) + steps * ldexp(sqrt((double)(m * k)), -37), "distance");
+}
+
+// Singular values near 0 shrink or stay where others do not: up to 128 x 128 and beyond, rows or columns the smaller side.  What a step
+// leaves grows as the map's slopes say, relative to X where X shrinks: by 2 a step at the fixed point 1 of (0.5, 0.5, 0); by 2 in all on the way to 0 of (0.75, 0.5, -0.25) from
+// singular values of 0.42 and less (1 + 1.33 s^2 a step, with s^2 falling by a third each); (1, 0.9, -0.9) takes what 145 steps to 1 leave off
+// again (slope -0.8 there); not at all far below 1.
+static void coefficients()
+{
+    for (int out = 0; out < 3; ++out) {
+        ortho(out, 1, 1, 0.5f, 0.5f, 0.0f, 7, 1.0, 1e-7f, 127);
+        ortho(out, 1, 200, 0.5f, 0.5f, 0.0f, 10, 1.0, 1e-7f, 1023);
+        ortho(out, 20, 30, 0.75f, 0.5f, -0.25f, 40, 1.0, 1e-7f, 80);
+        ortho(out, 140, 9, 0.75f, 0.5f, -0.25f, 40, 1.0, 1e-7f, 80);
+        // an update below eps whose X, at first a sixteenth, goes to 1 by way of b and c alone
+        ortho(out, 1, 40, 1.0f, 0.9f, -0.9f, 180, 0.0661, 1.0f, 180);
+        if (out == DGS_F32) ortho(out, 130, 1, 1.0f, 0.9f, -0.9f, 180, 0.0661, 1.0f, 180);
+        // ... and ones far below it, which `a` alone moves
+        ortho(out, 9, 20, 3.4445f, -4.7750f, 2.0315f, 5, 1e-9, 1.0f, 5);
+        ortho(out, 9, 140, 3.4445f, -4.7750f, 2.0315f, 5, 1e-9, 1.0f, 5);
+        ortho(out, 9, 20, 0.25f, 0.5f, 0.25f, 5, 1e-5, 1.0f, 5);
+        ortho(out, 9, 140, 0.25f, 0.5f, 0.25f, 5, 1e-5, 1.0f, 5);
+    }
+}
+
+int main(int, char **argv)
+{
+    const std::string what = argv[1];
+    if (what == "coefficients") coefficients();
+    printf("%llu values as expected\n", (unsigned long long)checks);
+    return 0;
+}
