@@ -7,10 +7,11 @@
 //
 // Numbers.  Sums, statistics and exponentials are fp32.  Logits are products of the operands as they are (bfloat16, half;
 // fp32 in two halves, 22 bits).  The gradient of the logits is divided by a power of two for each row (at least the larger
-// of the incoming gradients) and held in two halves, 22 bits of each value; dx in bfloat16 takes the first, 11 bits
-// where the result is rounded to 8, everything else both.  The other operand of these products is W or x in half,
+// of the incoming gradients) and held in two halves, the second times 2^11: 22 bits of a value down to 2^-28 of that power, below it steps
+// of 2^-49 (11 bits of what a softmax of 2^-38 leaves; with the second half as it is 2^-38 would be the step).  dx in bfloat16 takes
+// the first half, 11 bits where the result is rounded to 8, everything else both.  The other operand of these products is W or x in half,
 // scaled by powers of two so that the largest magnitude lies below 2^15: a bfloat16 value is exact there down to 2^-31 of the
-// largest, and what is lost of smaller ones is below 2^-39 of it.  x carries the rows' powers of two.
+// largest, and what is lost of smaller ones is below 2^-39 of it (fp32, in two halves: 2^-50).  x carries the rows' powers of two.
 #include "dgs_product.h"
 
 namespace dgs {
@@ -27,6 +28,7 @@ constexpr uint32_t RANGE_BLOCKS = 1024;      // of rows, and as many of W
 constexpr int NO_RANGE = -100000;           // nothing but zeros
 constexpr int TOP = 15;                     // the largest magnitude of a scaled operand lies below 2^TOP
 constexpr int GRAD_TOP = 14;                // a row's logit gradients are at most 2 after division
+constexpr uint32_t LOW = 11;                // second halves are held times 2^LOW
 
 // What a row of the backward pass needs: dlogit = pull * softmax - push * onehot, divided by 2^power and scaled to GRAD_TOP.
 struct HeadRow {
@@ -219,7 +221,7 @@ __global__ __launch_bounds__(256) void k_head_copy(CopyJobs jobs, Ranges ranges,
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = times_power(v[i], e);
-        halves8(v, h, l);
+        halves8<LOW>(v, h, l);
         *(u32x4 *)(j.hi + at * 8) = h;
         if (j.lo) *(u32x4 *)(j.lo + at * 8) = l;
     }
@@ -397,7 +399,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void k_head_few_dx(const T *w, uint
             const uint32_t row = t + (lane >> 5), v = v0 + (lane & 31u);
             const bool in = row < rows && v < end;
             const uint64_t at = in ? row * grad_stride + v : 0u;
-            grad[lane & 31u][row] = in ? half_value(hi[at]) + half_value(lo[at]) : 0.0f;
+            grad[lane & 31u][row] = in ? half_value(hi[at]) + half_value(lo[at]) * (1.0f / (1u << LOW)) : 0.0f;
         }
         __syncthreads();
         for (uint32_t v = 0; v < FEW_BLOCK && v0 + v < end; v += AHEAD) {
@@ -456,7 +458,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void k_head_few_dx(const T *w, uint
 template <class E, uint32_t M, uint32_t N, uint32_t WAVES_M, uint32_t WAVES_N, uint32_t STAGES, bool BACK>
 __global__ __launch_bounds__(STAGES ? WAVES_M *WAVES_N * 64 : FEW_WAVES * 64, 2) void k_head_logits(LogitArgs a)
 {
-    typedef Product<E, M, N, WAVES_M, WAVES_N, false, false, STAGES, PRODUCT_STEP> P;
+    typedef Product<E, M, N, WAVES_M, WAVES_N, false, false, STAGES, PRODUCT_STEP, __is_same(E, f16) ? LOW : 0> P;
     __shared__ __attribute__((aligned(16))) typename P::Lds lds;
     const TilePlace place = place_of_tile(tile_of_block(blockIdx.x, gridDim.x), a.v_tiles, a.t_tiles);
     const uint32_t tile_v = place.m, tile_t = place.n;
@@ -592,7 +594,7 @@ __global__ __launch_bounds__(STAGES ? WAVES_M *WAVES_N * 64 : FEW_WAVES * 64, 2)
             const uint32_t t = t0 + n, at_v = v0 - a.first + m;
             if (t >= a.rows || at_v >= a.grad_stride) return;
             u32x4 hi, lo;
-            halves8(v, hi, lo);
+            halves8<LOW>(v, hi, lo);
             *(u32x4 *)(a.grad[0] + t * a.grad_stride + at_v) = hi;
             *(u32x4 *)(a.grad[1] + t * a.grad_stride + at_v) = lo;
         });
@@ -685,7 +687,7 @@ struct GradientArgs {
 // of 8192 x 4096 x 32768, dx 1695 us (1297 TFLOP/s), dweight, of two halves, 3518 (1250).  Of 8192 x 768 x 30522 dx 374 and dweight 726:
 // 256 x 128, two workgroups to a compute unit, so that one's epilogue overlaps the other's product; 256 x 256 takes 882.
 template <uint32_t M, uint32_t N, uint32_t WAVES_M, uint32_t WAVES_N, uint32_t STAGES, bool TURN_A> struct GradientTile {
-    typedef Product<f16, M, N, WAVES_M, WAVES_N, TURN_A, true, STAGES, M == 256 && N == 128 ? 32 : PRODUCT_STEP> P;
+    typedef Product<f16, M, N, WAVES_M, WAVES_N, TURN_A, true, STAGES, M == 256 && N == 128 ? 32 : PRODUCT_STEP, LOW> P;
     static __device__ __forceinline__ void run(typename P::Lds &lds, const GradientArgs &a, uint32_t at);
 };
 template <uint32_t M, uint32_t N, uint32_t WAVES_M, uint32_t WAVES_N, uint32_t STAGES, bool TURN_A>

@@ -9,7 +9,8 @@
 // buffer's end and gets zeros.
 //
 // An operand may be held in two parts, whose sum it is (22 bits of a value as two halves).  The product then goes over the
-// same k once for every pair of parts that counts, as if the sum were so much longer.
+// same k once for every pair of parts that counts, as if the sum were so much longer.  Second parts may be held times 2^LOW: the
+// smallest of a half's numbers then cuts off 2^LOW times less.  Pairs with a second part go first, and what they sum to is divided once.
 #pragma once
 #include "dgs_rows.h"
 
@@ -156,7 +157,7 @@ __device__ __forceinline__ void in_order()
 #endif
 }
 
-template <class E, uint32_t M, uint32_t N, uint32_t WAVES_M, uint32_t WAVES_N, bool TURN_A, bool TURN_B, uint32_t STAGES, uint32_t STEP = PRODUCT_STEP> struct Product {
+template <class E, uint32_t M, uint32_t N, uint32_t WAVES_M, uint32_t WAVES_N, bool TURN_A, bool TURN_B, uint32_t STAGES, uint32_t STEP = PRODUCT_STEP, uint32_t LOW = 0> struct Product {
     static constexpr uint32_t WAVES = WAVES_M * WAVES_N, THREADS = WAVES * 64, I = M / 32 / WAVES_M, J = N / 32 / WAVES_N;
     typedef Staged<M, TURN_A, WAVES, STEP> A;
     typedef Staged<N, TURN_B, WAVES, STEP> B;
@@ -196,10 +197,10 @@ template <class E, uint32_t M, uint32_t N, uint32_t WAVES_M, uint32_t WAVES_N, b
         // what is loaded next; behind the last step nothing, in as many loads
         uint32_t next = 0, next_k = k_first, pair = 0, to = 0;
         auto next_step = [&]() {
-            // pairs: first with first, second with first, first with second
+            // pairs: first with first, second with first, first with second (LOW: first with first is the last)
             const uint32_t left = pair < pairs ? k_end - next_k : 0u;
-            la.step(a, pair == 1 && pairs > 1, m0, next_k, left);
-            lb.step(b, pair == 2 && pairs > 2, n0, next_k, left);
+            la.step(a, pair == (LOW ? 0 : 1) && pairs > 1, m0, next_k, left);
+            lb.step(b, pair == (LOW ? 1 : 2) && pairs > 2, n0, next_k, left);
             next_k += STEP;
             if (++next == per_pair) {
                 next = 0;
@@ -247,7 +248,18 @@ template <class E, uint32_t M, uint32_t N, uint32_t WAVES_M, uint32_t WAVES_N, b
         loads_meet<(STAGES - 1) * EACH>();
 #pragma unroll
         for (uint32_t r = 0; r < READS; ++r) read(0, 0, r);
+        // (sums of second parts are divided behind them)
+        const uint32_t second = LOW && pairs > 1 ? steps - per_pair : 0u;
         for (uint32_t step = 0, stage = 0; step < steps; ++step) {
+            if constexpr (LOW > 0) {
+                if (second && step == second) {
+                    in_order();      // (so that this stays a branch: a choice between both for every sum of every step costs small tiles a tenth)
+#pragma unroll
+                    for (uint32_t i = 0; i < I; ++i)
+#pragma unroll
+                        for (uint32_t j = 0; j < J; ++j) sums[i][j] *= 1.0f / (1u << LOW);
+                }
+            }
 #pragma unroll
             for (uint32_t s = 0; s + 1 < SLICES; ++s) slice(s, stage, false);
             next_step();
@@ -459,16 +471,17 @@ __device__ __forceinline__ float half_value(uint16_t bits)
     return (float)h;
 }
 
-// Eight values as halves, in two parts (22 bits of each).
+// Eight values as halves, in two parts (22 bits of each), the second times 2^LOW.  (Values below 2^16 leave less than 2^5 to it.)
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef f16 f16x2 __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ void halves8(const float (&v)[8], u32x4 &hi, u32x4 &lo)
+template <uint32_t LOW = 0> __device__ __forceinline__ void halves8(const float (&v)[8], u32x4 &hi, u32x4 &lo)
 {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const f32x2 w = {v[2 * i], v[2 * i + 1]};
         const f16x2 h = __builtin_convertvector(w, f16x2);
-        const f32x2 left = {w.x - (float)h.x, w.y - (float)h.y};
+        f32x2 left = {w.x - (float)h.x, w.y - (float)h.y};
+        if constexpr (LOW > 0) left = f32x2{left.x * (1u << LOW), left.y * (1u << LOW)};
         const f16x2 l = __builtin_convertvector(left, f16x2);
         hi[i] = __builtin_bit_cast(uint32_t, h);
         lo[i] = __builtin_bit_cast(uint32_t, l);

@@ -1,5 +1,6 @@
 // Where numbers are hard for the orthogonalising kernels and the output layer's, on the CPU, through the C ABI: coefficients that take
-// little or nothing off small singular values, against the same steps in double.
+// little or nothing off small singular values, against the same steps in double; entries of the vocabulary that are improbable, against
+// the definition.
 #include <hip/hip_runtime.h>
 #include "../../include/dgs_blocks.h"
 #include <functional>
@@ -126,10 +127,146 @@ static void coefficients()
     }
 }
 
+// A matrix in memory, and its values as they are held.
+struct Mat {
+    int type;
+    std::unique_ptr<char[]> store;
+    std::vector<double> v;
+    Mat(int t, uint64_t n, std::function<double(uint64_t)> value) : type(t), store(new char[n * (t == DGS_F32 ? 4 : 2) + 1]), v(n)
+    {
+        for (uint64_t i = 0; i < n; ++i) {
+            const float f = (float)value(i);
+            if (t == DGS_F32) ((float *)store.get())[i] = f;
+            else if (t == DGS_BF16) ((uint16_t *)store.get())[i] = (uint16_t)(__float_as_uint(f) >> 16);
+            else {
+                const _Float16 h = (_Float16)f;
+                memcpy((uint16_t *)store.get() + i, &h, 2);
+            }
+            v[i] = read_as(t, store.get(), i);
+        }
+    }
+    dgs_matrix view(uint64_t stride) { return dgs_matrix{store.get(), stride}; }
+    const float *floats() const { return (const float *)store.get(); }
+};
+
+static int power_of(double v) { int e; frexp(v, &e); return e; }      // smallest e with |v| < 2^e
+
+// Loss and gradients of x, W, bias and targets, against the definition.  Logits are off by what fp32's additions leave of `cols` products and, of
+// fp32 operands, by 2^-22 of each value and 2^-50 of its row's largest; that is what lse, the loss and, relatively, dz are off by, with 2^-20 for the
+// exponential and the logarithm.  dz is held in 22 bits, with steps of 2^-50 (half of it here) of its row's power of two.  x and W in the
+// gradients' products: 2^-22 and 2^-40 of the largest for fp32, nothing and 2^-40 for half and bfloat16; dx of bfloat16 takes 11 bits of dz.
+static void head(const char *what, int type, uint32_t rows, uint32_t cols, uint32_t vocab, const Mat &x, const Mat &w, const Mat *bias)
+{
+    name = std::string(what) + " " + std::to_string(type) + " " + std::to_string(rows) + "x" + std::to_string(cols) + "x" + std::to_string(vocab);
+    Mat dloss(DGS_F32, rows, [](uint64_t) { return normal(); }), dlse(DGS_F32, rows, [](uint64_t) { return 0.1 * normal(); });
+    auto none = [](uint64_t) { return NAN; };
+    Mat loss(DGS_F32, rows, none), lse(DGS_F32, rows, none), dx(type, rows * cols, none), dw(DGS_F32, vocab * cols, none), db(DGS_F32, vocab, none);
+    std::vector<int32_t> targets(rows);
+    for (uint32_t t = 0; t < rows; ++t) targets[t] = t % 5 == 3 ? -100 : (int32_t)(2 * (gen() % ((vocab + 1) / 2)));
+    dgs_head_args a = {};
+    a.rows = rows; a.cols = cols; a.vocab = vocab;
+    a.type = type; a.target_bytes = 4;
+    a.x = dgs_matrix{x.store.get(), cols}; a.weight = dgs_matrix{w.store.get(), cols};
+    a.bias = bias ? bias->floats() : nullptr;
+    a.targets = targets.data();
+    a.loss = (float *)loss.store.get(); a.lse = (float *)lse.store.get();
+    auto call = [&](int back) {
+        with_workspace(dgs_head_workspace(&a, back), [&](void *ws, uint64_t n) {
+            a.workspace = ws;
+            a.workspace_bytes = n;
+            return back ? dgs_head_backward(&a, nullptr) : dgs_head_forward(&a, nullptr);
+        }, back ? "backward" : "forward");
+    };
+    call(0);
+    std::vector<double> z(rows * vocab), dz(rows * vocab), terms(rows * vocab), rel(rows);
+    double w_most = 0.0, x_most = 0.0;
+    std::vector<double> w_row(vocab), x_row(rows), up(rows), power(rows);
+    for (uint32_t v = 0; v < vocab; ++v)
+        for (uint32_t c = 0; c < cols; ++c) w_row[v] = std::max(w_row[v], std::fabs(w.v[v * cols + c]));
+    for (double v : w_row) w_most = std::max(w_most, v);
+    for (uint32_t t = 0; t < rows; ++t) {
+        double top = -INFINITY, sum = 0.0, off = 0.0;
+        for (uint32_t c = 0; c < cols; ++c) x_row[t] = std::max(x_row[t], std::fabs(x.v[t * cols + c]));
+        for (uint32_t v = 0; v < vocab; ++v) {
+            double s = bias ? bias->v[v] : 0.0, m = std::fabs(s), least = 0.0;
+            for (uint32_t c = 0; c < cols; ++c) {
+                const double p = x.v[t * cols + c], q = w.v[v * cols + c];
+                s += p * q;
+                m += std::fabs(p * q);
+                least += std::fabs(p) * w_row[v] + std::fabs(q) * x_row[t];
+            }
+            z[t * vocab + v] = s;
+            top = std::max(top, s);
+            off = std::max(off, ldexp(m * (cols + 8), -24) + (type == DGS_F32 ? ldexp(m, -21) + ldexp(least, -50) : 0.0));
+        }
+        for (uint32_t v = 0; v < vocab; ++v) sum += exp(z[t * vocab + v] - top);
+        const double l = top + log(sum);
+        const bool counts = targets[t] >= 0;
+        off += ldexp(std::fabs(l) + 40.0, -22);
+        near(read_as(DGS_F32, lse.store.get(), t), l, off, "lse", t);
+        near(read_as(DGS_F32, loss.store.get(), t), counts ? l - z[t * vocab + targets[t]] : 0.0, counts ? 2 * off : 0.0, "loss", t);
+        rel[t] = 2 * off + ldexp(1.0, -20);
+        up[t] = counts ? dloss.v[t] : 0.0;
+        power[t] = power_of(std::max(std::fabs(up[t]), std::fabs(up[t] + dlse.v[t])));
+        for (uint32_t v = 0; v < vocab; ++v) {
+            const double p = (up[t] + dlse.v[t]) * exp(z[t * vocab + v] - l), one = (long)v == targets[t] ? up[t] : 0.0;
+            dz[t * vocab + v] = p - one;
+            terms[t * vocab + v] = std::fabs(p) * rel[t] + (std::fabs(p) + std::fabs(one)) * ldexp(1.0, -22) + ldexp(1.0, (int)power[t] - 50);
+        }
+        x_most = std::max(x_most, x_row[t] * ldexp(1.0, (int)power[t]));
+    }
+    a.dloss = dloss.floats();
+    a.dlse = dlse.floats();
+    a.dx = dx.view(cols);
+    a.dweight = (float *)dw.store.get();
+    a.dweight_stride = cols;
+    a.dbias = (float *)db.store.get();
+    call(1);
+    const double held = type == DGS_F32 ? ldexp(1.0, -22) : 0.0;
+    for (uint32_t t = 0; t < rows; ++t)
+        for (uint32_t c = 0; c < cols; ++c) {
+            double s = 0.0, off = 0.0;
+            for (uint32_t v = 0; v < vocab; ++v) {
+                const double d = std::fabs(dz[t * vocab + v]), q = std::fabs(w.v[v * cols + c]);
+                s += dz[t * vocab + v] * w.v[v * cols + c];
+                off += terms[t * vocab + v] * q + d * (q * (held + ldexp((double)vocab, -24)) + ldexp(w_most, -40));
+                if (type != DGS_F32) off += ldexp(d * q, -11) + ldexp(q, (int)power[t] - 39);
+            }
+            near(read_as(type, dx.store.get(), t * cols + c), s, off + std::fabs(s) * half_step(type) + (type == DGS_F16 ? ldexp(1.0, -25) : 0.0), "dx", t, c);
+        }
+    for (uint32_t v = 0; v < vocab; ++v) {
+        double s = 0.0, off = 0.0;
+        for (uint32_t t = 0; t < rows; ++t) s += dz[t * vocab + v], off += terms[t * vocab + v] + ldexp(std::fabs(dz[t * vocab + v]) * rows, -24);
+        near(read_as(DGS_F32, db.store.get(), v), s, off, "dbias", v);
+        for (uint32_t c = 0; c < cols; ++c) {
+            s = off = 0.0;
+            for (uint32_t t = 0; t < rows; ++t) {
+                const double d = std::fabs(dz[t * vocab + v]), p = std::fabs(x.v[t * cols + c]);
+                s += dz[t * vocab + v] * x.v[t * cols + c];
+                off += terms[t * vocab + v] * p + d * (p * (held + ldexp((double)rows, -24)) + ldexp(x_most, -40 - (int)power[t]));
+            }
+            near(read_as(DGS_F32, dw.store.get(), v * cols + c), s, off, "dweight", v, c);
+        }
+    }
+}
+
+// Half of the entries (no targets) lowered by their bias, to softmax of 2^-20 down to 2^-44: their weights' gradients keep their bits.
+static void improbable()
+{
+    for (int type = 0; type < 3; ++type)
+        for (double by : {10.0, 15.0, 20.0, 25.0}) {
+            const uint32_t rows = by == 15.0 ? 20 : 40, cols = 64, vocab = 200;
+            Mat x(type, rows * cols, [](uint64_t) { return normal(); }), w(type, vocab * cols, [](uint64_t) { return normal() / 8; });
+            Mat bias(DGS_F32, vocab, [&](uint64_t v) { return v & 1 ? -by : 0.0; });
+            head("improbable", type, rows, cols, vocab, x, w, &bias);
+        }
+}
+
 int main(int, char **argv)
 {
     const std::string what = argv[1];
     if (what == "coefficients") coefficients();
+    if (what == "improbable") improbable();
     printf("%llu values as expected\n", (unsigned long long)checks);
     return 0;
 }

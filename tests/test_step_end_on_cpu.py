@@ -8,7 +8,7 @@ import pytest
 
 from test_head_on_cpu import CLANG, CSRC, EMU, FLAGS
 
-RUNS = ["coefficients"]
+RUNS = ["coefficients", "improbable"]
 
 
 @pytest.fixture(scope="module")
