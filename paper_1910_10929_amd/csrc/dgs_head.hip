@@ -6,7 +6,7 @@
 // become the gradient of the logits, which is written in 16-bit parts (HeadRow), and two products take dx and dweight from it.
 //
 // Numbers.  Sums, statistics and exponentials are fp32.  Logits are products of the operands as they are (bfloat16, half;
-// fp32 in two halves, 22 bits).  The gradient of the logits is divided by a power of two for each row (at least the larger
+// fp32 in two halves, 22 bits, every row of x and of W scaled by a power of two of its own).  The gradient of the logits is divided by a power of two for each row (at least the larger
 // of the incoming gradients) and held in two halves, the second times 2^11: 22 bits of a value down to 2^-28 of that power, below it steps
 // of 2^-49 (11 bits of what a softmax of 2^-38 leaves; with the second half as it is 2^-38 would be the step).  dx in bfloat16 takes
 // the first half, 11 bits where the result is rounded to 8, everything else both.  The other operand of these products is W or x in half,
@@ -39,9 +39,9 @@ struct HeadRow {
 __device__ __forceinline__ bool nothing_arrives(const HeadRow &h) { return h.pull == 0.0f && h.push == 0.0f; }
 struct Ranges {
     int *x, *w;         // one for each workgroup: largest exponent of x (with the rows' powers), of W
-    int *row;           // of each row of x
+    int *row, *entry;   // of each row of x, of W
 };
-// Exponents by which the whole of x (with the rows' powers) and of W are multiplied.
+// Exponents by which the whole of x (with the rows' powers) and of W are multiplied in the gradients' products.
 struct Scales { int x, w; };
 
 __device__ __forceinline__ int exponent_of(uint32_t magnitude)      // smallest e with |v| < 2^e
@@ -105,7 +105,7 @@ __global__ __launch_bounds__(256) void k_head_range(const T *x, uint64_t x_strid
     const T *const m = of_w ? w : x;
     const uint64_t stride = of_w ? w_stride : x_stride;
     int most = NO_RANGE;
-    if (of_w ? to.w != nullptr : to.x != nullptr) {
+    if (of_w ? to.w != nullptr || to.entry != nullptr : to.x != nullptr) {
         for (uint32_t row = block * 4 + wave; row < count; row += RANGE_BLOCKS * 4) {
             uint32_t top = 0;
             for (uint32_t c = lane * 8; c < cols; c += 512) {
@@ -137,6 +137,8 @@ __global__ __launch_bounds__(256) void k_head_range(const T *x, uint64_t x_strid
                 }
                 if (lane == 0) to.row[row] = e;
                 e = e <= NO_RANGE / 2 || power <= NO_RANGE / 2 ? NO_RANGE : e + power;
+            } else if (to.entry && lane == 0) {
+                to.entry[row] = e;
             }
             most = max(most, e);
         }
@@ -152,7 +154,7 @@ __global__ __launch_bounds__(256) void k_head_range(const T *x, uint64_t x_strid
 
 enum CopyKind {
     COPY_PLAIN,      // 16-bit values as they are, in rows whose length is a multiple of eight
-    COPY_ROWS,       // halves of a matrix, each row scaled by itself
+    COPY_ROWS,       // halves of a matrix, each row scaled by itself (and once more, all by the same power)
     COPY_WEIGHED,    // ... all by the same power, and each row times its own
     COPY_ALL,        // ... all by the same power
 };
@@ -161,6 +163,8 @@ struct CopyJob {
     const void *from;
     uint64_t stride;
     uint16_t *hi, *lo;      // lo: absent where one part is wanted
+    uint16_t *all_hi, *all_lo;      // COPY_ROWS: of the other copy, or absent
+    const int *powers;      // COPY_ROWS: of the rows
     uint32_t rows, blocks;
     int32_t kind;
 };
@@ -186,8 +190,8 @@ __global__ __launch_bounds__(256) void k_head_copy(CopyJobs jobs, Ranges ranges,
             which = i;
         }
     int all = 0;
-    if (j.kind == COPY_WEIGHED || j.kind == COPY_ALL) {
-        const int *const r = j.kind == COPY_ALL ? ranges.w : ranges.x;
+    if (j.kind == COPY_WEIGHED || j.kind == COPY_ALL || j.all_hi) {
+        const int *const r = j.kind == COPY_WEIGHED ? ranges.x : ranges.w;
         int most = NO_RANGE;
 #pragma unroll
         for (uint32_t k = 0; k < RANGE_BLOCKS; k += 256) most = max(most, r[k + threadIdx.x]);
@@ -195,7 +199,7 @@ __global__ __launch_bounds__(256) void k_head_copy(CopyJobs jobs, Ranges ranges,
         if (lane_id() == 0) best[threadIdx.x >> 6] = most;
         __syncthreads();
         all = scale_of(max(max(best[0], best[1]), max(best[2], best[3])));
-        if (block == 0 && threadIdx.x == 0) (j.kind == COPY_ALL ? scales->w : scales->x) = all;
+        if (block == 0 && threadIdx.x == 0) (j.kind == COPY_WEIGHED ? scales->x : scales->w) = all;
     }
     const uint64_t step = (uint64_t)j.blocks * 256, end = (uint64_t)j.rows * jobs.pieces;
     for (uint64_t at = (uint64_t)block * 256 + threadIdx.x; at < end; at += step) {
@@ -210,7 +214,17 @@ __global__ __launch_bounds__(256) void k_head_copy(CopyJobs jobs, Ranges ranges,
         int e = all;
         float v[8];
         unpack8(raw, v);
-        if (j.kind == COPY_ROWS) e = scale_of(ranges.row[row]);
+        if (j.kind == COPY_ROWS) {
+            if (j.all_hi) {
+                float w[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) w[i] = times_power(v[i], all);
+                halves8<LOW>(w, h, l);
+                *(u32x4 *)(j.all_hi + at * 8) = h;
+                *(u32x4 *)(j.all_lo + at * 8) = l;
+            }
+            e = scale_of(j.powers[row]);
+        }
         if (j.kind == COPY_WEIGHED) {
             const HeadRow r = row_info[row];
             e = all + r.power;
@@ -238,8 +252,7 @@ struct LogitArgs {
     uint32_t v_tiles, t_tiles;
     const float *bias;
     Targets targets;
-    const int *x_powers;             // exponents that x's rows and W were multiplied by, fp32 only
-    const Scales *scales;
+    const int *x_powers, *w_powers;  // exponents of x's and W's rows, fp32 only
     // forward: a row's maximum and sum, for each tile of the vocabulary; the target's logit
     float2 *stats;
     float *target_logit;
@@ -467,6 +480,13 @@ __global__ __launch_bounds__(STAGES ? WAVES_M *WAVES_N * 64 : FEW_WAVES * 64, 2)
     if (a.bias) {      // (read behind the product's barriers)
         for (uint32_t m = threadIdx.x; m < M; m += P::THREADS) bias[m] = a.bias[min(v0 + m, a.end - 1u)];
     }
+    constexpr bool SPLIT = STAGES > 0 && __is_same(E, f16);      // (fp32 operands may have come in halves)
+    __shared__ __attribute__((aligned(16))) int w_power[SPLIT ? M : 4];
+    if constexpr (SPLIT) {
+        if (a.w_powers) {
+            for (uint32_t m = threadIdx.x; m < M; m += P::THREADS) w_power[m] = -scale_of(a.w_powers[min(v0 + m, a.end - 1u)]);
+        }
+    }
     typename P::Sums z;
     if constexpr (STAGES == 0) {
         __shared__ float part[FEW_WAVES - 1][16][64];
@@ -487,12 +507,15 @@ __global__ __launch_bounds__(STAGES ? WAVES_M *WAVES_N * 64 : FEW_WAVES * 64, 2)
         const uint32_t t = t0 + P::wave_n() + 32 * j + (lane & 31u);
         here[j] = t < a.rows;
         target[j] = here[j] ? target_of(a.targets, t) : a.vocab;
-        if (a.x_powers) {
-            const int e = here[j] ? -a.scales->w - scale_of(a.x_powers[t]) : 0;
+        if constexpr (SPLIT) {
+            if (a.x_powers) {
+                const int e = here[j] ? -scale_of(a.x_powers[t]) : 0;
 #pragma unroll
-            for (uint32_t i = 0; i < P::I; ++i)
+                for (uint32_t i = 0; i < P::I; ++i)
 #pragma unroll
-                for (uint32_t r = 0; r < 16; ++r) z[i][j][r] = times_power(z[i][j][r], e);
+                    for (uint32_t r = 0; r < 16; ++r)
+                        z[i][j][r] = times_power(z[i][j][r], e + w_power[P::wave_m() + 32 * i + row_in_square(r) + 4 * half]);
+            }
         }
     }
     if (a.bias) {
@@ -895,7 +918,7 @@ struct HeadPlan {
     HeadRow *row_info;
     Ranges ranges;
     Scales *scales;
-    uint16_t *x[2], *x_weighed[2], *w[2], *grad[2];
+    uint16_t *x[2], *x_weighed[2], *w[2], *w_all[2], *grad[2];      // (w_all: fp32's for dx)
     float *bias_parts, *dx_sums, *dw_sums;
 };
 
@@ -919,7 +942,7 @@ static HeadPlan plan_of(const dgs_head_args &p, bool back)
     // 32 rows 360 and 278; of 32000 x 1024 16 rows 67 and 67)
     h.few_dx = h.few && (f32 || p.rows <= 16);
     h.split = f32 && !h.few;
-    h.scale_w = h.split || (p.type == DGS_BF16 && h.wants_dx && !h.few_dx);
+    h.scale_w = h.wants_dx && (h.split || (p.type == DGS_BF16 && !h.few_dx));
     h.copy_x = !f32 && !h.few && !straight_ok(p.x, p.rows, p.cols);
     h.copy_w = !f32 && !straight_ok(p.weight, p.vocab, p.cols) && (!h.few || (p.type == DGS_F16 && h.wants_dx && !h.few_dx));
     h.logits = h.direct ? TILE_DIRECT : h.few ? TILE_FEW : logits_tile(p.vocab, p.rows, steps_of(p.cols, f32 ? BOTH_IN_TWO : ONE_PAIR));
@@ -934,6 +957,7 @@ static HeadPlan plan_of(const dgs_head_args &p, bool back)
         h.ranges.row = (int *)s.take((uint64_t)p.rows * 4);
         h.ranges.x = (int *)s.take(RANGE_BLOCKS * 4);
         h.ranges.w = (int *)s.take(RANGE_BLOCKS * 4);
+        if (h.split) h.ranges.entry = (int *)s.take((uint64_t)p.vocab * 4);
         h.scales = (Scales *)s.take(sizeof(Scales));
         if (!h.scale_w) h.ranges.w = nullptr;
     }
@@ -941,6 +965,8 @@ static HeadPlan plan_of(const dgs_head_args &p, bool back)
     if (h.split) h.x[1] = (uint16_t *)s.take(x_bytes);
     if (h.split || h.copy_w) h.w[0] = (uint16_t *)s.take(w_bytes);
     if (h.split) h.w[1] = (uint16_t *)s.take(w_bytes);
+    if (h.split && h.wants_dx)
+        for (uint16_t *&w : h.w_all) w = (uint16_t *)s.take(w_bytes);
     if (back) {
         h.row_info = (HeadRow *)s.take((uint64_t)p.rows * sizeof(HeadRow));
         if (h.wants_dw) h.x_weighed[0] = (uint16_t *)s.take(x_bytes);
@@ -985,12 +1011,16 @@ template <class T> static void prepare(const dgs_head_args &p, const HeadPlan &h
     auto job = [&](const dgs_matrix &m, uint32_t rows, int kind, uint16_t *hi, uint16_t *lo) {
         const uint64_t n = ((uint64_t)rows * jobs.pieces + 255) / 256;
         const uint32_t b = n < 4096 ? (uint32_t)n : 4096u;
-        jobs.job[jobs.count++] = CopyJob{m.data, m.stride, hi, lo, rows, b, kind};
+        jobs.job[jobs.count++] = CopyJob{m.data, m.stride, hi, lo, nullptr, nullptr, nullptr, rows, b, kind};
         blocks += b;
     };
     if (h.split) {
         job(p.x, p.rows, COPY_ROWS, h.x[0], h.x[1]);
-        job(p.weight, p.vocab, COPY_ALL, h.w[0], h.w[1]);
+        jobs.job[0].powers = h.ranges.row;
+        job(p.weight, p.vocab, COPY_ROWS, h.w[0], h.w[1]);
+        jobs.job[1].powers = h.ranges.entry;
+        jobs.job[1].all_hi = h.w_all[0];
+        jobs.job[1].all_lo = h.w_all[1];
     } else {
         if (h.copy_x) job(p.x, p.rows, COPY_PLAIN, h.x[0], nullptr);
         if (h.copy_w) job(p.weight, p.vocab, COPY_PLAIN, h.w[0], nullptr);
@@ -1078,7 +1108,7 @@ static LogitArgs logit_args(const dgs_head_args &p, const HeadPlan &h, const Tar
     a.bias = p.bias;
     a.targets = targets;
     a.x_powers = h.split ? h.ranges.row : nullptr;
-    a.scales = h.scales;
+    a.w_powers = h.split ? h.ranges.entry : nullptr;
     return a;
 }
 
@@ -1184,10 +1214,10 @@ extern "C" int dgs_head_backward(const dgs_head_args *args, void *hip_stream)
             few_dx(p, h, first, count, stride, st);
         } else if (h.wants_dx) {
             GradientArgs &g = dx;
-            const uint16_t *w = p.type == DGS_BF16 ? h.w[1] : h.copy_w ? h.w[0] : a.w.part[0];
-            const uint64_t w_stride = p.type == DGS_BF16 || h.copy_w ? h.width : a.w.stride;
+            const uint16_t *w = f32 ? h.w_all[0] : p.type == DGS_BF16 ? h.w[1] : h.copy_w ? h.w[0] : a.w.part[0];
+            const uint64_t w_stride = p.type != DGS_F16 || h.copy_w ? h.width : a.w.stride;
             g.a = Side{{h.grad[0], h.grad[1]}, stride, p.rows};
-            g.b = Side{{w + first * w_stride, f32 ? a.w.part[1] + first * w_stride : nullptr}, w_stride, p.cols};
+            g.b = Side{{w + first * w_stride, f32 ? h.w_all[1] + first * w_stride : nullptr}, w_stride, p.cols};
             g.depth = count;
             g.splits = h.dx.splits;
             g.split_depth = h.dx.split_depth;

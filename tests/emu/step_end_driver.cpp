@@ -1,6 +1,6 @@
 // Where numbers are hard for the orthogonalising kernels and the output layer's, on the CPU, through the C ABI: coefficients that take
-// little or nothing off small singular values, against the same steps in double; entries of the vocabulary that are improbable, against
-// the definition.
+// little or nothing off small singular values, against the same steps in double; entries of the vocabulary that are improbable, and
+// fp32 weights of very unlike size, against the definition.
 #include <hip/hip_runtime.h>
 #include "../../include/dgs_blocks.h"
 #include <functional>
@@ -152,9 +152,9 @@ struct Mat {
 static int power_of(double v) { int e; frexp(v, &e); return e; }      // smallest e with |v| < 2^e
 
 // Loss and gradients of x, W, bias and targets, against the definition.  Logits are off by what fp32's additions leave of `cols` products and, of
-// fp32 operands, by 2^-22 of each value and 2^-50 of its row's largest; that is what lse, the loss and, relatively, dz are off by, with 2^-20 for the
-// exponential and the logarithm.  dz is held in 22 bits, with steps of 2^-50 (half of it here) of its row's power of two.  x and W in the
-// gradients' products: 2^-22 and 2^-40 of the largest for fp32, nothing and 2^-40 for half and bfloat16; dx of bfloat16 takes 11 bits of dz.
+// fp32 operands, by 2^-22 of each value and 2^-50 of its row's largest; lse is off by their softmax mean (a tenth more for what is not linear) and 2^-22 of its
+// terms' exponents, a value of dz, relatively, by what its logit and lse are and 2^-20 for the exponential.  dz is held in 22 bits, with steps of 2^-50 (half of it here) of its row's power of two.  x and W in the
+// gradients' products: 2^-22 and 2^-50 of the largest for fp32, nothing and 2^-40 for half and bfloat16; dx of bfloat16 takes 11 bits of dz.
 static void head(const char *what, int type, uint32_t rows, uint32_t cols, uint32_t vocab, const Mat &x, const Mat &w, const Mat *bias)
 {
     name = std::string(what) + " " + std::to_string(type) + " " + std::to_string(rows) + "x" + std::to_string(cols) + "x" + std::to_string(vocab);
@@ -178,7 +178,7 @@ static void head(const char *what, int type, uint32_t rows, uint32_t cols, uint3
         }, back ? "backward" : "forward");
     };
     call(0);
-    std::vector<double> z(rows * vocab), dz(rows * vocab), terms(rows * vocab), rel(rows);
+    std::vector<double> z(rows * vocab), dz(rows * vocab), terms(rows * vocab), far(vocab);
     double w_most = 0.0, x_most = 0.0;
     std::vector<double> w_row(vocab), x_row(rows), up(rows), power(rows);
     for (uint32_t v = 0; v < vocab; ++v)
@@ -197,21 +197,21 @@ static void head(const char *what, int type, uint32_t rows, uint32_t cols, uint3
             }
             z[t * vocab + v] = s;
             top = std::max(top, s);
-            off = std::max(off, ldexp(m * (cols + 8), -24) + (type == DGS_F32 ? ldexp(m, -21) + ldexp(least, -50) : 0.0));
+            far[v] = std::isinf(s) ? 0.0 : ldexp(m * (cols + 8), -24) + (type == DGS_F32 ? ldexp(m, -21) + ldexp(least, -50) : 0.0);
         }
         for (uint32_t v = 0; v < vocab; ++v) sum += exp(z[t * vocab + v] - top);
         const double l = top + log(sum);
+        for (uint32_t v = 0; v < vocab; ++v) off += 1.1 * exp(z[t * vocab + v] - l) * far[v];
         const bool counts = targets[t] >= 0;
         off += ldexp(std::fabs(l) + 40.0, -22);
         near(read_as(DGS_F32, lse.store.get(), t), l, off, "lse", t);
-        near(read_as(DGS_F32, loss.store.get(), t), counts ? l - z[t * vocab + targets[t]] : 0.0, counts ? 2 * off : 0.0, "loss", t);
-        rel[t] = 2 * off + ldexp(1.0, -20);
+        near(read_as(DGS_F32, loss.store.get(), t), counts ? l - z[t * vocab + targets[t]] : 0.0, counts ? off + far[targets[t]] : 0.0, "loss", t);
         up[t] = counts ? dloss.v[t] : 0.0;
         power[t] = power_of(std::max(std::fabs(up[t]), std::fabs(up[t] + dlse.v[t])));
         for (uint32_t v = 0; v < vocab; ++v) {
             const double p = (up[t] + dlse.v[t]) * exp(z[t * vocab + v] - l), one = (long)v == targets[t] ? up[t] : 0.0;
             dz[t * vocab + v] = p - one;
-            terms[t * vocab + v] = std::fabs(p) * rel[t] + (std::fabs(p) + std::fabs(one)) * ldexp(1.0, -22) + ldexp(1.0, (int)power[t] - 50);
+            terms[t * vocab + v] = std::fabs(p) * (off + far[v] + ldexp(1.0, -20)) + (std::fabs(p) + std::fabs(one)) * ldexp(1.0, -22) + ldexp(1.0, (int)power[t] - 50);
         }
         x_most = std::max(x_most, x_row[t] * ldexp(1.0, (int)power[t]));
     }
@@ -223,13 +223,14 @@ static void head(const char *what, int type, uint32_t rows, uint32_t cols, uint3
     a.dbias = (float *)db.store.get();
     call(1);
     const double held = type == DGS_F32 ? ldexp(1.0, -22) : 0.0;
+    const int lost = type == DGS_F32 ? -50 : -40;
     for (uint32_t t = 0; t < rows; ++t)
         for (uint32_t c = 0; c < cols; ++c) {
             double s = 0.0, off = 0.0;
             for (uint32_t v = 0; v < vocab; ++v) {
                 const double d = std::fabs(dz[t * vocab + v]), q = std::fabs(w.v[v * cols + c]);
                 s += dz[t * vocab + v] * w.v[v * cols + c];
-                off += terms[t * vocab + v] * q + d * (q * (held + ldexp((double)vocab, -24)) + ldexp(w_most, -40));
+                off += terms[t * vocab + v] * q + d * (q * (held + ldexp((double)vocab, -24)) + ldexp(w_most, lost));
                 if (type != DGS_F32) off += ldexp(d * q, -11) + ldexp(q, (int)power[t] - 39);
             }
             near(read_as(type, dx.store.get(), t * cols + c), s, off + std::fabs(s) * half_step(type) + (type == DGS_F16 ? ldexp(1.0, -25) : 0.0), "dx", t, c);
@@ -243,7 +244,7 @@ static void head(const char *what, int type, uint32_t rows, uint32_t cols, uint3
             for (uint32_t t = 0; t < rows; ++t) {
                 const double d = std::fabs(dz[t * vocab + v]), p = std::fabs(x.v[t * cols + c]);
                 s += dz[t * vocab + v] * x.v[t * cols + c];
-                off += terms[t * vocab + v] * p + d * (p * (held + ldexp((double)rows, -24)) + ldexp(x_most, -40 - (int)power[t]));
+                off += terms[t * vocab + v] * p + d * (p * (held + ldexp((double)rows, -24)) + ldexp(x_most, lost - (int)power[t]));
             }
             near(read_as(DGS_F32, dw.store.get(), v * cols + c), s, off, "dweight", v, c);
         }
@@ -262,11 +263,32 @@ static void improbable()
         }
 }
 
+// fp32: one entry of W far above the others, in a column where x is 0: what is small beside it decides about all
+// logits but its own, which a bias takes out.  (From 33 rows on
+// operands are held in halves; up to 32 they are read as they are.)
+static void unlike()
+{
+    for (uint32_t rows : {32u, 33u, 70u})
+        for (double far : {1e9, 1e12, 1e25}) {
+            const uint32_t cols = 16, vocab = 64;
+            Mat x(DGS_F32, rows * cols, [&](uint64_t i) { return i % cols == 5 ? 0.0 : normal(); });
+            Mat w(DGS_F32, vocab * cols, [&](uint64_t i) { return i == 7 * cols + 5 ? far : normal(); });
+            Mat bias(DGS_F32, vocab, [](uint64_t v) { return v == 7 ? -INFINITY : 0.0; });
+            head("outlier", DGS_F32, rows, cols, vocab, x, w, &bias);
+            if (far > 1e9) continue;
+            // (x's columns 8 to 15 are 0 but in the odd rows, W's are large; entries take their logits from small numbers or large ones)
+            Mat y(DGS_F32, rows * cols, [&](uint64_t i) { return i % cols < 8 ? normal() : i / cols % 2 ? normal() / far : 0.0; });
+            Mat u(DGS_F32, vocab * cols, [&](uint64_t i) { return i % cols < 8 ? normal() : i / cols % 3 == 0 ? normal() * far : 0.0; });
+            head("unlike columns", DGS_F32, rows, cols, vocab, y, u, nullptr);
+        }
+}
+
 int main(int, char **argv)
 {
     const std::string what = argv[1];
     if (what == "coefficients") coefficients();
     if (what == "improbable") improbable();
+    if (what == "unlike") unlike();
     printf("%llu values as expected\n", (unsigned long long)checks);
     return 0;
 }

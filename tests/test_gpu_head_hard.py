@@ -90,3 +90,25 @@ def test_improbable_entries(size, dtype, lowered):
     """Half of the entries lowered by their bias, to softmax of 2^-22 down to 2^-48: their weights' gradients keep their bits."""
     print(size, dtype, lowered, flush=True)
     Case(*size, dtype, lowered=lowered).assert_near()
+
+
+@pytest.mark.parametrize("far", [1e9, 1e12, 1e25])
+@pytest.mark.parametrize("size", [(32, 64, 300), (33, 64, 300), (1000, 96, 4000), (4096, 128, 16384)], ids=lambda s: f"{s[0]}x{s[1]}x{s[2]}")
+def test_one_weight_far_above_the_others(size, far):
+    """fp32, in a column where x is 0, its entry taken out: every other logit is made of what is small beside it.  A logit of at most 60 here is
+    off by 2^-25 60 sqrt(cols) and 2^-22 of its terms, less than 2^-14 with lse's own error; gradients as ever, but that W as it meets dx has steps of
+    2^-50 of the largest, here on all entries of a row of dz, whose magnitudes sum to 2 of its power at most."""
+    print(size, far, flush=True)
+    c = Case(*size, F32)
+    c.w.mul_(4.0)
+    c.x[:, 5] = 0.0
+    c.w[7, 5], c.bias[7] = far, -float("inf")
+    want = torch.logsumexp((c.w.to(D) @ c.x.to(D).t()).t() + c.bias.to(D), 1)
+    lse = blocks.Head(c.w, c.bias).forward(c.x, c.targets)[1]
+    assert float((lse.to(D) - want).abs().max()) <= 2.0 ** -14
+    dx, dw, db = c.run()
+    want_dx, want_dw, want_db, power = c.exact()
+    rel = 2.0 ** -20 * c.cols ** 0.5 + 2.0 ** -16
+    assert float((dw.to(D) - want_dw).norm()) <= rel * float(want_dw.norm())
+    assert float((db.to(D) - want_db).norm()) <= rel * float(want_db.norm())
+    assert float((dx.to(D) - want_dx).norm()) <= rel * float(want_dx.norm()) + 2.0 ** -50 * far * 2.0 * float(power.norm()) * c.cols ** 0.5

@@ -8,7 +8,7 @@ import pytest
 
 from test_head_on_cpu import CLANG, CSRC, EMU, FLAGS
 
-RUNS = ["coefficients", "improbable"]
+RUNS = ["coefficients", "improbable", "unlike"]
 
 
 @pytest.fixture(scope="module")
