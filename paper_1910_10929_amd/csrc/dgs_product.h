@@ -65,7 +65,7 @@ __device__ __forceinline__ LdsPlace lds_place(uint16_t *p) { return uniform((uin
 // 16 bytes from `offset` on into LDS: lane l's `behind` + 16 l bytes behind `to`.  Nothing waits; loads_meet() does.
 __device__ __forceinline__ void load_to_lds(Window w, uint32_t offset, LdsPlace to, uint32_t behind)
 {
-    asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(w), "s"(behind) : "memory", "scc");
+    asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(w), "s"(behind) : "memory", "scc", "m0");
 }
 // Every wavefront's loads but its last LEFT have arrived, and what was read before has been.
 template <int LEFT> __device__ __forceinline__ void loads_meet() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory"); }
