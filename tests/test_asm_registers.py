@@ -12,7 +12,7 @@ def test_written_registers_are_declared():
         with open(path) as f:
             text = f.read()
         for statement in re.findall(r"\basm volatile\((.*?)\);", text, re.S):
-            template, _, rest = statement.partition('"::')
+            template, rest = (re.split(r'"\s*:', statement, maxsplit=1) + [""])[:2]
             clobbers = rest[rest.rfind(":"):] if ":" in rest else ""
             for register in set(re.findall(r"(?:^|\\n\\t|\")[a-z_0-9]+ (m0|vcc|exec|s\d+|v\d+)\b", template)):
                 found += 1
