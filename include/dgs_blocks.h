@@ -187,7 +187,7 @@ int dgs_checkpoint_weight_grad(const dgs_weight_grad_args *args /*host*/, void *
  *   forward    reads x, weight, bias, targets; writes loss (or NULL) and lse.
  *   backward   reads those and lse; writes dx, dweight (rows dweight_stride apart) and dbias, each or none of them.
  *              accumulate != 0: dweight and dbias are added to.
- * Outputs overlap nothing.  workspace: at least dgs_head_workspace() bytes for the same arguments (of the pointers their
+ * Outputs overlap nothing (a loss that overlaps lse: DGS_EINVAL).  workspace: at least dgs_head_workspace() bytes for the same arguments (of the pointers their
  * alignment counts), 16-byte aligned; as above.  More than 2^20 columns, 2^24 rows or entries, 2^34
  * values of x or 2^38 logits: DGS_ENOTSUP.
  */

@@ -1150,6 +1150,7 @@ extern "C" int dgs_head_forward(const dgs_head_args *args, void *hip_stream)
     if (!p.workspace || !aligned_to(p.workspace, 16)) return DGS_EINVAL;
     const HeadPlan h = plan_of(p, false);
     if (p.workspace_bytes < h.bytes) return DGS_ENOMEM;
+    if (p.loss && p.loss < p.lse + p.rows && p.lse < p.loss + p.rows) return DGS_EINVAL;      // (lse would be lost)
     const hipStream_t st = (hipStream_t)hip_stream;
     const Targets targets = {p.targets, p.target_bytes == 8, p.vocab};
     if (p.type == DGS_F32) prepare<float>(p, h, targets, st);
