@@ -62,11 +62,15 @@ __device__ __forceinline__ Window window_at(const void *p, uint32_t bytes)
 // Where in LDS a wavefront's loads go.
 typedef uint32_t LdsPlace;
 __device__ __forceinline__ LdsPlace lds_place(uint16_t *p) { return uniform((uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint16_t *)p); }
-// 16 bytes from `offset` on into LDS: lane l's `behind` + 16 l bytes behind `to`.  Nothing waits; loads_meet() does.
+// 16 bytes from `offset` on into LDS: lane l's `behind` + 16 l bytes behind `to`.  Nothing waits; loads_meet() does.  (The compiler keeps
+// nothing in m0, and warns that it would not save it; named, nothing of its own that sets and uses m0 is moved across.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void load_to_lds(Window w, uint32_t offset, LdsPlace to, uint32_t behind)
 {
     asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(w), "s"(behind) : "memory", "scc", "m0");
 }
+#pragma clang diagnostic pop
 // Every wavefront's loads but its last LEFT have arrived, and what was read before has been.
 template <int LEFT> __device__ __forceinline__ void loads_meet() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory"); }
 #endif
