@@ -176,8 +176,8 @@ int dgs_checkpoint_weight_grad(const dgs_weight_grad_args *args /*host*/, void *
  * Logits are not kept: the backward pass computes them again, a piece of the vocabulary at a time.
  *
  * x, weight and dx have `type`; bias, loss, lse, dweight and dbias are fp32.  Sums, exponentials and statistics are fp32, of
- * products that are exact (DGS_F32: 2^-22 off; of more than 32 rows, x and W in 22 bits, below 2^-28 of the largest of their row
- * in steps of 2^-49 of it).  dz is held in 22 bits, below
+ * products that are exact (DGS_F32: 2^-22 off; of more than 32 rows, x and W in 22 bits, below 2^-20 of the largest of their row
+ * in steps of 2^-41 of it).  dz is held in 22 bits, below
  * 2^-28 of its row's incoming gradients in steps of 2^-49 of them; a dx of DGS_BF16 takes 11 bits, and steps of 2^-38 (of at
  * most 16 rows all).  dbias is summed from fp32.  Of the other operands of the gradients' products, magnitudes below 2^-39 (DGS_F32: 2^-50) of
  * the largest (of W; of x times its row's gradients) are lost.  A bias of -infinity takes an entry out; where all of them are out, and where logits are infinite or

@@ -39,10 +39,15 @@ struct HeadRow {
 __device__ __forceinline__ bool nothing_arrives(const HeadRow &h) { return h.pull == 0.0f && h.push == 0.0f; }
 struct Ranges {
     int *x, *w;         // one for each workgroup: largest exponent of x (with the rows' powers), of W
+    int *w_least;       // ... and the smallest of a row of W that is not zeros
     int *row, *entry;   // of each row of x, of W
 };
-// Exponents by which the whole of x (with the rows' powers) and of W are multiplied in the gradients' products.
-struct Scales { int x, w; };
+// Exponents by which the whole of x (with the rows' powers) and of W are multiplied in the gradients' products.  even: no row of an fp32 W
+// lies so far below the largest that logits would miss its own power.
+struct Scales { int x, w, even; };
+// Logits of an fp32 W whose rows' largest values lie within 2^SPREAD take the copy that dx takes too: 22 bits of a value down to 2^-20 of
+// its row's largest then, steps of 2^-41 below.  (432 x 3920 x 59264 with dx: one copy 1884 us, two 2075.)
+constexpr int SPREAD = 8;
 
 __device__ __forceinline__ int exponent_of(uint32_t magnitude)      // smallest e with |v| < 2^e
 {
@@ -98,13 +103,13 @@ __global__ __launch_bounds__(256) void k_head_range(const T *x, uint64_t x_strid
                                                     uint32_t cols, Targets targets, const float *lse, const float *dloss,
                                                     const float *dlse, HeadRow *row_info, Ranges to)
 {
-    __shared__ int best[4];
+    __shared__ int best[4], worst[4];
     const uint32_t wave = uniform(threadIdx.x >> 6), lane = lane_id();
     const bool of_w = blockIdx.x >= RANGE_BLOCKS;
     const uint32_t block = of_w ? blockIdx.x - RANGE_BLOCKS : blockIdx.x, count = of_w ? targets.vocab : rows;
     const T *const m = of_w ? w : x;
     const uint64_t stride = of_w ? w_stride : x_stride;
-    int most = NO_RANGE;
+    int most = NO_RANGE, least = -NO_RANGE;
     if (of_w ? to.w != nullptr || to.entry != nullptr : to.x != nullptr) {
         for (uint32_t row = block * 4 + wave; row < count; row += RANGE_BLOCKS * 4) {
             uint32_t top = 0;
@@ -137,24 +142,29 @@ __global__ __launch_bounds__(256) void k_head_range(const T *x, uint64_t x_strid
                 }
                 if (lane == 0) to.row[row] = e;
                 e = e <= NO_RANGE / 2 || power <= NO_RANGE / 2 ? NO_RANGE : e + power;
-            } else if (to.entry && lane == 0) {
-                to.entry[row] = e;
+            } else {
+                if (to.entry && lane == 0) to.entry[row] = e;
+                least = e > NO_RANGE / 2 ? min(least, e) : least;
             }
             most = max(most, e);
         }
     }
-    if (lane == 0) best[wave] = most;
+    if (lane == 0) {
+        best[wave] = most;
+        worst[wave] = least;
+    }
     __syncthreads();
     if (threadIdx.x == 0) {
         const int v = max(max(best[0], best[1]), max(best[2], best[3]));
         if (of_w && to.w) to.w[block] = v;
+        if (of_w && to.w_least) to.w_least[block] = min(min(worst[0], worst[1]), min(worst[2], worst[3]));
         if (!of_w && to.x) to.x[block] = v;
     }
 }
 
 enum CopyKind {
     COPY_PLAIN,      // 16-bit values as they are, in rows whose length is a multiple of eight
-    COPY_ROWS,       // halves of a matrix, each row scaled by itself (and once more, all by the same power)
+    COPY_ROWS,       // halves of a matrix, each row scaled by itself (and once more, all by the same power; of an even one this alone)
     COPY_WEIGHED,    // ... all by the same power, and each row times its own
     COPY_ALL,        // ... all by the same power
 };
@@ -179,7 +189,7 @@ struct CopyJobs {
 template <class T>
 __global__ __launch_bounds__(256) void k_head_copy(CopyJobs jobs, Ranges ranges, const HeadRow *row_info, Scales *scales)
 {
-    __shared__ int best[4];
+    __shared__ int best[4], worst[4];
     uint32_t block = blockIdx.x, which = 0;
     CopyJob j = jobs.job[0];
 #pragma unroll
@@ -190,15 +200,29 @@ __global__ __launch_bounds__(256) void k_head_copy(CopyJobs jobs, Ranges ranges,
             which = i;
         }
     int all = 0;
+    bool even = false;
     if (j.kind == COPY_WEIGHED || j.kind == COPY_ALL || j.all_hi) {
         const int *const r = j.kind == COPY_WEIGHED ? ranges.x : ranges.w;
-        int most = NO_RANGE;
+        int most = NO_RANGE, least = -NO_RANGE;
 #pragma unroll
-        for (uint32_t k = 0; k < RANGE_BLOCKS; k += 256) most = max(most, r[k + threadIdx.x]);
+        for (uint32_t k = 0; k < RANGE_BLOCKS; k += 256) {
+            most = max(most, r[k + threadIdx.x]);
+            if (j.all_hi) least = min(least, ranges.w_least[k + threadIdx.x]);
+        }
         most = wave_max(most);
-        if (lane_id() == 0) best[threadIdx.x >> 6] = most;
+        least = -wave_max(-least);
+        if (lane_id() == 0) {
+            best[threadIdx.x >> 6] = most;
+            worst[threadIdx.x >> 6] = least;
+        }
         __syncthreads();
-        all = scale_of(max(max(best[0], best[1]), max(best[2], best[3])));
+        most = max(max(best[0], best[1]), max(best[2], best[3]));
+        least = min(min(worst[0], worst[1]), min(worst[2], worst[3]));
+        all = scale_of(most);
+        if (j.all_hi) {
+            even = most - least <= SPREAD;
+            if (block == 0 && threadIdx.x == 0) scales->even = even;
+        }
         if (block == 0 && threadIdx.x == 0) (j.kind == COPY_WEIGHED ? scales->x : scales->w) = all;
     }
     const uint64_t step = (uint64_t)j.blocks * 256, end = (uint64_t)j.rows * jobs.pieces;
@@ -214,7 +238,7 @@ __global__ __launch_bounds__(256) void k_head_copy(CopyJobs jobs, Ranges ranges,
         int e = all;
         float v[8];
         unpack8(raw, v);
-        if (j.kind == COPY_ROWS) {
+        if (j.kind == COPY_ROWS && !even) {
             if (j.all_hi) {
                 float w[8];
 #pragma unroll
@@ -253,6 +277,7 @@ struct LogitArgs {
     const float *bias;
     Targets targets;
     const int *x_powers, *w_powers;  // exponents of x's and W's rows, fp32 only
+    const Scales *scales;            // where dx takes a copy of its own of such a W
     // forward: a row's maximum and sum, for each tile of the vocabulary; the target's logit
     float2 *stats;
     float *target_logit;
@@ -484,7 +509,9 @@ __global__ __launch_bounds__(STAGES ? WAVES_M *WAVES_N * 64 : FEW_WAVES * 64, 2)
     __shared__ __attribute__((aligned(16))) int w_power[SPLIT ? M : 4];
     if constexpr (SPLIT) {
         if (a.w_powers) {
-            for (uint32_t m = threadIdx.x; m < M; m += P::THREADS) w_power[m] = -scale_of(a.w_powers[min(v0 + m, a.end - 1u)]);
+            const bool even = a.scales && a.scales->even;
+            for (uint32_t m = threadIdx.x; m < M; m += P::THREADS)
+                w_power[m] = even ? -a.scales->w : -scale_of(a.w_powers[min(v0 + m, a.end - 1u)]);
         }
     }
     typename P::Sums z;
@@ -704,6 +731,7 @@ struct GradientArgs {
     uint64_t out_stride;
     uint32_t add, whole;
     const Scales *scales;    // whole: x's exponent comes off
+    const uint16_t *even[2]; // of b, what takes its parts' place where W is even; or absent
 };
 
 // A tile of dx (of a piece's entries) or dweight (TURN_A: the first operand's k lies outside; the second's always does).  Bound by the matrix units:
@@ -723,7 +751,14 @@ __device__ __forceinline__ void GradientTile<M, N, WAVES_M, WAVES_N, STAGES, TUR
     const uint32_t first = min(split * a.split_depth, a.depth), end = min(first + a.split_depth, a.depth);
     float *const out = a.out + (a.whole ? 0u : (uint64_t)split * a.m * a.out_stride);
     typename P::Sums s;
-    P::run(lds, a.a, a.b, tile_m * M, tile_n * N, first, end, a.kind, s);
+    Side b = a.b;
+    if constexpr (!TURN_A) {
+        if (a.even[0] && a.scales->even) {
+            b.part[0] = a.even[0];
+            b.part[1] = a.even[1];
+        }
+    }
+    P::run(lds, a.a, b, tile_m * M, tile_n * N, first, end, a.kind, s);
     const int e = a.whole ? -GRAD_TOP - a.scales->x : 0;
     f32x4 old[2 * P::PASSES];
     P::by_fours(lds, s, [&](uint32_t p, uint32_t row, uint32_t col) {
@@ -957,7 +992,10 @@ static HeadPlan plan_of(const dgs_head_args &p, bool back)
         h.ranges.row = (int *)s.take((uint64_t)p.rows * 4);
         h.ranges.x = (int *)s.take(RANGE_BLOCKS * 4);
         h.ranges.w = (int *)s.take(RANGE_BLOCKS * 4);
-        if (h.split) h.ranges.entry = (int *)s.take((uint64_t)p.vocab * 4);
+        if (h.split) {
+            h.ranges.entry = (int *)s.take((uint64_t)p.vocab * 4);
+            h.ranges.w_least = (int *)s.take(RANGE_BLOCKS * 4);
+        }
         h.scales = (Scales *)s.take(sizeof(Scales));
         if (!h.scale_w) h.ranges.w = nullptr;
     }
@@ -1109,6 +1147,7 @@ static LogitArgs logit_args(const dgs_head_args &p, const HeadPlan &h, const Tar
     a.targets = targets;
     a.x_powers = h.split ? h.ranges.row : nullptr;
     a.w_powers = h.split ? h.ranges.entry : nullptr;
+    a.scales = h.split && h.wants_dx ? h.scales : nullptr;
     return a;
 }
 
@@ -1219,6 +1258,11 @@ extern "C" int dgs_head_backward(const dgs_head_args *args, void *hip_stream)
             const uint64_t w_stride = p.type != DGS_F16 || h.copy_w ? h.width : a.w.stride;
             g.a = Side{{h.grad[0], h.grad[1]}, stride, p.rows};
             g.b = Side{{w + first * w_stride, f32 ? h.w_all[1] + first * w_stride : nullptr}, w_stride, p.cols};
+            if (f32) {
+                g.even[0] = h.w[0] + first * w_stride;
+                g.even[1] = h.w[1] + first * w_stride;
+                g.scales = h.scales;
+            }
             g.depth = count;
             g.splits = h.dx.splits;
             g.split_depth = h.dx.split_depth;

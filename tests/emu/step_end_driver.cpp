@@ -152,7 +152,7 @@ struct Mat {
 static int power_of(double v) { int e; frexp(v, &e); return e; }      // smallest e with |v| < 2^e
 
 // Loss and gradients of x, W, bias and targets, against the definition.  Logits are off by what fp32's additions leave of `cols` products and, of
-// fp32 operands, by 2^-22 of each value and 2^-50 of its row's largest; lse is off by their softmax mean (a tenth more for what is not linear) and 2^-22 of its
+// fp32 operands, by 2^-22 of each value and 2^-50 of its row's largest (2^-42 where the rows of W lie within 2^8 of one another); lse is off by their softmax mean (a tenth more for what is not linear) and 2^-22 of its
 // terms' exponents, a value of dz, relatively, by what its logit and lse are and 2^-20 for the exponential.  dz is held in 22 bits, with steps of 2^-50 (half of it here) of its row's power of two.  x and W in the
 // gradients' products: 2^-22 and 2^-50 of the largest for fp32, nothing and 2^-40 for half and bfloat16; dx of bfloat16 takes 11 bits of dz.
 static void head(const char *what, int type, uint32_t rows, uint32_t cols, uint32_t vocab, const Mat &x, const Mat &w, const Mat *bias)
@@ -183,7 +183,9 @@ static void head(const char *what, int type, uint32_t rows, uint32_t cols, uint3
     std::vector<double> w_row(vocab), x_row(rows), up(rows), power(rows);
     for (uint32_t v = 0; v < vocab; ++v)
         for (uint32_t c = 0; c < cols; ++c) w_row[v] = std::max(w_row[v], std::fabs(w.v[v * cols + c]));
-    for (double v : w_row) w_most = std::max(w_most, v);
+    double w_least = INFINITY;
+    for (double v : w_row) w_most = std::max(w_most, v), w_least = v > 0.0 ? std::min(w_least, v) : w_least;
+    const int row_step = w_most > 0.0 && power_of(w_most) - power_of(w_least) <= 8 ? -42 : -50;
     for (uint32_t t = 0; t < rows; ++t) {
         double top = -INFINITY, sum = 0.0, off = 0.0;
         for (uint32_t c = 0; c < cols; ++c) x_row[t] = std::max(x_row[t], std::fabs(x.v[t * cols + c]));
@@ -197,7 +199,7 @@ static void head(const char *what, int type, uint32_t rows, uint32_t cols, uint3
             }
             z[t * vocab + v] = s;
             top = std::max(top, s);
-            far[v] = std::isinf(s) ? 0.0 : ldexp(m * (cols + 8), -24) + (type == DGS_F32 ? ldexp(m, -21) + ldexp(least, -50) : 0.0);
+            far[v] = std::isinf(s) ? 0.0 : ldexp(m * (cols + 8), -24) + (type == DGS_F32 ? ldexp(m, -21) + ldexp(least, row_step) : 0.0);
         }
         for (uint32_t v = 0; v < vocab; ++v) sum += exp(z[t * vocab + v] - top);
         const double l = top + log(sum);
@@ -281,6 +283,15 @@ static void unlike()
             Mat u(DGS_F32, vocab * cols, [&](uint64_t i) { return i % cols < 8 ? normal() : i / cols % 3 == 0 ? normal() * far : 0.0; });
             head("unlike columns", DGS_F32, rows, cols, vocab, y, u, nullptr);
         }
+    // rows of W up to 2^8 and 2^9 apart, some of them zeros: dx and logits from one copy, and from one each
+    for (int apart : {0, 8, 9, 60}) {
+        const uint32_t rows = 40, cols = 24, vocab = 70;
+        Mat x(DGS_F32, rows * cols, [&](uint64_t) { return normal(); });
+        Mat w(DGS_F32, vocab * cols, [&](uint64_t i) { return i / cols % 5 == 2 ? 0.0 : ldexp(1.0 + (double)gen() / 4294967296.0, i / cols % 2 ? -apart : 0) * (i % 3 ? 0.3 : -0.3); });
+        head(("apart by 2^" + std::to_string(apart)).c_str(), DGS_F32, rows, cols, vocab, x, w, nullptr);
+    }
+    Mat x(DGS_F32, 40 * 8, [&](uint64_t) { return normal(); }), zeros(DGS_F32, 50 * 8, [](uint64_t) { return 0.0; });
+    head("zeros", DGS_F32, 40, 8, 50, x, zeros, nullptr);
 }
 
 int main(int, char **argv)
