@@ -490,9 +490,9 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void k_head_few_dx(const T *w, uint
 }
 
 // Entries (m) and rows (n) of a tile.  E: the operands' type as they are staged; STAGES = 0: as they are read, a square to a wavefront.
-// Bound by the matrix units: of 8192 x 4096 x 32768 (2.2 TFLOP, bfloat16) 1695 us, 1297 TFLOP/s, with the gradient's halves written
-// (1.1 GB) 1835; of 8192 x 768 x 30522 376 and 527, since 12 steps a tile hide less of its epilogue.  One row of 768 columns: by W's reading,
-// 47 MB in 10.3 us.  No branch in the epilogue but for tiles at the edge or with a target: with them 16384 x 768 x 30522 760 us, without 671.
+// Bound by the matrix units: of 8192 x 4096 x 32768 (2.2 TFLOP, bfloat16) 1718 us, 1280 TFLOP/s, with the gradient's halves written
+// (1.1 GB) 1853; of 8192 x 768 x 30522 388 and 547, since 12 steps a tile hide less of its epilogue.  One row of 768 columns: by W's reading,
+// 47 MB in 10.7 us.  No branch in the epilogue but for tiles at the edge or with a target: with them 16384 x 768 x 30522 760 us, without 671.
 template <class E, uint32_t M, uint32_t N, uint32_t WAVES_M, uint32_t WAVES_N, uint32_t STAGES, bool BACK>
 __global__ __launch_bounds__(STAGES ? WAVES_M *WAVES_N * 64 : FEW_WAVES * 64, 2) void k_head_logits(LogitArgs a)
 {
@@ -735,7 +735,7 @@ struct GradientArgs {
 };
 
 // A tile of dx (of a piece's entries) or dweight (TURN_A: the first operand's k lies outside; the second's always does).  Bound by the matrix units:
-// of 8192 x 4096 x 32768, dx 1695 us (1297 TFLOP/s), dweight, of two halves, 3518 (1250).  Of 8192 x 768 x 30522 dx 374 and dweight 726:
+// of 8192 x 4096 x 32768, dx 1753 us (1254 TFLOP/s), dweight, of two halves, 3622 (1214).  Of 8192 x 768 x 30522 dx 379 and dweight 742:
 // 256 x 128, two workgroups to a compute unit, so that one's epilogue overlaps the other's product; 256 x 256 takes 882.
 template <uint32_t M, uint32_t N, uint32_t WAVES_M, uint32_t WAVES_N, uint32_t STAGES, bool TURN_A> struct GradientTile {
     typedef Product<f16, M, N, WAVES_M, WAVES_N, TURN_A, true, STAGES, M == 256 && N == 128 ? 32 : PRODUCT_STEP, LOW> P;
@@ -820,7 +820,7 @@ __global__ __launch_bounds__(256) void k_head_dbias(BiasArgs a)
 }
 
 // Gradients of little work in one launch: tiles of dweight, tiles of dx, and the bias gradient's sums.  Bound by the latency of few steps, so
-// that one beside the other costs little: 300 x 333 x 1009 of fp32 9.4 us, in three launches 8.4, 8.3 and 1.3 and what lies between them.
+// that one beside the other costs little: 300 x 333 x 1009 of fp32 10 us, in three launches 8.4, 8.3 and 1.3 and what lies between them.
 __global__ __launch_bounds__(256, 2) void k_head_gradients(GradientArgs dw, GradientArgs dx, BiasArgs bias, uint32_t dw_blocks, uint32_t dx_blocks)
 {
     typedef GradientTile<64, 64, 2, 2, 4, true> W;
@@ -974,7 +974,8 @@ static HeadPlan plan_of(const dgs_head_args &p, bool back)
     h.few = p.rows <= FEW_ROWS;
     h.direct = h.few && (f32 || !staged);
     // (dx alone, bfloat16 W of 32000 x 4096, by few_dx and by the matrix units from a copy of W: 8 rows 140 and 267 us, 16 rows 206 and 287,
-    // 32 rows 360 and 278; of 32000 x 1024 16 rows 67 and 67)
+    // 32 rows 360 and 278; of 32000 x 1024 16 rows 67 and 67.  fp32 has its halves beyond 32 rows only: 32000 x 4096, 32 rows forward 156 and
+    // dx 395, 33 rows 442 and 598)
     h.few_dx = h.few && (f32 || p.rows <= 16);
     h.split = f32 && !h.few;
     h.scale_w = h.wants_dx && (h.split || (p.type == DGS_BF16 && !h.few_dx));
@@ -1164,7 +1165,8 @@ static int refused(const dgs_head_args &p, bool back)
     if (back && p.dweight && (p.dweight_stride < p.cols || p.dweight_stride >= (1ull << 32))) return DGS_EINVAL;
     if (!aligned_to(p.dloss, 4) || !aligned_to(p.dlse, 4) || !aligned_to(p.dweight, 4) || !aligned_to(p.dbias, 4)) return DGS_EINVAL;
     if (p.cols > (1u << 20) || p.rows > (1u << 24) || p.vocab > (1u << 24)) return DGS_ENOTSUP;
-    // (a launch has less than 2^32 lanes: a lane for 128 logits, for eight values of dx)
+    // (a launch has less than 2^32 lanes: in tiles of 256 x 256, which products of that size take, a lane for 128 logits; a lane for eight values
+    // of dx)
     if ((uint64_t)p.rows * p.vocab > (1ull << 38) || (uint64_t)p.rows * p.cols > (1ull << 34)) return DGS_ENOTSUP;
     return DGS_OK;
 }

@@ -77,7 +77,7 @@ template <class T> __device__ __forceinline__ double squares(const T *m, uint64_
     return s;
 }
 
-// Sums of squares, at most NORM_PARTS a matrix.  Bound by memory: twelve of 2304 x 768 in fp32, 85 MB, 15.4 us (5.5 TB/s).
+// Sums of squares, at most NORM_PARTS a matrix.  Bound by memory: twelve of 2304 x 768 in fp32, 85 MB, 16.4 us (5.2 TB/s).
 template <class T>
 __global__ __launch_bounds__(256) void k_ortho_norm(Matrices in, uint32_t rows, uint32_t cols, double *parts)
 {
@@ -93,7 +93,7 @@ __global__ __launch_bounds__(256) void k_ortho_norm(Matrices in, uint32_t rows, 
 }
 
 // X from G, 64 x 64 of it to a workgroup, turned where that makes it wide.  Columns up to a multiple of eight are zeros.
-// Bound by memory: twelve of 2304 x 768, 85 MB read and as many written, 32 us (5.3 TB/s).  norm_parts = 0: every workgroup takes the norm
+// Bound by memory: twelve of 2304 x 768, 85 MB read and as many written, 34 us (5.0 TB/s).  norm_parts = 0: every workgroup takes the norm
 // of its matrix itself.
 template <class T>
 __global__ __launch_bounds__(256) void k_ortho_load(Matrices in, uint32_t rows, uint32_t cols, uint32_t turned, const double *parts, uint32_t norm_parts,
@@ -200,8 +200,8 @@ __device__ __forceinline__ int power_of_sums(const SquareArgs &a, uint32_t which
 }
 
 // The symmetric product of X with itself (POLY: of A with itself, from which the polynomial is made).  Bound by the matrix units:
-// 4096 x 4096 (69 GFLOP of tiles) 79 and 85 us, 192 x 192 so that 253 of 256 compute units have one tile each; 256 x 256, 136 tiles, takes 112
-// and 114.  333 x 1001 (five, three pairs): by latency, 48 steps of 64 x 64 in 17 us.
+// 4096 x 4096 (69 GFLOP of tiles) 78 and 84 us, 192 x 192 so that 253 of 256 compute units have one tile each; 256 x 256, 136 tiles, takes 93
+// and 94, 128 x 128 107 and 111.  333 x 1001 (five, three pairs): by latency, 48 steps of 64 x 64 in 17 us.
 template <uint32_t M, uint32_t WAVES_M, uint32_t WAVES_N, uint32_t STAGES, bool POLY>
 __global__ __launch_bounds__(WAVES_M *WAVES_N * 64, M == 192 ? 1 : 2) void k_ortho_square(SquareArgs a)
 {
@@ -319,7 +319,7 @@ template <class T> __device__ __forceinline__ void put8(T *p, uint32_t count, fl
 }
 
 // X of the next step: its rows times the polynomial's diagonal, plus the product of the rest with it.  4096 x 4096: 132 us (1040 TFLOP/s
-// with one round of tiles); twelve of 768 x 2304: 58 us, 212 MB of X's halves read twice over and written beside 33 GFLOP.
+// with one round of tiles); twelve of 768 x 2304: 62 us, 212 MB of X's halves read twice over and written beside 33 GFLOP.
 // T: the result's type in the last step, void in the others; TURNED: the result's rows are X's columns.
 template <uint32_t M, uint32_t WAVES_M, uint32_t WAVES_N, uint32_t STAGES, class T, bool TURNED>
 __global__ __launch_bounds__(WAVES_M *WAVES_N * 64, 2) void k_ortho_step(StepArgs a, Matrices results)
@@ -393,8 +393,9 @@ __global__ __launch_bounds__(WAVES_M *WAVES_N * 64, 2) void k_ortho_step(StepArg
 
 // Matrices of up to S x S, whole: a workgroup each, all steps in one launch.  A lane keeps its values of X and A in fp32; what the products
 // read of them lies in LDS in halves, transposed, so that the four rows that a lane has together are written together (A and the polynomial are
-// symmetric).  Bound by latency: 96 matrix instructions a wavefront at most between barriers.  A square of 32 x 32 to a wavefront, so that
-// four of them share a SIMD at 128 x 128: five steps of one in fp32 74 us (four wavefronts with four squares each: 102; in launches of their own, 16 of
+// symmetric).  Bound by latency: of 128 x 128 a product is 24 matrix instructions a wavefront between two barriers (eight slices, three pairs of parts), each
+// of two fragments from LDS, 768 KB in all: some 2.6 us of the 4.8 that a product takes.  A square of 32 x 32 to a wavefront, so that
+// four of them share a SIMD at 128 x 128: five steps of one in fp32 73 us (four wavefronts with four squares each: 102; in launches of their own, 16 of
 // them: 98); 64 x 64 31 (81); 32 of 128 x 128 in bfloat16 46 (89); 200 of 48 x 48 in fp32 245 (563).
 struct SmallArgs {
     uint32_t rows, cols, turned, type, out_type;      // of G

@@ -518,7 +518,7 @@ static inline uint32_t tiles_of(uint32_t n, uint32_t size) { return n ? (n - 1) 
 
 // Microseconds that `tiles` tiles of `steps` steps of 64 k take: what a tile takes besides its steps, and for a step with every
 // compute unit's places taken and with one workgroup to a compute unit at most, as timed.  (4096 x 4096 squares on and below the
-// diagonal, 64 steps: 256 x 256 110 us, 192 x 192 91, 128 x 128 114, 64 x 64 170; four of 1024 x 1024, 192 steps: 230, 128, 141; five of 333 x 333, 48
+// diagonal, 64 steps, by card: 256 x 256 93 to 110 us, 192 x 192 79 to 91, 128 x 128 107 to 114, 64 x 64 163 to 170; four of 1024 x 1024, 192 steps: 230, 128, 141; five of 333 x 333, 48
 // steps: 66, 33, 17; 30522 x 768 turned, 256 steps: 256 x 256 882, 256 x 128 775, 128 x 128 845.)
 static inline float tile_time(int tile, uint64_t tiles, uint32_t steps)
 {
